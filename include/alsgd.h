@@ -382,6 +382,45 @@ int alsgd_sched_import(alsgd_sched* s, const void* host_src, uint64_t bytes);
 int alsgd_pg_norm_static(const float* start, const float* p, uint64_t n, int32_t device, void* stream,
                          double* gnorm2_out, uint32_t* nonfinite_out);
 
+/* ------------------------------------------------------------------------------------------------
+ * Training operators of the workers (the paper runs its workers' forward and backward passes elsewhere; these
+ * are the pieces in front of alsgd_inner_adamw).  They need no context.  They allocate nothing, only enqueue on
+ * the given stream and may be captured in a CUDA graph.
+ * ---------------------------------------------------------------------------------------------- */
+
+#define ALSGD_F32 0u
+#define ALSGD_BF16 1u
+
+typedef struct alsgd_grad_desc {
+    const void* data;  /* device, numel values of the stated type, naturally aligned (16 bytes is faster) */
+    uint64_t numel;    /* may be 0 (data may then be NULL) */
+    uint64_t offset;   /* position in the flat vector, as alsgd_layout_size gives it */
+    uint32_t dtype;    /* ALSGD_F32 or ALSGD_BF16 */
+    uint32_t reserved;
+} alsgd_grad_desc;
+
+/* Global norm of a list of gradient tensors, and the clipped gradient as the flat vector that alsgd_inner_adamw
+ * (fp32) or alsgd_inner_adamw_bf16 takes:
+ *     norm = sqrt(sum over all tensors of g^2),  factor = 1 if norm <= max_norm else max_norm / norm,
+ *     out[offset + i] = factor * g[i], rounded once to out_dtype.
+ *   grads       host, n >= 1 entries, read during the call; the tensors stay where the backward pass left them
+ *   max_norm    > 0, may be +inf
+ *   out         device, out_elems values of out_dtype, or NULL for the norm alone.  Elements that belong to no tensor
+ *               (alignment padding) are not written.  A tensor may lie exactly at its place in out (in-place
+ *               clipping, same type); any other overlap is undefined
+ *   stats       device, two floats: norm, factor
+ *   work        device, 256-byte aligned, alsgd_clip_grads_bytes bytes, zero-filled once before its first use;
+ *               every call leaves it ready for the next.  Calls that share it must be ordered
+ * A norm that is NaN makes the factor NaN and with it the whole result; an infinite norm makes the factor 0
+ * (infinite entries become NaN).  Squares are summed so that neither 1e30 overflows nor 1e-30 vanishes; the order
+ * is fixed, so the same list gives the same bits on every call.
+ * ALSGD_E_ARG: null or misaligned pointer, n = 0, max_norm not above 0, unknown type.  ALSGD_E_RANGE: device ordinal
+ * outside 0..63, a tensor that does not fit out, 2^31 tiles of 16 KiB or more in one group of 512 tensors.
+ * ALSGD_E_NOMEM: work too small. */
+int alsgd_clip_grads_bytes(uint32_t n, uint64_t* bytes_out);
+int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float max_norm, void* out, uint32_t out_dtype,
+                     uint64_t out_elems, float* stats, void* work, uint64_t work_bytes, int32_t device, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

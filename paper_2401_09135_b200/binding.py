@@ -19,6 +19,7 @@ PG_DISPATCH, PG_CURRENT = 0, 1
 CFG_REPLICA_BF16, CFG_GRAD_STAGING, CFG_OUTER_BUFFERED, CFG_OUTER_SGDM, CFG_STABLE_PTRS = 1, 2, 4, 8, 16
 STALE_NONE, STALE_POLY, STALE_POLY_THRES = 0, 1, 2
 ARRIVE_RESEED, ARRIVE_NORM, ARRIVE_NANCHECK = 1, 2, 4
+F32, BF16 = 0, 1
 
 
 class TensorDesc(C.Structure):
@@ -54,6 +55,11 @@ class WorkerPtrs(C.Structure):
 
 class LrSched(C.Structure):
     _fields_ = [("eta_max", C.c_double), ("eta_min", C.c_double), ("t_warmup", C.c_uint64), ("T", C.c_uint64)]
+
+
+class GradDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("numel", C.c_uint64), ("offset", C.c_uint64), ("dtype", C.c_uint32),
+                ("reserved", C.c_uint32)]
 
 
 _vp = C.c_void_p
@@ -99,6 +105,9 @@ SIGNATURES = {
     "alsgd_sched_export": (C.c_int, [_vp, _vp, C.c_uint64]),
     "alsgd_sched_import": (C.c_int, [_vp, _vp, C.c_uint64]),
     "alsgd_pg_norm_static": (C.c_int, [_vp, _vp, C.c_uint64, C.c_int32, _vp, _vp, _vp]),
+    "alsgd_clip_grads_bytes": (C.c_int, [C.c_uint32, _u64p]),
+    "alsgd_clip_grads": (C.c_int, [C.POINTER(GradDesc), C.c_uint32, C.c_float, _vp, C.c_uint32, C.c_uint64, _vp, _vp, C.c_uint64,
+                                   C.c_int32, _vp]),
 }
 STATIC_MAX_ELEMS = 1 << 27
 
@@ -406,3 +415,55 @@ class Context:
             self.close()
         except Exception:
             pass
+
+
+# -- training operators of the workers -----------------------------------------------------------------
+def _dtype_code(torch, dtype):
+    if dtype == torch.float32:
+        return F32
+    if dtype == torch.bfloat16:
+        return BF16
+    raise AlsgdError(E_ARG, f"unsupported type {dtype}")
+
+
+def _stream(torch, device, stream):
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+class GradClip:
+    """Gradient clipping for one tensor table: keeps the sizes, offsets and types of the gradients and the call's
+    workspace; the tensors themselves are given at every call."""
+
+    def __init__(self, numels, offsets, dtypes, out_dtype, device=0):
+        import torch
+        self.torch = torch
+        self.device = torch.device("cuda", device)
+        n = len(numels)
+        assert n == len(offsets) == len(dtypes)
+        self.numels, self.dtypes = [int(x) for x in numels], list(dtypes)
+        self.out_dtype, self._out_code = out_dtype, _dtype_code(torch, out_dtype)
+        self._desc = (GradDesc * max(n, 1))()
+        for d, numel, off, t in zip(self._desc, self.numels, offsets, self.dtypes):
+            d.numel, d.offset, d.dtype = numel, int(off), _dtype_code(torch, t)
+        nbytes = C.c_uint64()
+        _check(lib().alsgd_clip_grads_bytes(n, C.byref(nbytes)), "alsgd_clip_grads_bytes")
+        self._work = torch.zeros(int(nbytes.value) + 256, dtype=torch.uint8, device=self.device)
+        self._work_ptr = -(-self._work.data_ptr() // 256) * 256
+        self._work_bytes = int(nbytes.value)
+        # the zeros are there before any stream uses the workspace
+        torch.cuda.current_stream(self.device).synchronize()
+
+    def alsgd_clip_grads(self, grads, max_norm, out, stats, stream=None):
+        """grads: one contiguous device tensor per table entry.  out: flat tensor of out_dtype, or None for the norm
+        alone.  stats: two fp32 values on the device (norm, factor)."""
+        assert len(grads) == len(self.numels) and stats.numel() == 2 and stats.dtype == self.torch.float32
+        assert stats.device == self.device and stats.is_contiguous()
+        for d, g, numel, t in zip(self._desc, grads, self.numels, self.dtypes):
+            assert g.numel() == numel and g.dtype == t and g.is_contiguous() and g.device == self.device
+            d.data = g.data_ptr()
+        if out is not None:
+            assert out.dtype == self.out_dtype and out.is_contiguous() and out.device == self.device
+        _check(lib().alsgd_clip_grads(self._desc, len(self.numels), float(max_norm), out.data_ptr() if out is not None else None,
+                                      self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work_ptr,
+                                      self._work_bytes, self.device.index, _stream(self.torch, self.device, stream)),
+               "alsgd_clip_grads")
