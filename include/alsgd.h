@@ -421,6 +421,58 @@ int alsgd_clip_grads_bytes(uint32_t n, uint64_t* bytes_out);
 int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float max_norm, void* out, uint32_t out_dtype,
                      uint64_t out_elems, float* stats, void* work, uint64_t work_bytes, int32_t device, void* stream);
 
+/* Attention of a decoder layer with a learned relative position bias, for training in the replica's bf16.
+ *     x[i][j] = scale * q_i . k_j + table[h][bucket(j - (q_pos + i))]   over the allowed keys j of query i
+ *     lse_i = log(sum_j exp(x[i][j])),   o_i = sum_j exp(x[i][j] - lse_i) v_j
+ * Key j of sequence b is allowed if j < kv_len[b] and, with ALSGD_ATTN_CAUSAL, j <= q_pos + i.  A query with no allowed
+ * key (or whose every allowed key has a bucket that is taken out) gives o_i = 0 and lse_i = -inf, and takes no part in
+ * any gradient.  Keys behind kv_len are never used, whatever they hold.  Query head h reads key head
+ * h / (heads_q / heads_kv).  Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 before
+ * they multiply v.
+ *
+ * Buckets of a distance r = key position - query position: one-sided (the default) a = max(-r, 0) and n = buckets;
+ * two-sided a = |r| and n = buckets / 2, with n added for r > 0.  With e = n / 2 (rounded down): a itself below e, else
+ *     min(n - 1, e + floor(log(a / e) / log(max_distance / e) * (n - e))).
+ * A table entry at or below -1e30 takes its bucket out: those keys are not allowed. */
+#define ALSGD_ATTN_CAUSAL 1u
+#define ALSGD_ATTN_BIAS_TWO_SIDED 2u
+
+typedef struct alsgd_attn_desc {
+    uint32_t batch, heads_q, heads_kv; /* >= 1; heads_q a multiple of heads_kv */
+    uint32_t len_q, len_kv;            /* positions, up to 2^22; may be 0 */
+    uint32_t dim;                      /* elements of a head: a multiple of 8, up to 128 */
+    uint32_t flags;                    /* ALSGD_ATTN_* */
+    uint32_t buckets;                  /* of the bias, up to 256 (even if two-sided); 0 = no bias */
+    uint32_t max_distance;             /* above e, up to 2048; ignored without a bias */
+    uint32_t table_dtype;              /* ALSGD_F32 or ALSGD_BF16; ignored without a bias */
+    int32_t q_pos;                     /* position of query 0 on the keys' axis (len_kv - len_q lines up the ends) */
+    float scale;                       /* > 0, finite; usually dim^-0.5 */
+    int32_t device;
+    uint32_t reserved;
+} alsgd_attn_desc;
+
+/* A bf16 operand [batch][position][head][dim] on the device: 16-byte aligned, steps in elements, multiples of 8, and
+ * consecutive elements within a head.  An input may have a step of 0 over the batch or the heads (broadcast). */
+typedef struct alsgd_attn_tensor {
+    void* data;
+    int64_t stride_batch, stride_pos, stride_head;
+} alsgd_attn_tensor;
+
+/* Forward pass.  table: device, [heads_q][buckets] of table_dtype, NULL exactly if buckets = 0.  kv_len: device, one
+ * int32 per sequence (values outside 0..len_kv are taken as the nearer end), or NULL for len_kv everywhere.  lse: device,
+ * fp32 [batch][heads_q][len_q].
+ * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step.  ALSGD_E_UNSUPPORTED: dim > 128,
+ * buckets > 256, max_distance > 2048.  ALSGD_E_RANGE: a length beyond 2^22, device ordinal outside 0..63. */
+int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const alsgd_attn_tensor* v,
+                   const void* table, const int32_t* kv_len, const alsgd_attn_tensor* o, float* lse, void* stream);
+
+/* Bucket of one distance (host arithmetic), for a caller that keeps or inspects the table. */
+int alsgd_attn_bucket(const alsgd_attn_desc* desc, int32_t distance, uint32_t* bucket_out);
+
+/* Waits inside the attention kernels are bounded.  *waits_out (host) is 0, or has bits set if a wait ever ran out on
+ * this device since the library was loaded; results since then are not to be trusted.  Waits for the device. */
+int alsgd_attn_status(int32_t device, uint32_t* waits_out);
+
 #ifdef __cplusplus
 }
 #endif

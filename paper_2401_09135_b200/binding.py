@@ -20,6 +20,7 @@ CFG_REPLICA_BF16, CFG_GRAD_STAGING, CFG_OUTER_BUFFERED, CFG_OUTER_SGDM, CFG_STAB
 STALE_NONE, STALE_POLY, STALE_POLY_THRES = 0, 1, 2
 ARRIVE_RESEED, ARRIVE_NORM, ARRIVE_NANCHECK = 1, 2, 4
 F32, BF16 = 0, 1
+ATTN_CAUSAL, ATTN_BIAS_TWO_SIDED = 1, 2
 
 
 class TensorDesc(C.Structure):
@@ -60,6 +61,17 @@ class LrSched(C.Structure):
 class GradDesc(C.Structure):
     _fields_ = [("data", C.c_void_p), ("numel", C.c_uint64), ("offset", C.c_uint64), ("dtype", C.c_uint32),
                 ("reserved", C.c_uint32)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("batch", C.c_uint32), ("heads_q", C.c_uint32), ("heads_kv", C.c_uint32), ("len_q", C.c_uint32),
+                ("len_kv", C.c_uint32), ("dim", C.c_uint32), ("flags", C.c_uint32), ("buckets", C.c_uint32),
+                ("max_distance", C.c_uint32), ("table_dtype", C.c_uint32), ("q_pos", C.c_int32), ("scale", C.c_float),
+                ("device", C.c_int32), ("reserved", C.c_uint32)]
+
+
+class AttnTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_pos", C.c_int64), ("stride_head", C.c_int64)]
 
 
 _vp = C.c_void_p
@@ -108,6 +120,9 @@ SIGNATURES = {
     "alsgd_clip_grads_bytes": (C.c_int, [C.c_uint32, _u64p]),
     "alsgd_clip_grads": (C.c_int, [C.POINTER(GradDesc), C.c_uint32, C.c_float, _vp, C.c_uint32, C.c_uint64, _vp, _vp, C.c_uint64,
                                    C.c_int32, _vp]),
+    "alsgd_attn_fwd": (C.c_int, [C.POINTER(AttnDesc)] + [C.POINTER(AttnTensor)] * 3 + [_vp, _vp, C.POINTER(AttnTensor), _vp, _vp]),
+    "alsgd_attn_bucket": (C.c_int, [C.POINTER(AttnDesc), C.c_int32, _u32p]),
+    "alsgd_attn_status": (C.c_int, [C.c_int32, _u32p]),
 }
 STATIC_MAX_ELEMS = 1 << 27
 
@@ -467,3 +482,57 @@ class GradClip:
                                       self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work_ptr,
                                       self._work_bytes, self.device.index, _stream(self.torch, self.device, stream)),
                "alsgd_clip_grads")
+
+
+def alsgd_attn_status(device=0):
+    """0, or bits of the waits inside the attention kernels that ran out on this device (waits for the device)."""
+    out = C.c_uint32()
+    _check(lib().alsgd_attn_status(int(device), C.byref(out)), "alsgd_attn_status")
+    return int(out.value)
+
+
+class Attention:
+    """Attention of one shape.  Operands are bf16 tensors [batch, position, head, dim] with any strides the ABI takes."""
+
+    def __init__(self, batch, len_q, len_kv, heads_q, heads_kv, dim, causal=True, scale=None, q_pos=None, buckets=0,
+                 max_distance=128, bidirectional=False, table_dtype=None, device=0):
+        import torch
+        self.torch = torch
+        self.device = torch.device("cuda", device)
+        d = self.desc = AttnDesc()
+        d.batch, d.heads_q, d.heads_kv, d.len_q, d.len_kv, d.dim = [int(x) for x in (batch, heads_q, heads_kv, len_q, len_kv, dim)]
+        d.flags = (ATTN_CAUSAL if causal else 0) | (ATTN_BIAS_TWO_SIDED if bidirectional else 0)
+        d.buckets, d.max_distance = int(buckets), int(max_distance)
+        self.table_dtype = table_dtype if table_dtype is not None else torch.float32
+        d.table_dtype = _dtype_code(torch, self.table_dtype)
+        d.q_pos = int(len_kv - len_q if q_pos is None else q_pos)
+        d.scale = float(dim ** -0.5 if scale is None else scale)
+        d.device = int(device)
+        self._q_shape, self._kv_shape = (batch, len_q, heads_q, dim), (batch, len_kv, heads_kv, dim)
+        self._lse_shape, self._table_shape = (batch, heads_q, len_q), (heads_q, buckets)
+
+    def _operand(self, t, shape):
+        assert t.dtype == self.torch.bfloat16 and t.shape == shape and t.device == self.device
+        b, s, h, d = t.stride()
+        assert d == 1
+        return AttnTensor(t.data_ptr(), b, s, h)
+
+    def _plain(self, t, shape, dtype):
+        if t is None:
+            return None
+        assert t.dtype == dtype and t.shape == shape and t.device == self.device and t.is_contiguous()
+        return t.data_ptr()
+
+    def alsgd_attn_fwd(self, q, k, v, out, lse, table=None, kv_len=None, stream=None):
+        """out and lse are written.  table: [heads_q, buckets]; kv_len: int32 per sequence."""
+        _check(lib().alsgd_attn_fwd(self.desc, self._operand(q, self._q_shape), self._operand(k, self._kv_shape),
+                                    self._operand(v, self._kv_shape), self._plain(table, self._table_shape, self.table_dtype),
+                                    self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
+                                    self._plain(lse, self._lse_shape, self.torch.float32),
+                                    _stream(self.torch, self.device, stream)), "alsgd_attn_fwd")
+
+    def alsgd_attn_bucket(self, distance):
+        """Bucket of a distance key position - query position."""
+        out = C.c_uint32()
+        _check(lib().alsgd_attn_bucket(self.desc, int(distance), C.byref(out)), "alsgd_attn_bucket")
+        return int(out.value)

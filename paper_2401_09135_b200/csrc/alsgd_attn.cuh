@@ -1,0 +1,190 @@
+// Shared by attention's forward and backward pass: the shape as the kernels see it, the relative position bias, the
+// checks of a call's arguments and the tensor maps.
+#pragma once
+#include "../../include/alsgd.h"
+#include "alsgd_ops.cuh"
+#include "alsgd_tc.cuh"
+
+#include <cmath>
+#include <cstring>
+
+namespace alsgd_attn {
+
+constexpr int kMaxDistance = 2048;     // the bias table by distance has to fit beside the tiles in shared memory
+constexpr int kMaxBuckets = 256;
+constexpr int kMaxLength = 1 << 22;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kMaskedOut = -1e30f;   // a table entry at or below this takes its bucket out
+
+struct Shape {
+    int batch, heads_q, heads_kv, group, len_q, len_kv, dim;
+    int causal, q_pos;
+    float scale, scale_log2;
+    const int* kv_len;                 // may be null
+};
+
+// Buckets of a distance: below `near` one each, then up to limits[0], limits[1], ..., the last open.
+struct Bias {
+    const void* table;                 // null: no bias
+    int bf16, buckets;
+    int per_side, near, two_sided;
+    int far;                           // distances from here on share the last bucket of their side
+    int n_limits;
+    int limits[kMaxBuckets / 2];
+};
+
+__device__ __forceinline__ int bucket_of(const Bias& s, int r) {
+    const int a = s.two_sided ? abs(r) : max(-r, 0);
+    int at = a;
+    if (a >= s.near) {
+        at = s.near;
+        for (int i = 0; i < s.n_limits; ++i) at += a >= s.limits[i];
+    }
+    return at + (s.two_sided && r > 0 ? s.per_side : 0);
+}
+
+__device__ __forceinline__ float table_entry(const Bias& s, int head, int bucket) {
+    const size_t i = (size_t)head * s.buckets + bucket;
+    return s.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(s.table)[i] << 16) : static_cast<const float*>(s.table)[i];
+}
+
+// The bias by distance in the exponent's base 2, lut[r + pad] for -pad <= r <= pad.  Threads [0, threads) fill it.
+__device__ __forceinline__ void fill_lut(const Bias& s, int head, float* lut, int pad, int thread, int threads) {
+    for (int i = thread; i <= 2 * pad; i += threads) {
+        const float v = table_entry(s, head, bucket_of(s, i - pad));
+        lut[i] = v <= kMaskedOut ? -INFINITY : v * kLog2e;
+    }
+}
+
+// What every row of a tile has in common.  Rows and columns are positions; r = column - row.
+enum Span { kSpanFarLeft, kSpanFarRight, kSpanMixed };
+__device__ __forceinline__ Span span_of(const Bias& s, int r_min, int r_max) {
+    return r_max <= -s.far ? kSpanFarLeft : r_min >= s.far ? kSpanFarRight : kSpanMixed;
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------
+
+// Edges of the logarithmic buckets: the smallest whole distances a with log(a/near)/log(max/near) * width >= i.
+inline void bucket_limits(int per_side, int near, int max_distance, Bias* out) {
+    const int width = per_side - near;
+    out->n_limits = 0;
+    for (int i = 1; i < width; ++i) {
+        const long double t = near * powl((long double)max_distance / near, (long double)i / width);
+        const long double whole = roundl(t);
+        out->limits[out->n_limits++] = (int)(fabsl(t - whole) < 1e-10L * t ? whole : ceill(t));
+    }
+    out->far = out->n_limits ? out->limits[out->n_limits - 1] : near;
+}
+
+inline int make_bias(const alsgd_attn_desc& d, const void* table, Bias* out) {
+    std::memset(out, 0, sizeof *out);
+    out->far = 1;
+    if (d.buckets == 0) return ALSGD_OK;
+    const bool two = d.flags & ALSGD_ATTN_BIAS_TWO_SIDED;
+    if (d.table_dtype != ALSGD_F32 && d.table_dtype != ALSGD_BF16) return ALSGD_E_ARG;
+    if (d.buckets > kMaxBuckets || d.max_distance > kMaxDistance) return ALSGD_E_UNSUPPORTED;
+    if (two && d.buckets % 2) return ALSGD_E_ARG;
+    const int per_side = (int)d.buckets / (two ? 2 : 1), near = per_side / 2;
+    if (near < 1 || (int)d.max_distance <= near) return ALSGD_E_ARG;
+    out->table = table;
+    out->bf16 = d.table_dtype == ALSGD_BF16;
+    out->buckets = (int)d.buckets;
+    out->per_side = per_side;
+    out->near = near;
+    out->two_sided = two;
+    bucket_limits(per_side, near, (int)d.max_distance, out);
+    return ALSGD_OK;
+}
+
+inline int check_desc(const alsgd_attn_desc* d) {
+    if (!d) return ALSGD_E_ARG;
+    if (d->batch == 0 || d->heads_q == 0 || d->heads_kv == 0 || d->heads_q % d->heads_kv) return ALSGD_E_ARG;
+    if (d->dim == 0 || d->dim % 8 || (d->flags & ~(ALSGD_ATTN_CAUSAL | ALSGD_ATTN_BIAS_TWO_SIDED))) return ALSGD_E_ARG;
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale)) return ALSGD_E_ARG;
+    if (d->dim > 128) return ALSGD_E_UNSUPPORTED;
+    if (d->len_q > kMaxLength || d->len_kv > kMaxLength || d->q_pos > kMaxLength || d->q_pos < -kMaxLength) return ALSGD_E_RANGE;
+    if ((uint64_t)d->batch * d->heads_q > 0x7FFFFFFFull) return ALSGD_E_RANGE;
+    if (d->device < 0 || d->device >= alsgd_ops::kMaxDevices) return ALSGD_E_RANGE;
+    Bias unused;
+    return make_bias(*d, nullptr, &unused);
+}
+
+// A [batch, position, head, dim] operand: 16-byte steps, no step of zero between elements that differ in an output.
+inline int check_tensor(const alsgd_attn_tensor* t, uint32_t batch, uint32_t len, uint32_t heads, bool output) {
+    if (!t) return ALSGD_E_ARG;
+    if (len == 0) return ALSGD_OK;
+    if (!t->data || reinterpret_cast<uintptr_t>(t->data) % 16) return ALSGD_E_ARG;
+    const int64_t step[3] = {t->stride_pos, t->stride_head, t->stride_batch};
+    const uint64_t extent[3] = {len, heads, batch};
+    for (int i = 0; i < 3; ++i) {
+        if (extent[i] == 1) continue;
+        if (step[i] < 0 || step[i] % 8 || step[i] >= (1ll << 39)) return ALSGD_E_ARG;
+        if (step[i] == 0 && (output || i == 0)) return ALSGD_E_ARG;
+    }
+    return ALSGD_OK;
+}
+
+inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
+    Shape s;
+    s.batch = (int)d.batch;
+    s.heads_q = (int)d.heads_q;
+    s.heads_kv = (int)d.heads_kv;
+    s.group = (int)(d.heads_q / d.heads_kv);
+    s.len_q = (int)d.len_q;
+    s.len_kv = (int)d.len_kv;
+    s.dim = (int)d.dim;
+    s.causal = (d.flags & ALSGD_ATTN_CAUSAL) != 0;
+    s.q_pos = d.q_pos;
+    s.scale = d.scale;
+    s.scale_log2 = d.scale * kLog2e;
+    s.kv_len = kv_len;
+    return s;
+}
+
+// An operand as the copy engine reads it.  A dimension with step 0 (an operand broadcast over the batch or the heads)
+// has extent 1 there and its coordinate is multiplied away.
+struct Operand {
+    CUtensorMap map;
+    int head_mul, batch_mul;
+};
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiled encode_tiled() {
+    static EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Boxes of 64 elements x `rows` positions of one head of one sequence, 128-byte swizzle, zeros outside.
+inline int make_operand(const alsgd_attn_tensor& t, uint32_t batch, uint32_t len, uint32_t heads, uint32_t dim, uint32_t rows, Operand* out) {
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return ALSGD_E_CUDA;
+    const uint64_t extent[3] = {len, heads, batch};
+    const int64_t step[3] = {t.stride_pos, t.stride_head, t.stride_batch};
+    cuuint64_t size[4] = {dim, 0, 0, 0}, bytes[3];
+    int mul[3];
+    for (int i = 0; i < 3; ++i) {
+        const bool one = extent[i] == 1 || step[i] == 0;
+        mul[i] = !one;
+        size[i + 1] = one ? 1 : extent[i];
+        bytes[i] = one ? 16 * ((dim * 2 + 15) / 16) : (uint64_t)step[i] * 2;
+    }
+    out->head_mul = mul[1];
+    out->batch_mul = mul[2];
+    const cuuint32_t box[4] = {64, rows, 1, 1}, unit[4] = {1, 1, 1, 1};
+    const CUresult r = encode(&out->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, t.data, size, bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ALSGD_OK : ALSGD_E_ARG;
+}
+
+}  // namespace alsgd_attn
