@@ -466,6 +466,22 @@ typedef struct alsgd_attn_tensor {
 int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const alsgd_attn_tensor* v,
                    const void* table, const int32_t* kv_len, const alsgd_attn_tensor* o, float* lse, void* stream);
 
+/* Backward pass: from q, k, v, table, kv_len, the forward pass's o and lse, and dout = d(loss)/d(o),
+ *     p[i][j] = exp(x[i][j] - lse_i),   ds[i][j] = p[i][j] (dout_i . v_j - dout_i . o_i)
+ *     dq_i = scale sum_j ds[i][j] k_j,  dk_j = scale sum_i ds[i][j] q_i,  dv_j = sum_i p[i][j] dout_i,
+ *     dtable[h][n] = sum over sequences and the pairs of bucket n of ds[i][j].
+ * dk and dv sum over the query heads that share a key head; keys nobody uses get zeros.  ds and p are rounded to bf16
+ * before the products with k, q and dout; dtable sums them unrounded.  Results are written, not added to; nothing
+ * depends on the order in which blocks run, so the same inputs give the same bits.
+ *   dtable   device, [heads_q][buckets] of table_dtype, NULL exactly if buckets = 0
+ *   work     device, 256-byte aligned, alsgd_attn_bwd_bytes bytes (may be NULL if that is 0), any content
+ * Errors as alsgd_attn_fwd; ALSGD_E_NOMEM: work too small. */
+int alsgd_attn_bwd_bytes(const alsgd_attn_desc* desc, uint64_t* bytes_out);
+int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const alsgd_attn_tensor* v,
+                   const void* table, const int32_t* kv_len, const alsgd_attn_tensor* o, const float* lse,
+                   const alsgd_attn_tensor* dout, const alsgd_attn_tensor* dq, const alsgd_attn_tensor* dk,
+                   const alsgd_attn_tensor* dv, void* dtable, void* work, uint64_t work_bytes, void* stream);
+
 /* Bucket of one distance (host arithmetic), for a caller that keeps or inspects the table. */
 int alsgd_attn_bucket(const alsgd_attn_desc* desc, int32_t distance, uint32_t* bucket_out);
 

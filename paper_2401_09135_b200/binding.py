@@ -121,6 +121,9 @@ SIGNATURES = {
     "alsgd_clip_grads": (C.c_int, [C.POINTER(GradDesc), C.c_uint32, C.c_float, _vp, C.c_uint32, C.c_uint64, _vp, _vp, C.c_uint64,
                                    C.c_int32, _vp]),
     "alsgd_attn_fwd": (C.c_int, [C.POINTER(AttnDesc)] + [C.POINTER(AttnTensor)] * 3 + [_vp, _vp, C.POINTER(AttnTensor), _vp, _vp]),
+    "alsgd_attn_bwd_bytes": (C.c_int, [C.POINTER(AttnDesc), _u64p]),
+    "alsgd_attn_bwd": (C.c_int, [C.POINTER(AttnDesc)] + [C.POINTER(AttnTensor)] * 3 + [_vp, _vp, C.POINTER(AttnTensor), _vp]
+                       + [C.POINTER(AttnTensor)] * 4 + [_vp, _vp, C.c_uint64, _vp]),
     "alsgd_attn_bucket": (C.c_int, [C.POINTER(AttnDesc), C.c_int32, _u32p]),
     "alsgd_attn_status": (C.c_int, [C.c_int32, _u32p]),
 }
@@ -510,6 +513,7 @@ class Attention:
         d.device = int(device)
         self._q_shape, self._kv_shape = (batch, len_q, heads_q, dim), (batch, len_kv, heads_kv, dim)
         self._lse_shape, self._table_shape = (batch, heads_q, len_q), (heads_q, buckets)
+        self._work = None                  # of the backward pass, made at its first call
 
     def _operand(self, t, shape):
         assert t.dtype == self.torch.bfloat16 and t.shape == shape and t.device == self.device
@@ -530,6 +534,23 @@ class Attention:
                                     self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
                                     self._plain(lse, self._lse_shape, self.torch.float32),
                                     _stream(self.torch, self.device, stream)), "alsgd_attn_fwd")
+
+    def alsgd_attn_bwd(self, q, k, v, out, lse, dout, dq, dk, dv, table=None, dtable=None, kv_len=None, stream=None):
+        """dq, dk, dv and dtable are written.  The workspace belongs to this object: calls on several streams must be
+        ordered by the caller."""
+        if self._work is None:
+            nbytes = C.c_uint64()
+            _check(lib().alsgd_attn_bwd_bytes(self.desc, C.byref(nbytes)), "alsgd_attn_bwd_bytes")
+            self._work = self.torch.empty(int(nbytes.value) + 256, dtype=self.torch.uint8, device=self.device)
+            self._work_ptr = -(-self._work.data_ptr() // 256) * 256
+            self._work_bytes = int(nbytes.value)
+        _check(lib().alsgd_attn_bwd(self.desc, self._operand(q, self._q_shape), self._operand(k, self._kv_shape),
+                                    self._operand(v, self._kv_shape), self._plain(table, self._table_shape, self.table_dtype),
+                                    self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
+                                    self._plain(lse, self._lse_shape, self.torch.float32), self._operand(dout, self._q_shape),
+                                    self._operand(dq, self._q_shape), self._operand(dk, self._kv_shape),
+                                    self._operand(dv, self._kv_shape), self._plain(dtable, self._table_shape, self.table_dtype),
+                                    self._work_ptr, self._work_bytes, _stream(self.torch, self.device, stream)), "alsgd_attn_bwd")
 
     def alsgd_attn_bucket(self, distance):
         """Bucket of a distance key position - query position."""

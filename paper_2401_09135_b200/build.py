@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libalsgd.so")
 LIB_DBG = os.path.join(HERE, "libalsgd_dbg.so")
 LIB_SWEEP = os.path.join(HERE, "libalsgd_sweep.so")
-SOURCES = ["alsgd_kernels.cu", "alsgd_ctx.cu", "alsgd_sched.cpp", "alsgd_static.cu", "alsgd_clip.cu", "alsgd_attn_fwd.cu"]
+SOURCES = ["alsgd_kernels.cu", "alsgd_ctx.cu", "alsgd_sched.cpp", "alsgd_static.cu", "alsgd_clip.cu", "alsgd_attn_fwd.cu",
+           "alsgd_attn_bwd.cu"]
 SWEEP_SOURCES = ["alsgd_sweep.cu"]
 HEADERS = [os.path.join(CSRC, "alsgd_kernels.cuh"), os.path.join(CSRC, "alsgd_kernels_impl.cuh"),
            os.path.join(CSRC, "alsgd_ops.cuh"), os.path.join(CSRC, "alsgd_tc.cuh"), os.path.join(CSRC, "alsgd_attn.cuh"),
@@ -29,7 +30,7 @@ NVCC_FLAGS = [
     # square root, denormals kept (results must not depend on how the compiler schedules the math)
     "-fmad=false", "-prec-div=true", "-prec-sqrt=true", "-ftz=false",
     "-Xcompiler", "-fPIC,-ffp-contract=off,-fno-fast-math",
-    "-shared",
+    "-shared", "--threads", "0",
 ]
 
 TARGETS = {

@@ -63,6 +63,8 @@ __device__ __forceinline__ Span span_of(const Bias& s, int r_min, int r_max) {
     return r_max <= -s.far ? kSpanFarLeft : r_min >= s.far ? kSpanFarRight : kSpanMixed;
 }
 
+bool bwd_wait_word(unsigned* out);     // alsgd_attn_bwd.cu
+
 // ---- host ---------------------------------------------------------------------------------------------------
 
 // Edges of the logarithmic buckets: the smallest whole distances a with log(a/near)/log(max/near) * width >= i.

@@ -382,9 +382,9 @@ extern "C" int alsgd_attn_status(int32_t device, uint32_t* waits_out) {
     if (device < 0 || device >= kMaxDevices) return ALSGD_E_RANGE;
     UseDevice use(device);
     if (!use.ok) return ALSGD_E_CUDA;
-    unsigned word = 0;
-    if (cudaMemcpyFromSymbol(&word, g_wait_error, sizeof word) != cudaSuccess) return ALSGD_E_CUDA;
-    *waits_out = word;
+    unsigned fwd = 0, bwd = 0;
+    if (cudaMemcpyFromSymbol(&fwd, g_wait_error, sizeof fwd) != cudaSuccess || !bwd_wait_word(&bwd)) return ALSGD_E_CUDA;
+    *waits_out = fwd | bwd;
     return ALSGD_OK;
 }
 

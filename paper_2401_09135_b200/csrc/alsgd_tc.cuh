@@ -37,7 +37,7 @@ static __device__ unsigned int g_wait_error;
 // waits give up at once) and returns false.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
     uint64_t t0, t1;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
     for (uint32_t i = 0; i < 0x40000000u; ++i) {
@@ -58,7 +58,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
 }
 
 // For a block that gives up: its own copies and products in flight get a second to land before it leaves.
-__device__ __noinline__ void drain(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ void drain(uint32_t bar, uint32_t parity) {
     uint64_t t0, t1;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
     for (uint32_t i = 0; i < 0x40000000u && !bar_test(bar, parity); ++i) {

@@ -74,3 +74,31 @@ class Case:
                 p = torch.where(ok, torch.exp(x - lse[b, h, :, None]), 0.0)
                 o[b, :, h], a[b, :, h] = p @ vv, p @ vv.abs()
         return o, lse, a
+
+    def backward(self, q, k, v, table, out, lse, dout):
+        """Gradients in 64 bits from the stored out and lse, as a dict name -> (gradient, sum of |ds| |k| and its like,
+        sum of p (|dp| + |delta|) |k| and its like): what the roundings of ds or p and the binary32 arithmetic scale with."""
+        f64 = dict(dtype=torch.float64, device="cuda")
+        shape = {"dq": q.shape, "dk": k.shape, "dv": v.shape, "dtable": (self.heads_q, max(1, self.buckets))}
+        r = {n: [torch.zeros(s, **f64) for _ in range(3)] for n, s in shape.items()}
+        for b in range(self.batch if self.len_kv else 0):
+            for h in range(self.heads_q):
+                hk = h // (self.heads_q // self.heads_kv)
+                qq, kk, vv, x, ok, at = self.head(q, k, v, table, b, h)
+                l = lse[b, h].double()[:, None]
+                live = l != -math.inf
+                do = torch.where(live, dout[b, :, h].double(), 0.0)
+                o = torch.where(live, out[b, :, h].double(), 0.0)
+                qq = torch.where(live, qq, 0.0)
+                p = torch.where(ok & live, torch.exp(x - l), 0.0)
+                dp, delta = do @ vv.T, (do * o).sum(1, keepdim=True)
+                ds, wide = p * (dp - delta), p * (dp.abs() + delta.abs())
+                terms = ((ds, p, 1), (ds.abs(), p, 2), (wide, p, 3))
+                for n, (e, pp, i) in enumerate(terms):
+                    m = (lambda t: t) if i == 1 else torch.abs
+                    r["dq"][n][b, :, h] += self.scale * (e @ m(kk))
+                    r["dk"][n][b, :, hk] += self.scale * (e.T @ m(qq))
+                    r["dv"][n][b, :, hk] += pp.T @ m(do)
+                    if at is not None:
+                        r["dtable"][n][h] += torch.zeros(self.buckets, **f64).index_add_(0, at.reshape(-1), e.reshape(-1))
+        return r
