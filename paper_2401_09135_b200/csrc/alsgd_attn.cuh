@@ -49,11 +49,19 @@ __device__ __forceinline__ float table_entry(const Bias& s, int head, int bucket
     return s.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(s.table)[i] << 16) : static_cast<const float*>(s.table)[i];
 }
 
-// The bias by distance in the exponent's base 2, lut[r + pad] for -pad <= r <= pad.  Threads [0, threads) fill it.
-__device__ __forceinline__ void fill_lut(const Bias& s, int head, float* lut, int pad, int thread, int threads) {
-    for (int i = thread; i <= 2 * pad; i += threads) {
-        const float v = table_entry(s, head, bucket_of(s, i - pad));
-        lut[i] = v <= kMaskedOut ? -INFINITY : v * kLog2e;
+// Bucket of every distance r = at - pad, once per block.
+__device__ __forceinline__ void fill_buckets(const Bias& s, uint8_t* bucket, int pad, int thread, int threads) {
+    for (int i = thread; i <= 2 * pad; i += threads) bucket[i] = (uint8_t)bucket_of(s, i - pad);
+}
+
+// One head's bias by distance in the exponent's base 2: lut[r + pad] for low <= r <= high, and the two ends.
+__device__ __forceinline__ void fill_lut(const Bias& s, int head, const uint8_t* bucket, float* lut, int pad, int low, int high, int thread, int threads) {
+    low = max(low, -pad);
+    high = min(high, pad);
+    for (int i = low - 2 + thread; i <= max(high, low - 1); i += threads) {
+        const int at = (i == low - 2 ? -pad : i == low - 1 ? pad : i) + pad;
+        const float v = table_entry(s, head, bucket[at]);
+        lut[at] = v <= kMaskedOut ? -INFINITY : v * kLog2e;
     }
 }
 
@@ -64,6 +72,84 @@ __device__ __forceinline__ Span span_of(const Bias& s, int r_min, int r_max) {
 }
 
 bool bwd_wait_word(unsigned* out);     // alsgd_attn_bwd.cu
+
+// An operand as the copy engine reads it.  A dimension with step 0 (an operand broadcast over the batch or the heads)
+// has extent 1 there and its coordinate is multiplied away.
+struct Operand {
+    CUtensorMap map;
+    int head_mul, batch_mul;
+    uint16_t* data;
+    int64_t step_pos, step_head, step_batch;   // in elements; 0 where the extent is 1
+};
+
+// Zeros in a row of an operand: an item without tiles has nothing to compute.
+__device__ __forceinline__ void zero_row(const Operand& t, int dim, int batch, int head, int pos) {
+    uint16_t* p = t.data + (int64_t)batch * t.step_batch + (int64_t)head * t.step_head + (int64_t)pos * t.step_pos;
+    for (int x = 0; x < dim; x += 8) *reinterpret_cast<uint4*>(p + x) = make_uint4(0, 0, 0, 0);
+}
+
+// 32 columns of a row of results (fp32 in registers), scaled, rounded and stored.
+__device__ __forceinline__ void store_columns(const Operand& t, int dim, int batch, int head, int pos, int from, const uint32_t (&x)[32], float scale) {
+    uint16_t* p = t.data + (int64_t)batch * t.step_batch + (int64_t)head * t.step_head + (int64_t)pos * t.step_pos + from;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (from + 8 * i >= dim) break;
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = alsgd_ops::pack_bf16(__uint_as_float(x[8 * i + 2 * e]) * scale, __uint_as_float(x[8 * i + 2 * e + 1]) * scale);
+        *reinterpret_cast<uint4*>(p + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// The tiles of a block's work items, one after the other.  item_at(ARGS, i) finds an item, whose `n` is the number of tiles;
+// items without any are passed over, by every warp alike: a barrier's phases must not run past one that waits on it.
+template <typename ARGS, typename ITEM>
+struct Cursor {
+    ITEM item;
+    int i, ordinal, j, tile;           // item, how many of the block's items with tiles came before it, tile within it, tiles before this one
+    bool more;
+    __device__ __forceinline__ void settle(const ARGS& a) {
+        for (; i < a.items; i += gridDim.x) {
+            item = item_at(a, i);
+            if (item.n > 0) break;
+        }
+        more = i < a.items;
+        j = 0;
+    }
+    __device__ __forceinline__ void start(const ARGS& a) {
+        i = blockIdx.x;
+        ordinal = tile = 0;
+        settle(a);
+    }
+    __device__ __forceinline__ void next(const ARGS& a) {
+        ++tile;
+        if (++j < item.n) return;
+        i += gridDim.x;
+        ++ordinal;
+        settle(a);
+    }
+};
+
+// 32 columns x 32 rows of results (fp32 in registers, one row per lane) scaled, rounded and stored as one box; `staging`
+// is 2 KB of the warp's own.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, const uint32_t (&x)[32], float scale, uint8_t* staging, int lane, int c, int pos, int head, int batch) {
+    uint8_t* line = staging + lane * 64;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = alsgd_ops::pack_bf16(__uint_as_float(x[8 * i + 2 * e]) * scale, __uint_as_float(x[8 * i + 2 * e + 1]) * scale);
+        *reinterpret_cast<uint4*>(line + ((i ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    alsgd_tc::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+        alsgd_tc::tma_store4(map, alsgd_tc::smem_u32(staging), c, pos, head, batch);
+        alsgd_tc::tma_store_commit();
+    }
+}
 
 // ---- host ---------------------------------------------------------------------------------------------------
 
@@ -77,6 +163,12 @@ inline void bucket_limits(int per_side, int near, int max_distance, Bias* out) {
         out->limits[out->n_limits++] = (int)(fabsl(t - whole) < 1e-10L * t ? whole : ceill(t));
     }
     out->far = out->n_limits ? out->limits[out->n_limits - 1] : near;
+}
+
+// Blocks of a persistent kernel that are resident together: `per_sm` of them, as far as shared memory allows.
+inline int blocks_at_once(size_t smem, int per_sm) {
+    const size_t room = 228 * 1024, fit = room / (smem + 1024);        // an SM's; each block takes 1 KB for itself
+    return alsgd_ops::kSMs * (fit < (size_t)per_sm ? (int)fit : per_sm);
 }
 
 inline int make_bias(const alsgd_attn_desc& d, const void* table, Bias* out) {
@@ -144,13 +236,6 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
     return s;
 }
 
-// An operand as the copy engine reads it.  A dimension with step 0 (an operand broadcast over the batch or the heads)
-// has extent 1 there and its coordinate is multiplied away.
-struct Operand {
-    CUtensorMap map;
-    int head_mul, batch_mul;
-};
-
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -167,8 +252,9 @@ inline EncodeTiled encode_tiled() {
     return fn;
 }
 
-// Boxes of 64 elements x `rows` positions of one head of one sequence, 128-byte swizzle, zeros outside.
-inline int make_operand(const alsgd_attn_tensor& t, uint32_t batch, uint32_t len, uint32_t heads, uint32_t dim, uint32_t rows, Operand* out) {
+// Boxes of `cols` elements (64, or 32 for results) x `rows` positions of one head of one sequence, swizzled over their
+// 128- or 64-byte rows, zeros outside.
+inline int make_operand(const alsgd_attn_tensor& t, uint32_t batch, uint32_t len, uint32_t heads, uint32_t dim, uint32_t rows, uint32_t cols, Operand* out) {
     EncodeTiled encode = encode_tiled();
     if (!encode) return ALSGD_E_CUDA;
     const uint64_t extent[3] = {len, heads, batch};
@@ -183,9 +269,13 @@ inline int make_operand(const alsgd_attn_tensor& t, uint32_t batch, uint32_t len
     }
     out->head_mul = mul[1];
     out->batch_mul = mul[2];
-    const cuuint32_t box[4] = {64, rows, 1, 1}, unit[4] = {1, 1, 1, 1};
+    out->data = static_cast<uint16_t*>(t.data);
+    out->step_pos = mul[0] ? step[0] : 0;
+    out->step_head = mul[1] ? step[1] : 0;
+    out->step_batch = mul[2] ? step[2] : 0;
+    const cuuint32_t box[4] = {cols, rows, 1, 1}, unit[4] = {1, 1, 1, 1};
     const CUresult r = encode(&out->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, t.data, size, bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? ALSGD_OK : ALSGD_E_ARG;
 }
 

@@ -2,13 +2,16 @@
 //
 //   x_ij = scale q_i.k_j + T[bucket(j - i)]  over the allowed j,   lse_i = log sum_j e^x_ij,   o_i = sum_j e^(x_ij - lse_i) v_j
 //
-// One block per 128 query rows of one head.  Keys come in tiles of 128; a row's running maximum and sum are kept by
-// one thread (the row's lane of tensor memory), so a tile is read once and nothing of size len_q x len_kv exists.
-//   warps 0-3  softmax: scores from tensor memory, maximum, e^x, sum; probabilities (bf16) back to tensor memory
-//   warp 4     copies q, then k and v tiles, through tensor maps
-//   warp 5     issues the products  S = q k^T  (operands in shared memory)  and  O += P v  (P in tensor memory)
-// Two blocks share an SM (256 tensor memory columns and about 100 KB each): one block's products and its start and
-// end run under the other's exponentials.
+// A work item is 128 query rows of one head; the resident blocks walk the items, those with the most keys first.  Keys come
+// in tiles; a row's running maximum and sum are kept by one thread (the row's lane of tensor memory), so a tile is read
+// once and nothing of size len_q x len_kv exists.
+//   warps 0-3  softmax: scores from tensor memory, maximum, e^x, sum; probabilities (bf16) back to tensor memory, over the
+//              scores they come from
+//   warp 4     copies q, k and v tiles through tensor maps and issues the products  S = q k^T  (operands in shared memory)
+//              and  O += P v  (P in tensor memory)
+// Within a block a tile's steps follow one another: S, softmax, O.  What fills the machine is other blocks: with heads of
+// up to 64, tiles of 64 keys take 128 columns of tensor memory and 52 KB, so four blocks share an SM and one's products,
+// copies and waits run under the others' exponentials.  Wider heads take tiles of 128 keys, two blocks per SM.
 //
 // Exponents are taken in base 2 relative to a reference that follows the running maximum only when that has grown by
 // more than 8: the sums then hold values up to 2^8, which binary32 and bf16 hold as well as values up to 1, and O in
@@ -22,11 +25,13 @@ using namespace alsgd_tc;
 
 namespace {
 
-constexpr int kRows = 128;              // query rows of a block
-constexpr int kKeys = 128;              // keys of a tile
-constexpr int kThreads = 192;
+constexpr int kRows = 128;              // query rows of an item
+constexpr int kSoftmax = 128;           // threads
+constexpr int kThreads = kSoftmax + 32;
+constexpr int kAll = 1;                 // named barrier of the softmax threads
+constexpr int kPolyOf4 = 0;             // of four pairs of exponentials, how many take the polynomial
 constexpr float kRescaleAt = 8.0f;
-constexpr uint32_t kTileBytes = 128 * 128;     // 128 rows of 64 bf16
+constexpr uint32_t kRowsBytes = kRows * 128;   // 64 bf16 of each row
 
 struct FwdArgs {
     Operand q, k, v, o;
@@ -34,68 +39,86 @@ struct FwdArgs {
     Bias bias;
     float* lse;
     int pad;                            // reach of the bias table by distance
+    int row_blocks, items, keys;
 };
 
-// HALVES: 64-column halves of the head dimension (1 up to 64, 2 up to 128).  With one half there is room to keep P beside S,
-// so the next tile's scores are computed while this tile's exponentials are; with two P takes S's place.
+// HALVES: 64-column halves of the head dimension (1 up to 64, 2 up to 128).
 template <int HALVES>
 struct FwdPlan {
-    static constexpr int stages = HALVES == 1 ? 2 : 1;
-    static constexpr bool p_apart = HALVES == 1;
-    static constexpr uint32_t columns = 256;
-    static constexpr uint32_t s_col = 0, p_col = p_apart ? 128 : 0, o_col = p_apart ? 192 : 128;
-    static constexpr uint32_t q_bytes = HALVES * kTileBytes, kv_bytes = HALVES * kTileBytes;
+    static constexpr int keys = HALVES == 1 ? 64 : 128, blocks = HALVES == 1 ? 4 : 2, stages = HALVES == 1 ? 2 : 1;
+    static constexpr uint32_t columns = HALVES == 1 ? 128 : 256, s_col = 0, p_col = 0, o_col = keys;
+    static constexpr uint32_t half_bytes = keys * 128;         // 64 columns of a k or v tile
+    static constexpr uint32_t q_bytes = HALVES * kRowsBytes, kv_bytes = HALVES * half_bytes;
     static constexpr uint32_t tiles_bytes = q_bytes + 2 * stages * kv_bytes;
-    static constexpr uint32_t bars = 6 + 4 * stages;
+    static constexpr uint32_t bars = 6 + 2 * stages;
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 128;
 };
 
 template <int HALVES>
 size_t fwd_smem(int pad, bool bias) {
-    return 1024 + FwdPlan<HALVES>::tiles_bytes + 256 + (bias ? (2 * pad + 1) * sizeof(float) : 0);
+    return 1024 + FwdPlan<HALVES>::fixed_bytes + (bias ? (2 * pad + 1) * (sizeof(float) + 1) : 0);
+}
+
+struct Item {
+    int b, h, q0, len, keys, n;        // sequence, head, first row, valid keys, keys any row sees, tiles
+};
+
+__device__ __forceinline__ Item item_at(const FwdArgs& a, int i) {
+    const Shape& sh = a.shape;
+    const int bh = sh.batch * sh.heads_q;
+    Item t;
+    t.q0 = (a.row_blocks - 1 - i / bh) * kRows;
+    t.b = i % bh / sh.heads_q;
+    t.h = i % bh % sh.heads_q;
+    t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
+    t.keys = t.len;
+    if (sh.causal) t.keys = min(t.keys, min(t.q0 + kRows, sh.len_q) + sh.q_pos);
+    t.n = t.keys > 0 ? (t.keys + a.keys - 1) / a.keys : 0;
+    return t;
 }
 
 template <int HALVES, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_constant__ FwdArgs a) {
+__global__ void __launch_bounds__(kThreads, FwdPlan<HALVES>::blocks) attn_fwd_kernel(const __grid_constant__ FwdArgs a) {
     using Plan = FwdPlan<HALVES>;
-    constexpr int ST = Plan::stages;
+    constexpr int ST = Plan::stages, KEYS = Plan::keys;
     extern __shared__ uint8_t raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const uint32_t base = smem_u32(smem);
     const uint32_t sq = base, sk = sq + Plan::q_bytes, sv = sk + ST * Plan::kv_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
-    const uint32_t q_full = bars, s_full = bars + 8, s_free = bars + 16, p_ready = bars + 24, pv_done = bars + 32, drained = bars + 40;
-    const uint32_t k_full = bars + 48, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST, v_empty = v_full + 8 * ST;
+    const uint32_t q_full = bars, s_full = bars + 8, p_ready = bars + 16, pv_done = bars + 24, o_free = bars + 32, drained = bars + 40;
+    const uint32_t k_full = bars + 48, v_full = k_full + 8 * ST;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
-    float* lut = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 256);
+    float* lut = reinterpret_cast<float*>(smem + Plan::fixed_bytes);
+    uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(lut + 2 * a.pad + 1);
 
     const Shape& sh = a.shape;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.x / sh.heads_q, h = blockIdx.x % sh.heads_q, hk = h / sh.group;
-    const int q0 = (gridDim.y - 1 - blockIdx.y) * kRows;       // the longest rows of a causal mask start first
 
     if (threadIdx.x == 0) {
         bar_init(q_full, 1);
         bar_init(s_full, 1);
-        bar_init(s_free, 4);
         bar_init(p_ready, 4);
         bar_init(pv_done, 1);
+        bar_init(o_free, 4);
         bar_init(drained, 1);
         for (int i = 0; i < ST; ++i) {
             bar_init(k_full + 8 * i, 1);
-            bar_init(k_empty + 8 * i, 1);
             bar_init(v_full + 8 * i, 1);
-            bar_init(v_empty + 8 * i, 1);
         }
         words[1] = 0;
         bar_init_fence();
     }
-    if (warp == 5) tmem_alloc(smem_u32(words), Plan::columns);
-    if (threadIdx.x == 128) {
-        tma_prefetch(&a.q.map);
-        tma_prefetch(&a.k.map);
-        tma_prefetch(&a.v.map);
-        tma_prefetch(&a.o.map);
+    if (warp == 4) {
+        tmem_alloc(smem_u32(words), Plan::columns);
+        if (lane == 0) {
+            tma_prefetch(&a.q.map);
+            tma_prefetch(&a.k.map);
+            tma_prefetch(&a.v.map);
+        }
+    } else if (BIAS) {
+        fill_buckets(a.bias, lut_bucket, a.pad, threadIdx.x, kSoftmax);
     }
     tc_fence_before();
     __syncthreads();
@@ -103,246 +126,255 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     const uint32_t tmem = words[0];
     grid_dependency_sync();
 
-    const int len = sh.kv_len ? min(max(sh.kv_len[b], 0), sh.len_kv) : sh.len_kv;
-    int keys = len;                                            // keys that any row of the block sees
-    if (sh.causal) keys = min(keys, min(q0 + kRows, sh.len_q) + sh.q_pos);
-    const int n = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
-
     if (warp == 4) {
-        if (lane == 0 && n > 0) {
-            bar_expect(q_full, Plan::q_bytes);
-            for (int c = 0; c < HALVES; ++c) tma_load4(sq + c * kTileBytes, &a.q.map, q_full, 64 * c, q0, h * a.q.head_mul, b * a.q.batch_mul);
-            int j = 0;
-            bool ok = true;
-            for (; j < n && ok; ++j) {
-                const int st = j % ST;
-                const uint32_t free_parity = ((j / ST) & 1) ^ 1;
-                ok = wait(k_empty + 8 * st, free_parity, dead, 1);
-                if (!ok) break;
-                bar_expect(k_full + 8 * st, Plan::kv_bytes);
+        // The warp walks together and one lane issues: what a product is given stays the same for all lanes.
+        constexpr uint32_t desc_s = mma_desc(KEYS, false), desc_o = mma_desc(64 * HALVES, true);
+        const bool leader = elect_one();
+        const uint64_t q_desc = desc_k_major(sq), k_desc = desc_k_major(sk), v_desc = desc_n_major(sv, Plan::half_bytes);
+        auto fetch_q = [&](const Item& t) {
+            if (leader) {
+                bar_expect(q_full, Plan::q_bytes);
                 for (int c = 0; c < HALVES; ++c)
-                    tma_load4(sk + st * Plan::kv_bytes + c * kTileBytes, &a.k.map, k_full + 8 * st, 64 * c, j * kKeys, hk * a.k.head_mul, b * a.k.batch_mul);
-                ok = wait(v_empty + 8 * st, free_parity, dead, 2);
-                if (!ok) {                                     // this tile's k copy is in flight
-                    drain(k_full + 8 * st, (j / ST) & 1);
-                    break;
-                }
-                bar_expect(v_full + 8 * st, Plan::kv_bytes);
+                    tma_load4(sq + c * kRowsBytes, &a.q.map, q_full, 64 * c, t.q0, t.h * a.q.head_mul, t.b * a.q.batch_mul);
+            }
+        };
+        auto fetch = [&](const Operand& x, uint32_t full, uint32_t to, const Item& t, int j, int st) {
+            if (leader) {
+                bar_expect(full + 8 * st, Plan::kv_bytes);
                 for (int c = 0; c < HALVES; ++c)
-                    tma_load4(sv + st * Plan::kv_bytes + c * kTileBytes, &a.v.map, v_full + 8 * st, 64 * c, j * kKeys, hk * a.v.head_mul, b * a.v.batch_mul);
+                    tma_load4(to + st * Plan::kv_bytes + c * Plan::half_bytes, &x.map, full + 8 * st, 64 * c, j * KEYS, t.h / sh.group * x.head_mul, t.b * x.batch_mul);
             }
-            // every copy has landed before the block may leave, whoever else has given up
-            drain(q_full, 0);
-            for (int i = max(0, j - ST); i < j; ++i) {
-                drain(k_full + 8 * (i % ST), (i / ST) & 1);
-                drain(v_full + 8 * (i % ST), (i / ST) & 1);
-            }
+        };
+        Cursor<FwdArgs, Item> at, load;                        // of the products, and of the k and v copies, ST tiles ahead
+        at.start(a);
+        load = at;
+        if (at.more) fetch_q(at.item);
+        for (int st = 0; st < ST && load.more; ++st) {
+            fetch(a.k, k_full, sk, load.item, load.j, st);
+            fetch(a.v, v_full, sv, load.item, load.j, st);
+            load.next(a);
         }
-    } else if (warp == 5) {
-        if (lane == 0 && n > 0) {
-            constexpr uint32_t desc_s = mma_desc(kKeys, false), desc_o = mma_desc(64 * HALVES, true);
-            const int steps = (sh.dim + 15) / 16;
-            auto scores = [&](int j) {
-                const int st = j % ST;
-                if (!wait(k_full + 8 * st, (j / ST) & 1, dead, 4)) return false;
-                tc_fence_after();
-                for (int i = 0; i < steps; ++i) {
-                    const uint32_t at = (i >> 2) * kTileBytes + (i & 3) * 32;
-                    mma_ss(tmem + Plan::s_col, desc_k_major(sq + at), desc_k_major(sk + st * Plan::kv_bytes + at), desc_s, i > 0);
-                }
-                mma_commit(k_empty + 8 * st);
+        int items = 0;                                         // whose O has been started
+        bool v_due = false;                                    // a v copy may start now that the place of the last tile's is free
+        while (at.more) {
+            const int st = at.tile % ST;
+            const uint32_t full_parity = (at.tile / ST) & 1, parity = at.tile & 1;
+            if (at.j == 0) wait_warp(q_full, at.ordinal & 1, dead, 1);
+            wait_warp(k_full + 8 * st, full_parity, dead, 2);
+            tc_fence_after();
+            const uint64_t kd = k_desc + st * (Plan::kv_bytes >> 4);
+            if (leader) {
+#pragma unroll
+                for (int i = 0; i < 4 * HALVES; ++i)           // 16 elements of the head each; behind dim they are zeros
+                    mma_ss(tmem + Plan::s_col, q_desc + (((i >> 2) * kRowsBytes + (i & 3) * 32) >> 4),
+                           kd + (((i >> 2) * Plan::half_bytes + (i & 3) * 32) >> 4), desc_s, i > 0);
                 mma_commit(s_full);
-                return true;
-            };
-            bool ok = wait(q_full, 0, dead, 8) && scores(0);
-            for (int j = 0; j < n && ok; ++j) {
-                const int st = j % ST;
-                if (Plan::p_apart && j + 1 < n) {
-                    ok = wait(s_free, j & 1, dead, 16) && scores(j + 1);
-                    if (!ok) break;
-                }
-                ok = wait(p_ready, j & 1, dead, 32) && wait(v_full + 8 * st, (j / ST) & 1, dead, 64);
-                if (!ok) break;
-                tc_fence_after();
-                const int k_steps = min(kKeys, keys - j * kKeys + 15) / 16;      // 16 keys each; those nobody sees are left out
-                for (int i = 0; i < k_steps; ++i)
-                    mma_ts(tmem + Plan::o_col, tmem + Plan::p_col + 8 * i, desc_n_major(sv + st * Plan::kv_bytes + i * 2048, kTileBytes),
-                           desc_o, j > 0 || i > 0);
-                mma_commit(v_empty + 8 * st);
-                mma_commit(pv_done);
-                if (!Plan::p_apart && j + 1 < n) ok = wait(pv_done, j & 1, dead, 128) && scores(j + 1);
             }
+            if (v_due) {
+                fetch(a.v, v_full, sv, load.item, load.j, load.tile % ST);
+                load.next(a);
+                v_due = false;
+            }
+            if (at.j == 0) {                                   // the last item's O has been read
+                wait_warp(o_free, (items & 1) ^ 1, dead, 4);
+                ++items;
+            }
+            wait_warp(v_full + 8 * st, full_parity, dead, 8);
+            wait_warp(p_ready, parity, dead, 16);
+            if (__any_sync(0xFFFFFFFFu, *dead)) break;
+            tc_fence_after();
+            const int keys = at.item.keys - at.j * KEYS;       // groups of 16 that nobody sees are left out
+            const uint64_t vd = v_desc + st * (Plan::kv_bytes >> 4);
+            const bool more = at.j > 0;
+            if (leader) {
+#pragma unroll
+                for (int i = 0; i < KEYS / 16; ++i)
+                    if (16 * i < keys) mma_ts(tmem + Plan::o_col, tmem + Plan::p_col + i * 8, vd + i * 128, desc_o, more || i > 0);
+                mma_commit(pv_done);
+            }
+            // the scores of this tile have been formed: its k's place is free, and behind the item's last tile q's
+            if (load.more) {
+                fetch(a.k, k_full, sk, load.item, load.j, st);
+                v_due = true;
+            }
+            at.next(a);
+            if (at.more && at.j == 0) fetch_q(at.item);
+            wait_warp(pv_done, parity, dead, 32);
+        }
+        // everything in flight lands before the block may leave, whoever has given up
+        if (leader) {
             mma_commit(drained);
             drain(drained, 0);
+            if (*dead) {
+                drain(q_full, 0);
+                drain(q_full, 1);
+                for (int i = 0; i < ST; ++i) {
+                    drain(k_full + 8 * i, 0);
+                    drain(k_full + 8 * i, 1);
+                    drain(v_full + 8 * i, 0);
+                    drain(v_full + 8 * i, 1);
+                }
+            }
         }
     } else {
         const int row = threadIdx.x;
-        const int pos = q0 + row + sh.q_pos;                   // the row's position among the keys
         const uint32_t lanes = tmem + ((uint32_t)warp << 21);
-        if (BIAS) {
-            fill_lut(a.bias, h, lut, a.pad, row, 128);
-            asm volatile("bar.sync 1, 128;" ::: "memory");
-        }
-        float ref = -INFINITY, sum = 0.0f;
-        bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            const int k0 = j * kKeys;
-            ok = wait_warp(s_full, j & 1, dead, 256);
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t v[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(v[c], lanes + Plan::s_col + 32 * c);
-            tmem_wait_ld();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_use(v[c]);
-            if (Plan::p_apart) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(s_free);
-            }
-
-            // x = v * mul + add, in base 2
-            float mul = sh.scale_log2, add = 0.0f;
-            if (BIAS) {
-                const Span span = span_of(a.bias, k0 - (q0 + kRows - 1 + sh.q_pos), k0 + kKeys - 1 - (q0 + sh.q_pos));
-                if (span == kSpanMixed) {
-                    const float* at = lut + a.pad + k0 - pos;
-#pragma unroll
-                    for (int c = 0; c < 128; ++c) v[c >> 5][c & 31] = __float_as_uint(fmaf(__uint_as_float(v[c >> 5][c & 31]), mul, at[c]));
-                    mul = 1.0f;
-                } else {
-                    add = lut[span == kSpanFarLeft ? 0 : 2 * a.pad];
+        int tile = 0;
+        for (int i = blockIdx.x; i < a.items; i += gridDim.x) {
+            const Item t = item_at(a, i);
+            const bool inside = t.q0 + row < sh.len_q;
+            float* lse = a.lse + ((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row;
+            if (t.n == 0) {
+                if (inside) {
+                    zero_row(a.o, sh.dim, t.b, t.h, t.q0 + row);
+                    *lse = -INFINITY;
                 }
+                continue;
             }
-            if (k0 + kKeys > len || (sh.causal && k0 + kKeys - 1 > q0 + sh.q_pos)) {
-                const int allowed = (sh.causal ? min(len, pos + 1) : len) - k0;
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (c >= allowed) v[c >> 5][c & 31] = 0xFF800000u;
+            const int pos = t.q0 + row + sh.q_pos;             // the row's position among the keys
+            if (BIAS) {
+                const int first = t.q0 + sh.q_pos;             // distances from the last row's first key to the first row's last
+                sync_threads(kAll, kSoftmax);
+                fill_lut(a.bias, t.h, lut_bucket, lut, a.pad, -(first + kRows - 1), sh.causal ? 0 : t.keys - 1 - first, threadIdx.x, kSoftmax);
+                sync_threads(kAll, kSoftmax);
             }
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(v[c >> 5][c & 31]));
-            const float high = fmaf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), mul, add);
-
-            if (j > 0) {                                       // O and P of the last tile are free
-                ok = wait_warp(pv_done, (j - 1) & 1, dead, 512);
-                if (!ok) break;
+            float ref = -INFINITY, sum = 0.0f;
+            for (int j = 0; j < t.n; ++j, ++tile) {
+                const int k0 = j * KEYS;
+                wait_warp(s_full, tile & 1, dead, 64);         // also: O holds the tiles before, P's place is free
                 tc_fence_after();
-            }
-            const bool grown = high > ref + kRescaleAt || (ref == -INFINITY && high > -INFINITY);
-            if (__any_sync(0xFFFFFFFFu, grown)) {
-                const float next = grown ? high : ref;
-                const float factor = next == -INFINITY ? 1.0f : exp2_fast(ref - next);
-                ref = next;
-                sum *= factor;
-                if (j > 0) {
+                uint32_t v[KEYS / 32][32];
 #pragma unroll
-                    for (int c = 0; c < 2 * HALVES; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32(o, lanes + Plan::o_col + 32 * c);
-                        tmem_wait_ld();
-                        tmem_use(o);
+                for (int c = 0; c < KEYS / 32; ++c) tmem_ld32(v[c], lanes + Plan::s_col + 32 * c);
+                tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
-                        tmem_st32(lanes + Plan::o_col + 32 * c, o);
+                for (int c = 0; c < KEYS / 32; ++c) tmem_use(v[c]);
+
+                // x = v * mul + add, in base 2
+                float mul = sh.scale_log2, add = 0.0f;
+                if (BIAS) {
+                    const Span span = span_of(a.bias, k0 - (t.q0 + kRows - 1 + sh.q_pos), k0 + KEYS - 1 - (t.q0 + sh.q_pos));
+                    if (span == kSpanMixed) {
+                        const float* at = lut + a.pad + k0 - pos;
+#pragma unroll
+                        for (int c = 0; c < KEYS; ++c) v[c >> 5][c & 31] = __float_as_uint(fmaf(__uint_as_float(v[c >> 5][c & 31]), mul, at[c]));
+                        mul = 1.0f;
+                    } else {
+                        add = lut[span == kSpanFarLeft ? 0 : 2 * a.pad];
                     }
                 }
-            }
-            const float off = add - (ref == -INFINITY ? 0.0f : ref);
-            const uint64_t mul2v = pack2(mul, mul), off2 = pack2(off, off);
-            uint64_t part[2] = {0, 0};
+                if (k0 + KEYS > t.len || (sh.causal && k0 + KEYS - 1 > t.q0 + sh.q_pos)) {
+                    const int allowed = (sh.causal ? min(t.len, pos + 1) : t.len) - k0;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t p[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float x, y;
-                    unpack2(fma2(pack2(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), mul2v, off2), x, y);
-                    x = exp2_fast(x);
-                    y = exp2_fast(y);
-                    part[i & 1] = add2(part[i & 1], pack2(x, y));
-                    p[i] = pack_bf16(x, y);
+                    for (int c = 0; c < KEYS; ++c)
+                        if (c >= allowed) v[c >> 5][c & 31] = 0xFF800000u;
                 }
-                tmem_st16(lanes + Plan::p_col + 16 * c, p);
-            }
-            float s0, s1;
-            unpack2(add2(part[0], part[1]), s0, s1);
-            sum += s0 + s1;
-            if (k0 + kKeys > len && len < sh.len_kv) {
-                // v rows behind the sequence's end are whatever the caller has there; 0 * NaN must not reach O
-                const int st = j % ST;
-                ok = wait_warp(v_full + 8 * st, (j / ST) & 1, dead, 1024);
-                if (!ok) break;
-                if (k0 + row >= len) {
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < HALVES; ++c)
+                for (int c = 0; c < KEYS; c += 2)
+                    top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1]));
+                const float high = fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);
+
+                const bool grown = high > ref + kRescaleAt || (ref == -INFINITY && high > -INFINITY);
+                if (__any_sync(0xFFFFFFFFu, grown)) {
+                    const float next = grown ? high : ref;
+                    const float factor = next == -INFINITY ? 1.0f : exp2_fast(ref - next);
+                    ref = next;
+                    sum *= factor;
+                    if (j > 0) {
+                        // eight columns at a time: the scores hold the registers
+#pragma unroll 1
+                        for (int c = 0; c < 64 * HALVES; c += 8) {
+                            uint32_t o[8];
+                            tmem_ld8(o, lanes + Plan::o_col + c);
+                            tmem_wait_ld();
+                            tmem_use(o);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            *reinterpret_cast<uint4*>(smem + (sv - base) + st * Plan::kv_bytes + c * kTileBytes + row * 128 + 16 * i) = make_uint4(0, 0, 0, 0);
+                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st8(lanes + Plan::o_col + c, o);
+                        }
+                    }
                 }
-                fence_async_smem();
+                if (!(high < INFINITY)) ref = NAN;             // an infinite score or a NaN: the row's result is NaN
+                const float off = add - (ref == -INFINITY ? 0.0f : ref);
+                const uint64_t mul2v = pack2(mul, mul), off2 = pack2(off, off);
+                uint64_t part[2] = {0, 0};
+#pragma unroll
+                for (int c = 0; c < KEYS / 32; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint64_t xy = fma2(pack2(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), mul2v, off2);
+                        float x, y;
+                        if ((e & 3) < kPolyOf4) {
+                            exp2_poly(xy, x, y);
+                        } else {
+                            unpack2(xy, x, y);
+                            x = exp2_fast(x);
+                            y = exp2_fast(y);
+                        }
+                        part[e & 1] = add2(part[e & 1], pack2(x, y));
+                        p[e] = pack_bf16(x, y);
+                    }
+                    tmem_st16(lanes + Plan::p_col + 16 * c, p);
+                }
+                float s0, s1;
+                unpack2(add2(part[0], part[1]), s0, s1);
+                sum += s0 + s1;
+                if (k0 + KEYS > t.len && t.len < sh.len_kv) {
+                    // v rows behind the sequence's end are whatever the caller has there; 0 * NaN must not reach O
+                    const int st = tile % ST;
+                    wait_warp(v_full + 8 * st, (tile / ST) & 1, dead, 128);
+                    if (row < KEYS && k0 + row >= t.len) {
+#pragma unroll
+                        for (int c = 0; c < HALVES; ++c)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                *reinterpret_cast<uint4*>(smem + (sv - base) + st * Plan::kv_bytes + c * Plan::half_bytes + row * 128 + 16 * e) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_ready);
             }
-            tmem_wait_st();
+            wait_warp(pv_done, (tile - 1) & 1, dead, 256);
+            tc_fence_after();
+            const bool none = ref == -INFINITY;                // no allowed key
+            const float inv = none ? 0.0f : 1.0f / sum + (ref - ref);
+            uint32_t o[HALVES * 2][32];
+#pragma unroll
+            for (int c = 0; c < 2 * HALVES; ++c) tmem_ld32(o[c], lanes + Plan::o_col + 32 * c);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 2 * HALVES; ++c) tmem_use(o[c]);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_ready);
-        }
-        if (n > 0 && ok) ok = wait_warp(pv_done, (n - 1) & 1, dead, 2048);
-        if (ok && q0 + 32 * warp < sh.len_q) {
-            tc_fence_after();
-            const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);      // a NaN stays one
-            // q's place in shared memory is free (its last product has completed): the rows go out through it
+            if (lane == 0) bar_arrive(o_free);
+            if (inside) {
 #pragma unroll
-            for (int c = 0; c < 2 * HALVES; ++c) {
-                uint32_t o[32];
-                if (n > 0) {
-                    tmem_ld32(o, lanes + Plan::o_col + 32 * c);
-                    tmem_wait_ld();
-                    tmem_use(o);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0;
-                }
-                uint8_t* line = smem + (c >> 1) * kTileBytes + row * 128;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w[e] = pack_bf16(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-                    *reinterpret_cast<uint4*>(line + ((((c & 1) * 4 + i) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                for (int c = 0; c < 2 * HALVES; ++c) store_columns(a.o, sh.dim, t.b, t.h, t.q0 + row, 32 * c, o[c], inv);
+                *lse = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                for (int c = 0; c < HALVES; ++c)
-                    if (64 * c < sh.dim)
-                        tma_store4(&a.o.map, sq + c * kTileBytes + warp * 4096, 64 * c, q0 + 32 * warp, h * a.o.head_mul, b * a.o.batch_mul);
-                tma_store_commit();
-            }
-            if (q0 + row < sh.len_q)
-                a.lse[((size_t)b * sh.heads_q + h) * sh.len_q + q0 + row] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
-            if (lane == 0) tma_store_wait_read();
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == 4) {
         tc_fence_after();
         tmem_free(tmem, Plan::columns);
     }
 }
 
 template <int HALVES, bool BIAS>
-int launch_fwd(const FwdArgs& a, cudaStream_t s) {
+int launch_fwd(FwdArgs& a, cudaStream_t s) {
     const size_t smem = fwd_smem<HALVES>(a.pad, BIAS);
     if (cudaFuncSetAttribute(attn_fwd_kernel<HALVES, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ALSGD_E_CUDA;
-    const dim3 grid(a.shape.batch * a.shape.heads_q, (a.shape.len_q + kRows - 1) / kRows);
-    return launch_dependent(attn_fwd_kernel<HALVES, BIAS>, grid, dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    const int wave = blocks_at_once(smem, FwdPlan<HALVES>::blocks);
+    return launch_dependent(attn_fwd_kernel<HALVES, BIAS>, dim3(a.items < wave ? a.items : wave), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK
+                                                                                                                                             : ALSGD_E_CUDA;
 }
 
 }  // namespace
@@ -366,12 +398,17 @@ extern "C" int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     a.shape = make_shape(d, kv_len);
     make_bias(d, table, &a.bias);
     a.lse = lse;
-    a.pad = a.bias.far + kRows + kKeys;
-    if ((rc = make_operand(*q, d.batch, d.len_q, d.heads_q, d.dim, kRows, &a.q)) != ALSGD_OK) return rc;
-    if ((rc = make_operand(*o, d.batch, d.len_q, d.heads_q, d.dim, 32, &a.o)) != ALSGD_OK) return rc;
+    a.keys = d.dim <= 64 ? FwdPlan<1>::keys : FwdPlan<2>::keys;
+    a.pad = a.bias.far + kRows + a.keys;
+    a.row_blocks = (int)((d.len_q + kRows - 1) / kRows);
+    const uint64_t items = (uint64_t)d.batch * d.heads_q * a.row_blocks;
+    if (items > 0x7FFFFFFFull - 2 * kSMs) return ALSGD_E_RANGE;
+    a.items = (int)items;
+    if ((rc = make_operand(*q, d.batch, d.len_q, d.heads_q, d.dim, kRows, 64, &a.q)) != ALSGD_OK) return rc;
+    if ((rc = make_operand(*o, d.batch, d.len_q, d.heads_q, d.dim, 32, 64, &a.o)) != ALSGD_OK) return rc;
     // without keys the kernel touches neither map
-    if ((rc = make_operand(d.len_kv ? *k : *q, d.batch, d.len_kv ? d.len_kv : d.len_q, d.len_kv ? d.heads_kv : d.heads_q, d.dim, kKeys, &a.k)) != ALSGD_OK) return rc;
-    if ((rc = make_operand(d.len_kv ? *v : *q, d.batch, d.len_kv ? d.len_kv : d.len_q, d.len_kv ? d.heads_kv : d.heads_q, d.dim, kKeys, &a.v)) != ALSGD_OK) return rc;
+    if ((rc = make_operand(d.len_kv ? *k : *q, d.batch, d.len_kv ? d.len_kv : d.len_q, d.len_kv ? d.heads_kv : d.heads_q, d.dim, a.keys, 64, &a.k)) != ALSGD_OK) return rc;
+    if ((rc = make_operand(d.len_kv ? *v : *q, d.batch, d.len_kv ? d.len_kv : d.len_q, d.len_kv ? d.heads_kv : d.heads_q, d.dim, a.keys, 64, &a.v)) != ALSGD_OK) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (d.dim <= 64) return d.buckets ? launch_fwd<1, true>(a, s) : launch_fwd<1, false>(a, s);
     return d.buckets ? launch_fwd<2, true>(a, s) : launch_fwd<2, false>(a, s);

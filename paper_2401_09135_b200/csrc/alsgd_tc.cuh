@@ -33,44 +33,48 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
 // What a wait that ran out leaves behind, read by alsgd_attn_status (one word per device and source file).
 static __device__ unsigned int g_wait_error;
 
-// Every wait in these kernels ends: after two seconds it records `code`, marks the block as dead (so that its other
-// waits give up at once) and returns false.
-constexpr uint64_t kWaitLimitNs = 2000000000ull;
+// Every wait in these kernels ends.  After kWaitTries tries (tenths of a second at least, against waits of
+// microseconds) it records `code` and marks the block as dead, so that the block's other waits end after a few tries; the
+// block then runs to its end on whatever is in its memory.  Nothing is handed back: a result that would have to be carried
+// through the loops costs more than the wait itself, which most often finds its phase complete.
+constexpr uint32_t kWaitTries = 1u << 22;
 
-static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
-    uint64_t t0, t1;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
-    for (uint32_t i = 0; i < 0x40000000u; ++i) {
-        if (bar_test(bar, parity)) return true;
-        if ((i & 63) != 63) continue;
-        if (*dead) return false;
-        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t1));
-        if (t1 - t0 > kWaitLimitNs) break;
-    }
-    *dead = 1;
-    atomicOr(&g_wait_error, code);
-    return false;
-}
-
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
-    if (bar_test(bar, parity)) return true;
-    return wait_slow(bar, parity, dead, code);
-}
-
-// For a block that gives up: its own copies and products in flight get a second to land before it leaves.
-static __device__ __noinline__ void drain(uint32_t bar, uint32_t parity) {
-    uint64_t t0, t1;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
-    for (uint32_t i = 0; i < 0x40000000u && !bar_test(bar, parity); ++i) {
-        if ((i & 63) != 63) continue;
-        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t1));
-        if (t1 - t0 > kWaitLimitNs / 2) break;
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
+    if (bar_test(bar, parity)) return;
+    for (uint32_t i = 1; !bar_test(bar, parity); ++i) {
+        if ((i & 63) != 0) continue;
+        if (*dead) return;
+        if (i >= kWaitTries) {
+            *dead = 1;
+            atomicOr(&g_wait_error, code);
+            return;
+        }
     }
 }
 
-// The same for a whole warp that goes on with warp-wide instructions: all lanes get one answer.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
-    return __all_sync(0xFFFFFFFFu, wait(bar, parity, dead, code));
+// The same for a warp that goes on with warp-wide instructions.
+__device__ __forceinline__ void wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
+    wait(bar, parity, dead, code);
+    __syncwarp();
+}
+
+// For a block that leaves: its own copies and products in flight land first (at once, unless it has given up).
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kWaitTries && !bar_test(bar, parity); ++i) {
+    }
+}
+
+// ---- named barriers ------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void sync_threads(int id, int threads) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Whether `p` holds in any of the threads that meet there.
+__device__ __forceinline__ bool sync_any(int id, int threads, bool p) {
+    uint32_t r;
+    asm volatile("{\n .reg .pred a, b;\n setp.ne.u32 a, %1, 0;\n barrier.cta.red.or.pred b, %2, %3, a;\n selp.u32 %0, 1, 0, b;\n}\n"
+                 : "=r"(r) : "r"((uint32_t)p), "r"(id), "r"(threads) : "memory");
+    return r != 0;
 }
 
 // ---- tensor-map copies (TMA) -----------------------------------------------------------------------------
@@ -135,6 +139,28 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]
           "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_use(uint32_t (&r)[16]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                      "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t (&r)[8], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_use(uint32_t (&r)[8]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -158,6 +184,12 @@ __device__ __forceinline__ uint64_t desc_n_major(uint32_t addr, uint32_t block) 
 // bf16 x bf16 -> fp32, M = 128.
 __host__ __device__ constexpr uint32_t mma_desc(uint32_t n, bool b_n_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_n_major ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
 }
 // D[tmem] (+)= A[smem] B[smem]
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool accumulate) {
@@ -204,6 +236,35 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+
+// The largest of three, or NaN if one is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x for two x at once without the special function unit (16 results a clock on an SM, the bound of an attention
+// kernel's inner loop): x = n + f with n whole and |f| <= 1/2 by adding and subtracting 1.5 * 2^23, a polynomial of degree 4
+// for 2^f (fitted for the least largest relative error on that interval, 2.7e-6 with its roundings; the fast
+// instruction has 2e-7), and n added to the exponent.  x below -126 and NaN are taken as -126: 1e-38 where 2^x would be
+// less, so a caller marks rows that hold a NaN itself; x = +inf gives NaN.
+__device__ __forceinline__ void exp2_poly(uint64_t x2, float& y0, float& y1) {
+    float x0, x1;
+    unpack2(x2, x0, x1);
+    x2 = pack2(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
+    const uint64_t magic = pack2(12582912.0f, 12582912.0f), back = pack2(-12582912.0f, -12582912.0f), minus = pack2(-1.0f, -1.0f);
+    const uint64_t t = add2(x2, magic);
+    const uint64_t f = fma2(add2(t, back), minus, x2);
+    uint64_t p = fma2(f, pack2(0x1.3997d6p-7f, 0x1.3997d6p-7f), pack2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
+    p = fma2(p, f, pack2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
+    p = fma2(p, f, pack2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
+    p = fma2(p, f, pack2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
+    float t0, t1;
+    unpack2(t, t0, t1);
+    unpack2(p, y0, y1);
+    y0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
+    y1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
 }
 
 }  // namespace alsgd_tc

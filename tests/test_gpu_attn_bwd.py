@@ -89,6 +89,15 @@ def test_shared_heads(heads, dim, causal):
     check(Case(batch=2, len_q=140, heads_q=heads[0], heads_kv=heads[1], dim=dim, causal=causal, buckets=32))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_more_items_than_blocks(causal, dim):
+    """Every block walks several items, empty sequences and short ones between full ones."""
+    lens = [(0, 300, 1, 129, 260)[i % 5] for i in range(50)]
+    check(Case(batch=50, len_q=300, heads_q=4, heads_kv=2, dim=dim, causal=causal, buckets=16, kv_len=lens))
+    check(Case(batch=50, len_q=270, heads_q=4, heads_kv=4, dim=dim, causal=causal))
+
+
 @pytest.mark.parametrize("two_sided", [False, True])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("buckets,max_distance", [(2, 2), (4, 5), (16, 64), (32, 128), (32, 1000), (64, 128), (256, 2048), (6, 20)])
