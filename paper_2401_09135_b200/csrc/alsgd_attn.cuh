@@ -17,11 +17,25 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMaskedOut = -1e30f;   // a table entry at or below this takes its bucket out
 
+// Division of 0 <= n < 2^31 by a divisor known at the launch: n * ceil(2^shift / d) >> shift with 2^(shift - 31) >= d, which
+// is exact for those n.  A kernel's walk over its items divides in every warp.
+struct Divide {
+    uint32_t factor, shift;
+    __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * factor >> shift); }
+};
+
+inline Divide divide_by(int d) {
+    uint32_t shift = 31;
+    while ((1ull << (shift - 31)) < (uint64_t)d) ++shift;
+    return {(uint32_t)(((1ull << shift) + d - 1) / d), shift};
+}
+
 struct Shape {
     int batch, heads_q, heads_kv, group, len_q, len_kv, dim;
     int causal, q_pos;
     float scale, scale_log2;
     const int* kv_len;                 // may be null
+    Divide by_heads_q, by_heads_kv, by_all_q, by_all_kv, by_group;     // heads, batch * heads, query heads per key head
 };
 
 // Buckets of a distance: below `near` one each, then up to limits[0], limits[1], ..., the last open.
@@ -54,18 +68,69 @@ __device__ __forceinline__ void fill_buckets(const Bias& s, uint8_t* bucket, int
     for (int i = thread; i <= 2 * pad; i += threads) bucket[i] = (uint8_t)bucket_of(s, i - pad);
 }
 
-// One head's bias by distance in the exponent's base 2: lut[r + pad] for low <= r <= high, and the two ends.
-__device__ __forceinline__ void fill_lut(const Bias& s, int head, const uint8_t* bucket, float* lut, int pad, int low, int high, int thread, int threads) {
-    low = max(low, -pad);
-    high = min(high, pad);
-    for (int i = low - 2 + thread; i <= max(high, low - 1); i += threads) {
-        const int at = (i == low - 2 ? -pad : i == low - 1 ? pad : i) + pad;
-        const float v = table_entry(s, head, bucket[at]);
-        lut[at] = v <= kMaskedOut ? -INFINITY : v * kLog2e;
+// One head's bias by distance in the exponent's base 2, as the tiles that lie within reach of the buckets' edges read it: a
+// thread wants consecutive distances from its own start on, its neighbour the same ones moved by one.  Two copies, the
+// second moved by one element, give every thread aligned pairs whatever its start; they lie 64 bytes (modulo 128) apart,
+// so that a warp's even and odd threads use different banks.
+struct LutShape {
+    int pad;                           // distances start at -pad
+    int copy;                          // floats from one copy to the next
+    int floats;                        // of one table: two copies, and the values of the two far ends
+};
+
+__host__ __device__ inline LutShape lut_shape(int far, int tile_a, int tile_b, bool causal) {
+    LutShape s;
+    s.pad = far + tile_a + tile_b;
+    const int reach = causal ? tile_a + tile_b : s.pad;        // no allowed key lies ahead; masked ones are read, whatever is there
+    s.copy = (s.pad + reach + 2 + 31) / 32 * 32 + 16;
+    s.floats = 2 * s.copy + 16;
+    return s;
+}
+
+// Where a thread reads the bias of distances r, r + 1, ... as pairs.
+__device__ __forceinline__ const float* lut_at(const float* lut, const LutShape& s, int r) {
+    const int x = r + s.pad;
+    return lut + (x & 1 ? s.copy + x - 1 : x);
+}
+__device__ __forceinline__ float lut_far(const float* lut, const LutShape& s, bool right) { return lut[2 * s.copy + right]; }
+
+__device__ __forceinline__ float lut_value(const Bias& s, int head, int bucket) {
+    if (!s.table) return 0.0f;
+    const float v = table_entry(s, head, bucket);
+    return v <= kMaskedOut ? -INFINITY : v * kLog2e;
+}
+
+// Fills one table for distances low .. high; `sign` -1 turns the axis round (distance r is kept at -r).  With a causal mask
+// the distances ahead are -inf, which masks: mask_ahead writes them, once, and a head's fill ends at 0.
+__device__ __forceinline__ void fill_lut(const Bias& s, int head, const uint8_t* bucket, float* lut, const LutShape& l, int low, int high, int sign,
+                                         int thread, int threads) {
+    low = max(low, -l.pad);
+    high = min(high, l.copy - 2 - l.pad);
+#pragma unroll 4
+    for (int r = low + thread; r <= high; r += threads) {
+        const float x = lut_value(s, head, bucket[sign * r + l.pad]);
+        lut[r + l.pad] = x;
+        if (r + l.pad > 0) lut[l.copy + r + l.pad - 1] = x;
+    }
+    if (thread < 2) lut[2 * l.copy + thread] = lut_value(s, head, bucket[thread ? 2 * l.pad : 0]);
+}
+__device__ __forceinline__ void mask_ahead(float* lut, const LutShape& l, int thread, int threads) {
+    for (int x = l.pad + 1 + thread; x < l.copy; x += threads) {
+        lut[x] = -INFINITY;
+        lut[l.copy + x - 1] = -INFINITY;
     }
 }
 
-// What every row of a tile has in common.  Rows and columns are positions; r = column - row.
+// The same on the turned axis.
+__device__ __forceinline__ void mask_behind(float* lut, const LutShape& l, int thread, int threads) {
+    for (int x = thread; x < l.pad; x += threads) {
+        lut[x] = -INFINITY;
+        if (x > 0) lut[l.copy + x - 1] = -INFINITY;
+    }
+}
+
+// What every row of a tile has in common: a bias, or (mixed) the table by distance, which also holds a causal mask.
+// Rows and columns are positions; r = column - row.
 enum Span { kSpanFarLeft, kSpanFarRight, kSpanMixed };
 __device__ __forceinline__ Span span_of(const Bias& s, int r_min, int r_max) {
     return r_max <= -s.far ? kSpanFarLeft : r_min >= s.far ? kSpanFarRight : kSpanMixed;
@@ -88,52 +153,52 @@ __device__ __forceinline__ void zero_row(const Operand& t, int dim, int batch, i
     for (int x = 0; x < dim; x += 8) *reinterpret_cast<uint4*>(p + x) = make_uint4(0, 0, 0, 0);
 }
 
-// 32 columns of a row of results (fp32 in registers), scaled, rounded and stored.
-__device__ __forceinline__ void store_columns(const Operand& t, int dim, int batch, int head, int pos, int from, const uint32_t (&x)[32], float scale) {
-    uint16_t* p = t.data + (int64_t)batch * t.step_batch + (int64_t)head * t.step_head + (int64_t)pos * t.step_pos + from;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (from + 8 * i >= dim) break;
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = alsgd_ops::pack_bf16(__uint_as_float(x[8 * i + 2 * e]) * scale, __uint_as_float(x[8 * i + 2 * e + 1]) * scale);
-        *reinterpret_cast<uint4*>(p + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+// A block's item in each round: forwards through the blocks, then backwards, so that with items sorted by their work the
+// blocks' shares come out nearly even.
+__device__ __forceinline__ int walk(int round) {
+    return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
 }
 
-// The tiles of a block's work items, one after the other.  item_at(ARGS, i) finds an item, whose `n` is the number of tiles;
-// items without any are passed over, by every warp alike: a barrier's phases must not run past one that waits on it.
+// The block's next item from `round` on, if there is one; `round` moves behind it.
+template <typename ARGS, typename ITEM>
+__device__ __forceinline__ bool next_item(const ARGS& a, int& round, ITEM& item) {
+    for (; round * (int)gridDim.x < a.items; ++round) {
+        const int i = walk(round);
+        if (i >= a.items) continue;
+        item = item_at(a, i);
+        ++round;
+        return true;
+    }
+    return false;
+}
+
+// The tiles of a block's items, one after the other.  item_at(ARGS, i) finds an item, whose `n` is the number of tiles; items
+// without any are passed over, by every warp alike: a barrier's phases must not run past one that waits on it.
 template <typename ARGS, typename ITEM>
 struct Cursor {
     ITEM item;
-    int i, ordinal, j, tile;           // item, how many of the block's items with tiles came before it, tile within it, tiles before this one
+    int round, ordinal, j, tile;       // the next round, how many of the block's items with tiles came before it, tile within it, tiles before this one
     bool more;
     __device__ __forceinline__ void settle(const ARGS& a) {
-        for (; i < a.items; i += gridDim.x) {
-            item = item_at(a, i);
-            if (item.n > 0) break;
-        }
-        more = i < a.items;
+        do more = next_item(a, round, item);
+        while (more && item.n == 0);
         j = 0;
     }
     __device__ __forceinline__ void start(const ARGS& a) {
-        i = blockIdx.x;
-        ordinal = tile = 0;
+        round = ordinal = tile = 0;
         settle(a);
     }
     __device__ __forceinline__ void next(const ARGS& a) {
         ++tile;
         if (++j < item.n) return;
-        i += gridDim.x;
         ++ordinal;
         settle(a);
     }
 };
 
-// 32 columns x 32 rows of results (fp32 in registers, one row per lane) scaled, rounded and stored as one box; `staging`
-// is 2 KB of the warp's own.
-__device__ __forceinline__ void store_box(const CUtensorMap* map, const uint32_t (&x)[32], float scale, uint8_t* staging, int lane, int c, int pos, int head, int batch) {
+// 32 columns x 32 rows of results (fp32 in registers, one row per lane), scaled and rounded, into 2 KB of the warp's own;
+// after a fence the leader stores the box.
+__device__ __forceinline__ void stage_box(const uint32_t (&x)[32], float scale, uint8_t* staging, int lane) {
     uint8_t* line = staging + lane * 64;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -143,13 +208,8 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, const uint32_t
             w[e] = alsgd_ops::pack_bf16(__uint_as_float(x[8 * i + 2 * e]) * scale, __uint_as_float(x[8 * i + 2 * e + 1]) * scale);
         *reinterpret_cast<uint4*>(line + ((i ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    alsgd_tc::fence_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-        alsgd_tc::tma_store4(map, alsgd_tc::smem_u32(staging), c, pos, head, batch);
-        alsgd_tc::tma_store_commit();
-    }
 }
+
 
 // ---- host ---------------------------------------------------------------------------------------------------
 
@@ -233,6 +293,11 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
     s.scale = d.scale;
     s.scale_log2 = d.scale * kLog2e;
     s.kv_len = kv_len;
+    s.by_heads_q = divide_by(s.heads_q);
+    s.by_heads_kv = divide_by(s.heads_kv);
+    s.by_all_q = divide_by(s.batch * s.heads_q);
+    s.by_all_kv = divide_by(s.batch * s.heads_kv);
+    s.by_group = divide_by(s.group);
     return s;
 }
 

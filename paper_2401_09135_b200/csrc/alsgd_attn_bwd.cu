@@ -11,11 +11,13 @@
 //   attn_dkv_kernel   128 keys against tiles of 64 query rows:    S', dP', dV += P' dO, dK += dS' Q (transposed tiles:
 //                     a lane holds one key); the query heads that share a key head are walked by the same block
 // One kernel that forms S and dP once would save two of the seven products and half of the exponentials, but has to
-// add dQ across blocks.
+// add dQ across blocks: 32 KB of binary32 for every 128 x 128 scores, which at a head of 64 costs the L2 more than the
+// second pass costs the tensor cores.
 //
-// Both are built like the forward kernel: blocks walk the work items, those with the most tiles first; warps 0-7 do the
-// arithmetic on a tile (warps w and w + 4 share 32 rows and take 32 columns each), warp 8 copies tiles, warp 9 issues the
-// products.
+// Both are built like the forward kernel: blocks walk work items sorted by their tiles; groups of four warps do the
+// arithmetic, one thread to a row of a tile; warps of their own copy tiles, issue S and dP, issue the sums, and lay out
+// the next item's bias by distance (with it the causal mask).  dq: two blocks per SM with one such group each.  dkv: one
+// block per SM with two groups that take the item's tiles in turn, because dV, dK and two tiles fill tensor memory.
 //
 // Everything is binary32 but the operands of the second products: p and ds are rounded to bf16 (the type of do, q and
 // k), as the forward pass rounds p.
@@ -29,12 +31,15 @@ namespace {
 
 constexpr int kOwn = 128;               // rows of an item
 constexpr int kStep = 64;               // rows of a streamed tile
-constexpr int kMath = 256;              // threads that do the arithmetic
-constexpr int kThreads = kMath + 64;
-constexpr int kAll = 5;                 // named barrier of those threads; 1 to 4 belong to the pairs of warps
 constexpr uint32_t kOwnBytes = 128 * 128;      // 128 rows of 64 bf16
 constexpr uint32_t kStepBytes = 64 * 128;
-constexpr int kDiagonals = 2 * 48;      // sums a warp keeps of its 32 x 32 part, in two groups of 16 columns
+constexpr int kGroup = 16, kGroups = kStep / kGroup;   // columns whose diagonals are summed in one chain, chains
+constexpr int kChain = kGroup + 32;     // sums a chain leaves, padded
+constexpr int kDiagonals = kGroups * kChain;
+
+// The threads of one item's arithmetic in attn_dq_kernel, named barrier 1.
+constexpr int kDqMath = 128, kDqThreads = 256;
+constexpr int kDqMathRegisters = 184, kDqOtherRegisters = 72;  // 128 threads each; launched with 128 a thread
 
 // =============================================================================================== dq
 
@@ -47,7 +52,8 @@ struct DqArgs {
     int64_t o_batch, o_pos, o_head;     // steps of o
     float* delta;                       // out: [batch][heads_q][len_q]
     float* partial;                     // out: [batch * heads_q][row blocks][buckets]
-    int pad, row_blocks, items;
+    LutShape lut;
+    int row_blocks, items;
 };
 
 struct DqItem {
@@ -56,12 +62,12 @@ struct DqItem {
 
 __device__ __forceinline__ DqItem item_at(const DqArgs& a, int i) {
     const Shape& sh = a.shape;
-    const int bh = sh.batch * sh.heads_q;
     DqItem t;
-    t.block = a.row_blocks - 1 - i / bh;
+    const int block = sh.by_all_q(i), bh = i - block * sh.batch * sh.heads_q;
+    t.block = a.row_blocks - 1 - block;
     t.q0 = t.block * kOwn;
-    t.b = i % bh / sh.heads_q;
-    t.h = i % bh % sh.heads_q;
+    t.b = sh.by_heads_q(bh);
+    t.h = bh - t.b * sh.heads_q;
     t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
     t.keys = t.len;
     if (sh.causal) t.keys = min(t.keys, min(t.q0 + kOwn, sh.len_q) + sh.q_pos);
@@ -74,21 +80,22 @@ struct DqPlan {
     static constexpr int stages = HALVES == 1 ? 2 : 1, own_bufs = HALVES == 1 ? 2 : 1;
     static constexpr bool apart = HALVES == 1;         // dS beside S, so that the next tile's scores need not wait for dQ
     static constexpr uint32_t columns = 256;
-    static constexpr uint32_t s_col = 0, dp_col = 64, dq_col = 128;
-    static constexpr uint32_t ds_col = apart ? 192 : 0, ds_half = apart ? 16 : 32;     // dS of columns 32-63 lies ds_half further
+    static constexpr uint32_t s_col = 0, dp_col = 64, dq_col = 128, ds_col = apart ? 192 : 0;
     static constexpr uint32_t own_bytes = HALVES * kOwnBytes, step_bytes = HALVES * kStepBytes;
     static constexpr uint32_t tiles_bytes = own_bufs * 2 * own_bytes + 2 * stages * step_bytes;
-    static constexpr uint32_t bars = 6 + 2 * own_bufs + 2 * stages;
-    static constexpr uint32_t fixed_bytes = tiles_bytes + 256 + 4 * kOwn * sizeof(float);
+    static constexpr uint32_t bars = 7 + 4 * own_bufs + 2 * stages;
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 256;
 };
 
 template <int HALVES>
-size_t dq_smem(int pad, int buckets) {
-    return 1024 + DqPlan<HALVES>::fixed_bytes + (buckets ? 8 * (kDiagonals + buckets) * sizeof(float) + (2 * pad + 1) * (sizeof(float) + 1) : 0);
+size_t dq_smem(const LutShape& l, bool lut, int buckets) {
+    return 1024 + DqPlan<HALVES>::fixed_bytes + (lut ? DqPlan<HALVES>::own_bufs * l.floats * sizeof(float) + 2 * l.pad + 16 : 0) +
+           (buckets ? 4 * (kDiagonals + buckets) * sizeof(float) : 0);
 }
 
-template <int HALVES, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_constant__ DqArgs a) {
+// LUT: there is a bias or a causal mask.  BIAS: there is a bias, and its gradient.
+template <int HALVES, bool LUT, bool BIAS>
+__global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_constant__ DqArgs a) {
     using Plan = DqPlan<HALVES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
     extern __shared__ uint8_t raw[];
@@ -97,28 +104,31 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
     const uint32_t sq = base, sdo = sq + OB * Plan::own_bytes, sk = sdo + OB * Plan::own_bytes, sv = sk + ST * Plan::step_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
     const uint32_t s_full = bars, s_free = bars + 8, ds_ready = bars + 16, dq_done = bars + 24, dq_free = bars + 32, drained = bars + 40;
-    const uint32_t own_full = bars + 48, own_empty = own_full + 8 * OB, full = own_empty + 8 * OB, empty = full + 8 * ST;
+    const uint32_t own_full = bars + 56, own_empty = own_full + 8 * OB, lut_full = own_empty + 8 * OB, lut_empty = lut_full + 8 * OB;
+    const uint32_t full = lut_empty + 8 * OB, empty = full + 8 * ST;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
-    float* shared_delta = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 256);    // [2][2][kOwn]: items in turn
-    float* diagonals = shared_delta + 4 * kOwn;
-    float* by_bucket = diagonals + 8 * kDiagonals;             // [8 warps][buckets]
-    float* lut = by_bucket + 8 * a.bias.buckets;
-    uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(lut + 2 * a.pad + 1);
+    float* diagonals = reinterpret_cast<float*>(smem + Plan::fixed_bytes);             // [4 warps][kDiagonals]
+    float* by_bucket = diagonals + (BIAS ? 4 * kDiagonals : 0);                        // [4 warps][buckets]
+    float* luts = by_bucket + (BIAS ? 4 * a.bias.buckets : 0);
+    uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + OB * a.lut.floats);
 
     const Shape& sh = a.shape;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         bar_init(s_full, 1);
-        bar_init(s_free, 8);
-        bar_init(ds_ready, 8);
+        bar_init(s_free, 4);
+        bar_init(ds_ready, 4);
         bar_init(dq_done, 1);
-        bar_init(dq_free, 8);
+        bar_init(dq_free, 4);
         bar_init(drained, 1);
+        bar_init(drained + 8, 1);
         for (int i = 0; i < OB; ++i) {
             bar_init(own_full + 8 * i, 1);
-            bar_init(own_empty + 8 * i, 8);
+            bar_init(own_empty + 8 * i, 4);
+            bar_init(lut_full + 8 * i, 1);
+            bar_init(lut_empty + 8 * i, 4);
         }
         for (int i = 0; i < ST; ++i) {
             bar_init(full + 8 * i, 1);
@@ -127,30 +137,35 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
         words[1] = 0;
         bar_init_fence();
     }
-    if (warp == 9) tmem_alloc(smem_u32(words), Plan::columns);
-    if (threadIdx.x == kMath) {
+    if (warp == 5) tmem_alloc(smem_u32(words), Plan::columns);
+    if (threadIdx.x == kDqMath) {
         tma_prefetch(&a.q.map);
         tma_prefetch(&a.dout.map);
         tma_prefetch(&a.k.map);
         tma_prefetch(&a.v.map);
         tma_prefetch(&a.dq.map);
     }
-    if (BIAS && warp < 8) fill_buckets(a.bias, lut_bucket, a.pad, threadIdx.x, kMath);
+    if (LUT && warp < 4) {
+        if (BIAS) fill_buckets(a.bias, lut_bucket, a.lut.pad, threadIdx.x, kDqMath);
+        if (sh.causal)
+            for (int i = 0; i < OB; ++i) mask_ahead(luts + i * a.lut.floats, a.lut, threadIdx.x, kDqMath);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_sync();
 
-    if (warp == 8) {
+    if (warp >= 4) give_registers<kDqOtherRegisters>();
+    if (warp == 4) {
         if (lane == 0) {
             int ordinal = 0, tile = 0;                         // items and tiles whose copies have been started
-            for (int i = blockIdx.x; i < a.items; i += gridDim.x) {
-                const DqItem t = item_at(a, i);
+            DqItem t;
+            for (int round = 0; next_item(a, round, t);) {
                 if (t.n == 0) continue;
-                const int hk = t.h / sh.group, buf = ordinal % OB;
-                wait(own_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 1 << 16);
                 if (*dead) break;
+                const int hk = sh.by_group(t.h), buf = ordinal % OB;
+                wait(own_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 1 << 16);
                 bar_expect(own_full + 8 * buf, 2 * Plan::own_bytes);
                 for (int c = 0; c < HALVES; ++c) {
                     const uint32_t at = buf * Plan::own_bytes + c * kOwnBytes;
@@ -158,138 +173,144 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                     tma_load4(sdo + at, &a.dout.map, own_full + 8 * buf, 64 * c, t.q0, t.h * a.dout.head_mul, t.b * a.dout.batch_mul);
                 }
                 ++ordinal;
-                for (int j = 0; j < t.n; ++j) {
+                for (int j = 0; j < t.n && !*dead; ++j, ++tile) {
                     const int st = tile % ST;
                     wait(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
-                    if (*dead) break;
                     bar_expect(full + 8 * st, 2 * Plan::step_bytes);
                     for (int c = 0; c < HALVES; ++c) {
                         const uint32_t at = st * Plan::step_bytes + c * kStepBytes;
                         tma_load4(sk + at, &a.k.map, full + 8 * st, 64 * c, j * kStep, hk * a.k.head_mul, t.b * a.k.batch_mul);
                         tma_load4(sv + at, &a.v.map, full + 8 * st, 64 * c, j * kStep, hk * a.v.head_mul, t.b * a.v.batch_mul);
                     }
-                    ++tile;
                 }
             }
             // every copy has landed before the block may leave, whoever else has given up
             for (int i = max(0, ordinal - OB); i < ordinal; ++i) drain(own_full + 8 * (i % OB), (i / OB) & 1);
             for (int i = max(0, tile - ST); i < tile; ++i) drain(full + 8 * (i % ST), (i / ST) & 1);
         }
-    } else if (warp == 9) {
-        // The warp walks together and one lane issues: what a product is given stays the same for all lanes, which is what
-        // its instruction wants, and a tile costs this warp little more than its products.
-        constexpr uint32_t desc_s = mma_desc(kStep, false), desc_q = mma_desc(64 * HALVES, true);
+    } else if (warp == 5) {
+        // The warp walks together and one lane issues: what a product is given stays the same for all lanes.
+        constexpr uint32_t desc = mma_desc(kStep, false);
         const bool leader = elect_one();
         const uint64_t q_desc = desc_k_major(sq), do_desc = desc_k_major(sdo), k_desc = desc_k_major(sk), v_desc = desc_k_major(sv);
-        const uint64_t kn_desc = desc_n_major(sk, kStepBytes);
-        Cursor<DqArgs, DqItem> ahead, at;                      // of S and dP, and of dQ
-        ahead.start(a);
-        at = ahead;
-        auto scores = [&]() {
-            const int st = ahead.tile % ST, buf = ahead.ordinal % OB;
-            if (ahead.j == 0) wait_warp(own_full + 8 * buf, (ahead.ordinal / OB) & 1, dead, 4 << 16);
-            wait_warp(full + 8 * st, (ahead.tile / ST) & 1, dead, 8 << 16);
+        Cursor<DqArgs, DqItem> at;
+        for (at.start(a); at.more; at.next(a)) {
+            const int st = at.tile % ST, buf = at.ordinal % OB;
+            if (at.j == 0) wait_warp(own_full + 8 * buf, (at.ordinal / OB) & 1, dead, 4 << 16);
+            wait_warp(full + 8 * st, (at.tile / ST) & 1, dead, 8 << 16);
+            // the last tile's S and dP have been read, or (dS in their place) used
+            if (at.tile > 0) wait_warp(Plan::apart ? s_free : dq_done, (at.tile - 1) & 1, dead, 16 << 16);
             tc_fence_after();
             const uint32_t own = buf * (Plan::own_bytes >> 4), step = st * (Plan::step_bytes >> 4);
             if (leader) {
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) {         // 16 elements of the head each; behind dim they are zeros
                     const uint32_t o = own + (((i >> 2) * kOwnBytes + (i & 3) * 32) >> 4), s = step + (((i >> 2) * kStepBytes + (i & 3) * 32) >> 4);
-                    mma_ss(tmem + Plan::s_col, q_desc + o, k_desc + s, desc_s, i > 0);
-                    mma_ss(tmem + Plan::dp_col, do_desc + o, v_desc + s, desc_s, i > 0);
+                    mma_ss(tmem + Plan::s_col, q_desc + o, k_desc + s, desc, i > 0);
+                    mma_ss(tmem + Plan::dp_col, do_desc + o, v_desc + s, desc, i > 0);
                 }
                 mma_commit(s_full);
             }
             __syncwarp();
-            ahead.next(a);
-        };
-        if (ahead.more) scores();
-        int items = 0;                                         // whose dQ has been started
-        while (at.more) {
-            const int st = at.tile % ST;
-            const uint32_t parity = at.tile & 1;
-            if (Plan::apart && ahead.more) {
-                wait_warp(s_free, parity, dead, 16 << 16);
-                scores();
-            }
-            if (at.j == 0) {                                   // the last item's dQ has been read
-                wait_warp(dq_free, (items & 1) ^ 1, dead, 32 << 16);
-                ++items;
-            }
-            wait_warp(ds_ready, parity, dead, 64 << 16);
-            tc_fence_after();
-            const uint64_t kd = kn_desc + st * (Plan::step_bytes >> 4);
-            const bool more = at.j > 0;
-            if (leader) {
-#pragma unroll
-                for (int i = 0; i < kStep / 16; ++i)
-                    mma_ts(tmem + Plan::dq_col, tmem + Plan::ds_col + (i >> 1) * Plan::ds_half + (i & 1) * 8, kd + i * 128, desc_q, more || i > 0);
-                mma_commit(empty + 8 * st);
-                mma_commit(dq_done);
-            }
-            __syncwarp();
-            if (!Plan::apart && ahead.more) {
-                wait_warp(dq_done, parity, dead, 128 << 16);
-                scores();
-            }
-            at.next(a);
         }
         if (leader) {
             mma_commit(drained);
             drain(drained, 0);
         }
-    } else {
-        const int half = warp >> 2, quad = warp & 3;
-        const int row = quad * 32 + lane, pair = 1 + quad;
-        const uint32_t lanes = tmem + ((uint32_t)quad << 21);
+    } else if (warp == 6) {
+        constexpr uint32_t desc = mma_desc(64 * HALVES, true);
+        const bool leader = elect_one();
+        const uint64_t k_desc = desc_n_major(sk, kStepBytes);
+        Cursor<DqArgs, DqItem> at;
+        for (at.start(a); at.more; at.next(a)) {
+            const int st = at.tile % ST;
+            if (at.j == 0) wait_warp(dq_free, (at.ordinal & 1) ^ 1, dead, 32 << 16);   // the last item's dQ has been read
+            wait_warp(ds_ready, at.tile & 1, dead, 64 << 16);
+            tc_fence_after();
+            const uint64_t kd = k_desc + st * (Plan::step_bytes >> 4);
+            const bool more = at.j > 0;
+            if (leader) {
+#pragma unroll
+                for (int i = 0; i < kStep / 16; ++i) mma_ts(tmem + Plan::dq_col, tmem + Plan::ds_col + i * 8, kd + i * 128, desc, more || i > 0);
+                mma_commit(dq_done);
+                mma_commit(empty + 8 * st);
+            }
+            __syncwarp();
+        }
+        if (leader) {
+            mma_commit(drained + 8);
+            drain(drained + 8, 0);
+        }
+    } else if (warp == 7) {
+        int ordinal = 0;
+        DqItem t;
+        for (int round = 0; LUT && next_item(a, round, t);) {
+            if (t.n == 0) continue;
+            const int buf = ordinal % OB, first = t.q0 + sh.q_pos;     // distances from the last row's first key to the first row's last
+            wait_warp(lut_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 128 << 16);
+            fill_lut(a.bias, t.h, lut_bucket, luts + buf * a.lut.floats, a.lut, -(first + kOwn - 1), sh.causal ? 0 : t.keys - 1 - first, 1, lane, 32);
+            __syncwarp();
+            if (lane == 0) bar_arrive(lut_full + 8 * buf);
+            ++ordinal;
+        }
+    } else if (warp < 4) {
+        take_registers<kDqMathRegisters>();
+        const int row = threadIdx.x;
+        const uint32_t lanes = tmem + ((uint32_t)warp << 21);
         float* sums = diagonals + warp * kDiagonals;
         float* bucket_sums = by_bucket + warp * a.bias.buckets;
         int ordinal = 0, tile = 0;
-        for (int i = blockIdx.x; i < a.items; i += gridDim.x) {
-            const DqItem t = item_at(a, i);
+        bool leaving = false;          // this warp's rows of the last item are on their way out of that item's q
+        auto release_own = [&](int buf) {
+            if (lane == 0) {
+                tma_store_wait_read();
+                bar_arrive(own_empty + 8 * buf);
+            }
+        };
+        // the row of o that delta wants, asked for one item ahead
+        uint4 o[8 * HALVES];
+        auto ask_for_o = [&](const DqItem& t) {
+            const uint16_t* p = a.o + (int64_t)t.b * a.o_batch + (int64_t)(t.q0 + row) * a.o_pos + (int64_t)t.h * a.o_head;
+#pragma unroll
+            for (int c = 0; c < 8 * HALVES; ++c)
+                o[c] = t.q0 + row < sh.len_q && 8 * c < sh.dim ? *reinterpret_cast<const uint4*>(p + 8 * c) : make_uint4(0, 0, 0, 0);
+        };
+        int round = 0;
+        DqItem t;
+        bool more = next_item(a, round, t);
+        if (more) ask_for_o(t);
+        while (more) {
             const int buf = ordinal % OB;
             const bool inside = t.q0 + row < sh.len_q;
-            const int pos = t.q0 + row + sh.q_pos;
             const size_t stat = ((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row;
             float* partial = a.partial + (((size_t)t.b * sh.heads_q + t.h) * a.row_blocks + t.block) * a.bias.buckets;
             if (t.n == 0) {
                 if (inside) {
-                    if (half == 0) {
-                        zero_row(a.dq, sh.dim, t.b, t.h, t.q0 + row);
-                        a.delta[stat] = 0.0f;
-                    }
+                    zero_row(a.dq, sh.dim, t.b, t.h, t.q0 + row);
+                    a.delta[stat] = 0.0f;
                 }
                 if (BIAS)
-                    for (int e = threadIdx.x; e < a.bias.buckets; e += kMath) partial[e] = 0.0f;
+                    for (int e = threadIdx.x; e < a.bias.buckets; e += kDqMath) partial[e] = 0.0f;
+                more = next_item(a, round, t);
+                if (more) ask_for_o(t);
                 continue;
             }
             const float lse = inside ? a.lse[stat] : -INFINITY;
             const bool live = lse != -INFINITY;
-            // delta: this thread's half of the row's do . o
-            uint4 o[4 * HALVES];
-#pragma unroll
-            for (int c = 0; c < 4 * HALVES; ++c) {
-                const int x = 8 * (4 * HALVES * half + c);
-                o[c] = live && x < sh.dim ? *reinterpret_cast<const uint4*>(a.o + (int64_t)t.b * a.o_batch + (int64_t)(t.q0 + row) * a.o_pos +
-                                                                            (int64_t)t.h * a.o_head + x)
-                                          : make_uint4(0, 0, 0, 0);
-            }
+            const int pos = t.q0 + row + sh.q_pos;
+            const float* lut = luts + buf * a.lut.floats;
             if (BIAS) {
-                const int first = t.q0 + sh.q_pos;             // distances from the last row's first key to the first row's last
-                sync_threads(kAll, kMath);
-                fill_lut(a.bias, t.h, lut_bucket, lut, a.pad, -(first + kOwn - 1), sh.causal ? 0 : t.keys - 1 - first, threadIdx.x, kMath);
                 for (int e = lane; e < a.bias.buckets; e += 32) bucket_sums[e] = 0.0f;
-                sync_threads(kAll, kMath);
+                __syncwarp();
             }
             wait_warp(own_full + 8 * buf, (ordinal / OB) & 1, dead, 256 << 16);
             float delta = 0.0f;
             if (live) {
                 float acc[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < 4 * HALVES; ++c) {
-                    const int chunk = 4 * HALVES * half + c;
-                    const uint4 y = *reinterpret_cast<const uint4*>(smem + (sdo - base) + buf * Plan::own_bytes + (chunk >> 3) * kOwnBytes + row * 128 +
-                                                                    (((chunk & 7) ^ (row & 7)) << 4));
+                for (int c = 0; c < 8 * HALVES; ++c) {
+                    const uint4 y = *reinterpret_cast<const uint4*>(smem + (sdo - base) + buf * Plan::own_bytes + (c >> 3) * kOwnBytes + row * 128 +
+                                                                    (((c & 7) ^ (row & 7)) << 4));
                     const uint32_t xs[4] = {o[c].x, o[c].y, o[c].z, o[c].w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -299,28 +320,30 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                 }
                 delta = acc[0] + acc[1];
             }
-            float* halves = shared_delta + (ordinal & 1) * 2 * kOwn;
-            halves[half * kOwn + row] = delta;
-            sync_threads(pair, 64);
-            delta += halves[(half ^ 1) * kOwn + row];
-            if (inside && half == 0) a.delta[stat] = delta;
+            if (inside) a.delta[stat] = delta;
 
             // A row with one allowed key has p = 1 whatever its score: ds = 0, where dp - delta would leave two sums' noise.
             const int seen = sh.causal ? min(t.len, pos + 1) : t.len;
-            const int used = live && seen > 1 ? seen : 0;
-            const bool some_cut = __any_sync(0xFFFFFFFFu, used == 0);
+            const bool used = live && seen > 1;
+            // rows whose every key up to the sequence's end lies within the causal mask need no other, unless what lies behind may be NaN
+            const bool cut = t.len < sh.len_kv || !(sh.causal && min(t.q0 + kOwn, sh.len_q) + sh.q_pos <= t.len);
+            const bool some_idle = __any_sync(0xFFFFFFFFu, !used);
             const float lse2 = live ? lse * kLog2e : 0.0f;
             float far_left = 0.0f, far_right = 0.0f;
             for (int j = 0; j < t.n; ++j, ++tile) {
-                const int k0 = j * kStep, col0 = k0 + 32 * half;
+                const int k0 = j * kStep;
                 wait_warp(s_full, tile & 1, dead, 512 << 16);
                 tc_fence_after();
-                uint32_t s[32], d[32];
-                tmem_ld32(s, lanes + Plan::s_col + 32 * half);
-                tmem_ld32(d, lanes + Plan::dp_col + 32 * half);
+                uint32_t s[2][32], d[2][32];
+                tmem_ld32(s[0], lanes + Plan::s_col);
+                tmem_ld32(s[1], lanes + Plan::s_col + 32);
+                tmem_ld32(d[0], lanes + Plan::dp_col);
+                tmem_ld32(d[1], lanes + Plan::dp_col + 32);
                 tmem_wait_ld();
-                tmem_use(s);
-                tmem_use(d);
+                tmem_use(s[0]);
+                tmem_use(s[1]);
+                tmem_use(d[0]);
+                tmem_use(d[1]);
                 if (Plan::apart) {
                     tc_fence_before();
                     __syncwarp();
@@ -329,50 +352,65 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                 // x - lse = s * mul + off in base 2
                 float mul = sh.scale_log2, off = -lse2;
                 Span span = kSpanMixed;
-                if (BIAS) {
+                if (LUT) {
+                    if (j == 0) wait_warp(lut_full + 8 * buf, (ordinal / OB) & 1, dead, 1024 << 16);
                     span = span_of(a.bias, k0 - (t.q0 + kOwn - 1 + sh.q_pos), k0 + kStep - 1 - (t.q0 + sh.q_pos));
                     if (span == kSpanMixed) {
-                        const float* at = lut + a.pad + col0 - pos;
+                        const float* at = lut_at(lut, a.lut, k0 - pos);
+                        const uint64_t mul2v = pack2(mul, mul);
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) s[c] = __float_as_uint(fmaf(__uint_as_float(s[c]), mul, at[c]));
+                        for (int c = 0; c < kStep; c += 2) {
+                            const float2 b = *reinterpret_cast<const float2*>(at + c);
+                            float x, y;
+                            unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
+                            s[c >> 5][c & 31] = __float_as_uint(x);
+                            s[c >> 5][(c & 31) + 1] = __float_as_uint(y);
+                        }
                         mul = 1.0f;
                     } else {
-                        off += lut[span == kSpanFarLeft ? 0 : 2 * a.pad];
+                        off += lut_far(lut, a.lut, span == kSpanFarRight);
+                    }
+                    if (j + 1 == t.n) {
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(lut_empty + 8 * buf);
                     }
                 }
                 const uint64_t mul2v = pack2(mul, mul), off2 = pack2(off, off), nd2 = pack2(-delta, -delta);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
+                for (int c = 0; c < kStep; c += 2) {
                     float x, y;
-                    unpack2(fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), mul2v, off2), x, y);
+                    unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, off2), x, y);
                     const uint64_t p = pack2(exp2_fast(x), exp2_fast(y));
-                    unpack2(mul2(p, add2(pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2)), x, y);
-                    d[e] = __float_as_uint(x);
-                    d[e + 1] = __float_as_uint(y);
+                    unpack2(mul2(p, add2(pack2(__uint_as_float(d[c >> 5][c & 31]), __uint_as_float(d[c >> 5][(c & 31) + 1])), nd2)), x, y);
+                    d[c >> 5][c & 31] = __float_as_uint(x);
+                    d[c >> 5][(c & 31) + 1] = __float_as_uint(y);
                 }
-                if (some_cut || k0 + kStep > t.len || (sh.causal && k0 + kStep - 1 > t.q0 + sh.q_pos)) {
-                    const int allowed = used - col0;
+                if (some_idle || (cut && k0 + kStep > t.len)) {
+                    const int end = used ? t.len - k0 : 0;
 #pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (c >= allowed) d[c] = 0;
+                    for (int c = 0; c < kStep; ++c)
+                        if (c >= end) d[c >> 5][c & 31] = 0;
                 }
                 if (j > 0 && Plan::apart) {                    // dS of the last tile has been used
-                    wait_warp(dq_done, (tile - 1) & 1, dead, 1024 << 16);
+                    wait_warp(dq_done, (tile - 1) & 1, dead, 2048 << 16);
                     tc_fence_after();
                 }
-                uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = pack_bf16(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
-                tmem_st16(lanes + Plan::ds_col + Plan::ds_half * half, w);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(__uint_as_float(d[c][2 * e]), __uint_as_float(d[c][2 * e + 1]));
+                    tmem_st16(lanes + Plan::ds_col + 16 * c, w);
+                }
                 if (k0 + kStep > t.len && t.len < sh.len_kv) {
                     // keys behind the sequence's end may hold anything; 0 * NaN must not reach dq
-                    const int st = tile % ST, r = threadIdx.x & (kStep - 1), part = threadIdx.x >> 6;
+                    const int st = tile % ST, r = row & (kStep - 1), part = row >> 6;
                     if (k0 + r >= t.len) {
 #pragma unroll
                         for (int c = 0; c < HALVES; ++c)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                *reinterpret_cast<uint4*>(smem + (sk - base) + st * Plan::step_bytes + c * kStepBytes + r * 128 + 32 * part + 16 * e) = make_uint4(0, 0, 0, 0);
+                            for (int e = 0; e < 4; ++e)
+                                *reinterpret_cast<uint4*>(smem + (sk - base) + st * Plan::step_bytes + c * kStepBytes + r * 128 + 64 * part + 16 * e) = make_uint4(0, 0, 0, 0);
                     }
                     fence_async_smem();
                 }
@@ -384,33 +422,39 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                     if (span != kSpanMixed) {
                         uint64_t both[2] = {0, 0};
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) both[e & 1] = add2(both[e & 1], pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])));
+                        for (int c = 0; c < kStep; c += 2)
+                            both[(c >> 1) & 1] = add2(both[(c >> 1) & 1], pack2(__uint_as_float(d[c >> 5][c & 31]), __uint_as_float(d[c >> 5][(c & 31) + 1])));
                         float x, y;
                         unpack2(add2(both[0], both[1]), x, y);
                         if (span == kSpanFarLeft) far_left += x + y; else far_right += x + y;
                     } else {
-                        // Sums along the diagonals of the warp's 32 x 32 part: a running sum moves one lane down per column and
-                        // leaves at lane 31, complete.  Two groups of 16 columns, whose chains of shuffles overlap.
-                        float run[2] = {0.0f, 0.0f};
+                        // Sums along the diagonals of the warp's 32 x 64 part: a running sum moves one lane down per column and
+                        // leaves at lane 31, complete.  Four groups of 16 columns, whose chains of shuffles overlap.
+                        float run[kGroups] = {};
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) {
+                        for (int c = 0; c < kGroup; ++c) {
 #pragma unroll
-                            for (int g = 0; g < 2; ++g) {
+                            for (int g = 0; g < kGroups; ++g) {
                                 run[g] = __shfl_up_sync(0xFFFFFFFFu, run[g], 1);
-                                run[g] = (lane == 0 ? 0.0f : run[g]) + __uint_as_float(d[16 * g + c]);
-                                if (lane == 31) sums[48 * g + c] = run[g];
+                                run[g] = (lane == 0 ? 0.0f : run[g]) + __uint_as_float(d[(kGroup * g + c) >> 5][(kGroup * g + c) & 31]);
+                                if (lane == 31) sums[kChain * g + c] = run[g];
                             }
                         }
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) sums[48 * g + (lane == 31 ? 47 : 46 - lane)] = lane == 31 ? 0.0f : run[g];
+                        for (int g = 0; g < kGroups; ++g) sums[kChain * g + (lane == 31 ? kChain - 1 : kChain - 2 - lane)] = lane == 31 ? 0.0f : run[g];
                         __syncwarp();
-                        const int first = col0 - (t.q0 + 32 * quad + 31 + sh.q_pos);
+                        const int first = k0 - (t.q0 + 32 * warp + 31 + sh.q_pos);     // distance of diagonal 0
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
+                        for (int e = 0; e < 3; ++e) {
                             // a bucket is a run of distances: sums within runs, and the last lane of each run adds to its bucket
                             const int at = 32 * e + lane;
-                            const int bucket = lut_bucket[a.pad + first + at];
-                            float x = (at < 47 ? sums[at] : 0.0f) + (at >= 16 ? sums[48 + at - 16] : 0.0f);
+                            const int bucket = lut_bucket[a.lut.pad + first + at];
+                            float x = 0.0f;
+#pragma unroll
+                            for (int g = 0; g < kGroups; ++g) {
+                                const int local = at - kGroup * g;
+                                if (local >= 0 && local < kChain) x += sums[kChain * g + local];
+                            }
 #pragma unroll
                             for (int o = 1; o < 32; o <<= 1) {
                                 const float y = __shfl_up_sync(0xFFFFFFFFu, x, o);
@@ -423,7 +467,14 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                         }
                     }
                 }
+                if (OB > 1 && leaving) {
+                    release_own((ordinal - 1) % OB);
+                    leaving = false;
+                }
             }
+            const DqItem last = t;
+            more = next_item(a, round, t);
+            if (more) ask_for_o(t);
             if (BIAS) {
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
@@ -432,44 +483,47 @@ __global__ void __launch_bounds__(kThreads, 2) attn_dq_kernel(const __grid_const
                 }
                 if (lane == 0) {
                     bucket_sums[lut_bucket[0]] += far_left;
-                    bucket_sums[lut_bucket[2 * a.pad]] += far_right;
+                    bucket_sums[lut_bucket[2 * a.lut.pad]] += far_right;
                 }
-                sync_threads(kAll, kMath);
-                for (int e = threadIdx.x; e < a.bias.buckets; e += kMath) {
-                    float x = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) x += by_bucket[w * a.bias.buckets + e];
-                    partial[e] = x;
-                }
+                sync_threads(1, kDqMath);
+                for (int e = threadIdx.x; e < a.bias.buckets; e += kDqMath)
+                    partial[e] = (by_bucket[e] + by_bucket[a.bias.buckets + e]) + (by_bucket[2 * a.bias.buckets + e] + by_bucket[3 * a.bias.buckets + e]);
+                sync_threads(1, kDqMath);
             }
-            wait_warp(dq_done, (tile - 1) & 1, dead, 2048 << 16);
+            wait_warp(dq_done, (tile - 1) & 1, dead, 4096 << 16);
             tc_fence_after();
             // dq goes out through q's place, which is free: its last product has completed
+            uint8_t* staging = smem + buf * Plan::own_bytes + warp * 2 * HALVES * 2048;
 #pragma unroll
-            for (int c = 0; c < HALVES; ++c) {
-                const int x = 32 * (HALVES * half + c);
+            for (int c = 0; c < 2 * HALVES; ++c) {
                 uint32_t r[32];
-                tmem_ld32(r, lanes + Plan::dq_col + x);
+                tmem_ld32(r, lanes + Plan::dq_col + 32 * c);
                 tmem_wait_ld();
                 tmem_use(r);
-                if (t.q0 + 32 * quad < sh.len_q && x < sh.dim)
-                    store_box(&a.dq.map, r, sh.scale, smem + buf * Plan::own_bytes + (warp * HALVES + c) * 2048, lane, x, t.q0 + 32 * quad,
-                              t.h * a.dq.head_mul, t.b * a.dq.batch_mul);
+                stage_box(r, sh.scale, staging + c * 2048, lane);
             }
             tc_fence_before();
+            fence_async_smem();
             __syncwarp();
             if (lane == 0) {
                 bar_arrive(dq_free);
-                tma_store_wait_read();
-                bar_arrive(own_empty + 8 * buf);
+                if (last.q0 + 32 * warp < sh.len_q) {
+                    for (int c = 0; c < 2 * HALVES; ++c)
+                        if (32 * c < sh.dim)
+                            tma_store4(&a.dq.map, smem_u32(staging) + c * 2048, 32 * c, last.q0 + 32 * warp, last.h * a.dq.head_mul, last.b * a.dq.batch_mul);
+                    tma_store_commit();
+                }
             }
+            if (OB > 1) leaving = true;                        // another q is ready: this one's place may wait
+            else release_own(buf);
             ++ordinal;
         }
+        if (leaving) release_own((ordinal - 1) % OB);
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 5) {
         tc_fence_after();
         tmem_free(tmem, Plan::columns);
     }
@@ -483,7 +537,8 @@ struct DkvArgs {
     Bias bias;
     const float* lse;
     const float* delta;
-    int pad, items;
+    LutShape lut;
+    int items;
 };
 
 struct DkvItem {
@@ -492,11 +547,11 @@ struct DkvItem {
 
 __device__ __forceinline__ DkvItem item_at(const DkvArgs& a, int i) {
     const Shape& sh = a.shape;
-    const int bh = sh.batch * sh.heads_kv;
     DkvItem t;
-    t.k0 = i / bh * kOwn;                                      // the first keys see the most queries: they come first
-    t.b = i % bh / sh.heads_kv;
-    t.hk = i % bh % sh.heads_kv;
+    const int block = sh.by_all_kv(i), bh = i - block * sh.batch * sh.heads_kv;
+    t.k0 = block * kOwn;                                       // the first keys see the most queries: they come first
+    t.b = sh.by_heads_kv(bh);
+    t.hk = bh - t.b * sh.heads_kv;
     t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
     const int q_tiles = (sh.len_q + kStep - 1) / kStep;
     t.q_first = 0;                                             // the first tile with a row that sees one of the keys
@@ -506,28 +561,33 @@ __device__ __forceinline__ DkvItem item_at(const DkvArgs& a, int i) {
     return t;
 }
 
+constexpr int kDkvMath = 256, kDkvThreads = 384;
+constexpr int kDkvMathRegisters = 208, kDkvOtherRegisters = 88;   // 256 and 128 threads; launched with 168 a thread
+
 template <int HALVES>
 struct DkvPlan {
-    static constexpr int stages = 2, own_bufs = HALVES == 1 ? 2 : 1;
-    static constexpr bool apart = HALVES == 2;         // P and dS beside S and dP; one block per SM has all 512 columns
-    static constexpr int blocks = HALVES == 1 ? 2 : 1;
-    static constexpr uint32_t columns = HALVES == 1 ? 256 : 512;
-    static constexpr uint32_t s_col = 0, dp_col = 64, dv_col = 128, dk_col = 128 + 64 * HALVES;
-    static constexpr uint32_t p_col = apart ? 384 : s_col, ds_col = apart ? 416 : dp_col, p_half = apart ? 16 : 32;
+    static constexpr int stages = HALVES == 1 ? 4 : 2, own_bufs = HALVES == 1 ? 2 : 1;
+    static constexpr bool apart = HALVES == 1;         // P and dS beside S and dP, so that the scores two tiles on need not wait for the sums
+    static constexpr uint32_t columns = 512;
+    static constexpr uint32_t s_col = 0, dp_col = 64, group_cols = 128;                // a group's S and dP; the other group's follow
+    static constexpr uint32_t dv_col = 256, dk_col = 256 + 64 * HALVES;
+    static constexpr uint32_t p_col = apart ? 384 : s_col, ds_col = apart ? 416 : dp_col, p_cols = apart ? 64 : 128;
     static constexpr uint32_t own_bytes = HALVES * kOwnBytes, step_bytes = HALVES * kStepBytes;
     static constexpr uint32_t tiles_bytes = own_bufs * 2 * own_bytes + 2 * stages * step_bytes;
-    static constexpr uint32_t bars = 6 + 2 * own_bufs + 3 * stages;
+    static constexpr uint32_t bars = 16 + 2 * own_bufs + 3 * stages;
     static constexpr uint32_t stat_floats = 2 * kStep + 4;     // (-lse in base 2)[64], (-delta)[64], whether the tile has holes
-    static constexpr uint32_t fixed_bytes = tiles_bytes + 256 + stages * stat_floats * sizeof(float);
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 512 + stages * stat_floats * sizeof(float);
 };
 
 template <int HALVES>
-size_t dkv_smem(int pad, bool bias) {
-    return 1024 + DkvPlan<HALVES>::fixed_bytes + (bias ? (2 * pad + 1) * (sizeof(float) + 1) : 0);
+size_t dkv_smem(const LutShape& l, bool lut) {
+    return 1024 + DkvPlan<HALVES>::fixed_bytes + (lut ? 2 * l.floats * sizeof(float) + 2 * l.pad + 1 : 0);
 }
 
-template <int HALVES, bool BIAS>
-__global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_kernel(const __grid_constant__ DkvArgs a) {
+// LUT: there is a bias or a causal mask.  The table by distance is kept for each of the two groups' current query head: table
+// (query head's ordinal) % 2, the axis turned round, since a thread's columns are queries.
+template <int HALVES, bool LUT>
+__global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_constant__ DkvArgs a) {
     using Plan = DkvPlan<HALVES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
     extern __shared__ uint8_t raw[];
@@ -535,24 +595,31 @@ __global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_ke
     const uint32_t base = smem_u32(smem);
     const uint32_t sk = base, sv = sk + OB * Plan::own_bytes, sq = sv + OB * Plan::own_bytes, sdo = sq + ST * Plan::step_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
-    const uint32_t s_full = bars, s_free = bars + 8, p_ready = bars + 16, acc_done = bars + 24, acc_free = bars + 32, drained = bars + 40;
-    const uint32_t own_full = bars + 48, own_empty = own_full + 8 * OB, full = own_empty + 8 * OB, empty = full + 8 * ST, stat_full = empty + 8 * ST;
+    const uint32_t s_full = bars, s_free = bars + 16, p_ready = bars + 32, sums_done = bars + 48;      // two each: a group's
+    const uint32_t acc_free = bars + 64, acc_done = bars + 72, drained = bars + 80;
+    const uint32_t own_full = bars + 96, own_empty = own_full + 8 * OB, lut_full = own_empty + 8 * OB, lut_empty = lut_full + 16;
+    const uint32_t full = lut_empty + 16, empty = full + 8 * ST, stat_full = empty + 8 * ST;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
-    float* stats = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 256);
-    float* lut = stats + ST * Plan::stat_floats;
-    uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(lut + 2 * a.pad + 1);
+    float* stats = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 512);
+    float* luts = stats + ST * Plan::stat_floats;
+    uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + 2 * a.lut.floats);
 
     const Shape& sh = a.shape;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        bar_init(s_full, 1);
-        bar_init(s_free, 8);
-        bar_init(p_ready, 8);
-        bar_init(acc_done, 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(s_full + 8 * i, 1);
+            bar_init(s_free + 8 * i, 4);
+            bar_init(p_ready + 8 * i, 4);
+            bar_init(sums_done + 8 * i, 1);
+            bar_init(lut_full + 8 * i, 1);
+            bar_init(lut_empty + 8 * i, 8);
+            bar_init(drained + 8 * i, 1);
+        }
         bar_init(acc_free, 8);
-        bar_init(drained, 1);
+        bar_init(acc_done, 1);
         for (int i = 0; i < OB; ++i) {
             bar_init(own_full + 8 * i, 1);
             bar_init(own_empty + 8 * i, 8);
@@ -566,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_ke
         bar_init_fence();
     }
     if (warp == 9) tmem_alloc(smem_u32(words), Plan::columns);
-    if (threadIdx.x == kMath) {
+    if (threadIdx.x == kDkvMath) {
         tma_prefetch(&a.q.map);
         tma_prefetch(&a.dout.map);
         tma_prefetch(&a.k.map);
@@ -574,21 +641,26 @@ __global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_ke
         tma_prefetch(&a.dk.map);
         tma_prefetch(&a.dv.map);
     }
-    if (BIAS && warp < 8) fill_buckets(a.bias, lut_bucket, a.pad, threadIdx.x, kMath);
+    if (LUT && warp < 8) {
+        if (a.bias.table) fill_buckets(a.bias, lut_bucket, a.lut.pad, threadIdx.x, kDkvMath);
+        if (sh.causal)
+            for (int i = 0; i < 2; ++i) mask_behind(luts + i * a.lut.floats, a.lut, threadIdx.x, kDkvMath);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_sync();
 
+    if (warp >= 8) give_registers<kDkvOtherRegisters>();
     if (warp == 8) {
         int ordinal = 0, tile = 0;                             // items and tiles whose copies have been started
-        for (int i = blockIdx.x; i < a.items; i += gridDim.x) {
-            const DkvItem t = item_at(a, i);
+        DkvItem t;
+        for (int round = 0; next_item(a, round, t);) {
             if (t.n == 0) continue;
+            if (__any_sync(0xFFFFFFFFu, *dead)) break;
             const int buf = ordinal % OB;
             wait_warp(own_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 1 << 16);
-            if (__any_sync(0xFFFFFFFFu, *dead)) break;
             if (lane == 0) {
                 bar_expect(own_full + 8 * buf, 2 * Plan::own_bytes);
                 for (int c = 0; c < HALVES; ++c) {
@@ -599,8 +671,24 @@ __global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_ke
             }
             ++ordinal;
             int head = t.hk * sh.group, q_tile = t.q_first;
-            for (int j = 0; j < t.n; ++j) {
+            for (int j = 0; j < t.n; ++j, ++tile) {
                 const int st = tile % ST, q0 = q_tile * kStep;
+                // lse and delta of the tile's rows, two per lane, on their way before the tile's place is free
+                float nl[2], nd[2];
+                bool hole = false;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = q0 + lane + 32 * e;
+                    nl[e] = -INFINITY;                         // a row behind len_q, or without allowed keys: p = 0
+                    nd[e] = 0.0f;
+                    if (r < sh.len_q) {
+                        const size_t at = ((size_t)t.b * sh.heads_q + head) * sh.len_q + r;
+                        const float lse = a.lse[at];
+                        if (lse == -INFINITY) hole = true; else nl[e] = -lse * kLog2e;
+                        nd[e] = -a.delta[at];
+                    }
+                }
+                hole = __any_sync(0xFFFFFFFFu, hole);
                 wait_warp(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                 if (__any_sync(0xFFFFFFFFu, *dead)) break;
                 if (lane == 0) {
@@ -611,255 +699,283 @@ __global__ void __launch_bounds__(kThreads, DkvPlan<HALVES>::blocks) attn_dkv_ke
                         tma_load4(sdo + at, &a.dout.map, full + 8 * st, 64 * c, q0, head * a.dout.head_mul, t.b * a.dout.batch_mul);
                     }
                 }
-                // lse and delta of the tile's rows, two per lane
                 float* stat = stats + st * Plan::stat_floats;
-                bool hole = false;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = lane + 32 * e;
-                    float nl = -INFINITY, nd = 0.0f;           // a row behind len_q, or without allowed keys: p = 0
-                    if (q0 + r < sh.len_q) {
-                        const size_t at = ((size_t)t.b * sh.heads_q + head) * sh.len_q + q0 + r;
-                        const float lse = a.lse[at];
-                        if (lse == -INFINITY) hole = true; else nl = -lse * kLog2e;
-                        nd = -a.delta[at];
-                    }
-                    stat[r] = nl;
-                    stat[kStep + r] = nd;
+                    stat[lane + 32 * e] = nl[e];
+                    stat[kStep + lane + 32 * e] = nd[e];
                 }
-                hole = __any_sync(0xFFFFFFFFu, hole);
-                if (lane == 0) {
-                    stat[2 * kStep] = hole ? 1.0f : 0.0f;
-                }
+                if (lane == 0) stat[2 * kStep] = hole ? 1.0f : 0.0f;
                 __syncwarp();
                 if (lane == 0) bar_arrive(stat_full + 8 * st);
                 if (++q_tile == t.q_first + t.per_head) {
                     q_tile = t.q_first;
                     ++head;
                 }
-                ++tile;
             }
         }
         // every copy has landed before the block may leave, whoever else has given up
         for (int i = max(0, ordinal - OB); i < ordinal; ++i) drain(own_full + 8 * (i % OB), (i / OB) & 1);
         for (int i = max(0, tile - ST); i < tile; ++i) drain(full + 8 * (i % ST), (i / ST) & 1);
     } else if (warp == 9) {
-        constexpr uint32_t desc_s = mma_desc(kStep, false), desc_acc = mma_desc(64 * HALVES, true);
+        constexpr uint32_t desc = mma_desc(kStep, false);
         const bool leader = elect_one();
         const uint64_t q_desc = desc_k_major(sq), do_desc = desc_k_major(sdo), k_desc = desc_k_major(sk), v_desc = desc_k_major(sv);
-        const uint64_t qn_desc = desc_n_major(sq, kStepBytes), don_desc = desc_n_major(sdo, kStepBytes);
-        Cursor<DkvArgs, DkvItem> ahead, at;                    // of S' and dP', and of dV and dK
-        ahead.start(a);
-        at = ahead;
-        auto scores = [&]() {
-            const int st = ahead.tile % ST, buf = ahead.ordinal % OB;
-            if (ahead.j == 0) wait_warp(own_full + 8 * buf, (ahead.ordinal / OB) & 1, dead, 4 << 16);
-            wait_warp(full + 8 * st, (ahead.tile / ST) & 1, dead, 8 << 16);
+        Cursor<DkvArgs, DkvItem> at;
+        for (at.start(a); at.more; at.next(a)) {
+            const int st = at.tile % ST, buf = at.ordinal % OB, g = at.tile & 1;
+            if (at.j == 0) wait_warp(own_full + 8 * buf, (at.ordinal / OB) & 1, dead, 4 << 16);
+            wait_warp(full + 8 * st, (at.tile / ST) & 1, dead, 8 << 16);
+            // the group's last S and dP have been read, or (P and dS in their place) used
+            if (at.tile > 1) wait_warp((Plan::apart ? s_free : sums_done) + 8 * g, ((at.tile >> 1) - 1) & 1, dead, 16 << 16);
             tc_fence_after();
-            const uint32_t own = buf * (Plan::own_bytes >> 4), step = st * (Plan::step_bytes >> 4);
+            const uint32_t own = buf * (Plan::own_bytes >> 4), step = st * (Plan::step_bytes >> 4), to = tmem + g * Plan::group_cols;
             if (leader) {
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) {
                     const uint32_t o = own + (((i >> 2) * kOwnBytes + (i & 3) * 32) >> 4), s = step + (((i >> 2) * kStepBytes + (i & 3) * 32) >> 4);
-                    mma_ss(tmem + Plan::s_col, k_desc + o, q_desc + s, desc_s, i > 0);
-                    mma_ss(tmem + Plan::dp_col, v_desc + o, do_desc + s, desc_s, i > 0);
+                    mma_ss(to + Plan::s_col, k_desc + o, q_desc + s, desc, i > 0);
+                    mma_ss(to + Plan::dp_col, v_desc + o, do_desc + s, desc, i > 0);
                 }
-                mma_commit(s_full);
+                mma_commit(s_full + 8 * g);
             }
             __syncwarp();
-            ahead.next(a);
-        };
-        if (ahead.more) scores();
-        int items = 0;                                         // whose dV and dK have been started
-        while (at.more) {
-            const int st = at.tile % ST;
-            const uint32_t parity = at.tile & 1;
-            // with one place for k and v, the next item's come only after this item's last products
-            const bool early = Plan::apart && ahead.more && (OB > 1 || ahead.j > 0);
-            if (early) {
-                wait_warp(s_free, parity, dead, 16 << 16);
-                scores();
-            }
-            if (at.j == 0) {                                   // the last item's dV and dK have been read
-                wait_warp(acc_free, (items & 1) ^ 1, dead, 32 << 16);
-                ++items;
-            }
-            wait_warp(p_ready, parity, dead, 64 << 16);
-            tc_fence_after();
-            const uint32_t step = st * (Plan::step_bytes >> 4);
-            const bool more = at.j > 0;
-            if (leader) {
-#pragma unroll
-                for (int i = 0; i < kStep / 16; ++i) {
-                    const uint32_t p = (i >> 1) * Plan::p_half + (i & 1) * 8;
-                    mma_ts(tmem + Plan::dv_col, tmem + Plan::p_col + p, don_desc + step + i * 128, desc_acc, more || i > 0);
-                    mma_ts(tmem + Plan::dk_col, tmem + Plan::ds_col + p, qn_desc + step + i * 128, desc_acc, more || i > 0);
-                }
-                mma_commit(empty + 8 * st);
-                mma_commit(acc_done);
-            }
-            __syncwarp();
-            if (!early && ahead.more) {
-                wait_warp(acc_done, parity, dead, 128 << 16);
-                scores();
-            }
-            at.next(a);
         }
         if (leader) {
             mma_commit(drained);
             drain(drained, 0);
         }
-    } else {
-        const int half = warp >> 2, quad = warp & 3;
+    } else if (warp == 10) {
+        constexpr uint32_t desc = mma_desc(64 * HALVES, true);
+        const bool leader = elect_one();
+        const uint64_t q_desc = desc_n_major(sq, kStepBytes), do_desc = desc_n_major(sdo, kStepBytes);
+        Cursor<DkvArgs, DkvItem> at;
+        for (at.start(a); at.more; at.next(a)) {
+            const int st = at.tile % ST, g = at.tile & 1;
+            if (at.j == 0) wait_warp(acc_free, (at.ordinal & 1) ^ 1, dead, 32 << 16);  // the last item's dV and dK have been read
+            wait_warp(p_ready + 8 * g, (at.tile >> 1) & 1, dead, 64 << 16);
+            tc_fence_after();
+            const uint32_t step = st * (Plan::step_bytes >> 4), p = tmem + Plan::p_col + g * Plan::p_cols, ds = tmem + Plan::ds_col + g * Plan::p_cols;
+            const bool more = at.j > 0, last = at.j + 1 == at.item.n;
+            if (leader) {
+#pragma unroll
+                for (int i = 0; i < kStep / 16; ++i) {
+                    mma_ts(tmem + Plan::dv_col, p + 8 * i, do_desc + step + i * 128, desc, more || i > 0);
+                    mma_ts(tmem + Plan::dk_col, ds + 8 * i, q_desc + step + i * 128, desc, more || i > 0);
+                }
+                mma_commit(sums_done + 8 * g);
+                mma_commit(empty + 8 * st);
+                if (last) mma_commit(acc_done);
+            }
+            __syncwarp();
+        }
+        if (leader) {
+            mma_commit(drained + 8);
+            drain(drained + 8, 0);
+        }
+    } else if (warp == 11) {
+        int heads = 0;                                         // query heads whose tables have been laid out
+        DkvItem t;
+        for (int round = 0; LUT && next_item(a, round, t);) {
+            if (t.n == 0) continue;
+            const int first = t.q_first * kStep + sh.q_pos;        // query positions, to the last tile's end: p = 0 there needs a finite bias
+            const int last = (t.q_first + t.per_head) * kStep - 1 + sh.q_pos;
+            for (int i = 0; i < sh.group; ++i, ++heads) {
+                const int buf = heads & 1;
+                wait_warp(lut_empty + 8 * buf, ((heads >> 1) & 1) ^ 1, dead, 128 << 16);
+                fill_lut(a.bias, t.hk * sh.group + i, lut_bucket, luts + buf * a.lut.floats, a.lut, sh.causal ? 0 : first - (t.k0 + kOwn - 1), last - t.k0, -1, lane, 32);
+                __syncwarp();
+                if (lane == 0) bar_arrive(lut_full + 8 * buf);
+            }
+        }
+    } else if (warp < 8) {
+        take_registers<kDkvMathRegisters>();
+        const int g = warp >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)quad << 21);
-        int ordinal = 0, tile = 0;
-        for (int i = blockIdx.x; i < a.items; i += gridDim.x) {
-            const DkvItem t = item_at(a, i);
+        const uint32_t s_at = lanes + g * Plan::group_cols + Plan::s_col, dp_at = lanes + g * Plan::group_cols + Plan::dp_col;
+        const uint32_t p_at = lanes + Plan::p_col + g * Plan::p_cols, ds_at = lanes + Plan::ds_col + g * Plan::p_cols;
+        int ordinal = 0, tile = 0, heads = 0;
+        bool leaving = false;          // this warp's rows of the last item are on their way out of that item's k or v
+        auto release_own = [&](int buf) {
+            if (lane == 0) {
+                tma_store_wait_read();
+                bar_arrive(own_empty + 8 * buf);
+            }
+        };
+        DkvItem t;
+        for (int round = 0; next_item(a, round, t);) {
             const int key = t.k0 + row, buf = ordinal % OB;
             if (t.n == 0) {
                 if (key < sh.len_kv) {
-                    if (half == 0) zero_row(a.dk, sh.dim, t.b, t.hk, key);
+                    if (g == 0) zero_row(a.dk, sh.dim, t.b, t.hk, key);
                     else zero_row(a.dv, sh.dim, t.b, t.hk, key);
                 }
                 continue;
             }
-            int head = t.hk * sh.group, q_tile = t.q_first;
+            int q_tile = t.q_first;
             for (int j = 0; j < t.n; ++j, ++tile) {
-                const int st = tile % ST, q0 = q_tile * kStep, pos0 = q0 + sh.q_pos, col0 = 32 * half;
-                if (BIAS && q_tile == t.q_first) {             // another query head: its table, once nobody uses the last one's
-                    const int last = (t.q_first + t.per_head) * kStep - 1 + sh.q_pos;
-                    sync_threads(kAll, kMath);
-                    fill_lut(a.bias, head, lut_bucket, lut, a.pad, t.k0 - last, sh.causal ? 0 : t.k0 + kOwn - 1 - pos0, threadIdx.x, kMath);
-                    sync_threads(kAll, kMath);
-                }
-                wait_warp(stat_full + 8 * st, (tile / ST) & 1, dead, 256 << 16);
-                const float* nl = stats + st * Plan::stat_floats;
-                const float* nd = nl + kStep;
-                wait_warp(s_full, tile & 1, dead, 512 << 16);
-                tc_fence_after();
-                const Span span = BIAS ? span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0) : kSpanFarLeft;
-                const float mul = BIAS && span == kSpanMixed ? 1.0f : sh.scale_log2;
-                const float add = BIAS && span != kSpanMixed ? lut[span == kSpanFarLeft ? 0 : 2 * a.pad] : 0.0f;
-                const bool holes = nl[2 * kStep] != 0.0f;      // rows inside len_q with nothing allowed
-                // 16 columns at a time, for the registers' sake
-#pragma unroll 1
-                for (int c0 = 0; c0 < 32; c0 += 16) {
-                    const int col = col0 + c0;
-                    uint32_t s[16], d[16];
-                    tmem_ld16(s, lanes + Plan::s_col + col);
-                    tmem_ld16(d, lanes + Plan::dp_col + col);
+                const int table = heads & 1;
+                const bool head_starts = q_tile == t.q_first, head_ends = q_tile + 1 == t.q_first + t.per_head;
+                const int st = tile % ST, pos0 = q_tile * kStep + sh.q_pos;
+                if (LUT && head_starts) wait_warp(lut_full + 8 * table, (heads >> 1) & 1, dead, 256 << 16);
+                if ((tile & 1) == g) {
+                    const uint32_t parity = (tile >> 1) & 1;
+                    wait_warp(stat_full + 8 * st, (tile / ST) & 1, dead, 512 << 16);
+                    const float* nl = stats + st * Plan::stat_floats;
+                    const float* nd = nl + kStep;
+                    wait_warp(s_full + 8 * g, parity, dead, 1024 << 16);
+                    tc_fence_after();
+                    uint32_t s[2][32], d[2][32];
+                    tmem_ld32(s[0], s_at);
+                    tmem_ld32(s[1], s_at + 32);
+                    tmem_ld32(d[0], dp_at);
+                    tmem_ld32(d[1], dp_at + 32);
                     tmem_wait_ld();
-                    tmem_use(s);
-                    tmem_use(d);
-                    if (Plan::apart && c0 == 16) {
+                    tmem_use(s[0]);
+                    tmem_use(s[1]);
+                    tmem_use(d[0]);
+                    tmem_use(d[1]);
+                    if (Plan::apart) {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) bar_arrive(s_free);
+                        if (lane == 0) bar_arrive(s_free + 8 * g);
                     }
-                    if (BIAS && span == kSpanMixed) {
-                        const float* at = lut + a.pad + key - (pos0 + col);
+                    float mul = sh.scale_log2, add = 0.0f;
+                    if (LUT) {
+                        const float* lut = luts + table * a.lut.floats;
+                        const Span span = span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0);
+                        if (span == kSpanMixed) {
+                            const float* at = lut_at(lut, a.lut, pos0 - key);          // of the turned axis: query - key
+                            const uint64_t mul2v = pack2(mul, mul);
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) s[c] = __float_as_uint(fmaf(__uint_as_float(s[c]), sh.scale_log2, at[-c]));
-                    }
-                    const int first = sh.causal ? key - (pos0 + col) : 0;      // rows before it do not see the key
-                    if (sh.causal && t.k0 + kOwn - 1 > pos0) {
-#pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (c < first) s[c] = 0xFF800000u;
+                            for (int c = 0; c < kStep; c += 2) {
+                                const float2 b = *reinterpret_cast<const float2*>(at + c);
+                                float x, y;
+                                unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
+                                s[c >> 5][c & 31] = __float_as_uint(x);
+                                s[c >> 5][(c & 31) + 1] = __float_as_uint(y);
+                            }
+                            mul = 1.0f;
+                        } else {
+                            add = lut_far(lut, a.lut, span == kSpanFarRight);
+                        }
                     }
                     const uint64_t mul2v = pack2(mul, mul), add2v = pack2(add, add);
-                    uint32_t wp[8], wd[8];
+                    uint32_t wp[2][16], wd[2][16];
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const float4 l = *reinterpret_cast<const float4*>(nl + col + e);
-                        const float4 m = *reinterpret_cast<const float4*>(nd + col + e);
+                    for (int c = 0; c < kStep; c += 4) {
+                        const float4 l = *reinterpret_cast<const float4*>(nl + c);
+                        const float4 m = *reinterpret_cast<const float4*>(nd + c);
                         const uint64_t ls[2] = {pack2(l.x, l.y), pack2(l.z, l.w)}, ms[2] = {pack2(m.x, m.y), pack2(m.z, m.w)};
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            const int at = e + 2 * u;
+                            const int i = c >> 5, e = (c & 31) + 2 * u;
                             float x, y;
-                            unpack2(fma2(pack2(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), mul2v, add2(ls[u], add2v)), x, y);
+                            unpack2(fma2(pack2(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1])), mul2v, add2(ls[u], add2v)), x, y);
                             x = exp2_fast(x);
                             y = exp2_fast(y);
-                            wp[at >> 1] = pack_bf16(x, y);
-                            unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[at]), __uint_as_float(d[at + 1])), ms[u])), x, y);
-                            wd[at >> 1] = pack_bf16(x, y);
+                            wp[i][e >> 1] = pack_bf16(x, y);
+                            unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[i][e]), __uint_as_float(d[i][e + 1])), ms[u])), x, y);
+                            wd[i][e >> 1] = pack_bf16(x, y);
                         }
                     }
                     if (t.len == 1 || (sh.causal && key == 0)) {       // rows that see one key alone: p = 1, ds = 0
+                        const int alone = key - pos0;
 #pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (t.len == 1 || c == first) wd[c >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                        for (int c = 0; c < kStep; ++c)
+                            if (t.len == 1 || c == alone) wd[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                     }
-                    if (holes) {                               // whatever their do and q hold
+                    if (nl[2 * kStep] != 0.0f) {
+                        // rows inside len_q with nothing allowed: their do and q may hold anything and must not reach a product
 #pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (nl[col + c] == -INFINITY) {
-                                wp[c >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                                wd[c >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                        for (int c = 0; c < kStep; ++c)
+                            if (nl[c] == -INFINITY) {
+                                wp[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                                wd[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                             }
+                        const int r = row & (kStep - 1), part = row >> 6;
+                        if (nl[r] == -INFINITY) {
+#pragma unroll
+                            for (int c = 0; c < HALVES; ++c)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const uint32_t at = st * Plan::step_bytes + c * kStepBytes + r * 128 + 64 * part + 16 * e;
+                                    *reinterpret_cast<uint4*>(smem + (sq - base) + at) = make_uint4(0, 0, 0, 0);
+                                    *reinterpret_cast<uint4*>(smem + (sdo - base) + at) = make_uint4(0, 0, 0, 0);
+                                }
+                        }
+                        fence_async_smem();
                     }
-                    if (j > 0 && Plan::apart && c0 == 0) {     // P and dS of the last tile have been used
-                        wait_warp(acc_done, (tile - 1) & 1, dead, 1024 << 16);
+                    if (Plan::apart && tile > 1) {             // P and dS of the group's last tile have been used
+                        wait_warp(sums_done + 8 * g, parity ^ 1, dead, 2048 << 16);
                         tc_fence_after();
                     }
-                    tmem_st8(lanes + Plan::p_col + Plan::p_half * half + (c0 >> 1), wp);
-                    tmem_st8(lanes + Plan::ds_col + Plan::p_half * half + (c0 >> 1), wd);
-                }
-                if (holes) {
-                    // and must not reach a product: 0 * NaN
-                    const int r = threadIdx.x & (kStep - 1), part = threadIdx.x >> 6;
-                    if (nl[r] == -INFINITY) {
 #pragma unroll
-                        for (int c = 0; c < HALVES; ++c)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t at = st * Plan::step_bytes + c * kStepBytes + r * 128 + 32 * part + 16 * e;
-                                *reinterpret_cast<uint4*>(smem + (sq - base) + at) = make_uint4(0, 0, 0, 0);
-                                *reinterpret_cast<uint4*>(smem + (sdo - base) + at) = make_uint4(0, 0, 0, 0);
-                            }
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_st16(p_at + 16 * c, wp[c]);
+                        tmem_st16(ds_at + 16 * c, wd[c]);
                     }
-                    fence_async_smem();
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_ready + 8 * g);
+                    if (OB > 1 && leaving) {
+                        release_own((ordinal - 1) % OB);
+                        leaving = false;
+                    }
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(p_ready);
-                if (++q_tile == t.q_first + t.per_head) {
+                if (head_ends) {
+                    if (LUT) {
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(lut_empty + 8 * table);
+                    }
+                    ++heads;
                     q_tile = t.q_first;
-                    ++head;
+                } else {
+                    ++q_tile;
                 }
             }
-            wait_warp(acc_done, (tile - 1) & 1, dead, 2048 << 16);
+            if (OB > 1 && leaving) {                           // an item of one tile, which was the other group's
+                release_own((ordinal - 1) % OB);
+                leaving = false;
+            }
+            wait_warp(acc_done, ordinal & 1, dead, 4096 << 16);
             tc_fence_after();
-            // dk (warps 0-3) and dv go out through k's and v's places, which are free: every product has completed.  Keys
+            // dk (the first group) and dv go out through k's and v's places, which are free: every product has completed.  Keys
             // behind the sequence's end get zeros
-            const uint32_t col = half == 0 ? Plan::dk_col : Plan::dv_col;
-            uint8_t* staging = smem + ((half == 0 ? sk : sv) - base) + buf * Plan::own_bytes + quad * 2 * HALVES * 2048;
+            uint8_t* staging = smem + ((g == 0 ? sk : sv) - base) + buf * Plan::own_bytes + quad * 2 * HALVES * 2048;
 #pragma unroll
             for (int c = 0; c < 2 * HALVES; ++c) {
                 uint32_t r[32];
-                tmem_ld32(r, lanes + col + 32 * c);
+                tmem_ld32(r, lanes + (g == 0 ? Plan::dk_col : Plan::dv_col) + 32 * c);
                 tmem_wait_ld();
                 tmem_use(r);
                 if (key >= t.len) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) r[e] = 0;
                 }
-                if (t.k0 + 32 * quad >= sh.len_kv || 32 * c >= sh.dim) continue;
-                if (half == 0) store_box(&a.dk.map, r, sh.scale, staging + c * 2048, lane, 32 * c, t.k0 + 32 * quad, t.hk * a.dk.head_mul, t.b * a.dk.batch_mul);
-                else store_box(&a.dv.map, r, 1.0f, staging + c * 2048, lane, 32 * c, t.k0 + 32 * quad, t.hk * a.dv.head_mul, t.b * a.dv.batch_mul);
+                stage_box(r, g == 0 ? sh.scale : 1.0f, staging + c * 2048, lane);
             }
             tc_fence_before();
+            fence_async_smem();
             __syncwarp();
             if (lane == 0) {
                 bar_arrive(acc_free);
-                tma_store_wait_read();
-                bar_arrive(own_empty + 8 * buf);
+                if (t.k0 + 32 * quad < sh.len_kv) {
+                    for (int c = 0; c < 2 * HALVES; ++c) {
+                        if (32 * c >= sh.dim) continue;
+                        if (g == 0) tma_store4(&a.dk.map, smem_u32(staging) + c * 2048, 32 * c, t.k0 + 32 * quad, t.hk * a.dk.head_mul, t.b * a.dk.batch_mul);
+                        else tma_store4(&a.dv.map, smem_u32(staging) + c * 2048, 32 * c, t.k0 + 32 * quad, t.hk * a.dv.head_mul, t.b * a.dv.batch_mul);
+                    }
+                    tma_store_commit();
+                }
             }
+            if (OB > 1) leaving = true;                        // other places are ready: these may wait
+            else release_own(buf);
             ++ordinal;
         }
+        if (leaving) release_own((ordinal - 1) % OB);
     }
     __syncwarp();
     tc_fence_before();
@@ -894,10 +1010,25 @@ __global__ void __launch_bounds__(256) attn_dtable_kernel(const float* partial, 
 }
 
 template <typename K, typename A>
-int launch(K kernel, int per_sm, size_t smem, const A& a, cudaStream_t s) {
+int launch(K kernel, int threads, int per_sm, size_t smem, const A& a, cudaStream_t s) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ALSGD_E_CUDA;
     const int wave = blocks_at_once(smem, per_sm);
-    return launch_dependent(kernel, dim3(a.items < wave ? a.items : wave), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    return launch_dependent(kernel, dim3(a.items < wave ? a.items : wave), dim3(threads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}
+
+template <int HALVES>
+int launch_dq(const DqArgs& a, cudaStream_t s) {
+    const bool bias = a.bias.table != nullptr, lut = bias || a.shape.causal;
+    const size_t smem = dq_smem<HALVES>(a.lut, lut, bias ? a.bias.buckets : 0);
+    if (bias) return launch(attn_dq_kernel<HALVES, true, true>, kDqThreads, 2, smem, a, s);
+    return lut ? launch(attn_dq_kernel<HALVES, true, false>, kDqThreads, 2, smem, a, s) : launch(attn_dq_kernel<HALVES, false, false>, kDqThreads, 2, smem, a, s);
+}
+
+template <int HALVES>
+int launch_dkv(const DkvArgs& a, cudaStream_t s) {
+    const bool lut = a.bias.table != nullptr || a.shape.causal;
+    const size_t smem = dkv_smem<HALVES>(a.lut, lut);
+    return lut ? launch(attn_dkv_kernel<HALVES, true>, kDkvThreads, 1, smem, a, s) : launch(attn_dkv_kernel<HALVES, false>, kDkvThreads, 1, smem, a, s);
 }
 
 uint64_t delta_bytes(const alsgd_attn_desc& d) { return ((uint64_t)d.batch * d.heads_q * d.len_q * 4 + 255) / 256 * 256; }
@@ -951,7 +1082,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
         DqArgs a;
         a.shape = make_shape(d, kv_len);
         make_bias(d, table, &a.bias);
-        a.pad = a.bias.far + kOwn + kStep;
+        a.lut = lut_shape(a.bias.far, kOwn, kStep, a.shape.causal);
         a.row_blocks = blocks;
         a.items = (int)q_items;
         a.lse = lse;
@@ -965,17 +1096,14 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
             (rc = operand(dq, true, 32, 32, &a.dq)) != ALSGD_OK || (rc = operand(k, false, kStep, 64, &a.k)) != ALSGD_OK ||
             (rc = operand(v, false, kStep, 64, &a.v)) != ALSGD_OK)
             return rc;
-        if (d.dim <= 64) rc = d.buckets ? launch(attn_dq_kernel<1, true>, 2, dq_smem<1>(a.pad, (int)d.buckets), a, s)
-                                        : launch(attn_dq_kernel<1, false>, 2, dq_smem<1>(a.pad, 0), a, s);
-        else rc = d.buckets ? launch(attn_dq_kernel<2, true>, 2, dq_smem<2>(a.pad, (int)d.buckets), a, s)
-                            : launch(attn_dq_kernel<2, false>, 2, dq_smem<2>(a.pad, 0), a, s);
+        rc = d.dim <= 64 ? launch_dq<1>(a, s) : launch_dq<2>(a, s);
         if (rc != ALSGD_OK) return rc;
     }
     if (d.len_kv) {
         DkvArgs a;
         a.shape = make_shape(d, kv_len);
         make_bias(d, table, &a.bias);
-        a.pad = a.bias.far + kOwn + kStep;
+        a.lut = lut_shape(a.bias.far, kOwn, kStep, false);     // on the turned axis the allowed keys lie ahead
         a.items = (int)kv_items;
         a.lse = lse;
         a.delta = delta;
@@ -983,10 +1111,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
             (rc = operand(k, false, kOwn, 64, &a.k)) != ALSGD_OK || (rc = operand(v, false, kOwn, 64, &a.v)) != ALSGD_OK ||
             (rc = operand(dk, false, 32, 32, &a.dk)) != ALSGD_OK || (rc = operand(dv, false, 32, 32, &a.dv)) != ALSGD_OK)
             return rc;
-        if (d.dim <= 64) rc = d.buckets ? launch(attn_dkv_kernel<1, true>, 2, dkv_smem<1>(a.pad, true), a, s)
-                                        : launch(attn_dkv_kernel<1, false>, 2, dkv_smem<1>(a.pad, false), a, s);
-        else rc = d.buckets ? launch(attn_dkv_kernel<2, true>, 1, dkv_smem<2>(a.pad, true), a, s)
-                            : launch(attn_dkv_kernel<2, false>, 1, dkv_smem<2>(a.pad, false), a, s);
+        rc = d.dim <= 64 ? launch_dkv<1>(a, s) : launch_dkv<2>(a, s);
         if (rc != ALSGD_OK) return rc;
     }
     if (d.buckets) {

@@ -64,6 +64,15 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
     }
 }
 
+// ---- registers ------------------------------------------------------------------------------------------------
+
+// A group of four warps gives back or takes registers; what all groups of a block hold together stays within what the
+// block was launched with.  All four warps execute it.
+template <int N>
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // ---- named barriers ------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void sync_threads(int id, int threads) {
@@ -215,6 +224,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float log2_fast(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // Two lanes in one instruction; every product that is followed by an addition is written as one fused operation.
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
     uint64_t r;
@@ -243,28 +257,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-// 2^x for two x at once without the special function unit (16 results a clock on an SM, the bound of an attention
-// kernel's inner loop): x = n + f with n whole and |f| <= 1/2 by adding and subtracting 1.5 * 2^23, a polynomial of degree 4
-// for 2^f (fitted for the least largest relative error on that interval, 2.7e-6 with its roundings; the fast
-// instruction has 2e-7), and n added to the exponent.  x below -126 and NaN are taken as -126: 1e-38 where 2^x would be
-// less, so a caller marks rows that hold a NaN itself; x = +inf gives NaN.
-__device__ __forceinline__ void exp2_poly(uint64_t x2, float& y0, float& y1) {
-    float x0, x1;
-    unpack2(x2, x0, x1);
-    x2 = pack2(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
-    const uint64_t magic = pack2(12582912.0f, 12582912.0f), back = pack2(-12582912.0f, -12582912.0f), minus = pack2(-1.0f, -1.0f);
-    const uint64_t t = add2(x2, magic);
-    const uint64_t f = fma2(add2(t, back), minus, x2);
-    uint64_t p = fma2(f, pack2(0x1.3997d6p-7f, 0x1.3997d6p-7f), pack2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
-    p = fma2(p, f, pack2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
-    p = fma2(p, f, pack2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
-    p = fma2(p, f, pack2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
-    float t0, t1;
-    unpack2(t, t0, t1);
-    unpack2(p, y0, y1);
-    y0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
-    y1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
 }
 
 }  // namespace alsgd_tc

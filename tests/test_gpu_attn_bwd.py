@@ -122,6 +122,15 @@ def test_ragged_batches_with_poison_behind_the_end(kv_len, causal, dim):
         assert bool((got[1][b, m:] == 0).all()) and bool((got[2][b, m:] == 0).all())
 
 
+@pytest.mark.parametrize("q_pos", [0, 3, 40, 63, 65, 100])
+def test_poison_behind_the_end_that_the_causal_mask_covers(q_pos):
+    """Rows that stop before the sequence's end, in a tile that reaches behind it."""
+    def poison(q, k, v, dout, table):
+        for b, m in enumerate((228, 130)):
+            k[b, m:], v[b, m:] = math.nan, math.inf
+    check(Case(batch=2, len_q=128, len_kv=400, q_pos=q_pos, buckets=32, kv_len=(228, 130)), poison=poison)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 def test_rows_without_keys_take_no_part(dim):
     """More queries than keys: the first rows are empty, and whatever their q and dout hold reaches nothing."""

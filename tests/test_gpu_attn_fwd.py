@@ -110,6 +110,37 @@ def test_ragged_batches_with_poison_behind_the_end(kv_len, causal, dim):
     compare(c, out, lse, q, k, v, table)
 
 
+@pytest.mark.parametrize("q_pos", [0, 3, 40, 63, 65, 100])
+def test_poison_behind_the_end_that_the_causal_mask_covers(q_pos):
+    """Rows that stop before the sequence's end, in a tile that reaches behind it."""
+    c = Case(batch=2, len_q=128, len_kv=400, q_pos=q_pos, buckets=32, kv_len=(228, 130))
+    q, k, v, _, table, lens = c.inputs()
+    for b, m in enumerate(c.kv_len):
+        k[b, m:], v[b, m:] = math.nan, math.inf
+    out, lse = outputs(c)
+    plan_of(c).alsgd_attn_fwd(q, k, v, out, lse, table=table, kv_len=lens)
+    compare(c, out, lse, q, k, v, table)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_nonfinite_keys_reach_the_rows_that_may_see_them_only(bad):
+    """A key with a NaN or an infinity (its value is finite): earlier rows of a causal mask are as without it, rows that see
+    it are NaN, as the definition makes them."""
+    for n, at in ((200, 70), (200, 130), (300, 299)):
+        c = Case(len_q=n, heads_q=3, buckets=32)
+        q, k, v, _, table, _ = c.inputs()
+        k[:, at, :, 5] = bad
+        out, lse = outputs(c)
+        plan_of(c).alsgd_attn_fwd(q, k, v, out, lse, table=table)
+        clean = k.clone()
+        clean[:, at] = 0
+        o64, lse64, a = c.forward(q, clean, v, table)
+        assert bool(((out.double() - o64).abs() <= 1.02 * 2.0 ** -8 * (a + o64.abs()))[:, :at].all())
+        assert bool(((lse.double() - lse64).abs() <= 3e-5)[:, :, :at].all())
+        if math.isnan(bad):
+            assert bool(out[:, at:].isnan().all()) and bool(lse[:, :, at:].isnan().all())
+
+
 def test_no_keys_and_no_queries():
     check(Case(batch=2, len_q=200, len_kv=0, causal=False))
     check(Case(batch=2, len_q=0, len_kv=5, causal=False))
