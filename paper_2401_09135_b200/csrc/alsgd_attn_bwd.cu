@@ -35,7 +35,7 @@ constexpr uint32_t kOwnBytes = 128 * 128;      // 128 rows of 64 bf16
 constexpr uint32_t kStepBytes = 64 * 128;
 constexpr int kGroup = 16, kGroups = kStep / kGroup;   // columns whose diagonals are summed in one chain, chains
 constexpr int kChain = kGroup + 32;     // sums a chain leaves, padded
-constexpr int kDiagonals = kGroups * kChain;
+constexpr int kDiagonals = kGroups * kChain;            // of a warp; lanes that have none to leave write as many beside them
 
 // The threads of one item's arithmetic in attn_dq_kernel, named barrier 1.
 constexpr int kDqMath = 128, kDqThreads = 256;
@@ -51,7 +51,7 @@ struct DqArgs {
     const uint16_t* o;
     int64_t o_batch, o_pos, o_head;     // steps of o
     float* delta;                       // out: [batch][heads_q][len_q]
-    float* partial;                     // out: [batch * heads_q][row blocks][buckets]
+    float* partial;                     // out: [batch * heads_q][row blocks][4 warps][buckets]
     LutShape lut;
     int row_blocks, items;
 };
@@ -90,7 +90,7 @@ struct DqPlan {
 template <int HALVES>
 size_t dq_smem(const LutShape& l, bool lut, int buckets) {
     return 1024 + DqPlan<HALVES>::fixed_bytes + (lut ? DqPlan<HALVES>::own_bufs * l.floats * sizeof(float) + 2 * l.pad + 16 : 0) +
-           (buckets ? 4 * (kDiagonals + buckets) * sizeof(float) : 0);
+           (buckets ? 4 * (kDiagonals + kGroups * kGroup + buckets) * sizeof(float) : 0);
 }
 
 // LUT: there is a bias or a causal mask.  BIAS: there is a bias, and its gradient.
@@ -108,8 +108,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     const uint32_t full = lut_empty + 8 * OB, empty = full + 8 * ST;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
-    float* diagonals = reinterpret_cast<float*>(smem + Plan::fixed_bytes);             // [4 warps][kDiagonals]
-    float* by_bucket = diagonals + (BIAS ? 4 * kDiagonals : 0);                        // [4 warps][buckets]
+    constexpr int kSums = kDiagonals + kGroups * kGroup;
+    float* diagonals = reinterpret_cast<float*>(smem + Plan::fixed_bytes);             // [4 warps][kSums]
+    float* by_bucket = diagonals + (BIAS ? 4 * kSums : 0);                             // [4 warps][buckets]
     float* luts = by_bucket + (BIAS ? 4 * a.bias.buckets : 0);
     uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + OB * a.lut.floats);
 
@@ -257,7 +258,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         take_registers<kDqMathRegisters>();
         const int row = threadIdx.x;
         const uint32_t lanes = tmem + ((uint32_t)warp << 21);
-        float* sums = diagonals + warp * kDiagonals;
+        float* sums = diagonals + warp * kSums;
+        float* leaves = lane == 31 ? sums : sums + kDiagonals;         // a chain's end, and a place nobody reads
+        const int leave_step = lane == 31 ? kChain : kGroup;
         float* bucket_sums = by_bucket + warp * a.bias.buckets;
         int ordinal = 0, tile = 0;
         bool leaving = false;          // this warp's rows of the last item are on their way out of that item's q
@@ -267,10 +270,12 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 bar_arrive(own_empty + 8 * buf);
             }
         };
-        // the row of o that delta wants, asked for one item ahead
+        // the row of o that delta wants, and its lse, asked for one item ahead
         uint4 o[8 * HALVES];
+        float next_lse = -INFINITY;
         auto ask_for_o = [&](const DqItem& t) {
             const uint16_t* p = a.o + (int64_t)t.b * a.o_batch + (int64_t)(t.q0 + row) * a.o_pos + (int64_t)t.h * a.o_head;
+            next_lse = t.q0 + row < sh.len_q ? a.lse[((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row] : -INFINITY;
 #pragma unroll
             for (int c = 0; c < 8 * HALVES; ++c)
                 o[c] = t.q0 + row < sh.len_q && 8 * c < sh.dim ? *reinterpret_cast<const uint4*>(p + 8 * c) : make_uint4(0, 0, 0, 0);
@@ -283,19 +288,19 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             const int buf = ordinal % OB;
             const bool inside = t.q0 + row < sh.len_q;
             const size_t stat = ((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row;
-            float* partial = a.partial + (((size_t)t.b * sh.heads_q + t.h) * a.row_blocks + t.block) * a.bias.buckets;
+            float* partial = a.partial + ((((size_t)t.b * sh.heads_q + t.h) * a.row_blocks + t.block) * 4 + warp) * a.bias.buckets;
             if (t.n == 0) {
                 if (inside) {
                     zero_row(a.dq, sh.dim, t.b, t.h, t.q0 + row);
                     a.delta[stat] = 0.0f;
                 }
                 if (BIAS)
-                    for (int e = threadIdx.x; e < a.bias.buckets; e += kDqMath) partial[e] = 0.0f;
+                    for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = 0.0f;
                 more = next_item(a, round, t);
                 if (more) ask_for_o(t);
                 continue;
             }
-            const float lse = inside ? a.lse[stat] : -INFINITY;
+            const float lse = next_lse;
             const bool live = lse != -INFINITY;
             const int pos = t.q0 + row + sh.q_pos;
             const float* lut = luts + buf * a.lut.floats;
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             const bool cut = t.len < sh.len_kv || !(sh.causal && min(t.q0 + kOwn, sh.len_q) + sh.q_pos <= t.len);
             const bool some_idle = __any_sync(0xFFFFFFFFu, !used);
             const float lse2 = live ? lse * kLog2e : 0.0f;
-            float far_left = 0.0f, far_right = 0.0f;
+            float far_left = 0.0f, far_right = 0.0f, left = 0.0f, right = 0.0f;
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int k0 = j * kStep;
                 wait_warp(s_full, tile & 1, dead, 512 << 16);
@@ -353,7 +358,11 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 float mul = sh.scale_log2, off = -lse2;
                 Span span = kSpanMixed;
                 if (LUT) {
-                    if (j == 0) wait_warp(lut_full + 8 * buf, (ordinal / OB) & 1, dead, 1024 << 16);
+                    if (j == 0) {
+                        wait_warp(lut_full + 8 * buf, (ordinal / OB) & 1, dead, 1024 << 16);
+                        left = lut_far(lut, a.lut, false);
+                        right = lut_far(lut, a.lut, true);
+                    }
                     span = span_of(a.bias, k0 - (t.q0 + kOwn - 1 + sh.q_pos), k0 + kStep - 1 - (t.q0 + sh.q_pos));
                     if (span == kSpanMixed) {
                         const float* at = lut_at(lut, a.lut, k0 - pos);
@@ -368,7 +377,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                         }
                         mul = 1.0f;
                     } else {
-                        off += lut_far(lut, a.lut, span == kSpanFarRight);
+                        off += span == kSpanFarRight ? right : left;
                     }
                     if (j + 1 == t.n) {
                         __syncwarp();
@@ -437,7 +446,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                             for (int g = 0; g < kGroups; ++g) {
                                 run[g] = __shfl_up_sync(0xFFFFFFFFu, run[g], 1);
                                 run[g] = (lane == 0 ? 0.0f : run[g]) + __uint_as_float(d[(kGroup * g + c) >> 5][(kGroup * g + c) & 31]);
-                                if (lane == 31) sums[kChain * g + c] = run[g];
+                                leaves[leave_step * g + c] = run[g];
                             }
                         }
 #pragma unroll
@@ -485,10 +494,8 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     bucket_sums[lut_bucket[0]] += far_left;
                     bucket_sums[lut_bucket[2 * a.lut.pad]] += far_right;
                 }
-                sync_threads(1, kDqMath);
-                for (int e = threadIdx.x; e < a.bias.buckets; e += kDqMath)
-                    partial[e] = (by_bucket[e] + by_bucket[a.bias.buckets + e]) + (by_bucket[2 * a.bias.buckets + e] + by_bucket[3 * a.bias.buckets + e]);
-                sync_threads(1, kDqMath);
+                __syncwarp();
+                for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = bucket_sums[e];
             }
             wait_warp(dq_done, (tile - 1) & 1, dead, 4096 << 16);
             tc_fence_after();
@@ -671,24 +678,19 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
             }
             ++ordinal;
             int head = t.hk * sh.group, q_tile = t.q_first;
-            for (int j = 0; j < t.n; ++j, ++tile) {
-                const int st = tile % ST, q0 = q_tile * kStep;
-                // lse and delta of the tile's rows, two per lane, on their way before the tile's place is free
-                float nl[2], nd[2];
-                bool hole = false;
+            float lse[2], delta[2];                            // of the tile's rows, two per lane, asked for one tile ahead
+            auto ask = [&](int head, int q_tile) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = q0 + lane + 32 * e;
-                    nl[e] = -INFINITY;                         // a row behind len_q, or without allowed keys: p = 0
-                    nd[e] = 0.0f;
-                    if (r < sh.len_q) {
-                        const size_t at = ((size_t)t.b * sh.heads_q + head) * sh.len_q + r;
-                        const float lse = a.lse[at];
-                        if (lse == -INFINITY) hole = true; else nl[e] = -lse * kLog2e;
-                        nd[e] = -a.delta[at];
-                    }
+                    const int r = q_tile * kStep + lane + 32 * e;
+                    const size_t at = ((size_t)t.b * sh.heads_q + head) * sh.len_q + r;
+                    lse[e] = r < sh.len_q ? a.lse[at] : INFINITY;      // behind len_q: p = 0
+                    delta[e] = r < sh.len_q ? a.delta[at] : 0.0f;
                 }
-                hole = __any_sync(0xFFFFFFFFu, hole);
+            };
+            ask(head, q_tile);
+            for (int j = 0; j < t.n; ++j, ++tile) {
+                const int st = tile % ST, q0 = q_tile * kStep;
                 wait_warp(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                 if (__any_sync(0xFFFFFFFFu, *dead)) break;
                 if (lane == 0) {
@@ -700,18 +702,22 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                     }
                 }
                 float* stat = stats + st * Plan::stat_floats;
+                bool hole = false;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    stat[lane + 32 * e] = nl[e];
-                    stat[kStep + lane + 32 * e] = nd[e];
+                    hole |= lse[e] == -INFINITY;               // a row without allowed keys: p = 0 too
+                    stat[lane + 32 * e] = lse[e] == -INFINITY ? -INFINITY : -lse[e] * kLog2e;
+                    stat[kStep + lane + 32 * e] = -delta[e];
                 }
-                if (lane == 0) stat[2 * kStep] = hole ? 1.0f : 0.0f;
-                __syncwarp();
-                if (lane == 0) bar_arrive(stat_full + 8 * st);
                 if (++q_tile == t.q_first + t.per_head) {
                     q_tile = t.q_first;
                     ++head;
                 }
+                if (j + 1 < t.n) ask(head, q_tile);
+                hole = __any_sync(0xFFFFFFFFu, hole);
+                if (lane == 0) stat[2 * kStep] = hole ? 1.0f : 0.0f;
+                __syncwarp();
+                if (lane == 0) bar_arrive(stat_full + 8 * st);
             }
         }
         // every copy has landed before the block may leave, whoever else has given up
@@ -814,11 +820,16 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                 continue;
             }
             int q_tile = t.q_first;
+            bool head_starts_for_me = false;
+            float left = 0.0f, right = 0.0f;                   // the bias of the head's far keys
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int table = heads & 1;
                 const bool head_starts = q_tile == t.q_first, head_ends = q_tile + 1 == t.q_first + t.per_head;
                 const int st = tile % ST, pos0 = q_tile * kStep + sh.q_pos;
-                if (LUT && head_starts) wait_warp(lut_full + 8 * table, (heads >> 1) & 1, dead, 256 << 16);
+                if (LUT && head_starts) {
+                    wait_warp(lut_full + 8 * table, (heads >> 1) & 1, dead, 256 << 16);
+                    head_starts_for_me = true;
+                }
                 if ((tile & 1) == g) {
                     const uint32_t parity = (tile >> 1) & 1;
                     wait_warp(stat_full + 8 * st, (tile / ST) & 1, dead, 512 << 16);
@@ -826,74 +837,80 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                     const float* nd = nl + kStep;
                     wait_warp(s_full + 8 * g, parity, dead, 1024 << 16);
                     tc_fence_after();
-                    uint32_t s[2][32], d[2][32];
-                    tmem_ld32(s[0], s_at);
-                    tmem_ld32(s[1], s_at + 32);
-                    tmem_ld32(d[0], dp_at);
-                    tmem_ld32(d[1], dp_at + 32);
-                    tmem_wait_ld();
-                    tmem_use(s[0]);
-                    tmem_use(s[1]);
-                    tmem_use(d[0]);
-                    tmem_use(d[1]);
-                    if (Plan::apart) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(s_free + 8 * g);
+                    if (LUT && head_starts_for_me) {
+                        left = lut_far(luts + table * a.lut.floats, a.lut, false);
+                        right = lut_far(luts + table * a.lut.floats, a.lut, true);
+                        head_starts_for_me = false;
                     }
-                    float mul = sh.scale_log2, add = 0.0f;
-                    if (LUT) {
-                        const float* lut = luts + table * a.lut.floats;
-                        const Span span = span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0);
-                        if (span == kSpanMixed) {
-                            const float* at = lut_at(lut, a.lut, pos0 - key);          // of the turned axis: query - key
-                            const uint64_t mul2v = pack2(mul, mul);
+                    const Span span = LUT ? span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0) : kSpanFarLeft;
+                    const bool mixed = LUT && span == kSpanMixed;
+                    const float mul = mixed ? 1.0f : sh.scale_log2, add = LUT && !mixed ? (span == kSpanFarRight ? right : left) : 0.0f;
+                    const float* bias_at = LUT ? lut_at(luts + table * a.lut.floats, a.lut, pos0 - key) : nullptr;     // on the turned axis: query - key
+                    const bool holes = nl[2 * kStep] != 0.0f, single = t.len == 1 || (sh.causal && key == 0);
+                    // half a tile at a time: lse and delta of its columns need registers too
 #pragma unroll
-                            for (int c = 0; c < kStep; c += 2) {
-                                const float2 b = *reinterpret_cast<const float2*>(at + c);
+                    for (int c0 = 0; c0 < kStep; c0 += 32) {
+                        uint32_t s[32], d[32];
+                        tmem_ld32(s, s_at + c0);
+                        tmem_ld32(d, dp_at + c0);
+                        tmem_wait_ld();
+                        tmem_use(s);
+                        tmem_use(d);
+                        if (Plan::apart && c0 == 32) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(s_free + 8 * g);
+                        }
+                        if (mixed) {
+                            const uint64_t scale2 = pack2(sh.scale_log2, sh.scale_log2);
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2) {
+                                const float2 b = *reinterpret_cast<const float2*>(bias_at + c0 + c);
                                 float x, y;
-                                unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
-                                s[c >> 5][c & 31] = __float_as_uint(x);
-                                s[c >> 5][(c & 31) + 1] = __float_as_uint(y);
+                                unpack2(fma2(pack2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, pack2(b.x, b.y)), x, y);
+                                s[c] = __float_as_uint(x);
+                                s[c + 1] = __float_as_uint(y);
                             }
-                            mul = 1.0f;
-                        } else {
-                            add = lut_far(lut, a.lut, span == kSpanFarRight);
                         }
-                    }
-                    const uint64_t mul2v = pack2(mul, mul), add2v = pack2(add, add);
-                    uint32_t wp[2][16], wd[2][16];
+                        const uint64_t mul2v = pack2(mul, mul), add2v = pack2(add, add);
+                        uint32_t wp[16], wd[16];
 #pragma unroll
-                    for (int c = 0; c < kStep; c += 4) {
-                        const float4 l = *reinterpret_cast<const float4*>(nl + c);
-                        const float4 m = *reinterpret_cast<const float4*>(nd + c);
-                        const uint64_t ls[2] = {pack2(l.x, l.y), pack2(l.z, l.w)}, ms[2] = {pack2(m.x, m.y), pack2(m.z, m.w)};
+                        for (int c = 0; c < 32; c += 4) {
+                            const float4 l = *reinterpret_cast<const float4*>(nl + c0 + c);
+                            const float4 m = *reinterpret_cast<const float4*>(nd + c0 + c);
+                            const uint64_t ls[2] = {pack2(l.x, l.y), pack2(l.z, l.w)}, ms[2] = {pack2(m.x, m.y), pack2(m.z, m.w)};
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int i = c >> 5, e = (c & 31) + 2 * u;
-                            float x, y;
-                            unpack2(fma2(pack2(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1])), mul2v, add2(ls[u], add2v)), x, y);
-                            x = exp2_fast(x);
-                            y = exp2_fast(y);
-                            wp[i][e >> 1] = pack_bf16(x, y);
-                            unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[i][e]), __uint_as_float(d[i][e + 1])), ms[u])), x, y);
-                            wd[i][e >> 1] = pack_bf16(x, y);
-                        }
-                    }
-                    if (t.len == 1 || (sh.causal && key == 0)) {       // rows that see one key alone: p = 1, ds = 0
-                        const int alone = key - pos0;
-#pragma unroll
-                        for (int c = 0; c < kStep; ++c)
-                            if (t.len == 1 || c == alone) wd[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                    }
-                    if (nl[2 * kStep] != 0.0f) {
-                        // rows inside len_q with nothing allowed: their do and q may hold anything and must not reach a product
-#pragma unroll
-                        for (int c = 0; c < kStep; ++c)
-                            if (nl[c] == -INFINITY) {
-                                wp[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                                wd[c >> 5][(c & 31) >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                            for (int u = 0; u < 2; ++u) {
+                                const int e = c + 2 * u;
+                                float x, y;
+                                unpack2(fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), mul2v, add2(ls[u], add2v)), x, y);
+                                x = exp2_fast(x);
+                                y = exp2_fast(y);
+                                wp[e >> 1] = pack_bf16(x, y);
+                                unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), ms[u])), x, y);
+                                wd[e >> 1] = pack_bf16(x, y);
                             }
+                        }
+                        if (single || holes) {
+                            // rows that see one key alone: p = 1, ds = 0.  Rows inside len_q with nothing allowed: whatever do and q hold
+                            const int alone = key - pos0 - c0;
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const uint32_t keep = c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                                const bool hole = holes && nl[c0 + c] == -INFINITY;
+                                if (hole) wp[c >> 1] &= keep;
+                                if (hole || (single && (t.len == 1 || c == alone))) wd[c >> 1] &= keep;
+                            }
+                        }
+                        if (Plan::apart && tile > 1 && c0 == 0) {      // P and dS of the group's last tile have been used
+                            wait_warp(sums_done + 8 * g, parity ^ 1, dead, 2048 << 16);
+                            tc_fence_after();
+                        }
+                        tmem_st16(p_at + (c0 >> 1), wp);
+                        tmem_st16(ds_at + (c0 >> 1), wd);
+                    }
+                    if (holes) {
+                        // and must not reach a product: 0 * NaN
                         const int r = row & (kStep - 1), part = row >> 6;
                         if (nl[r] == -INFINITY) {
 #pragma unroll
@@ -906,15 +923,6 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                                 }
                         }
                         fence_async_smem();
-                    }
-                    if (Plan::apart && tile > 1) {             // P and dS of the group's last tile have been used
-                        wait_warp(sums_done + 8 * g, parity ^ 1, dead, 2048 << 16);
-                        tc_fence_after();
-                    }
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        tmem_st16(p_at + 16 * c, wp[c]);
-                        tmem_st16(ds_at + 16 * c, wd[c]);
                     }
                     tmem_wait_st();
                     tc_fence_before();
@@ -997,8 +1005,8 @@ __global__ void __launch_bounds__(256) attn_dtable_kernel(const float* partial, 
     double s = 0.0;
     if (bucket < buckets)
         for (int i = threadIdx.y; i < batch * blocks; i += 8) {
-            const size_t row = ((size_t)(i / blocks) * heads + h) * blocks + i % blocks;
-            s += partial[row * buckets + bucket];
+            const float* row = partial + (((size_t)(i / blocks) * heads + h) * blocks + i % blocks) * 4 * buckets + bucket;
+            s += (double)(row[0] + row[buckets]) + (double)(row[2 * buckets] + row[3 * buckets]);
         }
     shared[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
@@ -1032,7 +1040,7 @@ int launch_dkv(const DkvArgs& a, cudaStream_t s) {
 }
 
 uint64_t delta_bytes(const alsgd_attn_desc& d) { return ((uint64_t)d.batch * d.heads_q * d.len_q * 4 + 255) / 256 * 256; }
-uint64_t partial_bytes(const alsgd_attn_desc& d) { return (uint64_t)d.batch * d.heads_q * ((d.len_q + kOwn - 1) / kOwn) * d.buckets * 4; }
+uint64_t partial_bytes(const alsgd_attn_desc& d) { return (uint64_t)d.batch * d.heads_q * ((d.len_q + kOwn - 1) / kOwn) * 4 * d.buckets * 4; }
 
 }  // namespace
 

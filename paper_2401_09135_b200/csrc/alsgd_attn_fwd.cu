@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
             const bool cut = t.len < sh.len_kv || !(sh.causal && min(t.q0 + kRows, sh.len_q) + sh.q_pos <= t.len);
             const int buf = ordinal % QB;
             const float* lut = luts + buf * a.lut.floats;
-            float ref = -INFINITY, sum = 0.0f;
+            float ref = -INFINITY, sum = 0.0f, left = 0.0f, right = 0.0f;
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int k0 = j * kKeys;
                 wait_warp(s_full, tile & 1, dead, 1024);
@@ -295,7 +295,11 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
                 // x = v * mul + add, in base 2
                 float mul = sh.scale_log2, add = 0.0f;
                 if (LUT) {
-                    if (j == 0) wait_warp(lut_full + 8 * buf, (ordinal / QB) & 1, dead, 1 << 15);
+                    if (j == 0) {
+                        wait_warp(lut_full + 8 * buf, (ordinal / QB) & 1, dead, 1 << 15);
+                        left = lut_far(lut, a.lut, false);
+                        right = lut_far(lut, a.lut, true);
+                    }
                     const Span span = span_of(a.bias, k0 - (t.q0 + kRows - 1 + sh.q_pos), k0 + kKeys - 1 - (t.q0 + sh.q_pos));
                     if (span == kSpanMixed) {
                         const float* at = lut_at(lut, a.lut, k0 - pos);
@@ -310,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
                         }
                         mul = 1.0f;
                     } else {
-                        add = lut_far(lut, a.lut, span == kSpanFarRight);
+                        add = span == kSpanFarRight ? right : left;
                     }
                     if (j + 1 == t.n) {
                         __syncwarp();
