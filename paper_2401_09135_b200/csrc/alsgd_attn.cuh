@@ -58,6 +58,21 @@ __device__ __forceinline__ int bucket_of(const Bias& s, int r) {
     return at + (s.two_sided && r > 0 ? s.per_side : 0);
 }
 
+// First and last distance r of a bucket (far beyond any tile where it is open; first > last where it is empty).
+__device__ __forceinline__ void bucket_span(const Bias& s, int bucket, int& first, int& last) {
+    const bool ahead = s.two_sided && bucket >= s.per_side;
+    const int n = ahead ? bucket - s.per_side : bucket;
+    auto edge = [&](int n) { return n <= s.near ? n : s.limits[n - s.near - 1]; };
+    const int low = edge(n), high = n + 1 == s.per_side ? 1 << 14 : edge(n + 1) - 1;     // of |r|
+    if (ahead) {
+        first = max(low, 1);
+        last = high;
+    } else {
+        first = -high;
+        last = n == 0 && !s.two_sided ? 1 << 14 : -low;
+    }
+}
+
 __device__ __forceinline__ float table_entry(const Bias& s, int head, int bucket) {
     const size_t i = (size_t)head * s.buckets + bucket;
     return s.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(s.table)[i] << 16) : static_cast<const float*>(s.table)[i];

@@ -39,7 +39,7 @@ constexpr int kDiagonals = kGroups * kChain;            // of a warp; lanes that
 
 // The threads of one item's arithmetic in attn_dq_kernel, named barrier 1.
 constexpr int kDqMath = 128, kDqThreads = 256;
-constexpr int kDqMathRegisters = 184, kDqOtherRegisters = 72;  // 128 threads each; launched with 128 a thread
+constexpr int kDqMathRegisters = 200, kDqOtherRegisters = 56;  // 128 threads each; launched with 128 a thread
 
 // =============================================================================================== dq
 
@@ -90,7 +90,7 @@ struct DqPlan {
 template <int HALVES>
 size_t dq_smem(const LutShape& l, bool lut, int buckets) {
     return 1024 + DqPlan<HALVES>::fixed_bytes + (lut ? DqPlan<HALVES>::own_bufs * l.floats * sizeof(float) + 2 * l.pad + 16 : 0) +
-           (buckets ? 4 * (kDiagonals + kGroups * kGroup + buckets) * sizeof(float) : 0);
+           (buckets ? 4 * (kDiagonals + kGroups * kGroup + buckets) * sizeof(float) + buckets * sizeof(short2) : 0);
 }
 
 // LUT: there is a bias or a causal mask.  BIAS: there is a bias, and its gradient.
@@ -111,7 +111,8 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     constexpr int kSums = kDiagonals + kGroups * kGroup;
     float* diagonals = reinterpret_cast<float*>(smem + Plan::fixed_bytes);             // [4 warps][kSums]
     float* by_bucket = diagonals + (BIAS ? 4 * kSums : 0);                             // [4 warps][buckets]
-    float* luts = by_bucket + (BIAS ? 4 * a.bias.buckets : 0);
+    short2* spans = reinterpret_cast<short2*>(by_bucket + (BIAS ? 4 * a.bias.buckets : 0));       // distances of a bucket
+    float* luts = reinterpret_cast<float*>(spans) + (BIAS ? (a.bias.buckets + 3) / 4 * 4 : 0);
     uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + OB * a.lut.floats);
 
     const Shape& sh = a.shape;
@@ -147,7 +148,14 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         tma_prefetch(&a.dq.map);
     }
     if (LUT && warp < 4) {
-        if (BIAS) fill_buckets(a.bias, lut_bucket, a.lut.pad, threadIdx.x, kDqMath);
+        if (BIAS) {
+            fill_buckets(a.bias, lut_bucket, a.lut.pad, threadIdx.x, kDqMath);
+            for (int e = threadIdx.x; e < a.bias.buckets; e += kDqMath) {
+                int first, last;
+                bucket_span(a.bias, e, first, last);
+                spans[e] = make_short2((short)first, (short)last);
+            }
+        }
         if (sh.causal)
             for (int i = 0; i < OB; ++i) mask_ahead(luts + i * a.lut.floats, a.lut, threadIdx.x, kDqMath);
     }
@@ -261,6 +269,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         float* sums = diagonals + warp * kSums;
         float* leaves = lane == 31 ? sums : sums + kDiagonals;         // a chain's end, and a place nobody reads
         const int leave_step = lane == 31 ? kChain : kGroup;
+        const float not_first = lane == 0 ? 0.0f : 1.0f;               // nothing comes into lane 0
         float* bucket_sums = by_bucket + warp * a.bias.buckets;
         int ordinal = 0, tile = 0;
         bool leaving = false;          // this warp's rows of the last item are on their way out of that item's q
@@ -270,7 +279,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 bar_arrive(own_empty + 8 * buf);
             }
         };
-        // the row of o that delta wants, and its lse, asked for one item ahead
+        // the row of o that delta wants, and its lse, asked for one item ahead (a row of 64; twice that would hold too many registers)
         uint4 o[8 * HALVES];
         float next_lse = -INFINITY;
         auto ask_for_o = [&](const DqItem& t) {
@@ -283,8 +292,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         int round = 0;
         DqItem t;
         bool more = next_item(a, round, t);
-        if (more) ask_for_o(t);
+        if (more && HALVES == 1) ask_for_o(t);
         while (more) {
+            if (HALVES == 2) ask_for_o(t);
             const int buf = ordinal % OB;
             const bool inside = t.q0 + row < sh.len_q;
             const size_t stat = ((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row;
@@ -297,7 +307,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 if (BIAS)
                     for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = 0.0f;
                 more = next_item(a, round, t);
-                if (more) ask_for_o(t);
+                if (more && HALVES == 1) ask_for_o(t);
                 continue;
             }
             const float lse = next_lse;
@@ -439,39 +449,52 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     } else {
                         // Sums along the diagonals of the warp's 32 x 64 part: a running sum moves one lane down per column and
                         // leaves at lane 31, complete.  Four groups of 16 columns, whose chains of shuffles overlap.
-                        float run[kGroups] = {};
+                        float run[kGroups][4];
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g) run[g][3] = 0.0f;
 #pragma unroll
                         for (int c = 0; c < kGroup; ++c) {
 #pragma unroll
                             for (int g = 0; g < kGroups; ++g) {
-                                run[g] = __shfl_up_sync(0xFFFFFFFFu, run[g], 1);
-                                run[g] = (lane == 0 ? 0.0f : run[g]) + __uint_as_float(d[(kGroup * g + c) >> 5][(kGroup * g + c) & 31]);
-                                leaves[leave_step * g + c] = run[g];
+                                const float moved = __shfl_up_sync(0xFFFFFFFFu, run[g][(c + 3) & 3], 1);
+                                run[g][c & 3] = fmaf(moved, not_first, __uint_as_float(d[(kGroup * g + c) >> 5][(kGroup * g + c) & 31]));
+                                if ((c & 3) == 3)
+                                    *reinterpret_cast<float4*>(leaves + leave_step * g + c - 3) = make_float4(run[g][0], run[g][1], run[g][2], run[g][3]);
                             }
                         }
 #pragma unroll
-                        for (int g = 0; g < kGroups; ++g) sums[kChain * g + (lane == 31 ? kChain - 1 : kChain - 2 - lane)] = lane == 31 ? 0.0f : run[g];
+                        for (int g = 0; g < kGroups; ++g) sums[kChain * g + (lane == 31 ? kChain - 1 : kChain - 2 - lane)] = lane == 31 ? 0.0f : run[g][3];
                         __syncwarp();
+                        // A bucket is a run of distances: sums within runs, 32 diagonals at a time, and the last lane of each run
+                        // adds to its bucket
                         const int first = k0 - (t.q0 + 32 * warp + 31 + sh.q_pos);     // distance of diagonal 0
+                        float x[3];
+                        int bucket[3], from[3], to[3];
 #pragma unroll
                         for (int e = 0; e < 3; ++e) {
-                            // a bucket is a run of distances: sums within runs, and the last lane of each run adds to its bucket
                             const int at = 32 * e + lane;
-                            const int bucket = lut_bucket[a.lut.pad + first + at];
-                            float x = 0.0f;
+                            bucket[e] = lut_bucket[a.lut.pad + first + at];
+                            const short2 span = spans[bucket[e]];
+                            from[e] = max(span.x - first - 32 * e, 0);
+                            to[e] = min(span.y - first - 32 * e, 31);
+                            x[e] = 0.0f;
 #pragma unroll
                             for (int g = 0; g < kGroups; ++g) {
                                 const int local = at - kGroup * g;
-                                if (local >= 0 && local < kChain) x += sums[kChain * g + local];
+                                if (local >= 0 && local < kChain) x[e] += sums[kChain * g + local];
                             }
+                        }
 #pragma unroll
-                            for (int o = 1; o < 32; o <<= 1) {
-                                const float y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-                                const int other = __shfl_up_sync(0xFFFFFFFFu, bucket, o);
-                                if (lane >= o && other == bucket) x += y;
+                        for (int o = 1; o < 32; o <<= 1) {
+#pragma unroll
+                            for (int e = 0; e < 3; ++e) {
+                                const float y = __shfl_up_sync(0xFFFFFFFFu, x[e], o);
+                                if (lane - o >= from[e]) x[e] += y;
                             }
-                            const int next = __shfl_down_sync(0xFFFFFFFFu, bucket, 1);
-                            if (lane == 31 || next != bucket) bucket_sums[bucket] += x;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 3; ++e) {
+                            if (lane == to[e]) bucket_sums[bucket[e]] += x[e];
                             __syncwarp();
                         }
                     }
@@ -483,7 +506,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             }
             const DqItem last = t;
             more = next_item(a, round, t);
-            if (more) ask_for_o(t);
+            if (more && HALVES == 1) ask_for_o(t);
             if (BIAS) {
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
