@@ -85,8 +85,8 @@ __device__ __forceinline__ void fill_buckets(const Bias& s, uint8_t* bucket, int
 
 // One head's bias by distance in the exponent's base 2, as the tiles that lie within reach of the buckets' edges read it: a
 // thread wants consecutive distances from its own start on, its neighbour the same ones moved by one.  Two copies, the
-// second moved by one element, give every thread aligned pairs whatever its start; they lie 64 bytes (modulo 128) apart,
-// so that a warp's even and odd threads use different banks.
+// second moved by one element, give every thread aligned pairs whatever its start.  They lie 72 bytes (modulo 128) apart:
+// the 16 threads of a half-warp then use 32 banks, when the first thread's start is even as `pad` is.
 struct LutShape {
     int pad;                           // distances start at -pad
     int copy;                          // floats from one copy to the next
@@ -95,10 +95,10 @@ struct LutShape {
 
 __host__ __device__ inline LutShape lut_shape(int far, int tile_a, int tile_b, bool causal) {
     LutShape s;
-    s.pad = far + tile_a + tile_b;
+    s.pad = (far + tile_a + tile_b + 1) / 2 * 2;
     const int reach = causal ? tile_a + tile_b : s.pad;        // no allowed key lies ahead; masked ones are read, whatever is there
-    s.copy = (s.pad + reach + 2 + 31) / 32 * 32 + 16;
-    s.floats = 2 * s.copy + 16;
+    s.copy = (s.pad + reach + 2 + 31) / 32 * 32 + 18;
+    s.floats = 2 * s.copy + 4;
     return s;
 }
 

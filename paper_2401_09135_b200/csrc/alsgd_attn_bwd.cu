@@ -344,7 +344,12 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             const bool cut = t.len < sh.len_kv || !(sh.causal && min(t.q0 + kOwn, sh.len_q) + sh.q_pos <= t.len);
             const bool some_idle = __any_sync(0xFFFFFFFFu, !used);
             const float lse2 = live ? lse * kLog2e : 0.0f;
-            float far_left = 0.0f, far_right = 0.0f, left = 0.0f, right = 0.0f;
+            float far_left = 0.0f, far_right = 0.0f, left = 0.0f, right = 0.0f;        // left, right: the far keys' bias
+            if (LUT) {
+                wait_warp(lut_full + 8 * buf, (ordinal / OB) & 1, dead, 1024 << 16);
+                left = lut_far(lut, a.lut, false);
+                right = lut_far(lut, a.lut, true);
+            }
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int k0 = j * kStep;
                 wait_warp(s_full, tile & 1, dead, 512 << 16);
@@ -364,45 +369,32 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     __syncwarp();
                     if (lane == 0) bar_arrive(s_free);
                 }
-                // x - lse = s * mul + off in base 2
-                float mul = sh.scale_log2, off = -lse2;
-                Span span = kSpanMixed;
-                if (LUT) {
-                    if (j == 0) {
-                        wait_warp(lut_full + 8 * buf, (ordinal / OB) & 1, dead, 1024 << 16);
-                        left = lut_far(lut, a.lut, false);
-                        right = lut_far(lut, a.lut, true);
-                    }
-                    span = span_of(a.bias, k0 - (t.q0 + kOwn - 1 + sh.q_pos), k0 + kStep - 1 - (t.q0 + sh.q_pos));
-                    if (span == kSpanMixed) {
-                        const float* at = lut_at(lut, a.lut, k0 - pos);
-                        const uint64_t mul2v = pack2(mul, mul);
+                const Span span = LUT ? span_of(a.bias, k0 - (t.q0 + kOwn - 1 + sh.q_pos), k0 + kStep - 1 - (t.q0 + sh.q_pos)) : kSpanFarLeft;
+                const bool mixed = LUT && span == kSpanMixed;
+                const uint64_t mul2v = pack2(sh.scale_log2, sh.scale_log2), nd2 = pack2(-delta, -delta);
+                // ds from x - lse = s * mul + off, in base 2
+                auto gradient = [&](auto off2) {
 #pragma unroll
-                        for (int c = 0; c < kStep; c += 2) {
-                            const float2 b = *reinterpret_cast<const float2*>(at + c);
-                            float x, y;
-                            unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
-                            s[c >> 5][c & 31] = __float_as_uint(x);
-                            s[c >> 5][(c & 31) + 1] = __float_as_uint(y);
-                        }
-                        mul = 1.0f;
-                    } else {
-                        off += span == kSpanFarRight ? right : left;
+                    for (int c = 0; c < kStep; c += 2) {
+                        float x, y;
+                        unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, off2(c)), x, y);
+                        const uint64_t p = pack2(exp2_fast(x), exp2_fast(y));
+                        unpack2(mul2(p, add2(pack2(__uint_as_float(d[c >> 5][c & 31]), __uint_as_float(d[c >> 5][(c & 31) + 1])), nd2)), x, y);
+                        d[c >> 5][c & 31] = __float_as_uint(x);
+                        d[c >> 5][(c & 31) + 1] = __float_as_uint(y);
                     }
-                    if (j + 1 == t.n) {
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(lut_empty + 8 * buf);
-                    }
-                }
-                const uint64_t mul2v = pack2(mul, mul), off2 = pack2(off, off), nd2 = pack2(-delta, -delta);
-#pragma unroll
-                for (int c = 0; c < kStep; c += 2) {
-                    float x, y;
-                    unpack2(fma2(pack2(__uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1])), mul2v, off2), x, y);
-                    const uint64_t p = pack2(exp2_fast(x), exp2_fast(y));
-                    unpack2(mul2(p, add2(pack2(__uint_as_float(d[c >> 5][c & 31]), __uint_as_float(d[c >> 5][(c & 31) + 1])), nd2)), x, y);
-                    d[c >> 5][c & 31] = __float_as_uint(x);
-                    d[c >> 5][(c & 31) + 1] = __float_as_uint(y);
+                };
+                if (mixed) {
+                    const float* at = lut_at(lut, a.lut, k0 - pos);
+                    const uint64_t lse2v = pack2(-lse2, -lse2);
+                    gradient([&](int c) {
+                        const float2 b = *reinterpret_cast<const float2*>(at + c);
+                        return add2(pack2(b.x, b.y), lse2v);
+                    });
+                } else {
+                    const float off = (LUT ? (span == kSpanFarRight ? right : left) : 0.0f) - lse2;
+                    const uint64_t off2v = pack2(off, off);
+                    gradient([&](int) { return off2v; });
                 }
                 if (some_idle || (cut && k0 + kStep > t.len)) {
                     const int end = used ? t.len - k0 : 0;
@@ -410,7 +402,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     for (int c = 0; c < kStep; ++c)
                         if (c >= end) d[c >> 5][c & 31] = 0;
                 }
-                if (j > 0 && Plan::apart) {                    // dS of the last tile has been used
+                if (Plan::apart) {                             // dS of the last tile has been used
                     wait_warp(dq_done, (tile - 1) & 1, dead, 2048 << 16);
                     tc_fence_after();
                 }
@@ -438,7 +430,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) bar_arrive(ds_ready);
                 if (BIAS) {
-                    if (span != kSpanMixed) {
+                    if (!mixed) {
                         uint64_t both[2] = {0, 0};
 #pragma unroll
                         for (int c = 0; c < kStep; c += 2)
@@ -503,6 +495,10 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     release_own((ordinal - 1) % OB);
                     leaving = false;
                 }
+            }
+            if (LUT) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(lut_empty + 8 * buf);
             }
             const DqItem last = t;
             more = next_item(a, round, t);
@@ -867,9 +863,12 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                     }
                     const Span span = LUT ? span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0) : kSpanFarLeft;
                     const bool mixed = LUT && span == kSpanMixed;
-                    const float mul = mixed ? 1.0f : sh.scale_log2, add = LUT && !mixed ? (span == kSpanFarRight ? right : left) : 0.0f;
                     const float* bias_at = LUT ? lut_at(luts + table * a.lut.floats, a.lut, pos0 - key) : nullptr;     // on the turned axis: query - key
-                    const bool holes = nl[2 * kStep] != 0.0f, single = t.len == 1 || (sh.causal && key == 0);
+                    const float add = LUT ? (span == kSpanFarRight ? right : left) : 0.0f;
+                    const uint64_t mul2v = pack2(sh.scale_log2, sh.scale_log2), add2v = pack2(add, add);
+                    const bool holes = nl[2 * kStep] != 0.0f;
+                    const int alone = key - pos0;              // the column that sees this key alone, if it is the first key
+                    const bool single = t.len == 1 || (sh.causal && key == 0 && alone >= 0 && alone < kStep);
                     // half a tile at a time: lse and delta of its columns need registers too
 #pragma unroll
                     for (int c0 = 0; c0 < kStep; c0 += 32) {
@@ -884,45 +883,39 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                             __syncwarp();
                             if (lane == 0) bar_arrive(s_free + 8 * g);
                         }
-                        if (mixed) {
-                            const uint64_t scale2 = pack2(sh.scale_log2, sh.scale_log2);
-#pragma unroll
-                            for (int c = 0; c < 32; c += 2) {
-                                const float2 b = *reinterpret_cast<const float2*>(bias_at + c0 + c);
-                                float x, y;
-                                unpack2(fma2(pack2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, pack2(b.x, b.y)), x, y);
-                                s[c] = __float_as_uint(x);
-                                s[c + 1] = __float_as_uint(y);
-                            }
-                        }
-                        const uint64_t mul2v = pack2(mul, mul), add2v = pack2(add, add);
                         uint32_t wp[16], wd[16];
+                        auto probabilities = [&](auto bias2) {
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const float4 l = *reinterpret_cast<const float4*>(nl + c0 + c);
-                            const float4 m = *reinterpret_cast<const float4*>(nd + c0 + c);
-                            const uint64_t ls[2] = {pack2(l.x, l.y), pack2(l.z, l.w)}, ms[2] = {pack2(m.x, m.y), pack2(m.z, m.w)};
+                            for (int c = 0; c < 32; c += 4) {
+                                const float4 l = *reinterpret_cast<const float4*>(nl + c0 + c);
+                                const float4 m = *reinterpret_cast<const float4*>(nd + c0 + c);
+                                const uint64_t ls[2] = {pack2(l.x, l.y), pack2(l.z, l.w)}, ms[2] = {pack2(m.x, m.y), pack2(m.z, m.w)};
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const int e = c + 2 * u;
-                                float x, y;
-                                unpack2(fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), mul2v, add2(ls[u], add2v)), x, y);
-                                x = exp2_fast(x);
-                                y = exp2_fast(y);
-                                wp[e >> 1] = pack_bf16(x, y);
-                                unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), ms[u])), x, y);
-                                wd[e >> 1] = pack_bf16(x, y);
+                                for (int u = 0; u < 2; ++u) {
+                                    const int e = c + 2 * u;
+                                    float x, y;
+                                    unpack2(fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), mul2v, add2(ls[u], bias2(e))), x, y);
+                                    x = exp2_fast(x);
+                                    y = exp2_fast(y);
+                                    wp[e >> 1] = pack_bf16(x, y);
+                                    unpack2(mul2(pack2(x, y), add2(pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), ms[u])), x, y);
+                                    wd[e >> 1] = pack_bf16(x, y);
+                                }
                             }
-                        }
+                        };
+                        if (mixed) probabilities([&](int e) {
+                            const float2 b = *reinterpret_cast<const float2*>(bias_at + c0 + e);
+                            return pack2(b.x, b.y);
+                        });
+                        else probabilities([&](int) { return add2v; });
                         if (single || holes) {
                             // rows that see one key alone: p = 1, ds = 0.  Rows inside len_q with nothing allowed: whatever do and q hold
-                            const int alone = key - pos0 - c0;
 #pragma unroll
                             for (int c = 0; c < 32; ++c) {
                                 const uint32_t keep = c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                                 const bool hole = holes && nl[c0 + c] == -INFINITY;
                                 if (hole) wp[c >> 1] &= keep;
-                                if (hole || (single && (t.len == 1 || c == alone))) wd[c >> 1] &= keep;
+                                if (hole || (single && (t.len == 1 || c0 + c == alone))) wd[c >> 1] &= keep;
                             }
                         }
                         if (Plan::apart && tile > 1 && c0 == 0) {      // P and dS of the group's last tile have been used

@@ -275,7 +275,12 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
             const bool cut = t.len < sh.len_kv || !(sh.causal && min(t.q0 + kRows, sh.len_q) + sh.q_pos <= t.len);
             const int buf = ordinal % QB;
             const float* lut = luts + buf * a.lut.floats;
-            float ref = -INFINITY, sum = 0.0f, left = 0.0f, right = 0.0f;
+            float ref = -INFINITY, sum = 0.0f, left = 0.0f, right = 0.0f;      // left, right: the far keys' bias
+            if (LUT) {
+                wait_warp(lut_full + 8 * buf, (ordinal / QB) & 1, dead, 1 << 15);
+                left = lut_far(lut, a.lut, false);
+                right = lut_far(lut, a.lut, true);
+            }
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int k0 = j * kKeys;
                 wait_warp(s_full, tile & 1, dead, 1024);
@@ -293,59 +298,48 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
                 }
 
                 // x = v * mul + add, in base 2
-                float mul = sh.scale_log2, add = 0.0f;
-                if (LUT) {
-                    if (j == 0) {
-                        wait_warp(lut_full + 8 * buf, (ordinal / QB) & 1, dead, 1 << 15);
-                        left = lut_far(lut, a.lut, false);
-                        right = lut_far(lut, a.lut, true);
-                    }
-                    const Span span = span_of(a.bias, k0 - (t.q0 + kRows - 1 + sh.q_pos), k0 + kKeys - 1 - (t.q0 + sh.q_pos));
-                    if (span == kSpanMixed) {
-                        const float* at = lut_at(lut, a.lut, k0 - pos);
-                        const uint64_t mul2v = pack2(mul, mul);
-#pragma unroll
-                        for (int c = 0; c < kKeys; c += 2) {
-                            const float2 b = *reinterpret_cast<const float2*>(at + c);
-                            float x, y;
-                            unpack2(fma2(pack2(__uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
-                            v[c >> 5][c & 31] = __float_as_uint(x);
-                            v[c >> 5][(c & 31) + 1] = __float_as_uint(y);
-                        }
-                        mul = 1.0f;
-                    } else {
-                        add = span == kSpanFarRight ? right : left;
-                    }
-                    if (j + 1 == t.n) {
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(lut_empty + 8 * buf);
-                    }
-                }
-                if (cut && k0 + kKeys > t.len) {
+                float mul = sh.scale_log2, add = 0.0f, top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto cut_off = [&] {
 #pragma unroll
                     for (int c = 0; c < kKeys; ++c)
                         if (k0 + c >= t.len) v[c >> 5][c & 31] = 0xFF800000u;
-                }
+                };
                 auto highest = [&] {
-                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int c = 0; c < kKeys; c += 2)
                         top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1]));
-                    return fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);
                 };
-                float high = highest();
-                if (LUT && sh.causal && __any_sync(0xFFFFFFFFu, !(high < INFINITY))) {
+                const Span span = LUT ? span_of(a.bias, k0 - (t.q0 + kRows - 1 + sh.q_pos), k0 + kKeys - 1 - (t.q0 + sh.q_pos)) : kSpanFarLeft;
+                if (LUT && span == kSpanMixed) {
+                    const float* at = lut_at(lut, a.lut, k0 - pos);
+                    const uint64_t mul2v = pack2(mul, mul);
+#pragma unroll
+                    for (int c = 0; c < kKeys; c += 2) {
+                        const float2 b = *reinterpret_cast<const float2*>(at + c);
+                        float x, y;
+                        unpack2(fma2(pack2(__uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1])), mul2v, pack2(b.x, b.y)), x, y);
+                        v[c >> 5][c & 31] = __float_as_uint(x);
+                        v[c >> 5][(c & 31) + 1] = __float_as_uint(y);
+                    }
+                    mul = 1.0f;
+                } else if (LUT) {
+                    add = span == kSpanFarRight ? right : left;
+                }
+                if (cut && k0 + kKeys > t.len) cut_off();
+                highest();
+                float high = fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);
+                if (LUT && __any_sync(0xFFFFFFFFu, !(high < INFINITY)) && sh.causal) {
                     // the mask was added: an infinite score or a NaN that it should have covered is taken out here
 #pragma unroll
                     for (int c = 0; c < kKeys; ++c)
                         if (k0 + c > pos) v[c >> 5][c & 31] = 0xFF800000u;
-                    high = highest();
+                    top[0] = top[1] = top[2] = top[3] = -INFINITY;
+                    highest();
+                    high = fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);
                 }
 
-                if (j > 0) {                                   // O and P of the last tile are free
-                    wait_warp(pv_done, (tile - 1) & 1, dead, 2048);
-                    tc_fence_after();
-                }
+                wait_warp(pv_done, (tile - 1) & 1, dead, 2048);        // O and P of the last tile are free
+                tc_fence_after();
                 const bool grown = high > ref + kRescaleAt || (ref == -INFINITY && high > -INFINITY);
                 if (__any_sync(0xFFFFFFFFu, grown)) {
                     const float next = grown ? high : ref;
@@ -408,6 +402,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
                     release_q((ordinal - 1) % QB);
                     leaving = false;
                 }
+            }
+            if (LUT) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(lut_empty + 8 * buf);
             }
             // O goes out through q's place in shared memory, which is free: q's last product has completed
             wait_warp(pv_done, (tile - 1) & 1, dead, 8192);
