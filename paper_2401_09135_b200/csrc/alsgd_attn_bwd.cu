@@ -39,7 +39,6 @@ constexpr int kDiagonals = kGroups * kChain;            // of a warp; lanes that
 
 // The threads of one item's arithmetic in attn_dq_kernel, named barrier 1.
 constexpr int kDqMath = 128, kDqThreads = 256;
-constexpr int kDqMathRegisters = 200, kDqOtherRegisters = 56;  // 128 threads each; launched with 128 a thread
 
 // =============================================================================================== dq
 
@@ -79,6 +78,7 @@ template <int HALVES>
 struct DqPlan {
     static constexpr int stages = HALVES == 1 ? 2 : 1, own_bufs = HALVES == 1 ? 2 : 1;
     static constexpr bool apart = HALVES == 1;         // dS beside S, so that the next tile's scores need not wait for dQ
+    static constexpr int math_registers = HALVES == 1 ? 200 : 184, other_registers = 256 - math_registers; // 128 threads each; launched with 128 a thread
     static constexpr uint32_t columns = 256;
     static constexpr uint32_t s_col = 0, dp_col = 64, dq_col = 128, ds_col = apart ? 192 : 0;
     static constexpr uint32_t own_bytes = HALVES * kOwnBytes, step_bytes = HALVES * kStepBytes;
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     using Plan = DqPlan<HALVES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
     extern __shared__ uint8_t raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);     // the tiles want 1024-byte lines; still seen to be shared memory
     const uint32_t base = smem_u32(smem);
     const uint32_t sq = base, sdo = sq + OB * Plan::own_bytes, sk = sdo + OB * Plan::own_bytes, sv = sk + ST * Plan::step_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     const uint32_t tmem = words[0];
     grid_dependency_sync();
 
-    if (warp >= 4) give_registers<kDqOtherRegisters>();
+    if (warp >= 4) give_registers<Plan::other_registers>();
     if (warp == 4) {
         if (lane == 0) {
             int ordinal = 0, tile = 0;                         // items and tiles whose copies have been started
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             ++ordinal;
         }
     } else if (warp < 4) {
-        take_registers<kDqMathRegisters>();
+        take_registers<Plan::math_registers>();
         const int row = threadIdx.x;
         const uint32_t lanes = tmem + ((uint32_t)warp << 21);
         float* sums = diagonals + warp * kSums;
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
     using Plan = DkvPlan<HALVES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
     extern __shared__ uint8_t raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);     // the tiles want 1024-byte lines; still seen to be shared memory
     const uint32_t base = smem_u32(smem);
     const uint32_t sk = base, sv = sk + OB * Plan::own_bytes, sq = sv + OB * Plan::own_bytes, sdo = sq + ST * Plan::step_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
@@ -1012,22 +1012,29 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
 
 // =============================================================================================== bias
 
-// dtable[h][n] = sum over the sequences and query blocks of one head, in that order.
-__global__ void __launch_bounds__(256) attn_dtable_kernel(const float* partial, int batch, int heads, int blocks, int buckets,
-                                                          float* out32, uint16_t* out16) {
-    __shared__ double shared[8][32];
+// dtable[h][n] = sum over the sequences and row blocks of one head, in that order.  A block per head and 32 buckets: 32 rows at
+// a time, so that a training batch's thousand rows are a few loads a thread.
+constexpr int kTableRows = 32;
+
+__global__ void __launch_bounds__(32 * kTableRows) attn_dtable_kernel(const float* partial, int batch, int heads, int blocks, int buckets,
+                                                                      float* out32, uint16_t* out16) {
+    __shared__ double shared[kTableRows][32];
     grid_dependency_sync();
     const int h = blockIdx.x, bucket = blockIdx.y * 32 + threadIdx.x;
     double s = 0.0;
-    if (bucket < buckets)
-        for (int i = threadIdx.y; i < batch * blocks; i += 8) {
-            const float* row = partial + (((size_t)(i / blocks) * heads + h) * blocks + i % blocks) * 4 * buckets + bucket;
+    if (bucket < buckets) {
+        int b = threadIdx.y / blocks, block = threadIdx.y % blocks;
+#pragma unroll 4
+        for (int i = threadIdx.y; i < batch * blocks; i += kTableRows) {
+            const float* row = partial + (((size_t)b * heads + h) * blocks + block) * 4 * buckets + bucket;
             s += (double)(row[0] + row[buckets]) + (double)(row[2 * buckets] + row[3 * buckets]);
+            for (block += kTableRows; block >= blocks; block -= blocks) ++b;
         }
+    }
     shared[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.y == 0 && bucket < buckets) {
-        for (int i = 1; i < 8; ++i) s += shared[i][threadIdx.x];
+        for (int i = 1; i < kTableRows; ++i) s += shared[i][threadIdx.x];
         if (out32) out32[(size_t)h * buckets + bucket] = (float)s;
         else out16[(size_t)h * buckets + bucket] = (uint16_t)(pack_bf16((float)s, 0.0f) & 0xFFFFu);
     }
@@ -1140,7 +1147,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     }
     if (d.buckets) {
         const bool wide = d.table_dtype == ALSGD_F32;
-        if (launch_dependent(attn_dtable_kernel, dim3(d.heads_q, (d.buckets + 31) / 32), dim3(32, 8), 0, s, (const float*)partial, (int)d.batch,
+        if (launch_dependent(attn_dtable_kernel, dim3(d.heads_q, (d.buckets + 31) / 32), dim3(32, kTableRows), 0, s, (const float*)partial, (int)d.batch,
                              (int)d.heads_q, blocks, (int)d.buckets, wide ? static_cast<float*>(dtable) : nullptr,
                              wide ? nullptr : static_cast<uint16_t*>(dtable)) != cudaSuccess)
             return ALSGD_E_CUDA;

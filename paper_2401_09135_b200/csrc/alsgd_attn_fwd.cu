@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     using Plan = FwdPlan<HALVES>;
     constexpr int ST = Plan::stages, QB = Plan::q_bufs;
     extern __shared__ uint8_t raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);     // the tiles want 1024-byte lines; still seen to be shared memory
     const uint32_t base = smem_u32(smem);
     const uint32_t sq = base, sk = sq + QB * Plan::q_bytes, sv = sk + ST * Plan::kv_bytes;
     const uint32_t bars = base + Plan::tiles_bytes;
