@@ -279,15 +279,52 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 bar_arrive(own_empty + 8 * buf);
             }
         };
-        // the row of o that delta wants, and its lse, asked for one item ahead (a row of 64; twice that would hold too many registers)
+        // The warp's rows of o, which delta wants, and lse, asked for one item ahead (rows of 64; twice that would hold too many
+        // registers).  Eight lanes to a row, four rows at a time: o[i] is 16 bytes of row 4 i + lane / 8.
         uint4 o[8 * HALVES];
         float next_lse = -INFINITY;
         auto ask_for_o = [&](const DqItem& t) {
-            const uint16_t* p = a.o + (int64_t)t.b * a.o_batch + (int64_t)(t.q0 + row) * a.o_pos + (int64_t)t.h * a.o_head;
+            const uint16_t* p = a.o + (int64_t)t.b * a.o_batch + (int64_t)t.h * a.o_head + 8 * (lane & 7);
             next_lse = t.q0 + row < sh.len_q ? a.lse[((size_t)t.b * sh.heads_q + t.h) * sh.len_q + t.q0 + row] : -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 8 * HALVES; ++c)
-                o[c] = t.q0 + row < sh.len_q && 8 * c < sh.dim ? *reinterpret_cast<const uint4*>(p + 8 * c) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < 8; ++i) {
+                const int r = t.q0 + 32 * warp + 4 * i + (lane >> 3);
+#pragma unroll
+                for (int c = 0; c < HALVES; ++c)
+                    o[c * 8 + i] = r < sh.len_q && 64 * c + 8 * (lane & 7) < sh.dim ? *reinterpret_cast<const uint4*>(p + (int64_t)r * a.o_pos + 64 * c)
+                                                                                : make_uint4(0, 0, 0, 0);
+            }
+        };
+        // this thread's row of do . o
+        auto delta_of = [&](const uint8_t* dout) {
+            float part[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = 32 * warp + 4 * i + (lane >> 3);
+                float acc[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < HALVES; ++c) {
+                    const uint4 x = o[c * 8 + i], y = *reinterpret_cast<const uint4*>(dout + c * kOwnBytes + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc[0] = fmaf(bf16_lo(xs[e]), bf16_lo(ys[e]), acc[0]);
+                        acc[1] = fmaf(bf16_hi(xs[e]), bf16_hi(ys[e]), acc[1]);
+                    }
+                }
+                part[i] = acc[0] + acc[1];
+            }
+            // sums over the eight lanes, halving what each lane still carries: lane 8 q + k ends with row 4 k + q
+#pragma unroll
+            for (int step = 4; step > 0; step >>= 1) {
+                const bool upper = lane & step;
+#pragma unroll
+                for (int i = 0; i < step; ++i) {
+                    const float give = upper ? part[i] : part[i + step], keep = upper ? part[i + step] : part[i];
+                    part[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, step);
+                }
+            }
+            return __shfl_sync(0xFFFFFFFFu, part[0], (lane & 3) * 8 + (lane >> 2));
         };
         int round = 0;
         DqItem t;
@@ -319,22 +356,8 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 __syncwarp();
             }
             wait_warp(own_full + 8 * buf, (ordinal / OB) & 1, dead, 256 << 16);
-            float delta = 0.0f;
-            if (live) {
-                float acc[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < 8 * HALVES; ++c) {
-                    const uint4 y = *reinterpret_cast<const uint4*>(smem + (sdo - base) + buf * Plan::own_bytes + (c >> 3) * kOwnBytes + row * 128 +
-                                                                    (((c & 7) ^ (row & 7)) << 4));
-                    const uint32_t xs[4] = {o[c].x, o[c].y, o[c].z, o[c].w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        acc[0] = fmaf(bf16_lo(xs[e]), bf16_lo(ys[e]), acc[0]);
-                        acc[1] = fmaf(bf16_hi(xs[e]), bf16_hi(ys[e]), acc[1]);
-                    }
-                }
-                delta = acc[0] + acc[1];
-            }
+            float delta = delta_of(smem + (sdo - base) + buf * Plan::own_bytes);
+            if (!live) delta = 0.0f;                           // whatever do holds
             if (inside) a.delta[stat] = delta;
 
             // A row with one allowed key has p = 1 whatever its score: ds = 0, where dp - delta would leave two sums' noise.
@@ -590,9 +613,9 @@ __device__ __forceinline__ DkvItem item_at(const DkvArgs& a, int i) {
 constexpr int kDkvMath = 256, kDkvThreads = 384;
 constexpr int kDkvMathRegisters = 208, kDkvOtherRegisters = 88;   // 256 and 128 threads; launched with 168 a thread
 
-template <int HALVES>
+template <int HALVES, int STAGES>
 struct DkvPlan {
-    static constexpr int stages = HALVES == 1 ? 4 : 2, own_bufs = HALVES == 1 ? 2 : 1;
+    static constexpr int stages = STAGES, own_bufs = HALVES == 1 ? 2 : 1;
     static constexpr bool apart = HALVES == 1;         // P and dS beside S and dP, so that the scores two tiles on need not wait for the sums
     static constexpr uint32_t columns = 512;
     static constexpr uint32_t s_col = 0, dp_col = 64, group_cols = 128;                // a group's S and dP; the other group's follow
@@ -605,16 +628,16 @@ struct DkvPlan {
     static constexpr uint32_t fixed_bytes = tiles_bytes + 512 + stages * stat_floats * sizeof(float);
 };
 
-template <int HALVES>
+template <int HALVES, int STAGES>
 size_t dkv_smem(const LutShape& l, bool lut) {
-    return 1024 + DkvPlan<HALVES>::fixed_bytes + (lut ? 2 * l.floats * sizeof(float) + 2 * l.pad + 1 : 0);
+    return 1024 + DkvPlan<HALVES, STAGES>::fixed_bytes + (lut ? 2 * l.floats * sizeof(float) + 2 * l.pad + 1 : 0);
 }
 
 // LUT: there is a bias or a causal mask.  The table by distance is kept for each of the two groups' current query head: table
 // (query head's ordinal) % 2, the axis turned round, since a thread's columns are queries.
-template <int HALVES, bool LUT>
+template <int HALVES, int STAGES, bool LUT>
 __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_constant__ DkvArgs a) {
-    using Plan = DkvPlan<HALVES>;
+    using Plan = DkvPlan<HALVES, STAGES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);     // the tiles want 1024-byte lines; still seen to be shared memory
@@ -1055,11 +1078,18 @@ int launch_dq(const DqArgs& a, cudaStream_t s) {
     return lut ? launch(attn_dq_kernel<HALVES, true, false>, kDqThreads, 2, smem, a, s) : launch(attn_dq_kernel<HALVES, false, false>, kDqThreads, 2, smem, a, s);
 }
 
-template <int HALVES>
+template <int HALVES, int STAGES>
 int launch_dkv(const DkvArgs& a, cudaStream_t s) {
     const bool lut = a.bias.table != nullptr || a.shape.causal;
-    const size_t smem = dkv_smem<HALVES>(a.lut, lut);
-    return lut ? launch(attn_dkv_kernel<HALVES, true>, kDkvThreads, 1, smem, a, s) : launch(attn_dkv_kernel<HALVES, false>, kDkvThreads, 1, smem, a, s);
+    const size_t smem = dkv_smem<HALVES, STAGES>(a.lut, lut);
+    return lut ? launch(attn_dkv_kernel<HALVES, STAGES, true>, kDkvThreads, 1, smem, a, s)
+               : launch(attn_dkv_kernel<HALVES, STAGES, false>, kDkvThreads, 1, smem, a, s);
+}
+
+// Four tiles on the way; two where wide heads and a table that reaches beyond about 700 leave no room for more.
+int launch_dkv(const DkvArgs& a, bool wide, cudaStream_t s) {
+    if (!wide) return launch_dkv<1, 4>(a, s);
+    return dkv_smem<2, 4>(a.lut, a.bias.table != nullptr || a.shape.causal) <= 227 * 1024 ? launch_dkv<2, 4>(a, s) : launch_dkv<2, 2>(a, s);
 }
 
 uint64_t delta_bytes(const alsgd_attn_desc& d) { return ((uint64_t)d.batch * d.heads_q * d.len_q * 4 + 255) / 256 * 256; }
@@ -1142,7 +1172,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
             (rc = operand(k, false, kOwn, 64, &a.k)) != ALSGD_OK || (rc = operand(v, false, kOwn, 64, &a.v)) != ALSGD_OK ||
             (rc = operand(dk, false, 32, 32, &a.dk)) != ALSGD_OK || (rc = operand(dv, false, 32, 32, &a.dv)) != ALSGD_OK)
             return rc;
-        rc = d.dim <= 64 ? launch_dkv<1>(a, s) : launch_dkv<2>(a, s);
+        rc = launch_dkv(a, d.dim > 64, s);
         if (rc != ALSGD_OK) return rc;
     }
     if (d.buckets) {
