@@ -8,6 +8,7 @@ borrowed device pointers.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -444,8 +445,9 @@ def _dtype_code(torch, dtype):
     raise AlsgdError(E_ARG, f"unsupported type {dtype}")
 
 
-def _stream(torch, device, stream):
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+def _stream(torch, index, stream):
+    """Raw handle of the given stream, or of the device's current one (without building a Stream object)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
 
 
 class GradClip:
@@ -463,6 +465,10 @@ class GradClip:
         self._desc = (GradDesc * max(n, 1))()
         for d, numel, off, t in zip(self._desc, self.numels, offsets, self.dtypes):
             d.numel, d.offset, d.dtype = numel, int(off), _dtype_code(torch, t)
+        # the descriptors' pointers as a strided array, so that a call fills them at once
+        import numpy as np
+        self._ptrs = np.frombuffer(self._desc, dtype=np.uint64).reshape(max(n, 1), C.sizeof(GradDesc) // 8)[:n, 0]
+        self._dtype_of, self._index = operator.attrgetter("dtype"), int(device)
         nbytes = C.c_uint64()
         _check(lib().alsgd_clip_grads_bytes(n, C.byref(nbytes)), "alsgd_clip_grads_bytes")
         self._work = torch.zeros(int(nbytes.value) + 256, dtype=torch.uint8, device=self.device)
@@ -474,16 +480,16 @@ class GradClip:
     def alsgd_clip_grads(self, grads, max_norm, out, stats, stream=None):
         """grads: one contiguous device tensor per table entry.  out: flat tensor of out_dtype, or None for the norm
         alone.  stats: two fp32 values on the device (norm, factor)."""
-        assert len(grads) == len(self.numels) and stats.numel() == 2 and stats.dtype == self.torch.float32
-        assert stats.device == self.device and stats.is_contiguous()
-        for d, g, numel, t in zip(self._desc, grads, self.numels, self.dtypes):
-            assert g.numel() == numel and g.dtype == t and g.is_contiguous() and g.device == self.device
-            d.data = g.data_ptr()
+        T = self.torch.Tensor
+        assert list(map(T.numel, grads)) == self.numels and list(map(self._dtype_of, grads)) == self.dtypes
+        assert all(map(T.is_contiguous, grads)) and all(i == self._index for i in map(T.get_device, grads))
+        assert stats.numel() == 2 and stats.dtype == self.torch.float32 and stats.get_device() == self._index and stats.is_contiguous()
+        self._ptrs[:] = list(map(T.data_ptr, grads))
         if out is not None:
-            assert out.dtype == self.out_dtype and out.is_contiguous() and out.device == self.device
-        _check(lib().alsgd_clip_grads(self._desc, len(self.numels), float(max_norm), out.data_ptr() if out is not None else None,
+            assert out.dtype == self.out_dtype and out.is_contiguous() and out.get_device() == self._index
+        _check(lib().alsgd_clip_grads(self._desc, len(self.numels), max_norm, out.data_ptr() if out is not None else None,
                                       self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work_ptr,
-                                      self._work_bytes, self.device.index, _stream(self.torch, self.device, stream)),
+                                      self._work_bytes, self._index, _stream(self.torch, self._index, stream)),
                "alsgd_clip_grads")
 
 
@@ -513,10 +519,11 @@ class Attention:
         d.device = int(device)
         self._q_shape, self._kv_shape = (batch, len_q, heads_q, dim), (batch, len_kv, heads_kv, dim)
         self._lse_shape, self._table_shape = (batch, heads_q, len_q), (heads_q, buckets)
+        self._bf16, self._index = torch.bfloat16, int(device)
         self._work = None                  # of the backward pass, made at its first call
 
     def _operand(self, t, shape):
-        assert t.dtype == self.torch.bfloat16 and t.shape == shape and t.device == self.device
+        assert t.dtype is self._bf16 and t.shape == shape and t.get_device() == self._index
         b, s, h, d = t.stride()
         assert d == 1
         return AttnTensor(t.data_ptr(), b, s, h)
@@ -524,7 +531,7 @@ class Attention:
     def _plain(self, t, shape, dtype):
         if t is None:
             return None
-        assert t.dtype == dtype and t.shape == shape and t.device == self.device and t.is_contiguous()
+        assert t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous()
         return t.data_ptr()
 
     def alsgd_attn_fwd(self, q, k, v, out, lse, table=None, kv_len=None, stream=None):
@@ -533,7 +540,7 @@ class Attention:
                                     self._operand(v, self._kv_shape), self._plain(table, self._table_shape, self.table_dtype),
                                     self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
                                     self._plain(lse, self._lse_shape, self.torch.float32),
-                                    _stream(self.torch, self.device, stream)), "alsgd_attn_fwd")
+                                    _stream(self.torch, self._index, stream)), "alsgd_attn_fwd")
 
     def alsgd_attn_bwd(self, q, k, v, out, lse, dout, dq, dk, dv, table=None, dtable=None, kv_len=None, stream=None):
         """dq, dk, dv and dtable are written.  The workspace belongs to this object: calls on several streams must be
@@ -550,7 +557,7 @@ class Attention:
                                     self._plain(lse, self._lse_shape, self.torch.float32), self._operand(dout, self._q_shape),
                                     self._operand(dq, self._q_shape), self._operand(dk, self._kv_shape),
                                     self._operand(dv, self._kv_shape), self._plain(dtable, self._table_shape, self.table_dtype),
-                                    self._work_ptr, self._work_bytes, _stream(self.torch, self.device, stream)), "alsgd_attn_bwd")
+                                    self._work_ptr, self._work_bytes, _stream(self.torch, self._index, stream)), "alsgd_attn_bwd")
 
     def alsgd_attn_bucket(self, distance):
         """Bucket of a distance key position - query position."""

@@ -32,7 +32,7 @@ inline Divide divide_by(int d) {
 
 struct Shape {
     int batch, heads_q, heads_kv, group, len_q, len_kv, dim;
-    int causal, q_pos;
+    int causal, q_pos, device;
     float scale, scale_log2;
     const int* kv_len;                 // may be null
     Divide by_heads_q, by_heads_kv, by_all_q, by_all_kv, by_group;     // heads, batch * heads, query heads per key head
@@ -305,6 +305,7 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
     s.dim = (int)d.dim;
     s.causal = (d.flags & ALSGD_ATTN_CAUSAL) != 0;
     s.q_pos = d.q_pos;
+    s.device = d.device;
     s.scale = d.scale;
     s.scale_log2 = d.scale * kLog2e;
     s.kv_len = kv_len;

@@ -1063,27 +1063,28 @@ __global__ void __launch_bounds__(32 * kTableRows) attn_dtable_kernel(const floa
     }
 }
 
-template <typename K, typename A>
-int launch(K kernel, int threads, int per_sm, size_t smem, const A& a, cudaStream_t s) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ALSGD_E_CUDA;
+template <auto KERNEL, typename A>
+int launch(int threads, int per_sm, size_t smem, const A& a, cudaStream_t s) {
+    static SmemLimit limit;
+    if (!limit.raise(KERNEL, a.shape.device, smem)) return ALSGD_E_CUDA;
     const int wave = blocks_at_once(smem, per_sm);
-    return launch_dependent(kernel, dim3(a.items < wave ? a.items : wave), dim3(threads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    return launch_dependent(KERNEL, dim3(a.items < wave ? a.items : wave), dim3(threads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
 template <int HALVES>
 int launch_dq(const DqArgs& a, cudaStream_t s) {
     const bool bias = a.bias.table != nullptr, lut = bias || a.shape.causal;
     const size_t smem = dq_smem<HALVES>(a.lut, lut, bias ? a.bias.buckets : 0);
-    if (bias) return launch(attn_dq_kernel<HALVES, true, true>, kDqThreads, 2, smem, a, s);
-    return lut ? launch(attn_dq_kernel<HALVES, true, false>, kDqThreads, 2, smem, a, s) : launch(attn_dq_kernel<HALVES, false, false>, kDqThreads, 2, smem, a, s);
+    if (bias) return launch<attn_dq_kernel<HALVES, true, true>>(kDqThreads, 2, smem, a, s);
+    return lut ? launch<attn_dq_kernel<HALVES, true, false>>(kDqThreads, 2, smem, a, s) : launch<attn_dq_kernel<HALVES, false, false>>(kDqThreads, 2, smem, a, s);
 }
 
 template <int HALVES, int STAGES>
 int launch_dkv(const DkvArgs& a, cudaStream_t s) {
     const bool lut = a.bias.table != nullptr || a.shape.causal;
     const size_t smem = dkv_smem<HALVES, STAGES>(a.lut, lut);
-    return lut ? launch(attn_dkv_kernel<HALVES, STAGES, true>, kDkvThreads, 1, smem, a, s)
-               : launch(attn_dkv_kernel<HALVES, STAGES, false>, kDkvThreads, 1, smem, a, s);
+    return lut ? launch<attn_dkv_kernel<HALVES, STAGES, true>>(kDkvThreads, 1, smem, a, s)
+               : launch<attn_dkv_kernel<HALVES, STAGES, false>>(kDkvThreads, 1, smem, a, s);
 }
 
 // Four tiles on the way; two where wide heads and a table that reaches beyond about 700 leave no room for more.

@@ -453,7 +453,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
 template <int HALVES, bool LUT>
 int launch_fwd(FwdArgs& a, cudaStream_t s) {
     const size_t smem = fwd_smem<HALVES>(a.lut, LUT);
-    if (cudaFuncSetAttribute(attn_fwd_kernel<HALVES, LUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ALSGD_E_CUDA;
+    static SmemLimit limit;
+    if (!limit.raise(attn_fwd_kernel<HALVES, LUT>, a.shape.device, smem)) return ALSGD_E_CUDA;
     const int wave = blocks_at_once(smem, 2);
     return launch_dependent(attn_fwd_kernel<HALVES, LUT>, dim3(a.items < wave ? a.items : wave), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK
                                                                                                                                              : ALSGD_E_CUDA;

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 namespace alsgd_ops {
@@ -45,6 +46,19 @@ inline cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block,
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
+
+// Raises a kernel's dynamic shared memory limit, once per device and size (the call costs more than a launch's other
+// host work).  One table per kernel; two threads that race on it both make the call.
+struct SmemLimit {
+    std::atomic<int> set[kMaxDevices] = {};
+    template <typename K>
+    bool raise(K kernel, int device, size_t bytes) {
+        if (set[device].load(std::memory_order_relaxed) >= (int)bytes) return true;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+        set[device].store((int)bytes, std::memory_order_relaxed);
+        return true;
+    }
+};
 
 // Lets the next launch of the stream place its blocks, then waits until the previous one has completed and its
 // writes are visible.  Does nothing in a launch without the attribute.
