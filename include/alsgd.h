@@ -415,7 +415,7 @@ typedef struct alsgd_grad_desc {
  * (infinite entries become NaN).  Squares are summed so that neither 1e30 overflows nor 1e-30 vanishes; the order
  * is fixed, so the same list gives the same bits on every call.
  * ALSGD_E_ARG: null or misaligned pointer, n = 0, max_norm not above 0, unknown type.  ALSGD_E_RANGE: device ordinal
- * outside 0..63, a tensor that does not fit out, 2^31 tiles of 16 KiB or more in one group of 512 tensors.
+ * outside 0..63, a tensor that does not fit out, 2^30 tiles of 32 KiB or more in one group of 512 tensors.
  * ALSGD_E_NOMEM: work too small. */
 int alsgd_clip_grads_bytes(uint32_t n, uint64_t* bytes_out);
 int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float max_norm, void* out, uint32_t out_dtype,

@@ -10,7 +10,8 @@
 // from the last to the first because the first pass left the end of the list in the 126 MB L2.
 //
 // Bound: memory.  The floor reads every gradient once and writes the flat vector once; a list beyond the L2 is read
-// again from HBM for all but the last ~100 MB.
+// again from HBM for all but the last ~100 MB.  Measured (B200): 22.9M fp32 elements 45 us, 109.5M bf16 to bf16 106 us,
+// 149.8M fp32 277 us, which is 6.5 TB/s over the three passes.
 #include "../../include/alsgd.h"
 #include "alsgd_ops.cuh"
 
@@ -21,9 +22,10 @@ using namespace alsgd_ops;
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kLoads = 4;                                   // 16-byte loads per thread per tile
-constexpr uint32_t kTileVecs = kBlock * kLoads;             // 16-byte vectors per tile: 4096 fp32 or 8192 bf16 elements
-constexpr uint32_t kNormBlocks = kSMs * 8;                  // one full wave of 256-thread blocks
+constexpr int kLoads = 8;                                   // 16-byte loads per thread per tile
+constexpr uint32_t kTileVecs = kBlock * kLoads;             // 16-byte vectors per tile: 8192 fp32 or 16384 bf16 elements
+constexpr int kNormPerSm = 4;                               // blocks that walk the tiles; 3 to 5 of them are alike, 8 with 4 loads cost 2-6 %
+constexpr uint32_t kNormBlocks = kSMs * kNormPerSm;
 constexpr size_t kWorkHead = 256;                           // ticket word, padded
 constexpr int kMaxGroup = 512;                              // tensors per launch
 
@@ -119,7 +121,7 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
 
 // last: partials of all launches of the call, or 0 where another norm launch follows this one.
 template <int CAP>
-__global__ void __launch_bounds__(kBlock) norm_kernel(const __grid_constant__ Tensors<CAP> t, double* partial, uint32_t first,
+__global__ void __launch_bounds__(kBlock, kNormPerSm) norm_kernel(const __grid_constant__ Tensors<CAP> t, double* partial, uint32_t first,
                                                       uint32_t last, unsigned* ticket, float max_norm, float* stats) {
     __shared__ double shared[kBlock / 32];
     __shared__ bool closing;
@@ -135,9 +137,15 @@ __global__ void __launch_bounds__(kBlock) norm_kernel(const __grid_constant__ Te
         const bool aligned = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
         const uint64_t e0 = (uint64_t)(tile - (at ? t.tile_end[at - 1] : 0)) * tile_elems(bf16);
         uint4 w[kLoads];
+        if (aligned && e0 + tile_elems(bf16) <= numel) {
+            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(src) + e0 * (bf16 ? 2 : 4)) + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            w[i] = load_vec(src, bf16, e0 + (uint64_t)(i * kBlock + threadIdx.x) * (bf16 ? 8 : 4), numel, aligned);
+            for (int i = 0; i < kLoads; ++i) w[i] = p[i * kBlock];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                w[i] = load_vec(src, bf16, e0 + (uint64_t)(i * kBlock + threadIdx.x) * (bf16 ? 8 : 4), numel, aligned);
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) acc += squares(w[i], bf16);
     }
@@ -258,7 +266,7 @@ int group_tiles(const alsgd_grad_desc* g, uint32_t n, uint64_t* tiles) {
     for (uint32_t i = 0; i < n; ++i) {
         const uint64_t per = (uint64_t)kTileVecs * (g[i].dtype == ALSGD_BF16 ? 8 : 4);
         *tiles += g[i].numel / per + (g[i].numel % per != 0);
-        if (*tiles > 0x7FFFFFFFull) return ALSGD_E_RANGE;
+        if (*tiles >= 1ull << 30) return ALSGD_E_RANGE;
     }
     return ALSGD_OK;
 }
