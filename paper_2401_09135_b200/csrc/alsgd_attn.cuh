@@ -5,6 +5,7 @@
 #include "alsgd_ops.cuh"
 #include "alsgd_tc.cuh"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -36,6 +37,7 @@ struct Shape {
     float scale, scale_log2;
     const int* kv_len;                 // may be null
     Divide by_heads_q, by_heads_kv, by_all_q, by_all_kv, by_group;     // heads, batch * heads, query heads per key head
+    Divide by_rows_q;                  // row blocks of a sequence's queries * heads
 };
 
 // Buckets of a distance: below `near` one each, then up to limits[0], limits[1], ..., the last open.
@@ -174,40 +176,142 @@ __device__ __forceinline__ int walk(int round) {
     return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
 }
 
+// The sequences of a ragged batch, the longest first, as every block finds them for itself: their lengths are on the device,
+// and a walk over items sorted by their work needs them.  Measured against the order in which they come: 4 sequences of 1531 to
+// 511 keys, 1000 queries, 16 heads of 128 that share 4: forward 79 -> 61 us, backward 293 -> 200 us (the four blocks of keys
+// too many for one per SM were empty ones).  At 128 short sequences both are alike (32 and 34 us forward, 132 and 127 us
+// backward): the items are many, and more sequences are taken as they come.  Compiled apart: its arithmetic in a walk that
+// does not need it cost 1 to 7 %.
+constexpr int kMaxRanked = 128;
+struct Ranks {
+    static constexpr bool on = true;
+    int len[kMaxRanked];               // keys of the sequence with this rank
+    uint8_t seq[kMaxRanked];
+};
+struct KeyRanks : Ranks {              // for items that are blocks of keys
+    int before[kMaxRanked];            // (block, sequence) pairs with keys, ahead of the blocks that only ranks up to this one fill
+};
+
+struct NoRanks {                       // without lengths, or with more sequences: as they come
+    static constexpr bool on = false;
+};
+
+inline bool by_rank(const Shape& sh) { return sh.kv_len && sh.batch <= kMaxRanked; }
+__device__ __forceinline__ int clamped_len(const Shape& sh, int b) { return sh.kv_len ? min(max(sh.kv_len[b], 0), sh.len_kv) : sh.len_kv; }
+
+__device__ __forceinline__ int blocks_of(int len, int rows) { return (len + rows - 1) / rows; }
+
+// All of the block's threads, at least kMaxRanked.
+__device__ __forceinline__ void rank_sequences(const Shape& sh, Ranks& ranks) {
+    const int b = threadIdx.x;
+    int len = 0, rank = 0;
+    if (b < sh.batch) ranks.len[b] = len = clamped_len(sh, b);
+    __syncthreads();
+    if (b < sh.batch)
+        for (int s = 0; s < sh.batch; ++s) rank += ranks.len[s] > len || (ranks.len[s] == len && s < b);
+    __syncthreads();
+    if (b < sh.batch) {
+        ranks.len[rank] = len;
+        ranks.seq[rank] = (uint8_t)b;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void rank_sequences(const Shape& sh, int rows, KeyRanks& ranks) {
+    rank_sequences(sh, ranks);
+    const int r = threadIdx.x;
+    if (r < sh.batch) {
+        const int blocks = r + 1 < sh.batch ? blocks_of(ranks.len[r + 1], rows) : 0;
+        int pairs = 0;
+        for (int s = 0; s < sh.batch; ++s) pairs += min(blocks_of(ranks.len[s], rows), blocks);
+        ranks.before[r] = pairs;
+    }
+    __syncthreads();
+}
+
+// The i-th (key block, sequence) pair: those with keys, block by block and rank by rank, then those without.  The blocks from
+// edge(r) to edge(r - 1) have keys in the sequences up to rank r and in no other.
+__device__ __forceinline__ void ranked_pair(const Shape& sh, const KeyRanks& ranks, int rows, int i, int& block, int& rank) {
+    auto edge = [&](int r) { return r + 1 < sh.batch ? blocks_of(ranks.len[r + 1], rows) : 0; };
+    const int filled = ranks.before[0] + edge(-1) - edge(0);           // pairs with keys: above edge(0) the longest sequence's alone
+    const bool keys = i < filled;
+    if (!keys) i -= filled;
+    auto ahead = [&](int r) {                                          // pairs of the wanted kind ahead of edge(r)
+        const int with = r < 0 ? filled : ranks.before[r];
+        return keys ? with : edge(r) * sh.batch - with;
+    };
+    int low = keys ? 0 : -1, high = sh.batch - 1;                      // the smallest r with ahead(r) <= i
+    while (low < high) {
+        const int mid = (low + high) >> 1;                             // rounds down for -1 too
+        if (ahead(mid) <= i) high = mid; else low = mid + 1;
+    }
+    const int count = keys ? low + 1 : sh.batch - 1 - low, at = i - ahead(low);
+    block = edge(low) + at / count;
+    rank = at % count + (keys ? 0 : low + 1);
+}
+
+// Row block, sequence, head and valid keys of the i-th item of a kernel whose items are query rows, the most keys first: with
+// a causal mask the last rows, else the longest sequences.
+template <typename RANKS>
+__device__ __forceinline__ void query_item(const Shape& sh, const RANKS& ranks, int row_blocks, int i, int& block, int& b, int& h, int& len) {
+    if constexpr (RANKS::on) {
+        if (!sh.causal) {
+            const int rank = sh.by_rows_q(i), rest = i - rank * row_blocks * sh.heads_q;
+            block = sh.by_heads_q(rest);
+            h = rest - block * sh.heads_q;
+            b = ranks.seq[rank];
+            len = ranks.len[rank];
+            return;
+        }
+    }
+    const int from_end = sh.by_all_q(i), bh = i - from_end * sh.batch * sh.heads_q;
+    block = row_blocks - 1 - from_end;
+    b = sh.by_heads_q(bh);
+    h = bh - b * sh.heads_q;
+    if constexpr (RANKS::on) {
+        len = ranks.len[b];
+        b = ranks.seq[b];
+    } else {
+        len = clamped_len(sh, b);
+    }
+}
+
 // The block's next item from `round` on, if there is one; `round` moves behind it.
-template <typename ARGS, typename ITEM>
-__device__ __forceinline__ bool next_item(const ARGS& a, int& round, ITEM& item) {
+template <typename ARGS, typename RANKS, typename ITEM>
+__device__ __forceinline__ bool next_item(const ARGS& a, const RANKS& ranks, int& round, ITEM& item) {
     for (; round * (int)gridDim.x < a.items; ++round) {
         const int i = walk(round);
         if (i >= a.items) continue;
-        item = item_at(a, i);
+        item = item_at(a, ranks, i);
         ++round;
         return true;
     }
     return false;
 }
 
-// The tiles of a block's items, one after the other.  item_at(ARGS, i) finds an item, whose `n` is the number of tiles; items
+// The tiles of a block's items, one after the other.  item_at(ARGS, ranks, i) finds an item, whose `n` is the number of tiles; items
 // without any are passed over, by every warp alike: a barrier's phases must not run past one that waits on it.
 template <typename ARGS, typename ITEM>
 struct Cursor {
     ITEM item;
     int round, ordinal, j, tile;       // the next round, how many of the block's items with tiles came before it, tile within it, tiles before this one
     bool more;
-    __device__ __forceinline__ void settle(const ARGS& a) {
-        do more = next_item(a, round, item);
+    template <typename RANKS>
+    __device__ __forceinline__ void settle(const ARGS& a, const RANKS& ranks) {
+        do more = next_item(a, ranks, round, item);
         while (more && item.n == 0);
         j = 0;
     }
-    __device__ __forceinline__ void start(const ARGS& a) {
+    template <typename RANKS>
+    __device__ __forceinline__ void start(const ARGS& a, const RANKS& ranks) {
         round = ordinal = tile = 0;
-        settle(a);
+        settle(a, ranks);
     }
-    __device__ __forceinline__ void next(const ARGS& a) {
+    template <typename RANKS>
+    __device__ __forceinline__ void next(const ARGS& a, const RANKS& ranks) {
         ++tile;
         if (++j < item.n) return;
         ++ordinal;
-        settle(a);
+        settle(a, ranks);
     }
 };
 
@@ -294,7 +398,8 @@ inline int check_tensor(const alsgd_attn_tensor* t, uint32_t batch, uint32_t len
     return ALSGD_OK;
 }
 
-inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
+// `rows`: query rows of a work item
+inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len, int rows) {
     Shape s;
     s.batch = (int)d.batch;
     s.heads_q = (int)d.heads_q;
@@ -314,6 +419,7 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len) {
     s.by_all_q = divide_by(s.batch * s.heads_q);
     s.by_all_kv = divide_by(s.batch * s.heads_kv);
     s.by_group = divide_by(s.group);
+    s.by_rows_q = divide_by(std::max(1, (s.len_q + rows - 1) / rows) * s.heads_q);
     return s;
 }
 

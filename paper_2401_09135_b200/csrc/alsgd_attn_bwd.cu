@@ -59,15 +59,12 @@ struct DqItem {
     int b, h, block, q0, len, keys, n;  // sequence, head, row block, first row, valid keys, keys any row sees, tiles
 };
 
-__device__ __forceinline__ DqItem item_at(const DqArgs& a, int i) {
+template <typename RANKS>
+__device__ __forceinline__ DqItem item_at(const DqArgs& a, const RANKS& ranks, int i) {
     const Shape& sh = a.shape;
     DqItem t;
-    const int block = sh.by_all_q(i), bh = i - block * sh.batch * sh.heads_q;
-    t.block = a.row_blocks - 1 - block;
+    query_item(sh, ranks, a.row_blocks, i, t.block, t.b, t.h, t.len);
     t.q0 = t.block * kOwn;
-    t.b = sh.by_heads_q(bh);
-    t.h = bh - t.b * sh.heads_q;
-    t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
     t.keys = t.len;
     if (sh.causal) t.keys = min(t.keys, min(t.q0 + kOwn, sh.len_q) + sh.q_pos);
     t.n = t.keys > 0 ? (t.keys + kStep - 1) / kStep : 0;
@@ -84,7 +81,7 @@ struct DqPlan {
     static constexpr uint32_t own_bytes = HALVES * kOwnBytes, step_bytes = HALVES * kStepBytes;
     static constexpr uint32_t tiles_bytes = own_bufs * 2 * own_bytes + 2 * stages * step_bytes;
     static constexpr uint32_t bars = 7 + 4 * own_bufs + 2 * stages;
-    static constexpr uint32_t fixed_bytes = tiles_bytes + 256;
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 256 + sizeof(Ranks);
 };
 
 template <int HALVES>
@@ -94,7 +91,7 @@ size_t dq_smem(const LutShape& l, bool lut, int buckets) {
 }
 
 // LUT: there is a bias or a causal mask.  BIAS: there is a bias, and its gradient.
-template <int HALVES, bool LUT, bool BIAS>
+template <int HALVES, bool LUT, bool BIAS, typename RANKS>
 __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_constant__ DqArgs a) {
     using Plan = DqPlan<HALVES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
@@ -109,6 +106,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
     constexpr int kSums = kDiagonals + kGroups * kGroup;
+    RANKS& ranks = *reinterpret_cast<RANKS*>(smem + Plan::tiles_bytes + 256);
     float* diagonals = reinterpret_cast<float*>(smem + Plan::fixed_bytes);             // [4 warps][kSums]
     float* by_bucket = diagonals + (BIAS ? 4 * kSums : 0);                             // [4 warps][buckets]
     short2* spans = reinterpret_cast<short2*>(by_bucket + (BIAS ? 4 * a.bias.buckets : 0));       // distances of a bucket
@@ -164,13 +162,14 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_sync();
+    if constexpr (RANKS::on) rank_sequences(sh, ranks);
 
     if (warp >= 4) give_registers<Plan::other_registers>();
     if (warp == 4) {
         if (lane == 0) {
             int ordinal = 0, tile = 0;                         // items and tiles whose copies have been started
             DqItem t;
-            for (int round = 0; next_item(a, round, t);) {
+            for (int round = 0; next_item(a, ranks, round, t);) {
                 if (t.n == 0) continue;
                 if (*dead) break;
                 const int hk = sh.by_group(t.h), buf = ordinal % OB;
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         const bool leader = elect_one();
         const uint64_t q_desc = desc_k_major(sq), do_desc = desc_k_major(sdo), k_desc = desc_k_major(sk), v_desc = desc_k_major(sv);
         Cursor<DqArgs, DqItem> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST, buf = at.ordinal % OB;
             if (at.j == 0) wait_warp(own_full + 8 * buf, (at.ordinal / OB) & 1, dead, 4 << 16);
             wait_warp(full + 8 * st, (at.tile / ST) & 1, dead, 8 << 16);
@@ -231,7 +230,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         const bool leader = elect_one();
         const uint64_t k_desc = desc_n_major(sk, kStepBytes);
         Cursor<DqArgs, DqItem> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST;
             if (at.j == 0) wait_warp(dq_free, (at.ordinal & 1) ^ 1, dead, 32 << 16);   // the last item's dQ has been read
             wait_warp(ds_ready, at.tile & 1, dead, 64 << 16);
@@ -253,7 +252,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
     } else if (warp == 7) {
         int ordinal = 0;
         DqItem t;
-        for (int round = 0; LUT && next_item(a, round, t);) {
+        for (int round = 0; LUT && next_item(a, ranks, round, t);) {
             if (t.n == 0) continue;
             const int buf = ordinal % OB, first = t.q0 + sh.q_pos;     // distances from the last row's first key to the first row's last
             wait_warp(lut_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 128 << 16);
@@ -328,7 +327,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
         };
         int round = 0;
         DqItem t;
-        bool more = next_item(a, round, t);
+        bool more = next_item(a, ranks, round, t);
         if (more && HALVES == 1) ask_for_o(t);
         while (more) {
             if (HALVES == 2) ask_for_o(t);
@@ -343,7 +342,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 }
                 if (BIAS)
                     for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = 0.0f;
-                more = next_item(a, round, t);
+                more = next_item(a, ranks, round, t);
                 if (more && HALVES == 1) ask_for_o(t);
                 continue;
             }
@@ -524,7 +523,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 if (lane == 0) bar_arrive(lut_empty + 8 * buf);
             }
             const DqItem last = t;
-            more = next_item(a, round, t);
+            more = next_item(a, ranks, round, t);
             if (more && HALVES == 1) ask_for_o(t);
             if (BIAS) {
 #pragma unroll
@@ -594,14 +593,26 @@ struct DkvItem {
     int b, hk, k0, len, q_first, per_head, n;  // sequence, key head, first key, valid keys, first query tile, tiles per query head, tiles
 };
 
-__device__ __forceinline__ DkvItem item_at(const DkvArgs& a, int i) {
+template <typename RANKS>
+__device__ __forceinline__ DkvItem item_at(const DkvArgs& a, const RANKS& ranks, int i) {
     const Shape& sh = a.shape;
     DkvItem t;
-    const int block = sh.by_all_kv(i), bh = i - block * sh.batch * sh.heads_kv;
-    t.k0 = block * kOwn;                                       // the first keys see the most queries: they come first
-    t.b = sh.by_heads_kv(bh);
-    t.hk = bh - t.b * sh.heads_kv;
-    t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
+    int block;                                                 // the first keys see the most queries: they come first
+    if constexpr (RANKS::on) {
+        const int pair = sh.by_heads_kv(i);
+        int rank;
+        ranked_pair(sh, ranks, kOwn, pair, block, rank);
+        t.hk = i - pair * sh.heads_kv;
+        t.b = ranks.seq[rank];
+        t.len = ranks.len[rank];
+    } else {
+        block = sh.by_all_kv(i);
+        const int bh = i - block * sh.batch * sh.heads_kv;
+        t.b = sh.by_heads_kv(bh);
+        t.hk = bh - t.b * sh.heads_kv;
+        t.len = clamped_len(sh, t.b);
+    }
+    t.k0 = block * kOwn;
     const int q_tiles = (sh.len_q + kStep - 1) / kStep;
     t.q_first = 0;                                             // the first tile with a row that sees one of the keys
     if (sh.causal && t.k0 > sh.q_pos) t.q_first = min((t.k0 - sh.q_pos) / kStep, q_tiles);
@@ -625,7 +636,8 @@ struct DkvPlan {
     static constexpr uint32_t tiles_bytes = own_bufs * 2 * own_bytes + 2 * stages * step_bytes;
     static constexpr uint32_t bars = 16 + 2 * own_bufs + 3 * stages;
     static constexpr uint32_t stat_floats = 2 * kStep + 4;     // (-lse in base 2)[64], (-delta)[64], whether the tile has holes
-    static constexpr uint32_t fixed_bytes = tiles_bytes + 512 + stages * stat_floats * sizeof(float);
+    static constexpr uint32_t ranks_bytes = sizeof(KeyRanks);
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 512 + ranks_bytes + stages * stat_floats * sizeof(float);
 };
 
 template <int HALVES, int STAGES>
@@ -635,7 +647,7 @@ size_t dkv_smem(const LutShape& l, bool lut) {
 
 // LUT: there is a bias or a causal mask.  The table by distance is kept for each of the two groups' current query head: table
 // (query head's ordinal) % 2, the axis turned round, since a thread's columns are queries.
-template <int HALVES, int STAGES, bool LUT>
+template <int HALVES, int STAGES, bool LUT, typename RANKS>
 __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_constant__ DkvArgs a) {
     using Plan = DkvPlan<HALVES, STAGES>;
     constexpr int ST = Plan::stages, OB = Plan::own_bufs;
@@ -650,7 +662,8 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
     const uint32_t full = lut_empty + 16, empty = full + 8 * ST, stat_full = empty + 8 * ST;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
-    float* stats = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 512);
+    RANKS& ranks = *reinterpret_cast<RANKS*>(smem + Plan::tiles_bytes + 512);
+    float* stats = reinterpret_cast<float*>(smem + Plan::tiles_bytes + 512 + Plan::ranks_bytes);
     float* luts = stats + ST * Plan::stat_floats;
     uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + 2 * a.lut.floats);
 
@@ -700,12 +713,13 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_sync();
+    if constexpr (RANKS::on) rank_sequences(sh, kOwn, ranks);
 
     if (warp >= 8) give_registers<kDkvOtherRegisters>();
     if (warp == 8) {
         int ordinal = 0, tile = 0;                             // items and tiles whose copies have been started
         DkvItem t;
-        for (int round = 0; next_item(a, round, t);) {
+        for (int round = 0; next_item(a, ranks, round, t);) {
             if (t.n == 0) continue;
             if (__any_sync(0xFFFFFFFFu, *dead)) break;
             const int buf = ordinal % OB;
@@ -770,7 +784,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
         const bool leader = elect_one();
         const uint64_t q_desc = desc_k_major(sq), do_desc = desc_k_major(sdo), k_desc = desc_k_major(sk), v_desc = desc_k_major(sv);
         Cursor<DkvArgs, DkvItem> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST, buf = at.ordinal % OB, g = at.tile & 1;
             if (at.j == 0) wait_warp(own_full + 8 * buf, (at.ordinal / OB) & 1, dead, 4 << 16);
             wait_warp(full + 8 * st, (at.tile / ST) & 1, dead, 8 << 16);
@@ -798,7 +812,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
         const bool leader = elect_one();
         const uint64_t q_desc = desc_n_major(sq, kStepBytes), do_desc = desc_n_major(sdo, kStepBytes);
         Cursor<DkvArgs, DkvItem> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST, g = at.tile & 1;
             if (at.j == 0) wait_warp(acc_free, (at.ordinal & 1) ^ 1, dead, 32 << 16);  // the last item's dV and dK have been read
             wait_warp(p_ready + 8 * g, (at.tile >> 1) & 1, dead, 64 << 16);
@@ -824,7 +838,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
     } else if (warp == 11) {
         int heads = 0;                                         // query heads whose tables have been laid out
         DkvItem t;
-        for (int round = 0; LUT && next_item(a, round, t);) {
+        for (int round = 0; LUT && next_item(a, ranks, round, t);) {
             if (t.n == 0) continue;
             const int first = t.q_first * kStep + sh.q_pos;        // query positions, to the last tile's end: p = 0 there needs a finite bias
             const int last = (t.q_first + t.per_head) * kStep - 1 + sh.q_pos;
@@ -852,7 +866,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
             }
         };
         DkvItem t;
-        for (int round = 0; next_item(a, round, t);) {
+        for (int round = 0; next_item(a, ranks, round, t);) {
             const int key = t.k0 + row, buf = ordinal % OB;
             if (t.n == 0) {
                 if (key < sh.len_kv) {
@@ -1071,26 +1085,27 @@ int launch(int threads, int per_sm, size_t smem, const A& a, cudaStream_t s) {
     return launch_dependent(KERNEL, dim3(a.items < wave ? a.items : wave), dim3(threads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
-template <int HALVES>
+template <int HALVES, typename RANKS>
 int launch_dq(const DqArgs& a, cudaStream_t s) {
     const bool bias = a.bias.table != nullptr, lut = bias || a.shape.causal;
     const size_t smem = dq_smem<HALVES>(a.lut, lut, bias ? a.bias.buckets : 0);
-    if (bias) return launch<attn_dq_kernel<HALVES, true, true>>(kDqThreads, 2, smem, a, s);
-    return lut ? launch<attn_dq_kernel<HALVES, true, false>>(kDqThreads, 2, smem, a, s) : launch<attn_dq_kernel<HALVES, false, false>>(kDqThreads, 2, smem, a, s);
+    if (bias) return launch<attn_dq_kernel<HALVES, true, true, RANKS>>(kDqThreads, 2, smem, a, s);
+    return lut ? launch<attn_dq_kernel<HALVES, true, false, RANKS>>(kDqThreads, 2, smem, a, s) : launch<attn_dq_kernel<HALVES, false, false, RANKS>>(kDqThreads, 2, smem, a, s);
 }
 
-template <int HALVES, int STAGES>
+template <int HALVES, int STAGES, typename RANKS>
 int launch_dkv(const DkvArgs& a, cudaStream_t s) {
     const bool lut = a.bias.table != nullptr || a.shape.causal;
     const size_t smem = dkv_smem<HALVES, STAGES>(a.lut, lut);
-    return lut ? launch<attn_dkv_kernel<HALVES, STAGES, true>>(kDkvThreads, 1, smem, a, s)
-               : launch<attn_dkv_kernel<HALVES, STAGES, false>>(kDkvThreads, 1, smem, a, s);
+    return lut ? launch<attn_dkv_kernel<HALVES, STAGES, true, RANKS>>(kDkvThreads, 1, smem, a, s)
+               : launch<attn_dkv_kernel<HALVES, STAGES, false, RANKS>>(kDkvThreads, 1, smem, a, s);
 }
 
 // Four tiles on the way; two where wide heads and a table that reaches beyond about 700 leave no room for more.
+template <typename RANKS>
 int launch_dkv(const DkvArgs& a, bool wide, cudaStream_t s) {
-    if (!wide) return launch_dkv<1, 4>(a, s);
-    return dkv_smem<2, 4>(a.lut, a.bias.table != nullptr || a.shape.causal) <= 227 * 1024 ? launch_dkv<2, 4>(a, s) : launch_dkv<2, 2>(a, s);
+    if (!wide) return launch_dkv<1, 4, RANKS>(a, s);
+    return dkv_smem<2, 4>(a.lut, a.bias.table != nullptr || a.shape.causal) <= 227 * 1024 ? launch_dkv<2, 4, RANKS>(a, s) : launch_dkv<2, 2, RANKS>(a, s);
 }
 
 uint64_t delta_bytes(const alsgd_attn_desc& d) { return ((uint64_t)d.batch * d.heads_q * d.len_q * 4 + 255) / 256 * 256; }
@@ -1142,7 +1157,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     if (q_items > 0x7FFFFFFFull - 2 * kSMs || kv_items > 0x7FFFFFFFull - 2 * kSMs) return ALSGD_E_RANGE;
     if (d.len_q) {
         DqArgs a;
-        a.shape = make_shape(d, kv_len);
+        a.shape = make_shape(d, kv_len, kOwn);
         make_bias(d, table, &a.bias);
         a.lut = lut_shape(a.bias.far, kOwn, kStep, a.shape.causal);
         a.row_blocks = blocks;
@@ -1158,12 +1173,13 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
             (rc = operand(dq, true, 32, 32, &a.dq)) != ALSGD_OK || (rc = operand(k, false, kStep, 64, &a.k)) != ALSGD_OK ||
             (rc = operand(v, false, kStep, 64, &a.v)) != ALSGD_OK)
             return rc;
-        rc = d.dim <= 64 ? launch_dq<1>(a, s) : launch_dq<2>(a, s);
+        if (by_rank(a.shape)) rc = d.dim <= 64 ? launch_dq<1, Ranks>(a, s) : launch_dq<2, Ranks>(a, s);
+        else rc = d.dim <= 64 ? launch_dq<1, NoRanks>(a, s) : launch_dq<2, NoRanks>(a, s);
         if (rc != ALSGD_OK) return rc;
     }
     if (d.len_kv) {
         DkvArgs a;
-        a.shape = make_shape(d, kv_len);
+        a.shape = make_shape(d, kv_len, kOwn);
         make_bias(d, table, &a.bias);
         a.lut = lut_shape(a.bias.far, kOwn, kStep, false);     // on the turned axis the allowed keys lie ahead
         a.items = (int)kv_items;
@@ -1173,7 +1189,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
             (rc = operand(k, false, kOwn, 64, &a.k)) != ALSGD_OK || (rc = operand(v, false, kOwn, 64, &a.v)) != ALSGD_OK ||
             (rc = operand(dk, false, 32, 32, &a.dk)) != ALSGD_OK || (rc = operand(dv, false, 32, 32, &a.dv)) != ALSGD_OK)
             return rc;
-        rc = launch_dkv(a, d.dim > 64, s);
+        rc = by_rank(a.shape) ? launch_dkv<KeyRanks>(a, d.dim > 64, s) : launch_dkv<NoRanks>(a, d.dim > 64, s);
         if (rc != ALSGD_OK) return rc;
     }
     if (d.buckets) {

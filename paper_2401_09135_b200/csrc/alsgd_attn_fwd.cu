@@ -55,7 +55,7 @@ struct FwdPlan {
     static constexpr uint32_t q_bytes = HALVES * kTileBytes, kv_bytes = HALVES * kTileBytes;
     static constexpr uint32_t tiles_bytes = q_bufs * q_bytes + 2 * stages * kv_bytes;
     static constexpr uint32_t bars = 7 + 4 * q_bufs + 4 * stages;
-    static constexpr uint32_t fixed_bytes = tiles_bytes + 256;
+    static constexpr uint32_t fixed_bytes = tiles_bytes + 256 + sizeof(Ranks);
 };
 
 template <int HALVES>
@@ -67,21 +67,20 @@ struct Item {
     int b, h, q0, len, keys, n;        // sequence, head, first row, valid keys, keys any row sees, tiles
 };
 
-__device__ __forceinline__ Item item_at(const FwdArgs& a, int i) {
+template <typename RANKS>
+__device__ __forceinline__ Item item_at(const FwdArgs& a, const RANKS& ranks, int i) {
     const Shape& sh = a.shape;
     Item t;
-    const int block = sh.by_all_q(i), bh = i - block * sh.batch * sh.heads_q;
-    t.q0 = (a.row_blocks - 1 - block) * kRows;
-    t.b = sh.by_heads_q(bh);
-    t.h = bh - t.b * sh.heads_q;
-    t.len = sh.kv_len ? min(max(sh.kv_len[t.b], 0), sh.len_kv) : sh.len_kv;
+    int block;
+    query_item(sh, ranks, a.row_blocks, i, block, t.b, t.h, t.len);
+    t.q0 = block * kRows;
     t.keys = t.len;
     if (sh.causal) t.keys = min(t.keys, min(t.q0 + kRows, sh.len_q) + sh.q_pos);
     t.n = t.keys > 0 ? (t.keys + kKeys - 1) / kKeys : 0;
     return t;
 }
 
-template <int HALVES, bool LUT>
+template <int HALVES, bool LUT, typename RANKS>
 __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_constant__ FwdArgs a) {
     using Plan = FwdPlan<HALVES>;
     constexpr int ST = Plan::stages, QB = Plan::q_bufs;
@@ -96,6 +95,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     const uint32_t lut_full = v_empty + 8 * ST, lut_empty = lut_full + 8 * QB;
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + Plan::tiles_bytes + 8 * Plan::bars);
     volatile uint32_t* dead = words + 1;
+    RANKS& ranks = *reinterpret_cast<RANKS*>(smem + Plan::tiles_bytes + 256);
     float* luts = reinterpret_cast<float*>(smem + Plan::fixed_bytes);
     uint8_t* lut_bucket = reinterpret_cast<uint8_t*>(luts + QB * a.lut.floats);
 
@@ -142,12 +142,13 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_sync();
+    if constexpr (RANKS::on) rank_sequences(sh, ranks);
 
     if (warp >= 4) give_registers<kOtherRegisters>();
     if (warp == 4) {
         int ordinal = 0, tile = 0;                             // items and tiles whose copies have been started
         Item t;
-        for (int round = 0; next_item(a, round, t);) {
+        for (int round = 0; next_item(a, ranks, round, t);) {
             if (t.n == 0) continue;
             if (*dead) break;
             const int hk = sh.by_group(t.h), buf = ordinal % QB;
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
         const bool leader = elect_one();
         const uint64_t q_desc = desc_k_major(sq), k_desc = desc_k_major(sk);
         Cursor<FwdArgs, Item> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST, buf = at.ordinal % QB;
             if (at.j == 0) wait_warp(q_full + 8 * buf, (at.ordinal / QB) & 1, dead, 8);
             wait_warp(k_full + 8 * st, (at.tile / ST) & 1, dead, 16);
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
         const bool leader = elect_one();
         const uint64_t v_desc = desc_n_major(sv, kTileBytes);
         Cursor<FwdArgs, Item> at;
-        for (at.start(a); at.more; at.next(a)) {
+        for (at.start(a, ranks); at.more; at.next(a, ranks)) {
             const int st = at.tile % ST;
             if (at.j == 0) wait_warp(o_free, (at.ordinal & 1) ^ 1, dead, 64);  // the last item's O has been read
             wait_warp(v_full + 8 * st, (at.tile / ST) & 1, dead, 256);
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     } else if (warp == 7) {
         int ordinal = 0;
         Item t;
-        for (int round = 0; LUT && next_item(a, round, t);) {
+        for (int round = 0; LUT && next_item(a, ranks, round, t);) {
             if (t.n == 0) continue;
             const int buf = ordinal % QB, first = t.q0 + sh.q_pos;     // distances from the last row's first key to the first row's last
             wait_warp(lut_empty + 8 * buf, ((ordinal / QB) & 1) ^ 1, dead, 1 << 14);
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
             }
         };
         Item t;
-        for (int round = 0; next_item(a, round, t);) {
+        for (int round = 0; next_item(a, ranks, round, t);) {
             if (t.n == 0) {
                 if (t.q0 + row < sh.len_q) {
                     zero_row(a.o, sh.dim, t.b, t.h, t.q0 + row);
@@ -450,14 +451,20 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
     }
 }
 
-template <int HALVES, bool LUT>
+template <int HALVES, bool LUT, typename RANKS>
 int launch_fwd(FwdArgs& a, cudaStream_t s) {
     const size_t smem = fwd_smem<HALVES>(a.lut, LUT);
     static SmemLimit limit;
-    if (!limit.raise(attn_fwd_kernel<HALVES, LUT>, a.shape.device, smem)) return ALSGD_E_CUDA;
+    if (!limit.raise(attn_fwd_kernel<HALVES, LUT, RANKS>, a.shape.device, smem)) return ALSGD_E_CUDA;
     const int wave = blocks_at_once(smem, 2);
-    return launch_dependent(attn_fwd_kernel<HALVES, LUT>, dim3(a.items < wave ? a.items : wave), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK
+    return launch_dependent(attn_fwd_kernel<HALVES, LUT, RANKS>, dim3(a.items < wave ? a.items : wave), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK
                                                                                                                                              : ALSGD_E_CUDA;
+}
+
+template <typename RANKS>
+int launch_fwd(FwdArgs& a, bool wide, bool lut, cudaStream_t s) {
+    if (wide) return lut ? launch_fwd<2, true, RANKS>(a, s) : launch_fwd<2, false, RANKS>(a, s);
+    return lut ? launch_fwd<1, true, RANKS>(a, s) : launch_fwd<1, false, RANKS>(a, s);
 }
 
 }  // namespace
@@ -475,16 +482,16 @@ extern "C" int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     if ((rc = check_tensor(o, d.batch, d.len_q, d.heads_q, true)) != ALSGD_OK) return rc;
     if (d.len_q == 0) return ALSGD_OK;
 
+    const uint64_t row_blocks = (d.len_q + kRows - 1) / kRows, items = (uint64_t)d.batch * d.heads_q * row_blocks;
+    if (items > 0x7FFFFFFFull - 2 * kSMs) return ALSGD_E_RANGE;
     UseDevice use(d.device);
     if (!use.ok) return ALSGD_E_CUDA;
     FwdArgs a;
-    a.shape = make_shape(d, kv_len);
+    a.shape = make_shape(d, kv_len, kRows);
     make_bias(d, table, &a.bias);
     a.lse = lse;
     a.lut = lut_shape(a.bias.far, kRows, kKeys, a.shape.causal);
-    a.row_blocks = (int)((d.len_q + kRows - 1) / kRows);
-    const uint64_t items = (uint64_t)d.batch * d.heads_q * a.row_blocks;
-    if (items > 0x7FFFFFFFull - 2 * kSMs) return ALSGD_E_RANGE;
+    a.row_blocks = (int)row_blocks;
     a.items = (int)items;
     if ((rc = make_operand(*q, d.batch, d.len_q, d.heads_q, d.dim, kRows, 64, &a.q)) != ALSGD_OK) return rc;
     if ((rc = make_operand(*o, d.batch, d.len_q, d.heads_q, d.dim, 32, 32, &a.o)) != ALSGD_OK) return rc;
@@ -493,8 +500,8 @@ extern "C" int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     if ((rc = make_operand(d.len_kv ? *v : *q, d.batch, d.len_kv ? d.len_kv : d.len_q, d.len_kv ? d.heads_kv : d.heads_q, d.dim, kKeys, 64, &a.v)) != ALSGD_OK) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool lut = d.buckets || a.shape.causal;
-    if (d.dim <= 64) return lut ? launch_fwd<1, true>(a, s) : launch_fwd<1, false>(a, s);
-    return lut ? launch_fwd<2, true>(a, s) : launch_fwd<2, false>(a, s);
+    if (by_rank(a.shape)) return launch_fwd<Ranks>(a, d.dim > 64, lut, s);
+    return launch_fwd<NoRanks>(a, d.dim > 64, lut, s);
 }
 
 extern "C" int alsgd_attn_status(int32_t device, uint32_t* waits_out) {

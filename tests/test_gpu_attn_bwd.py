@@ -98,6 +98,14 @@ def test_more_items_than_blocks(causal, dim):
     check(Case(batch=50, len_q=270, heads_q=4, heads_kv=4, dim=dim, causal=causal))
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("batch", [1, 2, 127, 128, 129, 200])
+def test_ragged_batches_of_many_sequences(batch, causal):
+    """Up to 128 sequences are walked in the order of their lengths, more as they come; equal lengths and empty ones among them."""
+    lens = [(97 * i + 13) % 430 if i % 7 else (0, 384, 385, 512)[i // 7 % 4] for i in range(batch)]
+    check(Case(batch=batch, len_q=200, len_kv=400, heads_q=2, heads_kv=1, q_pos=150, causal=causal, buckets=16, two_sided=not causal, kv_len=lens))
+
+
 @pytest.mark.parametrize("two_sided", [False, True])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("buckets,max_distance", [(2, 2), (4, 5), (16, 64), (32, 128), (32, 1000), (64, 128), (256, 2048), (6, 20)])
