@@ -122,7 +122,7 @@ __device__ __forceinline__ float lut_value(const Bias& s, int head, int bucket) 
 __device__ __forceinline__ void fill_lut(const Bias& s, int head, const uint8_t* bucket, float* lut, const LutShape& l, int low, int high, int sign,
                                          int thread, int threads) {
     low = max(low, -l.pad);
-    high = min(high, l.copy - 2 - l.pad);
+    high = min(high, l.pad);                                   // the bucket list's end; mixed tiles reach no further
 #pragma unroll 4
     for (int r = low + thread; r <= high; r += threads) {
         const float x = lut_value(s, head, bucket[sign * r + l.pad]);
