@@ -24,7 +24,7 @@
 //
 // Bound: the arithmetic warps, as in the forward kernel, with the exponentials taken twice (122 us of them at 2 x 4096 tokens,
 // 16 heads of 64).  Measured (B200), causal with 32 buckets, dq / dkv / dtable as profiled one by one:
-//   2 x 4096 tokens, 16 heads of 64:    185 / 195 / 5 us, 360 together: 0.47 PFLOP/s, tensor cores busy for 28 and 36 %
+//   2 x 4096 tokens, 16 heads of 64:    185 / 195 / 5 us, 355 to 370 together: 0.47 PFLOP/s, tensor cores busy for 28 and 36 %
 //   64 x 256 tokens, 16 heads of 64:    89 / 82 / 9 us, 174 together: 1.5 TB/s.  Every tile lies across the diagonal: the bias'
 //                                       gradient by distance is 16 us of it, delta 15 us, the rest items that begin and end
 //   1000 x 511 to 1531, heads of 128 in groups of 4: 200 us together, 0.47 PFLOP/s
