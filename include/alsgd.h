@@ -426,8 +426,8 @@ int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float max_norm, v
  *     lse_i = log(sum_j exp(x[i][j])),   o_i = sum_j exp(x[i][j] - lse_i) v_j
  * Key j of sequence b is allowed if j < kv_len[b] and, with ALSGD_ATTN_CAUSAL, j <= q_pos + i.  A query with no allowed
  * key (or whose every allowed key has a bucket that is taken out) gives o_i = 0 and lse_i = -inf, and takes no part in
- * any gradient.  Keys behind kv_len are never used, whatever they hold.  Query head h reads key head
- * h / (heads_q / heads_kv).  Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 before
+ * any gradient.  Keys behind kv_len, and keys that no query of the call may see, are never used, whatever they hold.  Query
+ * head h reads key head h / (heads_q / heads_kv).  Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 before
  * they multiply v.
  *
  * Buckets of a distance r = key position - query position: one-sided (the default) a = max(-r, 0) and n = buckets;

@@ -36,6 +36,7 @@ struct Shape {
     int causal, q_pos, device;
     float scale, scale_log2;
     const int* kv_len;                 // may be null
+    int keys_end;                      // keys from here on are no sequence's: len_kv, or the last query's end under a causal mask
     Divide by_heads_q, by_heads_kv, by_all_q, by_all_kv, by_group;     // heads, batch * heads, query heads per key head
     Divide by_rows_q;                  // row blocks of a sequence's queries * heads
 };
@@ -197,7 +198,8 @@ struct NoRanks {                       // without lengths, or with more sequence
 };
 
 inline bool by_rank(const Shape& sh) { return sh.kv_len && sh.batch <= kMaxRanked; }
-__device__ __forceinline__ int clamped_len(const Shape& sh, int b) { return sh.kv_len ? min(max(sh.kv_len[b], 0), sh.len_kv) : sh.len_kv; }
+// A sequence's keys end where its length does or where no query sees further: what lies behind is never used, whatever it holds.
+__device__ __forceinline__ int clamped_len(const Shape& sh, int b) { return sh.kv_len ? min(max(sh.kv_len[b], 0), sh.keys_end) : sh.keys_end; }
 
 __device__ __forceinline__ int blocks_of(int len, int rows) { return (len + rows - 1) / rows; }
 
@@ -414,6 +416,7 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len, int row
     s.scale = d.scale;
     s.scale_log2 = d.scale * kLog2e;
     s.kv_len = kv_len;
+    s.keys_end = s.causal ? std::min(s.len_kv, std::max(0, s.len_q + s.q_pos)) : s.len_kv;
     s.by_heads_q = divide_by(s.heads_q);
     s.by_heads_kv = divide_by(s.heads_kv);
     s.by_all_q = divide_by(s.batch * s.heads_q);
