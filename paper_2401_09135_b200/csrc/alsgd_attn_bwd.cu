@@ -187,14 +187,22 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     tma_load4(sdo + at, &a.dout.map, own_full + 8 * buf, 64 * c, t.q0, t.h * a.dout.head_mul, t.b * a.dout.batch_mul);
                 }
                 ++ordinal;
+                const int pos = t.q0 + sh.q_pos;               // of the first row
+                int left_end = 0, right = t.n;                 // tiles in between are copied, zeros instead of the others
+                if (BIAS) {
+                    const int l = (pos - a.bias.far + 1) / kStep, r = (a.bias.far + pos + kOwn - 1 + kStep - 1) / kStep;
+                    if (l > 0 && far_out(a.bias, t.h, 0)) left_end = l;
+                    if (r < t.n && far_out(a.bias, t.h, 1)) right = max(r, 0);
+                }
                 for (int j = 0; j < t.n && !*dead; ++j, ++tile) {
                     const int st = tile % ST;
+                    const int from = BIAS && (j < left_end || j >= right) ? sh.len_kv : j * kStep;
                     wait(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                     bar_expect(full + 8 * st, 2 * Plan::step_bytes);
                     for (int c = 0; c < HALVES; ++c) {
                         const uint32_t at = st * Plan::step_bytes + c * kStepBytes;
-                        tma_load4(sk + at, &a.k.map, full + 8 * st, 64 * c, j * kStep, hk * a.k.head_mul, t.b * a.k.batch_mul);
-                        tma_load4(sv + at, &a.v.map, full + 8 * st, 64 * c, j * kStep, hk * a.v.head_mul, t.b * a.v.batch_mul);
+                        tma_load4(sk + at, &a.k.map, full + 8 * st, 64 * c, from, hk * a.k.head_mul, t.b * a.k.batch_mul);
+                        tma_load4(sv + at, &a.v.map, full + 8 * st, 64 * c, from, hk * a.v.head_mul, t.b * a.v.batch_mul);
                     }
                 }
             }
@@ -262,7 +270,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             if (t.n == 0) continue;
             const int buf = ordinal % OB, first = t.q0 + sh.q_pos;     // distances from the last row's first key to the first row's last
             wait_warp(lut_empty + 8 * buf, ((ordinal / OB) & 1) ^ 1, dead, 128 << 16);
-            fill_lut(a.bias, t.h, lut_bucket, luts + buf * a.lut.floats, a.lut, -(first + kOwn - 1), sh.causal ? 0 : t.keys - 1 - first, 1, lane, 32);
+            const bool out = fill_lut(a.bias, t.h, lut_bucket, luts + buf * a.lut.floats, a.lut, -(first + kOwn - 1), sh.causal ? 0 : t.keys - 1 - first, 1, lane, 32);
+            const bool outs = __any_sync(0xFFFFFFFFu, out);
+            if (lane == 0) lut_set_outs(luts + buf * a.lut.floats, a.lut, outs);
             __syncwarp();
             if (lane == 0) bar_arrive(lut_full + 8 * buf);
             ++ordinal;
@@ -419,6 +429,18 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                         const float2 b = *reinterpret_cast<const float2*>(at + c);
                         return add2(pack2(b.x, b.y), lse2v);
                     });
+                    // the warp's part of the tile may hold masked pairs
+                    if ((sh.causal && k0 + kStep - 1 > t.q0 + 32 * warp + sh.q_pos) || (BIAS && lut_outs(lut, a.lut))) {
+                        float top[2] = {0.0f, 0.0f};
+#pragma unroll
+                        for (int c = 0; c < kStep; c += 2)
+                            top[(c >> 1) & 1] = max3(top[(c >> 1) & 1], __uint_as_float(d[c >> 5][c & 31]), __uint_as_float(d[c >> 5][(c & 31) + 1]));
+                        if (__builtin_expect(__any_sync(0xFFFFFFFFu, isnan(top[0]) || isnan(top[1])), 0)) {
+#pragma unroll
+                            for (int c = 0; c < kStep; ++c)
+                                if (lut_at(lut, a.lut, k0 - pos)[c] == -INFINITY) d[c >> 5][c & 31] = 0;
+                        }
+                    }
                 } else {
                     const float off = (LUT ? (span == kSpanFarRight ? right : left) : 0.0f) - lse2;
                     const uint64_t off2v = pack2(off, off);
@@ -751,16 +773,24 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                 }
             };
             ask(head, q_tile);
+            int ahead = 0, behind = 0;                         // the head's tiles that start in between are copied, zeros instead of the others
             for (int j = 0; j < t.n; ++j, ++tile) {
-                const int st = tile % ST, q0 = q_tile * kStep;
+                const int st = tile % ST, pos0 = q_tile * kStep + sh.q_pos;
+                if (LUT && q_tile == t.q_first) {
+                    ahead = t.k0 - a.bias.far - (kStep - 1);
+                    behind = t.k0 + kOwn - 1 + a.bias.far;
+                    if (ahead < pos0 || !far_out(a.bias, head, 1)) ahead = -(1 << 30);
+                    if (behind > pos0 + (t.per_head - 1) * kStep || !far_out(a.bias, head, 0)) behind = 1 << 30;
+                }
+                const int from = LUT && (pos0 <= ahead || pos0 >= behind) ? sh.len_q : q_tile * kStep;
                 wait_warp(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                 if (__any_sync(0xFFFFFFFFu, *dead)) break;
                 if (lane == 0) {
                     bar_expect(full + 8 * st, 2 * Plan::step_bytes);
                     for (int c = 0; c < HALVES; ++c) {
                         const uint32_t at = st * Plan::step_bytes + c * kStepBytes;
-                        tma_load4(sq + at, &a.q.map, full + 8 * st, 64 * c, q0, head * a.q.head_mul, t.b * a.q.batch_mul);
-                        tma_load4(sdo + at, &a.dout.map, full + 8 * st, 64 * c, q0, head * a.dout.head_mul, t.b * a.dout.batch_mul);
+                        tma_load4(sq + at, &a.q.map, full + 8 * st, 64 * c, from, head * a.q.head_mul, t.b * a.q.batch_mul);
+                        tma_load4(sdo + at, &a.dout.map, full + 8 * st, 64 * c, from, head * a.dout.head_mul, t.b * a.dout.batch_mul);
                     }
                 }
                 float* stat = stats + st * Plan::stat_floats;
@@ -851,7 +881,9 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
             for (int i = 0; i < sh.group; ++i, ++heads) {
                 const int buf = heads & 1;
                 wait_warp(lut_empty + 8 * buf, ((heads >> 1) & 1) ^ 1, dead, 128 << 16);
-                fill_lut(a.bias, t.hk * sh.group + i, lut_bucket, luts + buf * a.lut.floats, a.lut, sh.causal ? 0 : first - (t.k0 + kOwn - 1), last - t.k0, -1, lane, 32);
+                const bool out = fill_lut(a.bias, t.hk * sh.group + i, lut_bucket, luts + buf * a.lut.floats, a.lut, sh.causal ? 0 : first - (t.k0 + kOwn - 1), last - t.k0, -1, lane, 32);
+                const bool outs = __any_sync(0xFFFFFFFFu, out);
+                if (lane == 0) lut_set_outs(luts + buf * a.lut.floats, a.lut, outs);
                 __syncwarp();
                 if (lane == 0) bar_arrive(lut_full + 8 * buf);
             }
@@ -884,6 +916,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
             int q_tile = t.q_first;
             bool head_starts_for_me = false;
             float left = 0.0f, right = 0.0f;                   // the bias of the head's far keys
+            bool outs = false;                                 // whether a bucket of the head is taken out
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int table = heads & 1;
                 const bool head_starts = q_tile == t.q_first, head_ends = q_tile + 1 == t.q_first + t.per_head;
@@ -902,6 +935,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                     if (LUT && head_starts_for_me) {
                         left = lut_far(luts + table * a.lut.floats, a.lut, false);
                         right = lut_far(luts + table * a.lut.floats, a.lut, true);
+                        outs = lut_outs(luts + table * a.lut.floats, a.lut);
                         head_starts_for_me = false;
                     }
                     const Span span = LUT ? span_of(a.bias, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0) : kSpanFarLeft;
@@ -946,11 +980,29 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                                 }
                             }
                         };
-                        if (mixed) probabilities([&](int e) {
-                            const float2 b = *reinterpret_cast<const float2*>(bias_at + c0 + e);
-                            return pack2(b.x, b.y);
-                        });
-                        else probabilities([&](int) { return add2v; });
+                        if (mixed) {
+                            probabilities([&](int e) {
+                                const float2 b = *reinterpret_cast<const float2*>(bias_at + c0 + e);
+                                return pack2(b.x, b.y);
+                            });
+                            // the warp's part may hold masked pairs
+                            if (outs || (sh.causal && t.k0 + 32 * quad + 31 > pos0 + c0)) {
+                                uint32_t top = wd[0];
+#pragma unroll
+                                for (int e = 1; e < 16; ++e) top = max_bf16x2(top, wd[e]);
+                                if (__builtin_expect(__any_sync(0xFFFFFFFFu, (top & 0x7FFFu) > 0x7F80u || (top & 0x7FFF0000u) > 0x7F800000u), 0)) {
+#pragma unroll
+                                    for (int c = 0; c < 32; ++c) {
+                                        if (bias_at[c0 + c] != -INFINITY) continue;
+                                        const uint32_t keep = c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                                        wp[c >> 1] &= keep;
+                                        wd[c >> 1] &= keep;
+                                    }
+                                }
+                            }
+                        } else {
+                            probabilities([&](int) { return add2v; });
+                        }
                         if (single || holes) {
                             // rows that see one key alone: p = 1, ds = 0.  Rows inside len_q with nothing allowed: whatever do and q hold
 #pragma unroll

@@ -339,11 +339,17 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
                 if (cut && k0 + kKeys > t.len) cut_off();
                 highest();
                 float high = fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);
-                if (LUT && __any_sync(0xFFFFFFFFu, !(high < INFINITY)) && sh.causal) {
-                    // the mask was added: an infinite score or a NaN that it should have covered is taken out here
+                if (LUT && __any_sync(0xFFFFFFFFu, !(high < INFINITY))) {
+                    // a mask was added: an infinite score or a NaN that it should have covered is taken out here
+                    if (span == kSpanMixed) {
+                        const float* at = lut_at(lut, a.lut, k0 - pos);
 #pragma unroll
-                    for (int c = 0; c < kKeys; ++c)
-                        if (k0 + c > pos) v[c >> 5][c & 31] = 0xFF800000u;
+                        for (int c = 0; c < kKeys; ++c)
+                            if (at[c] == -INFINITY) v[c >> 5][c & 31] = 0xFF800000u;
+                    } else if (add == -INFINITY) {
+#pragma unroll
+                        for (int c = 0; c < kKeys; ++c) v[c >> 5][c & 31] = 0xFF800000u;
+                    }
                     top[0] = top[1] = top[2] = top[3] = -INFINITY;
                     highest();
                     high = fmaf(max3(max3(top[0], top[1], top[2]), top[3], top[3]), mul, add);

@@ -218,6 +218,13 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     return r;
 }
 
+// The larger bf16 of either half, or NaN if one is.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // The largest of three, or NaN if one is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
