@@ -411,9 +411,10 @@ typedef struct alsgd_grad_desc {
  *   stats       device, two floats: norm, factor
  *   work        device, 256-byte aligned, alsgd_clip_grads_bytes bytes, zero-filled once before its first use;
  *               every call leaves it ready for the next.  Calls that share it must be ordered
- * A norm that is NaN makes the factor NaN and with it the whole result; an infinite norm makes the factor 0
- * (infinite entries become NaN).  Squares are summed so that neither 1e30 overflows nor 1e-30 vanishes; the order
- * is fixed, so the same list gives the same bits on every call.
+ * A norm that is NaN makes the factor NaN and with it the whole result; an infinite entry makes the norm infinite and, unless
+ * max_norm is, the factor 0 (infinite entries become NaN).  Squares are summed so that neither 1e30 overflows nor 1e-30
+ * vanishes, and the factor comes from the binary64 norm: a finite list whose norm is beyond binary32 has the norm reported as
+ * infinite and is clipped like any other.  The order is fixed, so the same list gives the same bits on every call.
  * ALSGD_E_ARG: null or misaligned pointer, n = 0, max_norm not above 0, unknown type.  ALSGD_E_RANGE: device ordinal
  * outside 0..63, a tensor that does not fit out, 2^30 tiles of 32 KiB or more in one group of 512 tensors.
  * ALSGD_E_NOMEM: work too small. */

@@ -5,9 +5,10 @@
 // Two launches.  norm_kernel reads every tensor once: a thread adds 4 or 8 squares at a time in binary32 and
 // everything above in binary64, blocks leave one partial each, and the block that takes the last ticket adds the
 // partials in index order, so the same inputs give the same bits on every call.  A group of squares that leaves the
-// binary32 range (overflow, or everything below 2^-100) is formed again in binary64: no finite gradient list has an
-// infinite norm and no non-zero one a zero norm.  scale_kernel reads the tensors a second time, walking the tiles
-// from the last to the first because the first pass left the end of the list in the 126 MB L2.
+// binary32 range (overflow, or everything below 2^-100) is formed again in binary64, and so is the quotient by a norm
+// beyond it: no non-zero list has a zero norm, and a finite one whose norm is reported as infinite is clipped by its
+// value.  scale_kernel reads the tensors a second time, walking the tiles from the last to the first because the first
+// pass left the end of the list in the 126 MB L2.
 //
 // Bound: memory.  The floor reads every gradient once and writes the flat vector once; a list beyond the L2 is read
 // again from HBM for all but the last ~100 MB.  Measured (B200): 22.9M fp32 elements 45 us, 109.5M bf16 to bf16 106 us,
@@ -26,8 +27,16 @@ constexpr int kLoads = 8;                                   // 16-byte loads per
 constexpr uint32_t kTileVecs = kBlock * kLoads;             // 16-byte vectors per tile: 8192 fp32 or 16384 bf16 elements
 constexpr int kNormPerSm = 4;                               // blocks that walk the tiles; 3 to 5 of them are alike, 8 with 4 loads cost 2-6 %
 constexpr uint32_t kNormBlocks = kSMs * kNormPerSm;
-constexpr size_t kWorkHead = 256;                           // ticket word, padded
+constexpr size_t kWorkHead = 256;                           // Head, padded
 constexpr int kMaxGroup = 512;                              // tensors per launch
+
+// In front of the partials.  The factor that the elements are multiplied by is parts[0] * parts[1]: one that is below the
+// normal range goes as parts of its own size and 2^-64, so that its 24 bits stay.  One load brings both: every warp of the
+// scale pass asks for them, and a second request to their one line cost 2.5 us.
+struct Head {
+    unsigned ticket;
+    alignas(8) float2 parts;
+};
 
 template <int CAP>
 struct Tensors {
@@ -122,7 +131,7 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
 // last: partials of all launches of the call, or 0 where another norm launch follows this one.
 template <int CAP>
 __global__ void __launch_bounds__(kBlock, kNormPerSm) norm_kernel(const __grid_constant__ Tensors<CAP> t, double* partial, uint32_t first,
-                                                      uint32_t last, unsigned* ticket, float max_norm, float* stats) {
+                                                      uint32_t last, Head* head, float max_norm, float* stats) {
     __shared__ double shared[kBlock / 32];
     __shared__ bool closing;
     grid_dependency_sync();
@@ -153,7 +162,7 @@ __global__ void __launch_bounds__(kBlock, kNormPerSm) norm_kernel(const __grid_c
     if (threadIdx.x == 0) {
         partial[first + blockIdx.x] = s;
         __threadfence();
-        closing = last != 0 && atomicAdd(ticket, 1u) == gridDim.x - 1;
+        closing = last != 0 && atomicAdd(&head->ticket, 1u) == gridDim.x - 1;
     }
     __syncthreads();
     if (!closing) return;
@@ -163,10 +172,20 @@ __global__ void __launch_bounds__(kBlock, kNormPerSm) norm_kernel(const __grid_c
     __syncthreads();
     const double total = block_sum(acc, shared);
     if (threadIdx.x == 0) {
-        *ticket = 0;
-        const float norm = (float)sqrt(total);
+        head->ticket = 0;
+        const double root = sqrt(total);
+        const float norm = (float)root;
+        float factor = norm <= max_norm ? 1.0f : max_norm / norm;      // a norm that is NaN makes the factor NaN
+        float2 parts = make_float2(factor, 1.0f);
+        if (norm == INFINITY && factor == 0.0f) {              // beyond binary32 at least: by its 2^-64th
+            parts.x = max_norm / (float)(root * 0x1p-64);
+            factor = parts.x * 0x1p-64f;
+            if (factor < 0x1p-126f) parts.y = 0x1p-64f;
+            else parts.x = factor;
+        }
         stats[0] = norm;
-        stats[1] = norm <= max_norm ? 1.0f : max_norm / norm;   // a norm that is NaN makes the factor NaN
+        stats[1] = factor;
+        head->parts = parts;
     }
 }
 
@@ -194,7 +213,7 @@ __device__ __forceinline__ void store_vec(OUT* out, uint64_t e, uint64_t numel, 
 }
 
 template <int CAP, typename OUT>
-__global__ void __launch_bounds__(kBlock) scale_kernel(const __grid_constant__ Tensors<CAP> t, OUT* out, const float* stats) {
+__global__ void __launch_bounds__(kBlock) scale_kernel(const __grid_constant__ Tensors<CAP> t, OUT* out, const Head* head) {
     const uint32_t tile = gridDim.x - 1 - blockIdx.x;
     const uint32_t at = find(t, tile);
     const bool bf16 = t.bf16[at];
@@ -206,7 +225,7 @@ __global__ void __launch_bounds__(kBlock) scale_kernel(const __grid_constant__ T
     const bool out_aligned = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
     const uint64_t e0 = (uint64_t)(tile - (at ? t.tile_end[at - 1] : 0)) * tile_elems(bf16);
     grid_dependency_sync();
-    const float c = __ldcg(stats + 1);
+    const float2 c = __ldcg(&head->parts);
     uint4 w[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) w[i] = load_vec(src, bf16, e0 + (uint64_t)(i * kBlock + threadIdx.x) * per, numel, aligned);
@@ -216,7 +235,7 @@ __global__ void __launch_bounds__(kBlock) scale_kernel(const __grid_constant__ T
         float x[8];
         widen(w[i], bf16, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] * c;
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * c.x * c.y;
         store_vec(dst, e, numel, x, per, out_aligned);
     }
 }
@@ -242,23 +261,23 @@ void fill(Tensors<CAP>& t, const alsgd_grad_desc* g, uint32_t n) {
 
 // One group of tensors: its norm launch (out == nullptr) or its scaling launch.
 template <int CAP>
-cudaError_t launch_group(const alsgd_grad_desc* g, uint32_t n, double* partial, uint32_t first, uint32_t last, unsigned* ticket,
+cudaError_t launch_group(const alsgd_grad_desc* g, uint32_t n, double* partial, uint32_t first, uint32_t last, Head* head,
                          float max_norm, float* stats, void* out, uint32_t out_dtype, uint32_t grid, cudaStream_t s) {
     Tensors<CAP> t;
     fill(t, g, n);
-    if (!out) return launch_dependent(norm_kernel<CAP>, dim3(grid), dim3(kBlock), 0, s, t, partial, first, last, ticket, max_norm, stats);
+    if (!out) return launch_dependent(norm_kernel<CAP>, dim3(grid), dim3(kBlock), 0, s, t, partial, first, last, head, max_norm, stats);
     if (out_dtype == ALSGD_BF16)
-        return launch_dependent(scale_kernel<CAP, uint16_t>, dim3(grid), dim3(kBlock), 0, s, t, static_cast<uint16_t*>(out), stats);
-    return launch_dependent(scale_kernel<CAP, float>, dim3(grid), dim3(kBlock), 0, s, t, static_cast<float*>(out), stats);
+        return launch_dependent(scale_kernel<CAP, uint16_t>, dim3(grid), dim3(kBlock), 0, s, t, static_cast<uint16_t*>(out), head);
+    return launch_dependent(scale_kernel<CAP, float>, dim3(grid), dim3(kBlock), 0, s, t, static_cast<float*>(out), head);
 }
 
 // The table travels as a kernel argument; short lists take the short one (copying 14 KB of arguments costs a launch
 // about a microsecond).
-cudaError_t launch_any(const alsgd_grad_desc* g, uint32_t n, double* partial, uint32_t first, uint32_t last, unsigned* ticket,
+cudaError_t launch_any(const alsgd_grad_desc* g, uint32_t n, double* partial, uint32_t first, uint32_t last, Head* head,
                        float max_norm, float* stats, void* out, uint32_t out_dtype, uint32_t grid, cudaStream_t s) {
-    if (n <= 16) return launch_group<16>(g, n, partial, first, last, ticket, max_norm, stats, out, out_dtype, grid, s);
-    if (n <= 128) return launch_group<128>(g, n, partial, first, last, ticket, max_norm, stats, out, out_dtype, grid, s);
-    return launch_group<kMaxGroup>(g, n, partial, first, last, ticket, max_norm, stats, out, out_dtype, grid, s);
+    if (n <= 16) return launch_group<16>(g, n, partial, first, last, head, max_norm, stats, out, out_dtype, grid, s);
+    if (n <= 128) return launch_group<128>(g, n, partial, first, last, head, max_norm, stats, out, out_dtype, grid, s);
+    return launch_group<kMaxGroup>(g, n, partial, first, last, head, max_norm, stats, out, out_dtype, grid, s);
 }
 
 int group_tiles(const alsgd_grad_desc* g, uint32_t n, uint64_t* tiles) {
@@ -308,7 +327,7 @@ extern "C" int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float 
     UseDevice use(device);
     if (!use.ok) return ALSGD_E_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    unsigned* ticket = static_cast<unsigned*>(work);
+    Head* head = static_cast<Head*>(work);
     double* partial = reinterpret_cast<double*>(static_cast<char*>(work) + kWorkHead);
     uint32_t first = 0;
     for (uint32_t at = 0; at < n; at += kMaxGroup) {
@@ -318,7 +337,7 @@ extern "C" int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float 
         // an empty list still gets one block: it writes its zero partial and, as the last launch, the results
         const uint32_t grid = tiles == 0 ? 1 : tiles < kNormBlocks ? (uint32_t)tiles : kNormBlocks;
         const uint32_t last = at + m == n ? first + grid : 0;
-        if (launch_any(grads + at, m, partial, first, last, ticket, max_norm, stats, nullptr, 0, grid, s) != cudaSuccess) return ALSGD_E_CUDA;
+        if (launch_any(grads + at, m, partial, first, last, head, max_norm, stats, nullptr, 0, grid, s) != cudaSuccess) return ALSGD_E_CUDA;
         first += grid;
     }
     if (!out) return ALSGD_OK;
@@ -328,7 +347,7 @@ extern "C" int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float 
         uint64_t tiles;
         group_tiles(grads + at, m, &tiles);
         if (tiles == 0) continue;
-        if (launch_any(grads + at, m, partial, 0, 0, ticket, max_norm, stats, out, out_dtype, (uint32_t)tiles, s) != cudaSuccess) return ALSGD_E_CUDA;
+        if (launch_any(grads + at, m, partial, 0, 0, head, max_norm, stats, out, out_dtype, (uint32_t)tiles, s) != cudaSuccess) return ALSGD_E_CUDA;
     }
     return ALSGD_OK;
 }
