@@ -526,6 +526,8 @@ extern "C" int alsgd_attn_status(int32_t device, uint32_t* waits_out) {
     UseDevice use(device);
     if (!use.ok) return ALSGD_E_CUDA;
     unsigned fwd = 0, bwd = 0;
+    // the copies alone would wait for the default stream, but not for streams that are independent of it
+    if (cudaDeviceSynchronize() != cudaSuccess) return ALSGD_E_CUDA;
     if (cudaMemcpyFromSymbol(&fwd, g_wait_error, sizeof fwd) != cudaSuccess || !bwd_wait_word(&bwd)) return ALSGD_E_CUDA;
     *waits_out = fwd | bwd;
     return ALSGD_OK;

@@ -10,6 +10,18 @@ from test_gpu_clip import NORM_TOL, inside
 pytestmark = pytest.mark.gpu
 
 
+def test_the_status_waits_for_every_stream():
+    """A stream that does not wait for the default one is busy for some 100 ms; the answer comes behind it."""
+    s = torch.cuda.Stream()
+    done = torch.cuda.Event()
+    assert B.alsgd_attn_status() == 0
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+        done.record()
+    assert B.alsgd_attn_status() == 0
+    assert done.query()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("scale", [3e37, 1.0])
