@@ -1165,7 +1165,7 @@ int launch_dkv(const DkvArgs& a, cudaStream_t s) {
 template <typename RANKS>
 int launch_dkv(const DkvArgs& a, bool wide, cudaStream_t s) {
     if (!wide) return launch_dkv<1, 4, RANKS>(a, s);
-    return dkv_smem<2, 4>(a.lut, a.bias.table != nullptr || a.shape.causal) <= 227 * 1024 ? launch_dkv<2, 4, RANKS>(a, s) : launch_dkv<2, 2, RANKS>(a, s);
+    return dkv_smem<2, 4>(a.lut, a.bias.table != nullptr || a.shape.causal) <= SmemLimit::kMost ? launch_dkv<2, 4, RANKS>(a, s) : launch_dkv<2, 2, RANKS>(a, s);
 }
 
 uint64_t delta_bytes(const alsgd_attn_desc& d) { return ((uint64_t)d.batch * d.heads_q * d.len_q * 4 + 255) / 256 * 256; }

@@ -47,15 +47,18 @@ inline cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block,
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Raises a kernel's dynamic shared memory limit, once per device and size (the call costs more than a launch's other
-// host work).  One table per kernel; two threads that race on it both make the call.
+// Raises a kernel's dynamic shared memory limit to what a block may have, once per device (the call costs more than a launch's
+// other host work).  One table per kernel.  Threads that race on it set the same value: the runtime keeps the last one, so
+// that a limit of each call's own size could end below what another has been told.
 struct SmemLimit {
-    std::atomic<int> set[kMaxDevices] = {};
+    static constexpr int kMost = 227 * 1024;
+    std::atomic<bool> set[kMaxDevices] = {};
     template <typename K>
     bool raise(K kernel, int device, size_t bytes) {
-        if (set[device].load(std::memory_order_relaxed) >= (int)bytes) return true;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
-        set[device].store((int)bytes, std::memory_order_relaxed);
+        if (bytes > kMost) return false;
+        if (set[device].load(std::memory_order_relaxed)) return true;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return false;
+        set[device].store(true, std::memory_order_relaxed);
         return true;
     }
 };
