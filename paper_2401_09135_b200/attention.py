@@ -23,8 +23,8 @@ class _Attend(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, table, kv_len, out, lse = ctx.saved_tensors
-        # a gradient that arrives broadcast (the sum's, say) or transposed within a head is laid out first
-        if dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:3]) or dout.data_ptr() % 16:
+        # a gradient that arrives broadcast over positions or within a head (a sum's, say) or transposed is laid out first
+        if dout.stride(3) != 1 or dout.stride(1) == 0 or any(s % 8 for s in dout.stride()[:3]) or dout.data_ptr() % 16:
             dout = dout.contiguous()
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         dtable = None if table is None else torch.empty_like(table)
