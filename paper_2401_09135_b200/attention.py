@@ -23,9 +23,10 @@ class _Attend(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, table, kv_len, out, lse = ctx.saved_tensors
-        # a gradient that arrives broadcast over positions or within a head (a sum's, say) or transposed is laid out first
+        # a gradient that arrives broadcast over positions or within a head (a sum's, say), transposed, or as a part of
+        # something larger that starts anywhere is laid out first
         if dout.stride(3) != 1 or dout.stride(1) == 0 or any(s % 8 for s in dout.stride()[:3]) or dout.data_ptr() % 16:
-            dout = dout.contiguous()
+            dout = dout.clone(memory_format=torch.contiguous_format)
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         dtable = None if table is None else torch.empty_like(table)
         ctx.plan.alsgd_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, table=table, dtable=dtable, kv_len=kv_len)

@@ -86,6 +86,17 @@ def test_sums_over_some_dimensions(device, dims):
 
 
 @pytest.mark.parametrize("device", PLACES)
+@pytest.mark.parametrize("shift", [1, 3, 4])
+def test_a_gradient_that_is_not_aligned(device, shift):
+    """Behind other elements of one vector the gradient is contiguous and starts anywhere."""
+    n = math.prod(SHAPE)
+    w = torch.randn(n + shift, generator=torch.Generator().manual_seed(2)).bfloat16().to(device)
+    got = gradients(device, lambda o: (torch.cat([o.new_zeros(shift), o.flatten()]) * w).sum())
+    want = gradients(device, lambda o: (o.flatten() * w[shift:].clone()).sum())
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("device", PLACES)
 def test_gradients_turned_round(device):
     """Heads ahead of positions, and elements of a head that are not side by side."""
     w = torch.randn(SHAPE, generator=torch.Generator().manual_seed(3)).bfloat16().to(device)
