@@ -6,6 +6,7 @@ results' memory.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -21,6 +22,7 @@ class _Attend(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, table, kv_len, out, lse = ctx.saved_tensors
         # a gradient that arrives broadcast over positions or within a head (a sum's, say), transposed, or as a part of
@@ -34,6 +36,6 @@ class _Attend(torch.autograd.Function):
 
 
 def attend(plan: B.Attention, q, k, v, table=None, kv_len=None):
-    """Attention of bf16 operands [batch, position, head, dim] with gradients for q, k, v and the bias table.  `plan`
-    belongs to one stream: its workspace is used by every backward pass through it."""
+    """Attention of bf16 operands [batch, position, head, dim] with gradients for q, k, v and the bias table; second derivatives
+    raise.  `plan` belongs to one stream: its workspace is used by every backward pass through it."""
     return _Attend.apply(plan, q, k, v, table, kv_len)

@@ -105,3 +105,13 @@ def test_gradients_turned_round(device):
         turned = w.permute(order).contiguous()
         got = gradients(device, lambda o: (o.permute(order) * turned).sum())
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("device", PLACES)
+def test_second_derivatives_are_refused(device):
+    """The backward pass is not differentiable: a gradient penalty has to raise, not lose its part of the gradient."""
+    leaves = leaves_on(device)
+    loss = (attend(plan_on(device), *leaves).float() ** 2).sum()
+    first = torch.autograd.grad(loss, leaves, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (loss + sum((g.float() ** 2).sum() for g in first)).backward()
