@@ -459,7 +459,7 @@ typedef struct alsgd_attn_tensor {
     int64_t stride_batch, stride_pos, stride_head;
 } alsgd_attn_tensor;
 
-/* Forward pass.  table: device, [heads_q][buckets] of table_dtype, NULL exactly if buckets = 0.  kv_len: device, one
+/* Forward pass.  table: device, [heads_q][buckets] of table_dtype, naturally aligned, NULL exactly if buckets = 0.  kv_len: device, one
  * int32 per sequence (values outside 0..len_kv are taken as the nearer end), or NULL for len_kv everywhere.  lse: device,
  * fp32 [batch][heads_q][len_q].
  * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step.  ALSGD_E_UNSUPPORTED: dim > 128,
@@ -474,7 +474,7 @@ int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tensor* q, cons
  * dk and dv sum over the query heads that share a key head; keys nobody uses get zeros.  ds and p are rounded to bf16
  * before the products with k, q and dout; dtable sums them unrounded.  Results are written, not added to; nothing
  * depends on the order in which blocks run, so the same inputs give the same bits.
- *   dtable   device, [heads_q][buckets] of table_dtype, NULL exactly if buckets = 0
+ *   dtable   device, [heads_q][buckets] of table_dtype, naturally aligned, NULL exactly if buckets = 0
  *   work     device, 256-byte aligned, alsgd_attn_bwd_bytes bytes (may be NULL if that is 0), any content
  * Errors as alsgd_attn_fwd; ALSGD_E_NOMEM: work too small. */
 int alsgd_attn_bwd_bytes(const alsgd_attn_desc* desc, uint64_t* bytes_out);

@@ -405,6 +405,11 @@ inline int check_desc(const alsgd_attn_desc* d) {
     return make_bias(*d, nullptr, &unused);
 }
 
+// A bias table or its gradient lies where its values may lie: it can be a vector of a flat layout.
+inline bool table_aligned(const alsgd_attn_desc& d, const void* table) {
+    return reinterpret_cast<uintptr_t>(table) % (d.table_dtype == ALSGD_BF16 ? 2 : 4) == 0;
+}
+
 // A [batch, position, head, dim] operand: 16-byte steps, no step of zero between elements that differ in an output.
 inline int check_tensor(const alsgd_attn_tensor* t, uint32_t batch, uint32_t len, uint32_t heads, bool output) {
     if (!t) return ALSGD_E_ARG;

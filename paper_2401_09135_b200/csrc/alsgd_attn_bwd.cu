@@ -1189,7 +1189,7 @@ extern "C" int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     if (rc != ALSGD_OK) return rc;
     const alsgd_attn_desc& d = *desc;
     if ((d.buckets != 0) != (table != nullptr) || (d.buckets != 0) != (dtable != nullptr)) return ALSGD_E_ARG;
-    if (reinterpret_cast<uintptr_t>(table) % 4 || reinterpret_cast<uintptr_t>(dtable) % 4 || reinterpret_cast<uintptr_t>(kv_len) % 4) return ALSGD_E_ARG;
+    if (!table_aligned(d, table) || !table_aligned(d, dtable) || reinterpret_cast<uintptr_t>(kv_len) % 4) return ALSGD_E_ARG;
     if (d.len_q && (!lse || reinterpret_cast<uintptr_t>(lse) % 4)) return ALSGD_E_ARG;
     const struct { const alsgd_attn_tensor* t; bool query, output; } all[] = {
         {q, true, false}, {k, false, false}, {v, false, false}, {o, true, false}, {dout, true, false}, {dq, true, true}, {dk, false, true}, {dv, false, true}};

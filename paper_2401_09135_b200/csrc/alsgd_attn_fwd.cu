@@ -490,7 +490,7 @@ extern "C" int alsgd_attn_fwd(const alsgd_attn_desc* desc, const alsgd_attn_tens
     int rc = check_desc(desc);
     if (rc != ALSGD_OK) return rc;
     const alsgd_attn_desc& d = *desc;
-    if ((d.buckets != 0) != (table != nullptr) || reinterpret_cast<uintptr_t>(table) % 4 || reinterpret_cast<uintptr_t>(kv_len) % 4) return ALSGD_E_ARG;
+    if ((d.buckets != 0) != (table != nullptr) || !table_aligned(d, table) || reinterpret_cast<uintptr_t>(kv_len) % 4) return ALSGD_E_ARG;
     if (d.len_q && (!lse || reinterpret_cast<uintptr_t>(lse) % 4)) return ALSGD_E_ARG;
     if ((rc = check_tensor(q, d.batch, d.len_q, d.heads_q, false)) != ALSGD_OK) return rc;
     if ((rc = check_tensor(k, d.batch, d.len_kv, d.heads_kv, false)) != ALSGD_OK) return rc;

@@ -4,7 +4,11 @@ import math
 import pytest
 import torch
 
+from attn_ref import Case
 from paper_2401_09135_b200 import binding as B
+from test_gpu_attn_bwd import compare as compare_grads
+from test_gpu_attn_bwd import empty_grads
+from test_gpu_attn_fwd import compare, outputs, plan_of
 from test_gpu_clip import NORM_TOL, inside
 
 pytestmark = pytest.mark.gpu
@@ -20,6 +24,25 @@ def test_the_status_waits_for_every_stream():
         done.record()
     assert B.alsgd_attn_status() == 0
     assert done.query()
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_a_bf16_table_lies_anywhere(shift):
+    """As a vector of a flat layout without alignment does."""
+    c = Case(batch=2, len_q=150, buckets=32)
+    q, k, v, dout, table, _ = c.inputs(table_dtype=torch.bfloat16)
+    room = torch.full((3, table.numel() + shift + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    at, dat = (room[i, shift:shift + table.numel()].view(table.shape) for i in (0, 2))
+    at.copy_(table)
+    assert at.data_ptr() % 4 == 2 * (shift % 2)
+    out, lse = outputs(c)
+    plan = plan_of(c, torch.bfloat16)
+    plan.alsgd_attn_fwd(q, k, v, out, lse, table=at)
+    compare(c, out, lse, q, k, v, table)
+    got = empty_grads(q, k, v, None)[:3]
+    plan.alsgd_attn_bwd(q, k, v, out, lse, dout, *got, table=at, dtable=dat)
+    compare_grads(c, got + [dat], q, k, v, table, out, lse, dout)
+    assert bool((room[2, :shift] == 7.0).all()) and bool((room[2, shift + table.numel():] == 7.0).all())
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
