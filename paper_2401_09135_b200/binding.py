@@ -450,6 +450,23 @@ def _stream(torch, index, stream):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
 
 
+class _Workspace:
+    """Device memory of a plan.  It belongs to the stream that it was made for, and a stream that uses it besides is told to
+    the allocator: a plan may go while its last kernels still run, and the memory must not have another owner before them."""
+
+    def __init__(self, torch, nbytes, device, stream, zeroed=False):
+        self._stream_of = lambda raw: torch.cuda.ExternalStream(raw, device=device)
+        with torch.cuda.stream(self._stream_of(stream)):
+            self._bytes = (torch.zeros if zeroed else torch.empty)(nbytes + 256, dtype=torch.uint8, device=device)
+        self.ptr, self.nbytes = -(-self._bytes.data_ptr() // 256) * 256, nbytes
+        self._streams = {stream}
+
+    def used_on(self, stream):
+        if stream not in self._streams:
+            self._bytes.record_stream(self._stream_of(stream))
+            self._streams.add(stream)
+
+
 class GradClip:
     """Gradient clipping for one tensor table: keeps the sizes, offsets and types of the gradients and the call's
     workspace; the tensors themselves are given at every call."""
@@ -471,9 +488,7 @@ class GradClip:
         self._dtype_of, self._index = operator.attrgetter("dtype"), int(device)
         nbytes = C.c_uint64()
         _check(lib().alsgd_clip_grads_bytes(n, C.byref(nbytes)), "alsgd_clip_grads_bytes")
-        self._work = torch.zeros(int(nbytes.value) + 256, dtype=torch.uint8, device=self.device)
-        self._work_ptr = -(-self._work.data_ptr() // 256) * 256
-        self._work_bytes = int(nbytes.value)
+        self._work = _Workspace(torch, int(nbytes.value), self.device, _stream(torch, self._index, None), zeroed=True)
         # the zeros are there before any stream uses the workspace
         torch.cuda.current_stream(self.device).synchronize()
 
@@ -487,10 +502,11 @@ class GradClip:
         self._ptrs[:] = list(map(T.data_ptr, grads))
         if out is not None:
             assert out.dtype == self.out_dtype and out.is_contiguous() and out.get_device() == self._index
+        raw = _stream(self.torch, self._index, stream)
+        self._work.used_on(raw)
         _check(lib().alsgd_clip_grads(self._desc, len(self.numels), max_norm, out.data_ptr() if out is not None else None,
-                                      self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work_ptr,
-                                      self._work_bytes, self._index, _stream(self.torch, self._index, stream)),
-               "alsgd_clip_grads")
+                                      self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work.ptr,
+                                      self._work.nbytes, self._index, raw), "alsgd_clip_grads")
 
 
 def alsgd_attn_status(device=0):
@@ -545,19 +561,19 @@ class Attention:
     def alsgd_attn_bwd(self, q, k, v, out, lse, dout, dq, dk, dv, table=None, dtable=None, kv_len=None, stream=None):
         """dq, dk, dv and dtable are written.  The workspace belongs to this object: calls on several streams must be
         ordered by the caller."""
+        raw = _stream(self.torch, self._index, stream)
         if self._work is None:
             nbytes = C.c_uint64()
             _check(lib().alsgd_attn_bwd_bytes(self.desc, C.byref(nbytes)), "alsgd_attn_bwd_bytes")
-            self._work = self.torch.empty(int(nbytes.value) + 256, dtype=self.torch.uint8, device=self.device)
-            self._work_ptr = -(-self._work.data_ptr() // 256) * 256
-            self._work_bytes = int(nbytes.value)
+            self._work = _Workspace(self.torch, int(nbytes.value), self.device, raw)
+        self._work.used_on(raw)
         _check(lib().alsgd_attn_bwd(self.desc, self._operand(q, self._q_shape), self._operand(k, self._kv_shape),
                                     self._operand(v, self._kv_shape), self._plain(table, self._table_shape, self.table_dtype),
                                     self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
                                     self._plain(lse, self._lse_shape, self.torch.float32), self._operand(dout, self._q_shape),
                                     self._operand(dq, self._q_shape), self._operand(dk, self._kv_shape),
                                     self._operand(dv, self._kv_shape), self._plain(dtable, self._table_shape, self.table_dtype),
-                                    self._work_ptr, self._work_bytes, _stream(self.torch, self._index, stream)), "alsgd_attn_bwd")
+                                    self._work.ptr, self._work.nbytes, raw), "alsgd_attn_bwd")
 
     def alsgd_attn_bucket(self, distance):
         """Bucket of a distance key position - query position."""
