@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import operator
 import os
+import threading
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libalsgd.so")
@@ -486,6 +487,8 @@ class GradClip:
         import numpy as np
         self._ptrs = np.frombuffer(self._desc, dtype=np.uint64).reshape(max(n, 1), C.sizeof(GradDesc) // 8)[:n, 0]
         self._dtype_of, self._index = operator.attrgetter("dtype"), int(device)
+        # calls of several threads go out one by one: they share the descriptors and, in stream order, the workspace
+        self._lock = threading.Lock()
         nbytes = C.c_uint64()
         _check(lib().alsgd_clip_grads_bytes(n, C.byref(nbytes)), "alsgd_clip_grads_bytes")
         self._work = _Workspace(torch, int(nbytes.value), self.device, _stream(torch, self._index, None), zeroed=True)
@@ -499,14 +502,15 @@ class GradClip:
         assert list(map(T.numel, grads)) == self.numels and list(map(self._dtype_of, grads)) == self.dtypes
         assert all(map(T.is_contiguous, grads)) and all(i == self._index for i in map(T.get_device, grads))
         assert stats.numel() == 2 and stats.dtype == self.torch.float32 and stats.get_device() == self._index and stats.is_contiguous()
-        self._ptrs[:] = list(map(T.data_ptr, grads))
         if out is not None:
             assert out.dtype == self.out_dtype and out.is_contiguous() and out.get_device() == self._index
         raw = _stream(self.torch, self._index, stream)
-        self._work.used_on(raw)
-        _check(lib().alsgd_clip_grads(self._desc, len(self.numels), max_norm, out.data_ptr() if out is not None else None,
-                                      self._out_code, out.numel() if out is not None else 0, stats.data_ptr(), self._work.ptr,
-                                      self._work.nbytes, self._index, raw), "alsgd_clip_grads")
+        with self._lock:
+            self._ptrs[:] = list(map(T.data_ptr, grads))
+            self._work.used_on(raw)
+            _check(lib().alsgd_clip_grads(self._desc, len(self.numels), max_norm, out.data_ptr() if out is not None else None,
+                                          self._out_code, out.numel() if out is not None else 0, stats.data_ptr(),
+                                          self._work.ptr, self._work.nbytes, self._index, raw), "alsgd_clip_grads")
 
 
 def alsgd_attn_status(device=0):
@@ -537,6 +541,7 @@ class Attention:
         self._lse_shape, self._table_shape = (batch, heads_q, len_q), (heads_q, buckets)
         self._bf16, self._index = torch.bfloat16, int(device)
         self._work = None                  # of the backward pass, made at its first call
+        self._lock = threading.Lock()      # its calls go out one by one: they share the workspace, in stream order
 
     def _operand(self, t, shape):
         assert t.dtype is self._bf16 and t.shape == shape and t.get_device() == self._index
@@ -562,18 +567,19 @@ class Attention:
         """dq, dk, dv and dtable are written.  The workspace belongs to this object: calls on several streams must be
         ordered by the caller."""
         raw = _stream(self.torch, self._index, stream)
-        if self._work is None:
-            nbytes = C.c_uint64()
-            _check(lib().alsgd_attn_bwd_bytes(self.desc, C.byref(nbytes)), "alsgd_attn_bwd_bytes")
-            self._work = _Workspace(self.torch, int(nbytes.value), self.device, raw)
-        self._work.used_on(raw)
-        _check(lib().alsgd_attn_bwd(self.desc, self._operand(q, self._q_shape), self._operand(k, self._kv_shape),
-                                    self._operand(v, self._kv_shape), self._plain(table, self._table_shape, self.table_dtype),
-                                    self._plain(kv_len, self._q_shape[:1], self.torch.int32), self._operand(out, self._q_shape),
-                                    self._plain(lse, self._lse_shape, self.torch.float32), self._operand(dout, self._q_shape),
-                                    self._operand(dq, self._q_shape), self._operand(dk, self._kv_shape),
-                                    self._operand(dv, self._kv_shape), self._plain(dtable, self._table_shape, self.table_dtype),
-                                    self._work.ptr, self._work.nbytes, raw), "alsgd_attn_bwd")
+        operands = [self._operand(t, shape) for t, shape in (
+            (q, self._q_shape), (k, self._kv_shape), (v, self._kv_shape), (out, self._q_shape), (dout, self._q_shape),
+            (dq, self._q_shape), (dk, self._kv_shape), (dv, self._kv_shape))]
+        plain = [self._plain(table, self._table_shape, self.table_dtype), self._plain(kv_len, self._q_shape[:1], self.torch.int32),
+                 self._plain(lse, self._lse_shape, self.torch.float32), self._plain(dtable, self._table_shape, self.table_dtype)]
+        with self._lock:
+            if self._work is None:
+                nbytes = C.c_uint64()
+                _check(lib().alsgd_attn_bwd_bytes(self.desc, C.byref(nbytes)), "alsgd_attn_bwd_bytes")
+                self._work = _Workspace(self.torch, int(nbytes.value), self.device, raw)
+            self._work.used_on(raw)
+            _check(lib().alsgd_attn_bwd(self.desc, *operands[:3], *plain[:2], operands[3], plain[2], *operands[4:], plain[3],
+                                        self._work.ptr, self._work.nbytes, raw), "alsgd_attn_bwd")
 
     def alsgd_attn_bucket(self, distance):
         """Bucket of a distance key position - query position."""
