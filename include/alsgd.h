@@ -486,8 +486,9 @@ int alsgd_attn_bwd(const alsgd_attn_desc* desc, const alsgd_attn_tensor* q, cons
 /* Bucket of one distance (host arithmetic), for a caller that keeps or inspects the table. */
 int alsgd_attn_bucket(const alsgd_attn_desc* desc, int32_t distance, uint32_t* bucket_out);
 
-/* Waits inside the attention kernels are bounded.  *waits_out (host) is 0, or has bits set if a wait ever ran out on
- * this device since the library was loaded; results since then are not to be trusted.  Waits for all work on the device,
+/* Waits inside the attention kernels are bounded.  A block whose wait ran out hands out NaN for the rows that it was at and for
+ * all of its later ones.  *waits_out (host) is 0, or has bits set if a wait ever ran out on this device since the library
+ * was loaded; results since then are not to be trusted.  Waits for all work on the device,
  * whatever its stream, and so must not be called while one is being captured. */
 int alsgd_attn_status(int32_t device, uint32_t* waits_out);
 

@@ -373,6 +373,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             wait_warp(own_full + 8 * buf, (ordinal / OB) & 1, dead, 256 << 16);
             float delta = delta_of(smem + (sdo - base) + buf * Plan::own_bytes);
             if (!live) delta = 0.0f;                           // whatever do holds
+            if (*dead) delta = NAN;
             if (inside) a.delta[stat] = delta;
 
             // A row with one allowed key has p = 1 whatever its score: ds = 0, where dp - delta would leave two sums' noise.
@@ -553,6 +554,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
             const DqItem last = t;
             more = next_item(a, ranks, round, t);
             if (more && HALVES == 1) ask_for_o(t);
+            wait_warp(dq_done, (tile - 1) & 1, dead, 4096 << 16);
+            tc_fence_after();
+            const bool lost = *dead;                           // a wait has run out: the item's results show it
             if (BIAS) {
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
@@ -564,10 +568,8 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                     bucket_sums[lut_bucket[2 * a.lut.pad]] += far_right;
                 }
                 __syncwarp();
-                for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = bucket_sums[e];
+                for (int e = lane; e < a.bias.buckets; e += 32) partial[e] = lost ? NAN : bucket_sums[e];
             }
-            wait_warp(dq_done, (tile - 1) & 1, dead, 4096 << 16);
-            tc_fence_after();
             // dq goes out through q's place, which is free: its last product has completed
             uint8_t* staging = smem + buf * Plan::own_bytes + warp * 2 * HALVES * 2048;
 #pragma unroll
@@ -576,7 +578,7 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 tmem_ld32(r, lanes + Plan::dq_col + 32 * c);
                 tmem_wait_ld();
                 tmem_use(r);
-                stage_box(r, sh.scale, staging + c * 2048, lane);
+                stage_box(r, lost ? NAN : sh.scale, staging + c * 2048, lane);
             }
             tc_fence_before();
             fence_async_smem();
@@ -1063,6 +1065,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
             tc_fence_after();
             // dk (the first group) and dv go out through k's and v's places, which are free: every product has completed.  Keys
             // behind the sequence's end get zeros
+            const float factor = *dead ? NAN : g == 0 ? sh.scale : 1.0f;       // a wait has run out: the item's results show it
             uint8_t* staging = smem + ((g == 0 ? sk : sv) - base) + buf * Plan::own_bytes + quad * 2 * HALVES * 2048;
 #pragma unroll
             for (int c = 0; c < 2 * HALVES; ++c) {
@@ -1074,7 +1077,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
 #pragma unroll
                     for (int e = 0; e < 32; ++e) r[e] = 0;
                 }
-                stage_box(r, g == 0 ? sh.scale : 1.0f, staging + c * 2048, lane);
+                stage_box(r, factor, staging + c * 2048, lane);
             }
             tc_fence_before();
             fence_async_smem();

@@ -427,6 +427,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_kernel(const __grid_cons
             // O goes out through q's place in shared memory, which is free: q's last product has completed
             wait_warp(pv_done, (tile - 1) & 1, dead, 8192);
             tc_fence_after();
+            if (*dead) ref = NAN;                              // a wait has run out: the item's results show it
             const bool none = ref == -INFINITY;                // no allowed key
             const float inv = none ? 0.0f : 1.0f / sum + (ref - ref);
             uint8_t* staging = smem + buf * Plan::q_bytes + warp * 2 * HALVES * 2048;
