@@ -1120,7 +1120,7 @@ __global__ void __launch_bounds__(32 * kTableRows) attn_dtable_kernel(const floa
     grid_dependency_sync();
     const int h = blockIdx.x, bucket = blockIdx.y * 32 + threadIdx.x;
     double s = 0.0;
-    if (bucket < buckets) {
+    if (bucket < buckets && blocks > 0) {                      // without queries there are no rows
         int b = threadIdx.y / blocks, block = threadIdx.y % blocks;
 #pragma unroll 4
         for (int i = threadIdx.y; i < batch * blocks; i += kTableRows) {
