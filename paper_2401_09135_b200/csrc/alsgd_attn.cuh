@@ -47,7 +47,7 @@ struct Bias {
     int bf16, buckets;
     int per_side, near, two_sided;
     int far;                           // distances from here on share the last bucket of their side
-    int far_bucket[2];                 // those, of keys behind and ahead of the query
+    int far_bucket[2];                 // those, of keys behind (kSpanFarLeft) and ahead of the query
     int n_limits;
     int limits[kMaxBuckets / 2];
 };
@@ -116,7 +116,7 @@ __device__ __forceinline__ float lut_far(const float* lut, const LutShape& s, bo
 // Whether a bucket of the table's head is taken out.  A mask is a bias of -inf, and a score of +inf (finite operands whose
 // product overflows) under it is NaN; so is p (dp - delta) of a masked pair whose dp is infinite.  The backward kernels look
 // for a NaN in mixed tiles that may hold masked pairs, and take those out by the table.  Together with far_out: 173 -> 183 us at
-// 64 x 256 tokens, 355 -> 374 us at 2 x 4096 (the same look at tiles with one bias, in place of far_out: 380 to 390 us).
+// 64 x 256 tokens, 355 -> 371 us at 2 x 4096 (the same look at tiles with one bias, in place of far_out: 380 to 390 us).
 __device__ __forceinline__ void lut_set_outs(float* lut, const LutShape& s, bool outs) { lut[2 * s.copy + 2] = outs ? 1.0f : 0.0f; }
 __device__ __forceinline__ bool lut_outs(const float* lut, const LutShape& s) { return lut[2 * s.copy + 2] != 0.0f; }
 
@@ -168,10 +168,12 @@ __device__ __forceinline__ Span span_of(const Bias& s, int r_min, int r_max) {
 
 bool bwd_wait_word(unsigned* out);     // alsgd_attn_bwd.cu
 
-// Whether the bias of all keys far behind (side 0) or far ahead (1) is -inf for this head: nothing of their tiles is allowed.
-// The backward kernels copy zeros instead of such a tile (coordinates behind the end), so that its scores are finite.
-__device__ __forceinline__ bool far_out(const Bias& s, int head, int side) {
-    return s.table && table_entry(s, head, s.far_bucket[side]) <= kMaskedOut;
+// Whether a tile of distances r_min .. r_max lies in a far bucket that is taken out for this head: nothing of it is allowed.  The
+// backward kernels copy zeros instead of such a tile (coordinates behind the end), so that its scores are finite.  The entry
+// is read again for every far tile: kept for a head, with the tiles where it applies, it cost 3 us more of 371.
+__device__ __forceinline__ bool far_out(const Bias& s, int head, int r_min, int r_max) {
+    const Span span = span_of(s, r_min, r_max);
+    return s.table && span != kSpanMixed && table_entry(s, head, s.far_bucket[span]) <= kMaskedOut;
 }
 
 // An operand as the copy engine reads it.  A dimension with step 0 (an operand broadcast over the batch or the heads)

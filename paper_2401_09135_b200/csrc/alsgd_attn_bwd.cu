@@ -188,15 +188,9 @@ __global__ void __launch_bounds__(kDqThreads, 2) attn_dq_kernel(const __grid_con
                 }
                 ++ordinal;
                 const int pos = t.q0 + sh.q_pos;               // of the first row
-                int left_end = 0, right = t.n;                 // tiles in between are copied, zeros instead of the others
-                if (BIAS) {
-                    const int l = (pos - a.bias.far + 1) / kStep, r = (a.bias.far + pos + kOwn - 1 + kStep - 1) / kStep;
-                    if (l > 0 && far_out(a.bias, t.h, 0)) left_end = l;
-                    if (r < t.n && far_out(a.bias, t.h, 1)) right = max(r, 0);
-                }
                 for (int j = 0; j < t.n && !*dead; ++j, ++tile) {
                     const int st = tile % ST;
-                    const int from = BIAS && (j < left_end || j >= right) ? sh.len_kv : j * kStep;
+                    const int from = BIAS && far_out(a.bias, t.h, j * kStep - (pos + kOwn - 1), (j + 1) * kStep - 1 - pos) ? sh.len_kv : j * kStep;
                     wait(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                     bar_expect(full + 8 * st, 2 * Plan::step_bytes);
                     for (int c = 0; c < HALVES; ++c) {
@@ -775,16 +769,9 @@ __global__ void __launch_bounds__(kDkvThreads, 1) attn_dkv_kernel(const __grid_c
                 }
             };
             ask(head, q_tile);
-            int ahead = 0, behind = 0;                         // the head's tiles that start in between are copied, zeros instead of the others
             for (int j = 0; j < t.n; ++j, ++tile) {
                 const int st = tile % ST, pos0 = q_tile * kStep + sh.q_pos;
-                if (LUT && q_tile == t.q_first) {
-                    ahead = t.k0 - a.bias.far - (kStep - 1);
-                    behind = t.k0 + kOwn - 1 + a.bias.far;
-                    if (ahead < pos0 || !far_out(a.bias, head, 1)) ahead = -(1 << 30);
-                    if (behind > pos0 + (t.per_head - 1) * kStep || !far_out(a.bias, head, 0)) behind = 1 << 30;
-                }
-                const int from = LUT && (pos0 <= ahead || pos0 >= behind) ? sh.len_q : q_tile * kStep;
+                const int from = LUT && far_out(a.bias, head, t.k0 - (pos0 + kStep - 1), t.k0 + kOwn - 1 - pos0) ? sh.len_q : q_tile * kStep;
                 wait_warp(empty + 8 * st, ((tile / ST) & 1) ^ 1, dead, 2 << 16);
                 if (__any_sync(0xFFFFFFFFu, *dead)) break;
                 if (lane == 0) {
