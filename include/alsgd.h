@@ -427,9 +427,11 @@ int alsgd_clip_grads(const alsgd_grad_desc* grads, uint32_t n, float max_norm, v
  *     lse_i = log(sum_j exp(x[i][j])),   o_i = sum_j exp(x[i][j] - lse_i) v_j
  * Key j of sequence b is allowed if j < kv_len[b] and, with ALSGD_ATTN_CAUSAL, j <= q_pos + i.  A query with no allowed
  * key (or whose every allowed key has a bucket that is taken out) gives o_i = 0 and lse_i = -inf, and takes no part in
- * any gradient.  Keys behind kv_len, and keys that no query of the call may see, are never used, whatever they hold.  Query
- * head h reads key head h / (heads_q / heads_kv).  Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 before
- * they multiply v.
+ * any gradient.  Keys behind kv_len, and keys that no query of the call may see, are never used, whatever they hold.  Other
+ * pairs that are not allowed take no part whatever their scores are, infinite ones of finite operands included; but a NaN
+ * or infinity in v (in the backward pass: in k, q or dout) at a position that the call uses may reach rows near it that
+ * may not see it, as 0 * NaN.  Query head h reads key head h / (heads_q / heads_kv).  Scores, softmax statistics and sums are
+ * binary32; probabilities are rounded to bf16 before they multiply v.
  *
  * Buckets of a distance r = key position - query position: one-sided (the default) a = max(-r, 0) and n = buckets;
  * two-sided a = |r| and n = buckets / 2, with n added for r > 0.  With e = n / 2 (rounded down): a itself below e, else

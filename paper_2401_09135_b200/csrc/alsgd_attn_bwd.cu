@@ -23,11 +23,13 @@
 // k), as the forward pass rounds p.
 //
 // Bound: the arithmetic warps, as in the forward kernel, with the exponentials taken twice (122 us of them at 2 x 4096 tokens,
-// 16 heads of 64).  Measured (B200), causal with 32 buckets, dq / dkv / dtable as profiled one by one:
-//   2 x 4096 tokens, 16 heads of 64:    185 / 195 / 5 us, 355 to 370 together: 0.47 PFLOP/s, tensor cores busy for 28 and 36 %
-//   64 x 256 tokens, 16 heads of 64:    89 / 82 / 9 us, 174 together: 1.5 TB/s.  Every tile lies across the diagonal: the bias'
-//                                       gradient by distance is 16 us of it, delta 15 us, the rest items that begin and end
-//   1000 x 511 to 1531, heads of 128 in groups of 4: 200 us together, 0.47 PFLOP/s
+// 16 heads of 64).  Measured (B200), causal with 32 buckets, dq / dkv / dtable one after the other without overlap:
+//   2 x 4096 tokens, 16 heads of 64:    180 / 183 / 4 us, 372 to 385 together (the higher at the power limit): 0.46 PFLOP/s,
+//                                       tensor cores busy for 26 and 35 %; 337 us without a bias
+//   64 x 256 tokens, 16 heads of 64:    95 / 85 / 7 us, 184 together: 1.5 TB/s.  Every tile lies across the diagonal: the bias'
+//                                       gradient by distance is 16 us of it, delta 15 us, the look for masked pairs whose
+//                                       scores overflow 10 us, the rest items that begin and end; 151 us without a bias
+//   1000 x 511 to 1531, heads of 128 in groups of 4: 108 / 83 / 3 us, 199 together, 0.47 PFLOP/s
 #include "alsgd_attn.cuh"
 
 using namespace alsgd_attn;
@@ -1149,9 +1151,9 @@ int launch_dkv(const DkvArgs& a, cudaStream_t s) {
                : launch<attn_dkv_kernel<HALVES, STAGES, false, RANKS>>(kDkvThreads, 1, smem, a, s);
 }
 
-// Four tiles on the way; two where wide heads and a table that reaches beyond about 700 leave no room for more (heads of 128 in
-// groups of 4, 1000 queries, 511 to 1531 keys, all kernels: 197 us with four, 210 us with two).  Narrow heads have a plan of
-// their own in both kernels: at 2 x 4096 tokens and heads of 64, 355 us, and 563 us with the plans for wide ones.
+// Four tiles on the way; two where wide heads and a table that reaches 703 or further leave no room for more (heads of 128 in
+// groups of 4, 1000 queries, 511 to 1531 keys, all kernels: 199 us with four, 213 us with two).  Narrow heads have a plan of
+// their own in both kernels: at 2 x 4096 tokens and heads of 64, 373 us, and 578 us with the plans for wide ones.
 template <typename RANKS>
 int launch_dkv(const DkvArgs& a, bool wide, cudaStream_t s) {
     if (!wide) return launch_dkv<1, 4, RANKS>(a, s);

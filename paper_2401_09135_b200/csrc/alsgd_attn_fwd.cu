@@ -22,10 +22,10 @@
 //
 // Bound: the softmax warps.  A score costs one exponential (16 per clock and SM) and about five more instructions (product
 // and bias, maximum, sum, rounding, loads and stores of tensor memory); the products of one tile run under another's.
-// Measured (B200), causal with 32 buckets: 2 x 4096 tokens, 16 heads of 64: 119 us, 0.58 PFLOP/s, where the exponentials
-// alone are 61 us and the tensor cores are busy for 27 %.  64 x 256 tokens: 43 us, 3.1 TB/s: items of one or two tiles, whose
-// beginning and end (q and table in, O out) do not hide behind each other.  77 tokens, 6 heads: 10 us in the kernel, the
-// latency of one item.  Heads of 128 in groups of 4, 1000 queries, 511 to 1531 keys: 61 us, 0.62 PFLOP/s.
+// Measured (B200), causal with 32 buckets: 2 x 4096 tokens, 16 heads of 64: 114 us, 0.60 PFLOP/s (110 us without a bias), where
+// the exponentials alone are 61 us and the tensor cores are busy for 27 %.  64 x 256 tokens: 42 us, 3.2 TB/s: items of one or
+// two tiles, whose beginning and end (q and table in, O out) do not hide behind each other.  77 tokens, 6 heads: 10 us in the
+// kernel, the latency of one item.  Heads of 128 in groups of 4, 1000 queries, 511 to 1531 keys: 59 us, 0.64 PFLOP/s.
 // Also built and measured: 64-key tiles with four blocks per SM (189 us at 2 x 4096), eight softmax warps that share a row
 // (140 us), the exponential as a polynomial on the multiply-add units for part of the scores (slower at every share).
 #include "alsgd_attn.cuh"
@@ -55,7 +55,7 @@ struct FwdArgs {
 
 // HALVES: 64-column halves of the head dimension (1 up to 64, 2 up to 128).  With one half there is room to keep P beside S,
 // so the next tile's scores are computed while this tile's exponentials are, and for a second q; with two, P takes S's place.
-// Heads of 64 at 2 x 4096 tokens: 119 us with one half, 146 us with the plan for two.
+// Heads of 64 at 2 x 4096 tokens: 114 us with one half, 141 us with the plan for two.
 template <int HALVES>
 struct FwdPlan {
     static constexpr int stages = HALVES == 1 ? 2 : 1, q_bufs = HALVES == 1 ? 2 : 1;

@@ -36,7 +36,8 @@ static __device__ unsigned int g_wait_error;
 // Every wait in these kernels ends.  After kWaitTries tries (tenths of a second at least, against waits of
 // microseconds) it records `code` and marks the block as dead, so that the block's other waits end after a few tries; the
 // block then runs to its end on whatever is in its memory, and what it writes from there on is NaN (a result is scaled by NaN
-// where the block is marked at its item's end, which every wait of the item's comes before).  Nothing is handed back: a result that would have to be carried
+// where the block is marked at its item's end, which every wait of the item comes before).  Nothing is handed back: a result
+// that would have to be carried
 // through the loops costs more than the wait itself, which most often finds its phase complete.
 constexpr uint32_t kWaitTries = 1u << 22;
 
