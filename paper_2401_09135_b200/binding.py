@@ -456,9 +456,14 @@ class _Workspace:
     the allocator: a plan may go while its last kernels still run, and the memory must not have another owner before them."""
 
     def __init__(self, torch, nbytes, device, stream, zeroed=False):
-        self._stream_of = lambda raw: torch.cuda.ExternalStream(raw, device=device)
-        with torch.cuda.stream(self._stream_of(stream)):
-            self._bytes = (torch.zeros if zeroed else torch.empty)(nbytes + 256, dtype=torch.uint8, device=device)
+        # the default stream under its own name: under another the allocator kept nothing of it for the next plan
+        self._stream_of = lambda raw: torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+        make = lambda: (torch.zeros if zeroed else torch.empty)(nbytes + 256, dtype=torch.uint8, device=device)  # noqa: E731
+        if stream == _stream(torch, device.index, None):
+            self._bytes = make()
+        else:
+            with torch.cuda.stream(self._stream_of(stream)):
+                self._bytes = make()
         self.ptr, self.nbytes = -(-self._bytes.data_ptr() // 256) * 256, nbytes
         self._streams = {stream}
 

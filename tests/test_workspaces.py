@@ -78,3 +78,34 @@ def test_memory_in_use_on_another_stream_is_not_handed_out(kind):
     assert not done.query(), "the stream was not busy for long enough"
     assert all(t.data_ptr() != at for t in others)
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["attention", "clip"])
+@pytest.mark.parametrize("where", ["default", "current", "given"])
+def test_a_next_plan_takes_the_memory_of_the_last(kind, where):
+    """New plans allocate nothing on the device once one has come and gone, whatever stream they are used on."""
+    side = torch.cuda.Stream()
+    q = torch.randn(1, 256, 2, 64, device="cuda").bfloat16()
+    lse, outs, stats = torch.zeros(1, 2, 256, device="cuda"), [torch.empty_like(q) for _ in range(4)], torch.zeros(2, device="cuda")
+    torch.cuda.synchronize()
+
+    def use(stream):
+        if kind == "attention":
+            B.Attention(1, 256, 256, 2, 2, 64).alsgd_attn_bwd(q, q, q, outs[3], lse, q, *outs[:3], stream=stream)
+        else:
+            B.GradClip([q.numel()], [0], [q.dtype], torch.bfloat16).alsgd_clip_grads([q], 1.0, outs[0].view(-1), stats, stream=stream)
+        torch.cuda.synchronize()
+
+    def once():
+        if where == "current":
+            with torch.cuda.stream(side):
+                return use(None)
+        use(side if where == "given" else None)
+    segments = lambda: torch.cuda.memory_stats()["segment.all.allocated"]  # noqa: E731
+    for _ in range(2):
+        once()
+    before = segments()
+    for _ in range(20):
+        once()
+    assert segments() == before
