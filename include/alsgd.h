@@ -390,6 +390,8 @@ int alsgd_pg_norm_static(const float* start, const float* p, uint64_t n, int32_t
 
 #define ALSGD_F32 0u
 #define ALSGD_BF16 1u
+#define ALSGD_I32 2u /* whole numbers: indices and positions */
+#define ALSGD_I64 3u
 
 typedef struct alsgd_grad_desc {
     const void* data;  /* device, numel values of the stated type, naturally aligned (16 bytes is faster) */
@@ -493,6 +495,102 @@ int alsgd_attn_bucket(const alsgd_attn_desc* desc, int32_t distance, uint32_t* b
  * was loaded; results since then are not to be trusted.  Waits for all work on the device,
  * whatever its stream, and so must not be called while one is being captured. */
 int alsgd_attn_status(int32_t device, uint32_t* waits_out);
+
+/* Rotary positions: every head of q and k turned by angles that grow with the token's position, for attention without a bias
+ * (or beside one).  The first `rot` elements of a head form rot / 2 pairs; pair i of a token at position p becomes
+ *     (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t),   t = p f_i,   f_i = base^(-2i / rot),
+ * the other elements are copied.  Pair i is elements (i, i + rot/2), or with ALSGD_ROPE_INTERLEAVED (2i, 2i + 1).
+ * For contexts longer than the trained one, with factor > 1: r = context f_i / (2 pi) is the pair's number of turns over the
+ * trained context, keep = clamp((r - turns_low) / (turns_high - turns_low), 0, 1) (0 for every pair if turns_high = 0), and
+ * f_i <- keep f_i + (1 - keep) f_i / factor.
+ * With ALSGD_ROPE_INVERSE t is -p f_i: the backward pass, from the gradients of the results to those of the operands.
+ * Angles are formed in binary64, everything else in binary32, results are rounded once. */
+#define ALSGD_ROPE_INTERLEAVED 1u
+#define ALSGD_ROPE_INVERSE 2u
+
+typedef struct alsgd_rope_desc {
+    uint32_t batch, heads_q, heads_k;  /* batch, heads_q >= 1; heads_k may be 0 (k is then not looked at) */
+    uint32_t len;                      /* tokens of a sequence, up to 2^22; may be 0 */
+    uint32_t dim;                      /* elements of a head: a multiple of 8, up to 256 */
+    uint32_t rot;                      /* of them turned: even, 2 .. dim */
+    uint32_t flags;                    /* ALSGD_ROPE_* */
+    uint32_t dtype;                    /* of q, k and the results: ALSGD_BF16 or ALSGD_F32 */
+    uint32_t position_dtype;           /* ALSGD_I32 or ALSGD_I64 */
+    int32_t device;
+    int64_t pos0;                      /* without positions: token s of every sequence is at pos0 + s */
+    double base;                       /* > 1 */
+    double factor, context, turns_low, turns_high; /* factor >= 1; the others unused at 1.  turns_high above turns_low >= 0, or 0 */
+    double amplitude;                  /* finite, not 0; usually 1 */
+} alsgd_rope_desc;
+
+/* Operands and results as attention's (steps of fp32 tensors: multiples of 4 elements).  positions: device, [batch][len] of
+ * position_dtype, or NULL.  Results may be the operands themselves (same address and steps); any other overlap is undefined.
+ * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step.  ALSGD_E_UNSUPPORTED: dim > 256.
+ * ALSGD_E_RANGE: len beyond 2^22, more than 2^16 heads, 2^31 tokens, device ordinal outside 0..63. */
+int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const void* positions,
+               const alsgd_attn_tensor* q_out, const alsgd_attn_tensor* k_out, void* stream);
+
+/* f_i of every pair (host, rot / 2 values), for a caller that inspects or reports them. */
+int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out);
+
+/* Losses over the vocabulary without its logits, for training in the replica's bf16.  x: the rows behind the last norm,
+ * w: the (tied) embedding.
+ *     z[i][j] = scale x_i . w_j,   lse_i = log(sum_j exp z[i][j])
+ *   labels (alsgd_xent_*):     loss_i = lse_i - z[i][target_i]
+ *   teacher (alsgd_distill_*): t_ik = softmax over k of scale * teacher[i][k],
+ *                              loss_i = sum_k t_ik (log t_ik - z[i][index_ik] + lse_i)
+ * the Kullback-Leibler divergence of the teacher's highest logits from the whole softmax of the row; scale is 1/temperature (a
+ * factor temperature^2 is the caller's, in dloss).  A row whose target is outside 0..vocab-1 (-100, say) takes no part: its
+ * loss and lse are 0, its dx is 0, and whatever its x holds reaches nothing.  A teacher's entry whose index is outside
+ * 0..vocab-1 or whose logit is -inf takes no part; a row without entries takes none.  Entries may come in any order, and one
+ * index several times.
+ * Backward, from lse as the forward pass left it and dloss_i = d(total)/d(loss_i):
+ *     dz[i][j] = dloss_i scale (exp(z[i][j] - lse_i) - sum_k t_ik [index_ik = j])    (labels: t = 1)
+ *     dx_i = sum_j dz[i][j] w_j,   dw_j = sum_i dz[i][j] x_i
+ * Logits, sums and statistics are binary32; dz is rounded to bf16 before the products with w and x.  Results are written, not
+ * added to, and do not depend on the order in which blocks run.  The workspace holds a copy of the rows that take part and,
+ * backward, dz of a piece of the vocabulary: 256 MiB, or 8 KiB a row where that is more, and sums of dx.
+ * A NaN or infinity in w or in the x of a row that takes part reaches what is computed from it: the row's loss, all of dw. */
+typedef struct alsgd_vocab_desc {
+    uint32_t rows;                     /* up to 2^22; may be 0 */
+    uint32_t vocab;                    /* 1 .. 2^22 */
+    uint32_t dim;                      /* a multiple of 8, up to 16384 */
+    uint32_t top;                      /* teacher's entries of a row, up to 128; 0 = labels */
+    uint32_t index_dtype;              /* of targets and indices: ALSGD_I32 or ALSGD_I64 */
+    uint32_t teacher_dtype;            /* ALSGD_F32 or ALSGD_BF16; ignored with labels */
+    float scale;                       /* > 0, finite */
+    int32_t device;
+} alsgd_vocab_desc;
+
+/* A bf16 matrix on the device: 16-byte aligned, rows stride_row elements apart (a multiple of 8; at least dim, except for x,
+ * whose rows may also overlap or be one). */
+typedef struct alsgd_matrix {
+    void* data;
+    int64_t stride_row;
+} alsgd_matrix;
+
+/* Bytes of workspace for the forward or the backward pass. */
+int alsgd_vocab_bytes(const alsgd_vocab_desc* desc, int backward_pass, uint64_t* bytes_out);
+
+/* target: device, [rows] of index_dtype.  index, teacher: device, [rows][top].  loss, lse: device, fp32 [rows].  dloss: device,
+ * fp32, dloss_step (>= 0) elements apart: 0 gives every row the same.  dx: [rows][dim], dw: [vocab][dim].  work: device, 256-byte
+ * aligned, alsgd_vocab_bytes bytes, any content; calls that share it must be ordered.
+ * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step, labels with top > 0 or a teacher without.
+ * ALSGD_E_UNSUPPORTED: top > 128, dim > 16384.  ALSGD_E_RANGE: rows or vocab beyond 2^22, device ordinal outside 0..63.
+ * ALSGD_E_NOMEM: work too small. */
+int alsgd_xent_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, float* loss, float* lse,
+                   void* work, uint64_t work_bytes, void* stream);
+int alsgd_xent_bwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, const float* lse,
+                   const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw, void* work,
+                   uint64_t work_bytes, void* stream);
+int alsgd_distill_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* index, const void* teacher,
+                      float* loss, float* lse, void* work, uint64_t work_bytes, void* stream);
+int alsgd_distill_bwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* index, const void* teacher,
+                      const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw,
+                      void* work, uint64_t work_bytes, void* stream);
+
+/* alsgd_attn_status for the vocabulary kernels: their waits are bounded too, and results behind one that ran out are NaN. */
+int alsgd_vocab_status(int32_t device, uint32_t* waits_out);
 
 #ifdef __cplusplus
 }

@@ -21,8 +21,9 @@ PG_DISPATCH, PG_CURRENT = 0, 1
 CFG_REPLICA_BF16, CFG_GRAD_STAGING, CFG_OUTER_BUFFERED, CFG_OUTER_SGDM, CFG_STABLE_PTRS = 1, 2, 4, 8, 16
 STALE_NONE, STALE_POLY, STALE_POLY_THRES = 0, 1, 2
 ARRIVE_RESEED, ARRIVE_NORM, ARRIVE_NANCHECK = 1, 2, 4
-F32, BF16 = 0, 1
+F32, BF16, I32, I64 = 0, 1, 2, 3
 ATTN_CAUSAL, ATTN_BIAS_TWO_SIDED = 1, 2
+ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
 
 
 class TensorDesc(C.Structure):
@@ -74,6 +75,22 @@ class AttnDesc(C.Structure):
 
 class AttnTensor(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_pos", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("batch", C.c_uint32), ("heads_q", C.c_uint32), ("heads_k", C.c_uint32), ("len", C.c_uint32), ("dim", C.c_uint32),
+                ("rot", C.c_uint32), ("flags", C.c_uint32), ("dtype", C.c_uint32), ("position_dtype", C.c_uint32), ("device", C.c_int32),
+                ("pos0", C.c_int64), ("base", C.c_double), ("factor", C.c_double), ("context", C.c_double), ("turns_low", C.c_double),
+                ("turns_high", C.c_double), ("amplitude", C.c_double)]
+
+
+class VocabDesc(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("vocab", C.c_uint32), ("dim", C.c_uint32), ("top", C.c_uint32), ("index_dtype", C.c_uint32),
+                ("teacher_dtype", C.c_uint32), ("scale", C.c_float), ("device", C.c_int32)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_row", C.c_int64)]
 
 
 _vp = C.c_void_p
@@ -128,6 +145,16 @@ SIGNATURES = {
                        + [C.POINTER(AttnTensor)] * 4 + [_vp, _vp, C.c_uint64, _vp]),
     "alsgd_attn_bucket": (C.c_int, [C.POINTER(AttnDesc), C.c_int32, _u32p]),
     "alsgd_attn_status": (C.c_int, [C.c_int32, _u32p]),
+    "alsgd_rope": (C.c_int, [C.POINTER(RopeDesc)] + [C.POINTER(AttnTensor)] * 2 + [_vp] + [C.POINTER(AttnTensor)] * 2 + [_vp]),
+    "alsgd_rope_frequencies": (C.c_int, [C.POINTER(RopeDesc), _f64p]),
+    "alsgd_vocab_bytes": (C.c_int, [C.POINTER(VocabDesc), C.c_int, _u64p]),
+    "alsgd_xent_fwd": (C.c_int, [C.POINTER(VocabDesc)] + [C.POINTER(Matrix)] * 2 + [_vp] * 4 + [C.c_uint64, _vp]),
+    "alsgd_xent_bwd": (C.c_int, [C.POINTER(VocabDesc)] + [C.POINTER(Matrix)] * 2 + [_vp] * 3 + [C.c_int64] + [C.POINTER(Matrix)] * 2
+                       + [_vp, C.c_uint64, _vp]),
+    "alsgd_distill_fwd": (C.c_int, [C.POINTER(VocabDesc)] + [C.POINTER(Matrix)] * 2 + [_vp] * 5 + [C.c_uint64, _vp]),
+    "alsgd_distill_bwd": (C.c_int, [C.POINTER(VocabDesc)] + [C.POINTER(Matrix)] * 2 + [_vp] * 4 + [C.c_int64] + [C.POINTER(Matrix)] * 2
+                          + [_vp, C.c_uint64, _vp]),
+    "alsgd_vocab_status": (C.c_int, [C.c_int32, _u32p]),
 }
 STATIC_MAX_ELEMS = 1 << 27
 
@@ -446,6 +473,14 @@ def _dtype_code(torch, dtype):
     raise AlsgdError(E_ARG, f"unsupported type {dtype}")
 
 
+def _whole_code(torch, dtype):
+    if dtype == torch.int32:
+        return I32
+    if dtype == torch.int64:
+        return I64
+    raise AlsgdError(E_ARG, f"unsupported type {dtype}")
+
+
 def _stream(torch, index, stream):
     """Raw handle of the given stream, or of the device's current one (without building a Stream object)."""
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
@@ -591,3 +626,142 @@ class Attention:
         out = C.c_uint32()
         _check(lib().alsgd_attn_bucket(self.desc, int(distance), C.byref(out)), "alsgd_attn_bucket")
         return int(out.value)
+
+
+def alsgd_vocab_status(device=0):
+    """0, or bits of the waits inside the vocabulary kernels that ran out on this device (waits for the device)."""
+    out = C.c_uint32()
+    _check(lib().alsgd_vocab_status(int(device), C.byref(out)), "alsgd_vocab_status")
+    return int(out.value)
+
+
+class Rotary:
+    """Rotary positions of one shape.  Operands are tensors [batch, position, head, dim] of `dtype` with any strides the ABI
+    takes; `turns` = (turns_low, turns_high)."""
+
+    def __init__(self, batch, length, heads_q, heads_k, dim, rot=None, interleaved=False, base=10000.0, factor=1.0, context=0.0,
+                 turns=(0.0, 0.0), amplitude=1.0, pos0=0, dtype=None, device=0):
+        import torch
+        self.torch = torch
+        self.dtype = dtype if dtype is not None else torch.bfloat16
+        descs = []
+        for flags in (0, ROPE_INVERSE):
+            d = RopeDesc()
+            d.batch, d.len, d.heads_q, d.heads_k, d.dim = [int(x) for x in (batch, length, heads_q, heads_k, dim)]
+            d.rot = int(dim if rot is None else rot)
+            d.flags = flags | (ROPE_INTERLEAVED if interleaved else 0)
+            d.dtype, d.position_dtype = _dtype_code(torch, self.dtype), I32
+            d.pos0, d.device = int(pos0), int(device)
+            d.base, d.factor, d.context, d.amplitude = float(base), float(factor), float(context), float(amplitude)
+            d.turns_low, d.turns_high = float(turns[0]), float(turns[1])
+            descs.append(d)
+        # a call's direction and the positions' type choose among descriptors, so that calls of several threads share nothing
+        self._descs = {}
+        for d in descs:
+            for code in (I32, I64):
+                e = RopeDesc.from_buffer_copy(d)
+                e.position_dtype = code
+                self._descs[bool(d.flags & ROPE_INVERSE), code] = e
+        self._q_shape, self._k_shape = (batch, length, heads_q, dim), (batch, length, heads_k, dim)
+        self._index = int(device)
+
+    def _operand(self, t, shape):
+        assert t.dtype is self.dtype and t.shape == shape and t.get_device() == self._index
+        b, s, h, d = t.stride()
+        assert d == 1
+        return AttnTensor(t.data_ptr(), b, s, h)
+
+    def alsgd_rope(self, q, k, q_out, k_out, positions=None, inverse=False, stream=None):
+        """q_out and k_out are written and may be q and k; k and k_out are None without key heads.  positions: int32 or int64
+        [batch, position]; inverse: the backward pass, on gradients."""
+        code = I32
+        if positions is not None:
+            assert positions.shape == self._q_shape[:2] and positions.is_contiguous() and positions.get_device() == self._index
+            code = _whole_code(self.torch, positions.dtype)
+        keys = self._k_shape[2] > 0
+        assert keys or (k is None and k_out is None)
+        _check(lib().alsgd_rope(self._descs[bool(inverse), code], self._operand(q, self._q_shape),
+                                self._operand(k, self._k_shape) if keys else None, positions.data_ptr() if positions is not None else None,
+                                self._operand(q_out, self._q_shape), self._operand(k_out, self._k_shape) if keys else None,
+                                _stream(self.torch, self._index, stream)), "alsgd_rope")
+
+    def alsgd_rope_frequencies(self):
+        """Angle per position of every pair, scaled as the plan says."""
+        d = self._descs[False, I32]
+        out = (C.c_double * (d.rot // 2))()
+        _check(lib().alsgd_rope_frequencies(d, out), "alsgd_rope_frequencies")
+        return [float(x) for x in out]
+
+
+class VocabLoss:
+    """Losses of `rows` rows over a vocabulary: labels (top = 0) or a teacher's `top` highest logits.  x: bf16 [rows, dim],
+    w: bf16 [vocab, dim], rows any aligned distance apart.  The workspaces belong to this object: calls on several streams must
+    be ordered by the caller."""
+
+    def __init__(self, rows, vocab, dim, top=0, scale=1.0, index_dtype=None, teacher_dtype=None, device=0):
+        import torch
+        self.torch = torch
+        self.device = torch.device("cuda", device)
+        self.index_dtype = index_dtype if index_dtype is not None else torch.int64
+        self.teacher_dtype = teacher_dtype if teacher_dtype is not None else torch.float32
+        d = self.desc = VocabDesc()
+        d.rows, d.vocab, d.dim, d.top, d.device = [int(x) for x in (rows, vocab, dim, top, device)]
+        d.index_dtype, d.teacher_dtype, d.scale = _whole_code(torch, self.index_dtype), _dtype_code(torch, self.teacher_dtype), float(scale)
+        self._x_shape, self._w_shape, self._rows = (rows, dim), (vocab, dim), (rows,)
+        self._labels_shape = (rows, top) if top else (rows,)
+        self._index = int(device)
+        self._work = {}                    # of either pass, made at its first call
+        self._lock = threading.Lock()      # its calls go out one by one: they share the workspaces, in stream order
+
+    def _matrix(self, t, shape):
+        assert t.dtype is self.torch.bfloat16 and t.shape == shape and t.get_device() == self._index
+        assert t.stride(1) == 1 or shape[1] == 1
+        return Matrix(t.data_ptr(), t.stride(0))
+
+    def _plain(self, t, shape, dtype):
+        assert t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous()
+        return t.data_ptr()
+
+    def _call(self, name, backward, operands, stream):
+        raw = _stream(self.torch, self._index, stream)
+        with self._lock:
+            work = self._work.get(backward)
+            if work is None:
+                nbytes = C.c_uint64()
+                _check(lib().alsgd_vocab_bytes(self.desc, int(backward), C.byref(nbytes)), "alsgd_vocab_bytes")
+                work = self._work[backward] = _Workspace(self.torch, int(nbytes.value), self.device, raw)
+            work.used_on(raw)
+            _check(getattr(lib(), name)(self.desc, *operands, work.ptr, work.nbytes, raw), name)
+
+    def _forward(self, name, x, w, labels, loss, lse, stream):
+        f32 = self.torch.float32
+        self._call(name, False, (self._matrix(x, self._x_shape), self._matrix(w, self._w_shape), *labels, self._plain(loss, self._rows, f32),
+                                 self._plain(lse, self._rows, f32)), stream)
+
+    def _backward(self, name, x, w, labels, lse, dloss, dx, dw, stream):
+        f32 = self.torch.float32
+        assert dloss.dtype is f32 and dloss.shape == self._rows and dloss.get_device() == self._index
+        self._call(name, True, (self._matrix(x, self._x_shape), self._matrix(w, self._w_shape), *labels, self._plain(lse, self._rows, f32),
+                                dloss.data_ptr(), dloss.stride(0), self._matrix(dx, self._x_shape), self._matrix(dw, self._w_shape)), stream)
+
+    def _labels(self, index):
+        return (self._plain(index, self._labels_shape, self.index_dtype),)
+
+    def _teacher(self, index, teacher):
+        return self._labels(index) + (self._plain(teacher, self._labels_shape, self.teacher_dtype),)
+
+    def alsgd_xent_fwd(self, x, w, target, loss, lse, stream=None):
+        """loss and lse (fp32 [rows]) are written.  target: [rows]; a row whose target is no word takes no part."""
+        self._forward("alsgd_xent_fwd", x, w, self._labels(target), loss, lse, stream)
+
+    def alsgd_xent_bwd(self, x, w, target, lse, dloss, dx, dw, stream=None):
+        """dx and dw are written.  dloss: fp32 [rows], which may be one number expanded."""
+        self._backward("alsgd_xent_bwd", x, w, self._labels(target), lse, dloss, dx, dw, stream)
+
+    def alsgd_distill_fwd(self, x, w, index, teacher, loss, lse, stream=None):
+        """index, teacher: [rows, top], the teacher's words and logits; an entry whose index is no word takes no part."""
+        self._forward("alsgd_distill_fwd", x, w, self._teacher(index, teacher), loss, lse, stream)
+
+    def alsgd_distill_bwd(self, x, w, index, teacher, lse, dloss, dx, dw, stream=None):
+        """dx and dw are written.  dloss: fp32 [rows], which may be one number expanded."""
+        self._backward("alsgd_distill_bwd", x, w, self._teacher(index, teacher), lse, dloss, dx, dw, stream)

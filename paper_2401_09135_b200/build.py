@@ -17,10 +17,11 @@ LIB = os.path.join(HERE, "libalsgd.so")
 LIB_DBG = os.path.join(HERE, "libalsgd_dbg.so")
 LIB_SWEEP = os.path.join(HERE, "libalsgd_sweep.so")
 SOURCES = ["alsgd_kernels.cu", "alsgd_ctx.cu", "alsgd_sched.cpp", "alsgd_static.cu", "alsgd_clip.cu", "alsgd_attn_fwd.cu",
-           "alsgd_attn_bwd.cu"]
+           "alsgd_attn_bwd.cu", "alsgd_rope.cu", "alsgd_vocab.cu"]
 SWEEP_SOURCES = ["alsgd_sweep.cu"]
 HEADERS = [os.path.join(CSRC, "alsgd_kernels.cuh"), os.path.join(CSRC, "alsgd_kernels_impl.cuh"),
            os.path.join(CSRC, "alsgd_ops.cuh"), os.path.join(CSRC, "alsgd_tc.cuh"), os.path.join(CSRC, "alsgd_attn.cuh"),
+           os.path.join(CSRC, "alsgd_pair.cuh"),
            os.path.join(HERE, "..", "include", "alsgd.h"), os.path.join(HERE, "..", "include", "alsgd_sweep.h")]
 
 NVCC_FLAGS = [

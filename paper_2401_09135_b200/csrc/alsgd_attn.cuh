@@ -453,26 +453,10 @@ inline Shape make_shape(const alsgd_attn_desc& d, const int32_t* kv_len, int row
     return s;
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-inline EncodeTiled encode_tiled() {
-    static EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
 // Boxes of `cols` elements (64, or 32 for results) x `rows` positions of one head of one sequence, swizzled over their
 // 128- or 64-byte rows, zeros outside.
 inline int make_operand(const alsgd_attn_tensor& t, uint32_t batch, uint32_t len, uint32_t heads, uint32_t dim, uint32_t rows, uint32_t cols, Operand* out) {
-    EncodeTiled encode = encode_tiled();
+    alsgd_tc::EncodeTiled encode = alsgd_tc::encode_tiled();
     if (!encode) return ALSGD_E_CUDA;
     const uint64_t extent[3] = {len, heads, batch};
     const int64_t step[3] = {t.stride_pos, t.stride_head, t.stride_batch};

@@ -1,0 +1,333 @@
+// Rotary positions: every head of q and k turned, pair by pair, by an angle that grows with the token's position.
+//
+//     (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t),   t = position * f_i,   f_i = base^(-2i / rot), scaled
+//
+// Bytes bound it: q and k are read once and written once.  A block takes a few tokens, whose cosines and sines all heads
+// share: they are formed once, in binary64 up to the reduced angle (a position of 2^20 times a frequency has no fraction
+// worth using in binary32), while the block's first loads are on their way.  A thread holds both elements of every pair that
+// it turns, so results may overwrite operands.
+#include "../../include/alsgd.h"
+#include "alsgd_ops.cuh"
+
+#include <cmath>
+#include <cstring>
+
+namespace {
+
+using namespace alsgd_ops;
+
+constexpr int kThreads = 256;
+constexpr int kMaxDim = 256;
+constexpr int kUnits = 4;              // units of 16 elements that a thread has in flight
+constexpr int kMaxTokens = 16;         // of a block
+
+struct RopeArgs {
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_step[3], k_step[3], q_out_step[3], k_out_step[3];    // batch, position, head
+    const void* positions;             // may be null
+    int wide_positions;                // binary64 whole numbers
+    int64_t pos0;
+    int len, heads_q, heads, dim, rot, interleaved, tokens, per_block;
+    int units, angles;                 // of a head
+    float amplitude, turn;             // turn: 1, or -1 for the inverse
+    double turns[kMaxDim / 2];         // f_i / (2 pi)
+};
+
+// Eight elements as 32-bit floats.
+struct Eight {
+    float v[8];
+};
+__device__ __forceinline__ void load8(const uint16_t* p, uint4 (&raw)[2]) { raw[0] = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void load8(const float* p, uint4 (&raw)[2]) {
+    raw[0] = reinterpret_cast<const uint4*>(p)[0];
+    raw[1] = reinterpret_cast<const uint4*>(p)[1];
+}
+__device__ __forceinline__ Eight widen(const uint16_t*, const uint4 (&raw)[2]) {
+    const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e.v[2 * i] = bf16_lo(w[i]);
+        e.v[2 * i + 1] = bf16_hi(w[i]);
+    }
+    return e;
+}
+__device__ __forceinline__ Eight widen(const float*, const uint4 (&raw)[2]) {
+    Eight e;
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i] = __uint_as_float(w[i]);
+    return e;
+}
+__device__ __forceinline__ void store8(uint16_t* p, const Eight& e) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(e.v[0], e.v[1]), pack_bf16(e.v[2], e.v[3]), pack_bf16(e.v[4], e.v[5]), pack_bf16(e.v[6], e.v[7]));
+}
+__device__ __forceinline__ void store8(float* p, const Eight& e) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(e.v[0], e.v[1], e.v[2], e.v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(e.v[4], e.v[5], e.v[6], e.v[7]);
+}
+__device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)pack_bf16(v, 0.0f); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+
+__device__ __forceinline__ void turn_pair(float2 cs, float& a, float& b) {
+    const float x = a, y = b;
+    a = fmaf(x, cs.x, -(y * cs.y));
+    b = fmaf(x, cs.y, y * cs.x);
+}
+
+// Cosine and sine (times the amplitude) of the block's tokens, [token][angle].
+__device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, int token0, int tokens) {
+    for (int i = threadIdx.x; i < tokens * a.angles; i += kThreads) {
+        const int t = i / a.angles, n = i - t * a.angles, token = token0 + t;
+        int64_t pos;
+        if (!a.positions) pos = a.pos0 + token % a.len;
+        else pos = a.wide_positions ? static_cast<const int64_t*>(a.positions)[token] : static_cast<const int32_t*>(a.positions)[token];
+        const double turns = (double)pos * a.turns[n];
+        float s, c;
+        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+        table[i] = make_float2(c * a.amplitude, s * (a.amplitude * a.turn));
+    }
+}
+
+// Where a unit's two groups of eight elements start; one that starts at dim or beyond does not exist.
+//   interleaved: 16 elements in a row.  half: eight of either half of the turned part, then the rest in a row.
+struct Unit {
+    int64_t from, to;                  // of the head's first element
+    int at[2];
+    int token, n;                      // token of the block, unit of the head
+    bool is_q;
+};
+__device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
+    Unit u;
+    const int per_token = a.heads * a.units;
+    u.token = i / per_token;
+    const int rest = i - u.token * per_token;
+    int head = rest / a.units;
+    u.n = rest - head * a.units;
+    const int token = token0 + u.token, b = token / a.len, s = token - b * a.len;
+    u.is_q = head < a.heads_q;
+    const int64_t* from = u.is_q ? a.q_step : a.k_step;
+    const int64_t* to = u.is_q ? a.q_out_step : a.k_out_step;
+    if (!u.is_q) head -= a.heads_q;
+    u.from = b * from[0] + s * from[1] + head * from[2];
+    u.to = b * to[0] + s * to[1] + head * to[2];
+    const int turned = a.rot / 16;
+    const bool halves = !a.interleaved && u.n < turned;
+    u.at[0] = halves ? 8 * u.n : 16 * u.n;
+    u.at[1] = halves ? a.rot / 2 + 8 * u.n : u.at[0] + 8;
+    return u;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+    extern __shared__ float2 table[];
+    grid_dependency_sync();
+    const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
+    const int units = tokens * a.heads * a.units;
+    const bool copies = a.q != a.q_out || a.k != a.k_out;              // in place, what is not turned stays
+    bool angles = false;
+    for (int u0 = threadIdx.x; u0 < units || !angles; u0 += kThreads * kUnits) {
+        uint4 raw[kUnits][2][2];
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) {
+            const int i = u0 + j * kThreads;
+            if (i >= units) continue;
+            const Unit u = unit_of(a, token0, i);
+            const T* p = static_cast<const T*>(u.is_q ? a.q : a.k) + u.from;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (u.at[h] < a.dim) load8(p + u.at[h], raw[j][h]);
+        }
+        if (!angles) {
+            fill_angles(a, table, token0, tokens);
+            __syncthreads();
+            angles = true;
+        }
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) {
+            const int i = u0 + j * kThreads;
+            if (i >= units) continue;
+            const Unit u = unit_of(a, token0, i);
+            T* p = static_cast<T*>(u.is_q ? a.q_out : a.k_out) + u.to;
+            const float2* cs = table + u.token * a.angles;
+            Eight e[2] = {widen(p, raw[j][0]), widen(p, raw[j][1])};
+            if (a.interleaved) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int pair = u.at[h] / 2 + x;
+                        if (pair < a.angles) turn_pair(cs[pair], e[h].v[2 * x], e[h].v[2 * x + 1]);
+                    }
+                if (!copies && u.at[0] >= a.rot) continue;
+            } else if (u.n < a.rot / 16) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) turn_pair(cs[8 * u.n + x], e[0].v[x], e[1].v[x]);
+            } else if (!copies) {
+                continue;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (u.at[h] < a.dim) store8(p + u.at[h], e[h]);
+        }
+    }
+}
+
+// Halves that do not begin on 16 bytes (a turned part that is no multiple of 16): element by element, a unit is a pair or an
+// element of the rest.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_elements_kernel(const __grid_constant__ RopeArgs a) {
+    extern __shared__ float2 table[];
+    grid_dependency_sync();
+    const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
+    fill_angles(a, table, token0, tokens);
+    __syncthreads();
+    const int per_head = a.angles + a.dim - a.rot, per_token = a.heads * per_head;
+    for (int i = threadIdx.x; i < tokens * per_token; i += kThreads) {
+        const int t = i / per_token, rest = i - t * per_token, token = token0 + t, b = token / a.len, s = token - b * a.len;
+        int head = rest / per_head;
+        const int n = rest - head * per_head;
+        const bool is_q = head < a.heads_q;
+        const int64_t* from = is_q ? a.q_step : a.k_step;
+        const int64_t* to = is_q ? a.q_out_step : a.k_out_step;
+        if (!is_q) head -= a.heads_q;
+        const T* x = static_cast<const T*>(is_q ? a.q : a.k) + b * from[0] + s * from[1] + head * from[2];
+        T* y = static_cast<T*>(is_q ? a.q_out : a.k_out) + b * to[0] + s * to[1] + head * to[2];
+        if (n >= a.angles) {
+            const int at = n + a.angles;
+            y[at] = x[at];
+            continue;
+        }
+        float lo = load1(x + n), hi = load1(x + n + a.angles);
+        turn_pair(table[t * a.angles + n], lo, hi);
+        store1(y + n, lo);
+        store1(y + n + a.angles, hi);
+    }
+}
+
+int check_rope_tensor(const alsgd_attn_tensor* t, const alsgd_rope_desc& d, uint32_t heads, bool output) {
+    if (!t) return ALSGD_E_ARG;
+    if (!t->data || reinterpret_cast<uintptr_t>(t->data) % 16) return ALSGD_E_ARG;
+    const int64_t step[3] = {t->stride_pos, t->stride_head, t->stride_batch};
+    const uint64_t extent[3] = {d.len, heads, d.batch};
+    const int64_t unit = d.dtype == ALSGD_F32 ? 4 : 8;
+    for (int i = 0; i < 3; ++i) {
+        if (extent[i] == 1) continue;
+        if (step[i] < 0 || step[i] % unit || step[i] >= (1ll << 39)) return ALSGD_E_ARG;
+        if (step[i] == 0 && output) return ALSGD_E_ARG;
+    }
+    return ALSGD_OK;
+}
+
+void steps_of(const alsgd_attn_tensor& t, int64_t (&step)[3]) {
+    step[0] = t.stride_batch;
+    step[1] = t.stride_pos;
+    step[2] = t.stride_head;
+}
+
+int check_rope(const alsgd_rope_desc* d) {
+    if (!d) return ALSGD_E_ARG;
+    if (d->batch == 0 || d->heads_q == 0 || d->dim == 0 || d->dim % 8 || d->rot == 0 || d->rot % 2 || d->rot > d->dim) return ALSGD_E_ARG;
+    if (d->flags & ~(ALSGD_ROPE_INTERLEAVED | ALSGD_ROPE_INVERSE)) return ALSGD_E_ARG;
+    if (d->dtype != ALSGD_F32 && d->dtype != ALSGD_BF16) return ALSGD_E_ARG;
+    if (d->position_dtype != ALSGD_I32 && d->position_dtype != ALSGD_I64) return ALSGD_E_ARG;
+    if (!(d->base > 1.0) || !std::isfinite(d->base) || !(d->factor >= 1.0) || !std::isfinite(d->factor)) return ALSGD_E_ARG;
+    if (!std::isfinite(d->amplitude) || d->amplitude == 0.0) return ALSGD_E_ARG;
+    if (!(d->context >= 0.0) || !std::isfinite(d->context) || !(d->turns_low >= 0.0) || !std::isfinite(d->turns_high)) return ALSGD_E_ARG;
+    if (d->turns_high != 0.0 && !(d->turns_high > d->turns_low)) return ALSGD_E_ARG;
+    if (d->dim > kMaxDim) return ALSGD_E_UNSUPPORTED;
+    if (d->len > 1u << 22 || (uint64_t)d->heads_q + d->heads_k > 1u << 16) return ALSGD_E_RANGE;
+    // a block's units are counted in 32 bits; kMaxTokens * 2^16 heads * 256 elements stay below 2^31, tokens must as well
+    if ((uint64_t)d->batch * d->len > 0x7FFFFFFFull - kMaxTokens) return ALSGD_E_RANGE;
+    if (d->device < 0 || d->device >= kMaxDevices) return ALSGD_E_RANGE;
+    return ALSGD_OK;
+}
+
+void frequencies(const alsgd_rope_desc& d, double* f) {
+    const double two_pi = 6.283185307179586476925;
+    for (uint32_t i = 0; i < d.rot / 2; ++i) {
+        double v = std::pow(d.base, -2.0 * i / d.rot);
+        if (d.factor != 1.0) {
+            double keep = 0.0;
+            if (d.turns_high != 0.0) {
+                keep = (d.context * v / two_pi - d.turns_low) / (d.turns_high - d.turns_low);
+                keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            }
+            v = v * keep + v / d.factor * (1.0 - keep);
+        }
+        f[i] = v;
+    }
+}
+
+}  // namespace
+
+extern "C" int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out) {
+    const int rc = check_rope(desc);
+    if (rc != ALSGD_OK) return rc;
+    if (!out) return ALSGD_E_ARG;
+    frequencies(*desc, out);
+    return ALSGD_OK;
+}
+
+extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const void* positions,
+                          const alsgd_attn_tensor* q_out, const alsgd_attn_tensor* k_out, void* stream) {
+    int rc = check_rope(desc);
+    if (rc != ALSGD_OK) return rc;
+    const alsgd_rope_desc& d = *desc;
+    if (reinterpret_cast<uintptr_t>(positions) % (d.position_dtype == ALSGD_I64 ? 8 : 4)) return ALSGD_E_ARG;
+    if (d.len == 0) return ALSGD_OK;
+    if ((rc = check_rope_tensor(q, d, d.heads_q, false)) != ALSGD_OK) return rc;
+    if ((rc = check_rope_tensor(q_out, d, d.heads_q, true)) != ALSGD_OK) return rc;
+    if (d.heads_k) {
+        if ((rc = check_rope_tensor(k, d, d.heads_k, false)) != ALSGD_OK) return rc;
+        if ((rc = check_rope_tensor(k_out, d, d.heads_k, true)) != ALSGD_OK) return rc;
+    }
+    UseDevice use(d.device);
+    if (!use.ok) return ALSGD_E_CUDA;
+
+    RopeArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.q = q->data;
+    a.q_out = q_out->data;
+    steps_of(*q, a.q_step);
+    steps_of(*q_out, a.q_out_step);
+    if (d.heads_k) {
+        a.k = k->data;
+        a.k_out = k_out->data;
+        steps_of(*k, a.k_step);
+        steps_of(*k_out, a.k_out_step);
+    }
+    a.positions = positions;
+    a.wide_positions = d.position_dtype == ALSGD_I64;
+    a.pos0 = d.pos0;
+    a.len = (int)d.len;
+    a.heads_q = (int)d.heads_q;
+    a.heads = (int)(d.heads_q + d.heads_k);
+    a.dim = (int)d.dim;
+    a.rot = (int)d.rot;
+    a.interleaved = (d.flags & ALSGD_ROPE_INTERLEAVED) != 0;
+    a.tokens = (int)(d.batch * d.len);
+    a.angles = a.rot / 2;
+    a.amplitude = (float)d.amplitude;
+    a.turn = d.flags & ALSGD_ROPE_INVERSE ? -1.0f : 1.0f;
+    frequencies(d, a.turns);
+    for (int i = 0; i < a.angles; ++i) a.turns[i] *= 1.0 / 6.283185307179586476925;
+    const bool by_element = !a.interleaved && a.rot % 16;
+    a.units = (a.dim + 15) / 16;
+    // enough tokens for every thread's kUnits, but no fewer than two blocks per SM as long as there are tokens for them
+    const int per_token = a.heads * a.units;
+    a.per_block = (kThreads * kUnits + per_token - 1) / per_token;
+    if (a.per_block > a.tokens / (2 * kSMs)) a.per_block = a.tokens / (2 * kSMs);
+    if (a.per_block > kMaxTokens) a.per_block = kMaxTokens;
+    if (a.per_block < 1) a.per_block = 1;
+    const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kThreads);
+    const size_t smem = (size_t)a.per_block * a.angles * sizeof(float2);       // at most 16 KB
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (d.dtype == ALSGD_F32) e = launch_dependent(by_element ? rope_elements_kernel<float> : rope_kernel<float>, grid, block, smem, s, a);
+    else e = launch_dependent(by_element ? rope_elements_kernel<uint16_t> : rope_kernel<uint16_t>, grid, block, smem, s, a);
+    return e == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}

@@ -1,0 +1,1196 @@
+// Losses over a vocabulary whose logits are never kept: the cross entropy with a label per row, and the distillation from a
+// teacher's highest logits, which is the same loss with a few weighted labels per row.
+//
+//     z[i][j] = scale x_i . w_j,   lse_i = log sum_j exp z[i][j],   loss_i = sum_k t_ik (log t_ik - z[i][index_ik] + lse_i)
+//     dz[i][j] = dloss_i scale (exp(z[i][j] - lse_i) - sum_k t_ik [index_ik = j]),   dx = dz w,   dw = dz^T x
+//
+// Forward: tiles of 256 rows x 256 words; a tile's maxima, sums of exponentials and the labels' logits leave the chip, the
+// logits do not.  Backward, a piece of the vocabulary at a time: the logits again, dz of the piece in bf16 (at most a
+// workspace's size), then dx += dz w and dw = dz^T x in one launch.
+//
+// The rows that take part are gathered first (a padded batch pays for its tokens, not for its padding; what the other rows
+// hold reaches nothing) and everything behind works on their number, which only the device knows.
+//
+// The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
+// of either operand, so that a tile needs half of the shared memory traffic of two single ones.  One warp copies, one
+// issues products, eight take the finished tile out of tensor memory while the next one is formed in its other half.
+#include "../../include/alsgd.h"
+#include "alsgd_ops.cuh"
+#include "alsgd_pair.cuh"
+
+#include <cfloat>
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+namespace {
+
+using namespace alsgd_ops;
+using namespace alsgd_tc;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTile = 256;             // rows and columns of a pair's tile
+constexpr int kStep = 64;              // of the products' inner axis: one 128-byte row of bf16
+constexpr int kPairs = kSMs / 2;
+constexpr int kMaxTop = 128;
+constexpr uint64_t kPieceBytes = 256ull << 20;
+constexpr int kLeastPiece = 16;        // tiles of a piece: below that, adding dx up would cost more than the memory is worth
+constexpr int kMaxSplits = 64;
+
+// ---------------------------------------------------------------------------------------------- rows that take part
+
+struct Labels {
+    const void* index;                 // [rows] or [rows][top]
+    const void* teacher;               // [rows][top]; null: a label per row
+    int wide, bf16;                    // 64-bit indices; teacher's type
+    int rows, top, vocab;
+};
+
+__device__ __forceinline__ int label_at(const Labels& l, size_t i) {
+    const int64_t v = l.wide ? static_cast<const int64_t*>(l.index)[i] : static_cast<const int32_t*>(l.index)[i];
+    return v >= 0 && v < l.vocab ? (int)v : -1;
+}
+__device__ __forceinline__ float teacher_at(const Labels& l, size_t i) {
+    return l.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(l.teacher)[i] << 16) : static_cast<const float*>(l.teacher)[i];
+}
+
+constexpr int kCountRows = 256;        // rows of a counting block
+
+// Which rows take part: their number in each block of rows, and each row's place among its block's (-1 - place among those
+// that do not).
+__global__ void __launch_bounds__(kCountRows) count_kernel(Labels l, int padded, int* block_count, int* place) {
+    __shared__ int warp_count[kCountRows / 32];
+    grid_dependency_sync();
+    const int r0 = blockIdx.x * kCountRows, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    bool mine = false;
+    if (!l.teacher) {
+        const int r = r0 + threadIdx.x;
+        mine = r < l.rows && label_at(l, r) >= 0;
+    } else {
+        // a warp looks at its 32 rows one by one
+        for (int i = 0; i < 32; ++i) {
+            const int r = r0 + 32 * warp + i;
+            bool any = false;
+            if (r < l.rows)
+                for (int k = lane; k < l.top; k += 32) {
+                    const size_t at = (size_t)r * l.top + k;
+                    any |= label_at(l, at) >= 0 && teacher_at(l, at) != -INFINITY;
+                }
+            any = __any_sync(~0u, any);
+            if (lane == i) mine = any;
+        }
+    }
+    const uint32_t votes = __ballot_sync(~0u, mine);
+    if (lane == 0) warp_count[warp] = __popc(votes);
+    __syncthreads();
+    int before = __popc(votes & ((1u << lane) - 1)), total = 0;
+    for (int w = 0; w < kCountRows / 32; ++w) {
+        if (w < warp) before += warp_count[w];
+        total += warp_count[w];
+    }
+    if (r0 + (int)threadIdx.x < padded) place[r0 + threadIdx.x] = mine ? before : -1 - ((int)threadIdx.x - before);
+    if (threadIdx.x == 0) block_count[blockIdx.x] = total;
+}
+
+struct GatherArgs {
+    Labels l;
+    const uint16_t* x;
+    int64_t x_step;
+    const float *lse, *dloss;          // backward only
+    int64_t dloss_step;
+    float scale;
+    int padded, blocks, dim, tiles;    // rows in whole tiles; counting blocks; tiles of the vocabulary
+    const int *block_count, *place;
+    int* count;                        // one: rows that take part
+    int* slot;                         // [rows]: place among them, or -1
+    int* row;                          // [padded]: the row at a place
+    uint16_t* xc;                      // [padded][dim]
+    int* target;                       // [padded]; labels only
+    int* index;                        // [padded][top] ascending, then places that take no part; teacher only
+    float* weight;                     // [padded][top]
+    float* entropy;                    // [padded]: sum t log t
+    uint8_t* first;                    // [padded][tiles + 1]: entries below each tile's first word
+    float *lse2, *coef;                // [padded]; backward only
+};
+
+constexpr int kGatherWarps = 4;
+
+// One warp per row: its place, its copy of x, its labels, what the gradient scales by.
+__global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_constant__ GatherArgs a) {
+    __shared__ int s_index[kGatherWarps][kMaxTop], s_sorted[kGatherWarps][kMaxTop];
+    __shared__ int s_sum[2];
+    grid_dependency_sync();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int r0 = blockIdx.x * kGatherWarps, r = r0 + warp, block = r0 / kCountRows;     // a block's rows share a counting block
+    int before = 0, total = 0;
+    for (int i = threadIdx.x; i < a.blocks; i += 32 * kGatherWarps) {
+        const int n = a.block_count[i];
+        total += n;
+        if (i < block) before += n;
+    }
+    if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
+    __syncthreads();
+    before = __reduce_add_sync(~0u, before);
+    total = __reduce_add_sync(~0u, total);
+    if (lane == 0) {
+        atomicAdd(&s_sum[0], before);          // whole numbers: any order
+        atomicAdd(&s_sum[1], total);
+    }
+    __syncthreads();
+    before = s_sum[0];
+    const int count = s_sum[1];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = count;
+    if (r >= a.padded) return;
+    const int place = a.place[r];
+    const bool used = place >= 0;
+    // rows that do not take part fill the places behind; of those only the last tile's are looked at
+    const int slot = used ? before + place : count + (block * kCountRows - before) + (-1 - place);
+    if (lane == 0 && r < a.l.rows) a.slot[r] = used ? slot : -1;
+    if (slot >= (count + kTile - 1) / kTile * kTile) return;
+
+    uint16_t* to = a.xc + (size_t)slot * a.dim;
+    const uint16_t* from = a.x + r * a.x_step;
+    for (int c = 8 * lane; c < a.dim; c += 256)
+        *reinterpret_cast<uint4*>(to + c) = used ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0, 0, 0, 0);
+    if (lane == 0) {
+        a.row[slot] = r;
+        if (a.lse) {
+            a.lse2[slot] = used ? a.lse[r] * kLog2e : 0.0f;
+            a.coef[slot] = used ? a.dloss[r * a.dloss_step] * a.scale : 0.0f;
+        }
+        if (a.target) a.target[slot] = used ? label_at(a.l, r) : -1;
+    }
+    if (a.target) return;
+
+    // the teacher's softmax over the entries that take part, then the entries in ascending order of their words
+    uint8_t* first = a.first + (size_t)slot * (a.tiles + 1);
+    if (!used) {
+        for (int t = lane; t <= a.tiles; t += 32) first[t] = 0;
+        return;
+    }
+    constexpr int E = kMaxTop / 32;
+    const float c = a.scale * kLog2e;
+    int at[E];
+    float v[E], top = -INFINITY, sum = 0.0f;
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int k = lane + 32 * e;
+        at[e] = INT_MAX;
+        v[e] = -INFINITY;
+        if (k < a.l.top) {
+            const size_t i = (size_t)r * a.l.top + k;
+            const int word = label_at(a.l, i);
+            const float t = teacher_at(a.l, i);
+            if (word >= 0 && t != -INFINITY) {
+                at[e] = word;
+                v[e] = t;
+            }
+            s_index[warp][k] = at[e];
+        }
+        nan |= v[e] != v[e];
+        top = fmaxf(top, v[e]);
+    }
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    if (__any_sync(~0u, nan)) top = NAN;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c);
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    const float inv = 1.0f / sum, log_sum = logf(sum);
+    float entropy = 0.0f;
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int k = lane + 32 * e;
+        if (k >= a.l.top) continue;
+        const float t = at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c) * inv;
+        if (at[e] != INT_MAX) entropy += t * ((v[e] - top) * a.scale - log_sum);
+        int rank = 0;
+        for (int j = 0; j < a.l.top; ++j) rank += s_index[warp][j] < at[e] || (s_index[warp][j] == at[e] && j < k);
+        s_sorted[warp][rank] = at[e];
+        a.index[(size_t)slot * a.l.top + rank] = at[e];
+        a.weight[(size_t)slot * a.l.top + rank] = t;
+    }
+    for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
+    if (lane == 0) a.entropy[slot] = entropy;
+    __syncwarp();
+    for (int t = lane; t <= a.tiles; t += 32) {
+        const int word = min(t * kTile, a.l.vocab);            // places that take no part are behind every word
+        int low = 0, high = a.l.top;
+        while (low < high) {
+            const int mid = (low + high) / 2;
+            if (s_sorted[warp][mid] < word) low = mid + 1;
+            else high = mid;
+        }
+        first[t] = (uint8_t)low;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- the pair's machinery
+
+constexpr int kThreads = 320;          // copies, products, eight warps that take tiles out
+constexpr int kOutWarps = 8;
+constexpr int kStageBytes = 32768;     // of a block: 128 x 64 of A, up to 128 x 64 of B
+constexpr int kAccColumns = 256;
+constexpr int kStagingBytes = 4096;    // of a warp: 32 rows of 64 bf16
+
+template <int STAGES>
+struct Bars {
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem, dead;
+};
+
+// What every warp of a block knows about its pair's shared memory.
+template <int STAGES>
+struct Pair {
+    uint32_t stage0, full, empty, acc_full, acc_empty, rank, tmem;
+    volatile uint32_t* dead;
+
+    __device__ __forceinline__ uint32_t a(int s) const { return stage0 + s * kStageBytes; }
+    __device__ __forceinline__ uint32_t b(int s) const { return stage0 + s * kStageBytes + kStageBytes / 2; }
+};
+
+// Barriers and tensor memory of both blocks.  Full: one arrival (the first block's copying thread, for the bytes of
+// both).  Empty, finished tile: one arrival, by the tensor core, on either block's.  Tile taken out: every warp of both blocks.
+template <int STAGES>
+__device__ __forceinline__ Pair<STAGES> pair_begin(uint8_t* stages, Bars<STAGES>* bars) {
+    Pair<STAGES> p;
+    p.stage0 = smem_u32(stages);
+    p.full = smem_u32(bars->full);
+    p.empty = smem_u32(bars->empty);
+    p.acc_full = smem_u32(bars->acc_full);
+    p.acc_empty = smem_u32(bars->acc_empty);
+    p.rank = cluster_rank();
+    p.dead = &bars->dead;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            bar_init(p.full + 8 * s, 1);
+            bar_init(p.empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(p.acc_full + 8 * b, 1);
+            bar_init(p.acc_empty + 8 * b, 2 * kOutWarps);
+        }
+        bars->dead = 0;
+        bar_init_fence();
+    }
+    if (threadIdx.x / 32 == 1) tmem_alloc_pair(smem_u32(&bars->tmem), 2 * kAccColumns);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    p.tmem = bars->tmem;
+    return p;
+}
+
+// The blocks leave together: neither's shared memory goes while the other's copies or products may touch it.  `steps`:
+// stages that the copying thread filled in all.
+template <int STAGES>
+__device__ __forceinline__ void pair_end(const Pair<STAGES>& p) {
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (threadIdx.x / 32 == 1) {
+        tc_fence_after();
+        tmem_free_pair(p.tmem, 2 * kAccColumns);
+    }
+}
+
+// The copying thread's and the product thread's place in the ring of stages.
+struct Ring {
+    int stage = 0;
+    uint32_t phase = 0;
+    template <int STAGES>
+    __device__ __forceinline__ void next() {
+        if (++stage == STAGES) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// Wait codes, one bit each.
+enum : uint32_t { kWaitEmpty = 1, kWaitFull = 2, kWaitAccEmpty = 4, kWaitAccFull = 8 };
+
+// Before the copying thread leaves, everything that it started has landed and been consumed (at once, unless it gave up).
+template <int STAGES>
+__device__ __forceinline__ void ring_drain(const Pair<STAGES>& p, Ring ring) {
+    for (int s = 0; s < STAGES; ++s) {
+        drain(p.empty + 8 * ring.stage, ring.phase ^ 1);
+        ring.next<STAGES>();
+    }
+}
+
+// One tile's products: `steps` stages, each four products of 16 along the inner axis.  a_step / b_step: bytes of shared memory
+// from one to the next.
+template <int STAGES, typename DESC_A, typename DESC_B>
+__device__ __forceinline__ void tile_products(const Pair<STAGES>& p, Ring& ring, int tile, int steps, uint32_t desc, DESC_A a, DESC_B b) {
+    const int buf = tile & 1;
+    wait_cluster(p.acc_empty + 8 * buf, ((tile >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
+    tc_fence_after();
+    const uint32_t d = p.tmem + buf * kAccColumns;
+    for (int k = 0; k < steps; ++k) {
+        wait_cluster(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
+        tc_fence_after();
+        const uint32_t sa = p.a(ring.stage), sb = p.b(ring.stage);
+#pragma unroll
+        for (int i = 0; i < kStep / 16; ++i) mma_ss_pair(d, a(sa, i), b(sb, i), desc, k || i);
+        mma_commit_pair(p.empty + 8 * ring.stage);
+        ring.next<STAGES>();
+    }
+    mma_commit_pair(p.acc_full + 8 * buf);
+}
+
+// The warp has taken its part of tile `tile` out of tensor memory.
+template <int STAGES>
+__device__ __forceinline__ void tile_taken(const Pair<STAGES>& p, int tile, int lane) {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (tile & 1), 0));
+}
+
+// ---------------------------------------------------------------------------------------------- logits
+
+struct LogitArgs {
+    CUtensorMap x, w;                  // gathered rows, words: boxes of 64 x 128
+    const int* count;
+    int dim, vocab, top;
+    int tile0, tiles, all_tiles;       // of the vocabulary: this launch's, all of them
+    float scale2;                      // scale * log2 e
+    const int* target;
+    const int* index;
+    const float* weight;
+    const uint8_t* first;
+    int padded;
+    float2* stats;                     // forward: [2 * all_tiles][padded]: maximum of z / scale, sum of exponentials
+    float* label_z;                    // forward: [padded][max(1, top)]: z / scale at the labels
+    const float *lse2, *coef;          // backward
+    uint8_t* dz;                       // backward: blocks of 128 rows x 64 words, [row block][word block]
+};
+
+constexpr int kGroup = 8;              // row tiles whose x stays in the L2 while the words go by
+
+// Tiles in an order that lets the blocks at work share operands: the words' tiles in turn for a group of row tiles.
+__device__ __forceinline__ void tile_at(int i, int row_tiles, int tiles, int& rt, int& ct) {
+    const int group = i / (kGroup * tiles), g0 = group * kGroup, n = min(kGroup, row_tiles - g0), rest = i - g0 * tiles;
+    ct = rest / n;
+    rt = g0 + rest - ct * n;
+}
+
+constexpr int kLogitStages = 6;
+
+struct LogitSmem {
+    uint8_t stages[kLogitStages * kStageBytes];
+    uint8_t staging[kOutWarps * kStagingBytes];
+    Bars<kLogitStages> bars;
+};
+
+// Replaces / reads the value of one of 32 registers, chosen at run time.
+__device__ __forceinline__ float pick(const uint32_t (&z)[32], int at) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v = i == at ? __uint_as_float(z[i]) : v;
+    return v;
+}
+
+template <bool BACKWARD, bool TOP>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_kernel(const __grid_constant__ LogitArgs a) {
+    extern __shared__ uint8_t raw[];
+    LogitSmem& sm = *reinterpret_cast<LogitSmem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        tma_prefetch(&a.x);
+        tma_prefetch(&a.w);
+    }
+    const Pair<kLogitStages> p = pair_begin<kLogitStages>(sm.stages, &sm.bars);
+    grid_dependency_sync();
+    const int count = *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
+    const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            Ring ring;
+            for (int i = first; i < tiles; i += pairs) {
+                int rt, ct;
+                tile_at(i, row_tiles, a.tiles, rt, ct);
+                const int row = rt * kTile + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
+                for (int k = 0; k < steps; ++k) {
+                    wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * kStageBytes);
+                    const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
+                    tma_load2_pair(p.a(ring.stage), &a.x, full, k * kStep, row);
+                    tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
+                    ring.next<kLogitStages>();
+                }
+            }
+            ring_drain(p, ring);
+        }
+    } else if (warp == 1) {
+        if (p.rank == 0 && elect_one()) {
+            Ring ring;
+            int tile = 0;
+            for (int i = first; i < tiles; i += pairs, ++tile)
+                tile_products(p, ring, tile, steps, mma_desc_pair(kTile, false, false), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+                              [](uint32_t s, int i) { return desc_k_major(s + 32 * i); });
+        }
+    } else {
+        const int quad = warp & 3, half = (warp - 2) / 4;          // tensor memory's lanes that the warp may read; the tile's columns
+        const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
+        const uint32_t staging = smem_u32(sm.staging) + (warp - 2) * kStagingBytes;
+        uint8_t* const line = sm.staging + (warp - 2) * kStagingBytes + lane * 128;
+        int tile = 0;
+        for (int i = first; i < tiles; i += pairs, ++tile) {
+            int rt, ct;
+            tile_at(i, row_tiles, a.tiles, rt, ct);
+            const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
+            const int c0 = (a.tile0 + ct) * kTile + half * 128;    // first word
+            int label = -1, e = 0, e_end = 0;
+            float weight = 1.0f;
+            const size_t list = (size_t)row * a.top;
+            if (TOP) {
+                const uint8_t* f = a.first + (size_t)row * (a.all_tiles + 1) + a.tile0 + ct;
+                e = f[0];
+                e_end = f[1];
+                // the other half's entries are its own
+                while (e < e_end && a.index[list + e] < c0) ++e;
+                if (e < e_end) {
+                    label = a.index[list + e];
+                    weight = a.weight[list + e];
+                }
+            } else {
+                label = a.target[row];
+            }
+            const bool used = row < count;
+            float lse2 = 0.0f, coef = 0.0f;
+            if (BACKWARD) {
+                lse2 = a.lse2[row];
+                coef = a.coef[row];
+            }
+            float top = -INFINITY, sum = 0.0f;
+            wait_warp(p.acc_full + 8 * (tile & 1), (tile >> 1) & 1, p.dead, kWaitAccFull);
+            tc_fence_after();
+            const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t z[32];
+                tmem_ld32(z, lanes + (tile & 1) * kAccColumns + half * 128 + 32 * c);
+                tmem_wait_ld();
+                tmem_use(z);
+                if (c == 3) tile_taken(p, tile, lane);
+                const int w0 = c0 + 32 * c;
+                if (!BACKWARD) {
+                    if (w0 + 32 > a.vocab) {                       // words behind the last have no logits
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = w0 + j < a.vocab ? z[j] : 0xFF800000u;
+                    }
+                    if (TOP) {
+                        while (e < e_end && label < w0 + 32) {
+                            a.label_z[list + e] = pick(z, label - w0);
+                            if (++e < e_end) label = a.index[list + e];
+                        }
+                    } else if ((uint32_t)(label - w0) < 32u) {
+                        a.label_z[row] = pick(z, label - w0);
+                    }
+                    __syncwarp();
+                    float m = top;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) m = fmaxf(m, __uint_as_float(z[j]));
+                    const float ref = m == -INFINITY ? 0.0f : m * a.scale2;
+                    sum *= exp2_fast(fmaf(top, a.scale2, -ref));
+                    top = m;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum += exp2_fast(fmaf(__uint_as_float(z[j]), a.scale2, -ref));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] = __float_as_uint(coef * exp2_fast(fmaf(__uint_as_float(z[j]), a.scale2, -lse2)));
+                    if (TOP) {
+                        while (e < e_end && label < w0 + 32) {
+                            const float t = coef * weight;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == label - w0) z[j] = __float_as_uint(__uint_as_float(z[j]) - t);
+                            if (++e < e_end) {
+                                label = a.index[list + e];
+                                weight = a.weight[list + e];
+                            }
+                        }
+                    } else if ((uint32_t)(label - w0) < 32u) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j == label - w0) z[j] = __float_as_uint(__uint_as_float(z[j]) - coef);
+                    }
+                    __syncwarp();
+                    if (dead) z[0] = 0x7FC00000u;
+                    if ((c & 1) == 0) {                            // the staged block before this one has left
+                        if (lane == 0) tma_store_wait_read();
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
+                            // rows that fill the last tile, words behind the last: zeros, whatever the operands hold
+                            const int word = w0 + 8 * j + 2 * h;
+                            if (!used || word >= a.vocab) v[h] = 0;
+                            else if (word + 1 >= a.vocab) v[h] &= 0xFFFFu;
+                        }
+                        const int chunk = 4 * (c & 1) + j;
+                        *reinterpret_cast<uint4*>(line + ((chunk ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                    if (c & 1) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const size_t block = (size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4 + half * 2 + c / 2;
+                            bulk_store(a.dz + block * 16384 + quad * 4096, staging, kStagingBytes);
+                            tma_store_commit();
+                        }
+                    }
+                }
+            }
+            if (!BACKWARD) a.stats[(size_t)(2 * (a.tile0 + ct) + half) * a.padded + row] = make_float2(top, dead ? NAN : sum);
+        }
+        if (BACKWARD && lane == 0) bulk_store_wait();
+    }
+    pair_end(p);
+}
+
+// ---------------------------------------------------------------------------------------------- the loss from the tiles' sums
+
+struct LossArgs {
+    const float2* stats;
+    const float* label_z;
+    const float *weight, *entropy;     // teacher only
+    const int *index;
+    const int *slot, *count;
+    int rows, padded, parts, top;      // parts: 2 * tiles
+    float scale, scale2;
+    float *loss, *lse;
+};
+
+constexpr int kLossRows = 32, kLossParts = 8;
+
+// 32 rows in gathered order, eight threads for each.  The rows that take no part get zeros.
+__global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a, const int* row_of) {
+    __shared__ float s_top[kLossParts][kLossRows], s_sum[kLossParts][kLossRows], s_z[kLossParts][kLossRows], s_weight[kLossParts][kLossRows];
+    grid_dependency_sync();
+    const int count = *a.count, i = threadIdx.x % kLossRows, part = threadIdx.x / kLossRows, row = blockIdx.x * kLossRows + i;
+    if (threadIdx.x < kLossRows && row < a.rows && a.slot[row] < 0) a.loss[row] = a.lse[row] = 0.0f;
+    if (blockIdx.x * kLossRows >= count) return;
+    float top = -INFINITY, sum = 0.0f;
+    for (int t = part; t < a.parts; t += kLossParts) {
+        const float2 s = a.stats[(size_t)t * a.padded + row];
+        const float m = fmaxf(top, s.x), ref = m == -INFINITY ? 0.0f : m * a.scale2;
+        sum = sum * exp2f(fmaf(top, a.scale2, -ref)) + s.y * exp2f(fmaf(s.x, a.scale2, -ref));
+        top = m;
+    }
+    float z = 0.0f, weight = 0.0f;                             // sum t z, sum t
+    if (row < count)
+        for (int k = part; k < a.top; k += kLossParts) {
+            const size_t at = (size_t)row * a.top + k;
+            if (a.index[at] == INT_MAX) break;
+            z = fmaf(a.weight[at], a.label_z[at], z);
+            weight += a.weight[at];
+        }
+    s_top[part][i] = top;
+    s_sum[part][i] = sum;
+    s_z[part][i] = z;
+    s_weight[part][i] = weight;
+    __syncthreads();
+    if (part || row >= count) return;
+    for (int q = 1; q < kLossParts; ++q) {
+        const float m = fmaxf(top, s_top[q][i]), ref = m == -INFINITY ? 0.0f : m * a.scale2;
+        sum = sum * exp2f(fmaf(top, a.scale2, -ref)) + s_sum[q][i] * exp2f(fmaf(s_top[q][i], a.scale2, -ref));
+        top = m;
+        z += s_z[q][i];
+        weight += s_weight[q][i];
+    }
+    const float lse = fmaf(top, a.scale, logf(sum));
+    const int r = row_of[row];
+    a.loss[r] = a.top ? a.entropy[row] - a.scale * z + lse * weight : lse - a.scale * a.label_z[row];
+    a.lse[r] = lse;
+}
+
+// ---------------------------------------------------------------------------------------------- dx += dz w, dw = dz^T x
+
+struct ProductArgs {
+    CUtensorMap dz, x, w;              // boxes of 64 x 64; dz's rows are those of its blocks
+    const int* count;
+    int dim, vocab;
+    int tile0, tiles;                  // of the vocabulary: the piece
+    int splits, split_steps;           // of dx's inner axis
+    int n, dim_tiles;                  // columns of a tile, tiles of dim
+    int padded, add;                   // add: dx's sums so far are read
+    float* dx;                         // [splits][padded][dim]
+    uint16_t* dw;
+    int64_t dw_step;
+};
+
+constexpr int kProductStages = 7;
+
+struct ProductSmem {
+    uint8_t stages[kProductStages * kStageBytes];
+    Bars<kProductStages> bars;
+};
+
+struct Item {
+    bool is_dw;
+    int rt, dt, split, k0, steps;      // row tile (of rows or of words)
+};
+
+// A pair's items: the longer kind first, dealt in turn; then the shorter kind, at first to the pairs that got one less of the
+// longer, until they are even.
+struct Deal {
+    int long_n, short_n, extra, pair, pairs;
+    bool dw_long;
+    __device__ __forceinline__ bool at(int i, bool& is_dw, int& item) const {
+        const int rest = long_n % pairs, mine = long_n / pairs + (pair < rest);
+        if (i < mine) {
+            is_dw = dw_long;
+            item = pair + i * pairs;
+            return true;
+        }
+        is_dw = !dw_long;
+        i -= mine;
+        const int late = pairs - rest;                             // pairs with one less
+        if (pair >= rest) {
+            if (i < extra) {
+                item = pair - rest + i * late;
+                return item < short_n;
+            }
+            i -= extra;
+        }
+        item = extra * late + pair + i * pairs;
+        return item < short_n;
+    }
+};
+
+__device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pair, int pairs) {
+    const int dx_n = (count + kTile - 1) / kTile * a.dim_tiles * a.splits, dw_n = a.tiles * a.dim_tiles;
+    const int dx_cost = a.split_steps + 4, dw_cost = (count + kStep - 1) / kStep + 4;
+    Deal d;
+    d.dw_long = dw_cost >= dx_cost;
+    d.long_n = d.dw_long ? dw_n : dx_n;
+    d.short_n = d.dw_long ? dx_n : dw_n;
+    d.pair = pair;
+    d.pairs = pairs;
+    const int more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
+    d.extra = d.long_n % pairs ? (more + less / 2) / less : 0;
+    return d;
+}
+
+__device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int count, int i, Item& t) {
+    int n;
+    if (!d.at(i, t.is_dw, n)) return false;
+    t.dt = n % a.dim_tiles;
+    n /= a.dim_tiles;
+    if (t.is_dw) {
+        t.rt = n;
+        t.split = 0;
+        t.k0 = 0;
+        t.steps = (count + kStep - 1) / kStep;
+    } else {
+        t.split = n % a.splits;
+        t.rt = n / a.splits;
+        t.k0 = t.split * a.split_steps;
+        t.steps = min(a.split_steps, a.tiles * 4 - t.k0);
+    }
+    return true;
+}
+
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+    extern __shared__ uint8_t raw[];
+    ProductSmem& sm = *reinterpret_cast<ProductSmem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        tma_prefetch(&a.dz);
+        tma_prefetch(&a.x);
+        tma_prefetch(&a.w);
+    }
+    const Pair<kProductStages> p = pair_begin<kProductStages>(sm.stages, &sm.bars);
+    grid_dependency_sync();
+    const int count = *a.count, pairs = gridDim.x / 2;
+    const Deal deal = deal_of(a, count, blockIdx.x / 2, pairs);
+    const int boxes = (a.n / 2 + 63) / 64;                         // of B in either block
+
+    if (count == 0) {
+        // nobody takes part: dw of the piece is zero, and nothing reads dx
+        const int per_row = a.dim / 8, words = min(a.vocab - a.tile0 * kTile, a.tiles * kTile);
+        for (int64_t i = blockIdx.x * kThreads + threadIdx.x; i < (int64_t)words * per_row; i += (int64_t)gridDim.x * kThreads) {
+            const int64_t v = i / per_row;
+            *reinterpret_cast<uint4*>(a.dw + (a.tile0 * (int64_t)kTile + v) * a.dw_step + 8 * (i - v * per_row)) = make_uint4(0, 0, 0, 0);
+        }
+    } else if (warp == 0) {
+        if (elect_one()) {
+            Ring ring;
+            Item t;
+            for (int i = 0; item_at(a, deal, count, i, t); ++i) {
+                const int d0 = t.dt * a.n + p.rank * (a.n / 2), half_blocks = a.tiles * 4;
+                for (int k = t.k0; k < t.k0 + t.steps; ++k) {
+                    wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * (16384 + boxes * 8192));
+                    const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
+                    if (t.is_dw) {
+                        // 64 rows x 128 words: half of each of two blocks
+                        const int64_t block = (int64_t)(k / 2) * half_blocks + t.rt * 4 + p.rank * 2;
+                        const int y = (int)(block * 128 + (k & 1) * 64);
+                        tma_load2_pair(p.a(ring.stage), &a.dz, full, 0, y);
+                        tma_load2_pair(p.a(ring.stage) + 8192, &a.dz, full, 0, y + 128);
+                        for (int b = 0; b < boxes; ++b) tma_load2_pair(p.b(ring.stage) + b * 8192, &a.x, full, d0 + 64 * b, k * kStep);
+                    } else {
+                        // 128 rows x 64 words: a whole block
+                        const int y = (int)(((int64_t)(t.rt * 2 + p.rank) * half_blocks + k) * 128);
+                        tma_load2_pair(p.a(ring.stage), &a.dz, full, 0, y);
+                        tma_load2_pair(p.a(ring.stage) + 8192, &a.dz, full, 0, y + 64);
+                        for (int b = 0; b < boxes; ++b)
+                            tma_load2_pair(p.b(ring.stage) + b * 8192, &a.w, full, d0 + 64 * b, a.tile0 * kTile + k * kStep);
+                    }
+                    ring.next<kProductStages>();
+                }
+            }
+            ring_drain(p, ring);
+        }
+    } else if (warp == 1) {
+        if (p.rank == 0 && elect_one()) {
+            Ring ring;
+            Item t;
+            for (int i = 0; item_at(a, deal, count, i, t); ++i) {
+                if (t.is_dw)
+                    tile_products(p, ring, i, t.steps, mma_desc_pair(a.n, true, true), [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); },
+                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
+                else
+                    tile_products(p, ring, i, t.steps, mma_desc_pair(a.n, false, true), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
+            }
+        }
+    } else {
+        const int quad = warp & 3, half = (warp - 2) / 4;
+        const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
+        Item t;
+        for (int i = 0; item_at(a, deal, count, i, t); ++i) {
+            const int row = t.rt * kTile + p.rank * 128 + 32 * quad + lane;
+            wait_warp(p.acc_full + 8 * (i & 1), (i >> 1) & 1, p.dead, kWaitAccFull);
+            tc_fence_after();
+            const bool dead = *p.dead != 0;
+            const int64_t word = (int64_t)a.tile0 * kTile + row;
+            const bool writes = t.is_dw ? word < a.vocab : row < count;
+            uint16_t* dw = a.dw + word * a.dw_step;
+            float* dx = a.dx + ((size_t)t.split * a.padded + row) * a.dim;
+            for (int c = half; c < a.n / 32; c += 2) {
+                uint32_t v[32];
+                tmem_ld32(v, lanes + (i & 1) * kAccColumns + 32 * c);
+                tmem_wait_ld();
+                tmem_use(v);
+                const int d0 = t.dt * a.n + 32 * c;
+                if (dead) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!writes || d0 + 8 * j >= a.dim) break;
+                    if (t.is_dw) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) o[h] = pack_bf16(__uint_as_float(v[8 * j + 2 * h]), __uint_as_float(v[8 * j + 2 * h + 1]));
+                        *reinterpret_cast<uint4*>(dw + d0 + 8 * j) = make_uint4(o[0], o[1], o[2], o[3]);
+                    } else {
+                        float4* to = reinterpret_cast<float4*>(dx + d0 + 8 * j);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float4 o = make_float4(__uint_as_float(v[8 * j + 4 * h]), __uint_as_float(v[8 * j + 4 * h + 1]),
+                                                   __uint_as_float(v[8 * j + 4 * h + 2]), __uint_as_float(v[8 * j + 4 * h + 3]));
+                            if (a.add) {
+                                const float4 s = to[h];
+                                o.x += s.x;
+                                o.y += s.y;
+                                o.z += s.z;
+                                o.w += s.w;
+                            }
+                            to[h] = o;
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            tile_taken(p, i, lane);
+        }
+    }
+    pair_end(p);
+}
+
+// dx of every row: the splits' sums, rounded; zeros for the rows that take no part.
+__global__ void __launch_bounds__(256) dx_kernel(const float* sums, const int* slot, int rows, int dim, int splits, int64_t split_elems, uint16_t* dx,
+                                                 int64_t dx_step) {
+    grid_dependency_sync();
+    const int per_row = dim / 8;
+    const int64_t all = (int64_t)rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int row = (int)(i / per_row), d = 8 * (int)(i - (int64_t)row * per_row), s = slot[row];
+        float v[8] = {};
+        if (s >= 0) {
+            const float* from = sums + (int64_t)s * dim + d;
+            for (int k = 0; k < splits; ++k, from += split_elems) {
+                const float4 lo = reinterpret_cast<const float4*>(from)[0], hi = reinterpret_cast<const float4*>(from)[1];
+                const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += add[j];
+            }
+        }
+        *reinterpret_cast<uint4*>(dx + row * dx_step + d) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+// Sizes and places in the workspace.
+struct Plan {
+    int padded, count_blocks, tiles, labels;
+    int piece, pieces, splits, split_steps, n, dim_tiles;
+    uint64_t block_count, place, count, slot, row, xc, target, index, weight, entropy, first, stats, label_z, lse2, coef, dz, dx, bytes;
+};
+
+Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
+    Plan p;
+    std::memset(&p, 0, sizeof p);
+    p.padded = (int)((d.rows + kTile - 1) / kTile * kTile);
+    p.count_blocks = p.padded / kCountRows;
+    p.tiles = (int)((d.vocab + kTile - 1) / kTile);
+    p.labels = d.top ? (int)d.top : 1;
+    p.dim_tiles = (int)((d.dim + 255) / 256);
+    p.n = (int)((d.dim + p.dim_tiles * 32 - 1) / (p.dim_tiles * 32) * 32);
+    // pieces of the vocabulary: dz of one in kPieceBytes, or in kLeastPiece tiles' worth where the rows are many; all alike
+    const uint64_t tile_bytes = (uint64_t)p.padded * kTile * 2;
+    uint64_t piece = tile_bytes ? kPieceBytes / tile_bytes : p.tiles;
+    if (piece < kLeastPiece) piece = kLeastPiece;
+    if (piece > (uint64_t)p.tiles) piece = p.tiles;
+    p.pieces = (int)((p.tiles + piece - 1) / piece);
+    p.piece = (p.tiles + p.pieces - 1) / p.pieces;
+    p.pieces = (p.tiles + p.piece - 1) / p.piece;
+    // dx's inner axis is split while one of its tiles would take longer than its share of the launch
+    const int64_t row_tiles = p.padded / kTile, dx_steps = 4ll * p.piece;
+    const int64_t all = row_tiles * p.dim_tiles * dx_steps + (int64_t)p.piece * p.dim_tiles * (p.padded / kStep);
+    const int64_t share = all / kPairs > 8 ? all / kPairs : 8;
+    int64_t splits = (dx_steps + share - 1) / share;
+    if (splits > kMaxSplits) splits = kMaxSplits;
+    p.split_steps = (int)((dx_steps + splits - 1) / splits);
+    p.splits = (int)((dx_steps + p.split_steps - 1) / p.split_steps);
+
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t start = at;
+        at += (bytes + 255) / 256 * 256;
+        return start;
+    };
+    const uint64_t padded = (uint64_t)p.padded;
+    p.block_count = take(4ull * p.count_blocks);
+    p.place = take(4 * padded);
+    p.count = take(4);
+    p.slot = take(4ull * d.rows);
+    p.row = take(4 * padded);
+    p.xc = take(2 * padded * d.dim);
+    if (d.top) {
+        p.index = take(4 * padded * d.top);
+        p.weight = take(4 * padded * d.top);
+        p.entropy = take(4 * padded);
+        p.first = take(padded * (p.tiles + 1));
+    } else {
+        p.target = take(4 * padded);
+    }
+    if (backward) {
+        p.lse2 = take(4 * padded);
+        p.coef = take(4 * padded);
+        p.dz = take(tile_bytes * p.piece);
+        p.dx = take(4ull * p.splits * padded * d.dim);
+    } else {
+        p.stats = take(16 * padded * p.tiles);
+        p.label_z = take(4 * padded * p.labels);
+    }
+    p.bytes = at;
+    return p;
+}
+
+int check_desc(const alsgd_vocab_desc* d) {
+    if (!d) return ALSGD_E_ARG;
+    if (d->vocab == 0 || d->dim == 0 || d->dim % 8) return ALSGD_E_ARG;
+    if (d->index_dtype != ALSGD_I32 && d->index_dtype != ALSGD_I64) return ALSGD_E_ARG;
+    if (d->top && d->teacher_dtype != ALSGD_F32 && d->teacher_dtype != ALSGD_BF16) return ALSGD_E_ARG;
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale) || !std::isfinite(d->scale * kLog2e)) return ALSGD_E_ARG;
+    if (d->top > (uint32_t)kMaxTop || d->dim > 1u << 14) return ALSGD_E_UNSUPPORTED;
+    if (d->rows > 1u << 22 || d->vocab > 1u << 22) return ALSGD_E_RANGE;
+    if (d->device < 0 || d->device >= kMaxDevices) return ALSGD_E_RANGE;
+    return ALSGD_OK;
+}
+
+int check_matrix(const alsgd_matrix* m, uint32_t rows, uint32_t dim, bool output) {
+    if (!m) return ALSGD_E_ARG;
+    if (rows == 0) return ALSGD_OK;
+    if (!m->data || reinterpret_cast<uintptr_t>(m->data) % 16) return ALSGD_E_ARG;
+    if (rows == 1) return ALSGD_OK;
+    if (m->stride_row < 0 || m->stride_row % 8 || m->stride_row >= (1ll << 39)) return ALSGD_E_ARG;
+    if (output && m->stride_row < (int64_t)dim) return ALSGD_E_ARG;
+    return ALSGD_OK;
+}
+
+// Boxes of 64 columns x box_rows rows of a bf16 matrix, swizzled over their 128-byte rows, or as they are; zeros outside.
+int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t step_bytes, uint32_t box_rows, bool swizzle, CUtensorMap* out) {
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return ALSGD_E_CUDA;
+    const cuuint64_t size[2] = {cols, rows}, bytes[1] = {step_bytes};
+    const cuuint32_t box[2] = {64, box_rows}, unit[2] = {1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(data), size, bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ALSGD_OK : ALSGD_E_ARG;
+}
+
+struct Call {
+    const alsgd_vocab_desc* d;
+    const alsgd_matrix *x, *w;
+    const void *index, *teacher;
+    void* work;
+    uint64_t work_bytes;
+    cudaStream_t stream;
+};
+
+uint64_t step_of(const alsgd_matrix& m, uint32_t rows, uint32_t dim) {
+    return rows == 1 || m.stride_row == 0 ? (uint64_t)dim : (uint64_t)m.stride_row;
+}
+
+int check_call(const Call& c, bool teacher) {
+    const int rc = check_desc(c.d);
+    if (rc != ALSGD_OK) return rc;
+    const alsgd_vocab_desc& d = *c.d;
+    if ((d.top != 0) != teacher) return ALSGD_E_ARG;
+    int e;
+    if ((e = check_matrix(c.x, d.rows, d.dim, false)) != ALSGD_OK) return e;
+    if ((e = check_matrix(c.w, d.vocab, d.dim, false)) != ALSGD_OK) return e;
+    if (d.vocab > 1 && c.w->stride_row < (int64_t)d.dim) return ALSGD_E_ARG;
+    if (d.rows) {
+        if (!c.index || reinterpret_cast<uintptr_t>(c.index) % (d.index_dtype == ALSGD_I64 ? 8 : 4)) return ALSGD_E_ARG;
+        if (teacher && (!c.teacher || reinterpret_cast<uintptr_t>(c.teacher) % (d.teacher_dtype == ALSGD_BF16 ? 2 : 4))) return ALSGD_E_ARG;
+        if (!c.work || reinterpret_cast<uintptr_t>(c.work) % 256) return ALSGD_E_ARG;
+    }
+    return ALSGD_OK;
+}
+
+template <typename T>
+T* at(const Call& c, uint64_t offset) {
+    return reinterpret_cast<T*>(static_cast<uint8_t*>(c.work) + offset);
+}
+
+// Rows that take part, their copies and labels.
+int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dloss, int64_t dloss_step) {
+    const alsgd_vocab_desc& d = *c.d;
+    GatherArgs g;
+    std::memset(&g, 0, sizeof g);
+    g.l = {c.index, c.teacher, d.index_dtype == ALSGD_I64, d.teacher_dtype == ALSGD_BF16, (int)d.rows, (int)d.top, (int)d.vocab};
+    g.x = static_cast<const uint16_t*>(c.x->data);
+    g.x_step = d.rows == 1 ? 0 : c.x->stride_row;
+    g.lse = lse;
+    g.dloss = dloss;
+    g.dloss_step = dloss_step;
+    g.scale = d.scale;
+    g.padded = p.padded;
+    g.blocks = p.count_blocks;
+    g.dim = (int)d.dim;
+    g.tiles = p.tiles;
+    g.block_count = at<int>(c, p.block_count);
+    g.place = at<int>(c, p.place);
+    g.count = at<int>(c, p.count);
+    g.slot = at<int>(c, p.slot);
+    g.row = at<int>(c, p.row);
+    g.xc = at<uint16_t>(c, p.xc);
+    if (d.top) {
+        g.index = at<int>(c, p.index);
+        g.weight = at<float>(c, p.weight);
+        g.entropy = at<float>(c, p.entropy);
+        g.first = at<uint8_t>(c, p.first);
+    } else {
+        g.target = at<int>(c, p.target);
+    }
+    if (lse) {
+        g.lse2 = at<float>(c, p.lse2);
+        g.coef = at<float>(c, p.coef);
+    }
+    if (launch_dependent(count_kernel, dim3(p.count_blocks), dim3(kCountRows), 0, c.stream, g.l, p.padded, at<int>(c, p.block_count), at<int>(c, p.place)) !=
+        cudaSuccess)
+        return ALSGD_E_CUDA;
+    return launch_dependent(gather_kernel, dim3(p.padded / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}
+
+int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
+    const alsgd_vocab_desc& d = *c.d;
+    std::memset(a, 0, sizeof *a);
+    int rc;
+    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 128, true, &a->x)) != ALSGD_OK) return rc;
+    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, true, &a->w)) != ALSGD_OK) return rc;
+    a->count = at<int>(c, p.count);
+    a->dim = (int)d.dim;
+    a->vocab = (int)d.vocab;
+    a->top = (int)d.top;
+    a->all_tiles = p.tiles;
+    a->scale2 = d.scale * kLog2e;
+    a->padded = p.padded;
+    if (d.top) {
+        a->index = at<int>(c, p.index);
+        a->weight = at<float>(c, p.weight);
+        a->first = at<uint8_t>(c, p.first);
+    } else {
+        a->target = at<int>(c, p.target);
+    }
+    return ALSGD_OK;
+}
+
+int grid_of(int64_t tiles) { return 2 * (int)(tiles < kPairs ? tiles : kPairs); }
+
+template <bool BACKWARD, bool TOP>
+int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
+    static SmemLimit limit;
+    constexpr size_t smem = sizeof(LogitSmem) + 1024;
+    if (!limit.raise(logit_kernel<BACKWARD, TOP>, device, smem)) return ALSGD_E_CUDA;
+    const int64_t tiles = (int64_t)(a.padded / kTile) * a.tiles;
+    return launch_dependent(logit_kernel<BACKWARD, TOP>, dim3(grid_of(tiles)), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}
+
+int forward(const Call& c, bool teacher, float* loss, float* lse) {
+    int rc = check_call(c, teacher);
+    if (rc != ALSGD_OK) return rc;
+    const alsgd_vocab_desc& d = *c.d;
+    if (d.rows == 0) return ALSGD_OK;
+    if (!loss || !lse || reinterpret_cast<uintptr_t>(loss) % 4 || reinterpret_cast<uintptr_t>(lse) % 4) return ALSGD_E_ARG;
+    const Plan p = make_plan(d, false);
+    if (c.work_bytes < p.bytes) return ALSGD_E_NOMEM;
+    UseDevice use(d.device);
+    if (!use.ok) return ALSGD_E_CUDA;
+    LogitArgs a;
+    if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
+    if ((rc = gather_rows(c, p, nullptr, nullptr, 0)) != ALSGD_OK) return rc;
+    a.tiles = p.tiles;
+    a.stats = at<float2>(c, p.stats);
+    a.label_z = at<float>(c, p.label_z);
+    if ((rc = d.top ? launch_logits<false, true>(a, d.device, c.stream) : launch_logits<false, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
+    LossArgs l;
+    std::memset(&l, 0, sizeof l);
+    l.stats = a.stats;
+    l.label_z = a.label_z;
+    if (d.top) {
+        l.weight = a.weight;
+        l.entropy = at<float>(c, p.entropy);
+        l.index = a.index;
+    }
+    l.slot = at<int>(c, p.slot);
+    l.count = a.count;
+    l.rows = (int)d.rows;
+    l.padded = p.padded;
+    l.parts = 2 * p.tiles;
+    l.top = (int)d.top;
+    l.scale = d.scale;
+    l.scale2 = a.scale2;
+    l.loss = loss;
+    l.lse = lse;
+    const int* row_of = at<int>(c, p.row);
+    return launch_dependent(loss_kernel, dim3(p.padded / kLossRows), dim3(kLossRows * kLossParts), 0, c.stream, l, row_of) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}
+
+int backward(const Call& c, bool teacher, const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw) {
+    int rc = check_call(c, teacher);
+    if (rc != ALSGD_OK) return rc;
+    const alsgd_vocab_desc& d = *c.d;
+    if ((rc = check_matrix(dx, d.rows, d.dim, true)) != ALSGD_OK || (rc = check_matrix(dw, d.vocab, d.dim, true)) != ALSGD_OK) return rc;
+    if (d.rows && (!lse || !dloss || reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(dloss) % 4 || dloss_step < 0)) return ALSGD_E_ARG;
+    const Plan p = make_plan(d, true);
+    if (d.rows && c.work_bytes < p.bytes) return ALSGD_E_NOMEM;
+    UseDevice use(d.device);
+    if (!use.ok) return ALSGD_E_CUDA;
+    const uint64_t dw_step = step_of(*dw, d.vocab, d.dim);
+    if (d.rows == 0)
+        return cudaMemset2DAsync(dw->data, 2 * dw_step, 0, 2ull * d.dim, d.vocab, c.stream) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    LogitArgs a;
+    ProductArgs m;
+    std::memset(&m, 0, sizeof m);
+    if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
+    a.lse2 = at<float>(c, p.lse2);
+    a.coef = at<float>(c, p.coef);
+    a.dz = at<uint8_t>(c, p.dz);
+    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, true, &m.x)) != ALSGD_OK) return rc;
+    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, true, &m.w)) != ALSGD_OK) return rc;
+    if ((rc = make_map(a.dz, (uint64_t)p.padded * p.piece * 4, 64, 128, 64, false, &m.dz)) != ALSGD_OK) return rc;
+    m.count = a.count;
+    m.dim = (int)d.dim;
+    m.vocab = (int)d.vocab;
+    m.n = p.n;
+    m.dim_tiles = p.dim_tiles;
+    m.padded = p.padded;
+    m.dx = at<float>(c, p.dx);
+    m.dw = static_cast<uint16_t*>(dw->data);
+    m.dw_step = (int64_t)dw_step;
+    if ((rc = gather_rows(c, p, lse, dloss, dloss_step)) != ALSGD_OK) return rc;
+    static SmemLimit limit;
+    constexpr size_t smem = sizeof(ProductSmem) + 1024;
+    if (!limit.raise(product_kernel, d.device, smem)) return ALSGD_E_CUDA;
+    for (int i = 0; i < p.pieces; ++i) {
+        a.tile0 = m.tile0 = i * p.piece;
+        a.tiles = m.tiles = p.tiles - a.tile0 < p.piece ? p.tiles - a.tile0 : p.piece;
+        // the first piece writes all of dx's sums; a shorter last one adds to as many as it has steps for
+        m.split_steps = p.split_steps;
+        m.splits = (4 * m.tiles + p.split_steps - 1) / p.split_steps;
+        m.add = i > 0;
+        if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
+        const int64_t items = (int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles;
+        if (launch_dependent(product_kernel, dim3(grid_of(items)), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
+    }
+    const int64_t groups = (int64_t)d.rows * (d.dim / 8), blocks = (groups + 255) / 256;
+    return launch_dependent(dx_kernel, dim3((unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs)), dim3(256), 0, c.stream, (const float*)m.dx,
+                            (const int*)at<int>(c, p.slot), (int)d.rows, (int)d.dim, p.splits, (int64_t)p.padded * d.dim, static_cast<uint16_t*>(dx->data),
+                            (int64_t)step_of(*dx, d.rows, d.dim)) == cudaSuccess
+               ? ALSGD_OK
+               : ALSGD_E_CUDA;
+}
+
+}  // namespace
+
+extern "C" int alsgd_vocab_bytes(const alsgd_vocab_desc* desc, int backward_pass, uint64_t* bytes_out) {
+    if (!bytes_out) return ALSGD_E_ARG;
+    const int rc = check_desc(desc);
+    if (rc != ALSGD_OK) return rc;
+    *bytes_out = desc->rows ? make_plan(*desc, backward_pass != 0).bytes : 0;
+    return ALSGD_OK;
+}
+
+extern "C" int alsgd_xent_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, float* loss, float* lse,
+                              void* work, uint64_t work_bytes, void* stream) {
+    return forward({desc, x, w, target, nullptr, work, work_bytes, static_cast<cudaStream_t>(stream)}, false, loss, lse);
+}
+
+extern "C" int alsgd_xent_bwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, const float* lse,
+                              const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw, void* work, uint64_t work_bytes,
+                              void* stream) {
+    return backward({desc, x, w, target, nullptr, work, work_bytes, static_cast<cudaStream_t>(stream)}, false, lse, dloss, dloss_step, dx, dw);
+}
+
+extern "C" int alsgd_distill_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* index, const void* teacher,
+                                 float* loss, float* lse, void* work, uint64_t work_bytes, void* stream) {
+    return forward({desc, x, w, index, teacher, work, work_bytes, static_cast<cudaStream_t>(stream)}, true, loss, lse);
+}
+
+extern "C" int alsgd_distill_bwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* index, const void* teacher,
+                                 const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw, void* work,
+                                 uint64_t work_bytes, void* stream) {
+    return backward({desc, x, w, index, teacher, work, work_bytes, static_cast<cudaStream_t>(stream)}, true, lse, dloss, dloss_step, dx, dw);
+}
+
+extern "C" int alsgd_vocab_status(int32_t device, uint32_t* waits_out) {
+    if (!waits_out) return ALSGD_E_ARG;
+    if (device < 0 || device >= kMaxDevices) return ALSGD_E_RANGE;
+    UseDevice use(device);
+    if (!use.ok) return ALSGD_E_CUDA;
+    unsigned word = 0;
+    // the copy alone would wait for the default stream, but not for streams that are independent of it
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&word, g_wait_error, sizeof word) != cudaSuccess) return ALSGD_E_CUDA;
+    *waits_out = word;
+    return ALSGD_OK;
+}

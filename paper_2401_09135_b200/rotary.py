@@ -1,0 +1,42 @@
+"""alsgd_rope as one differentiable function of torch tensors.
+
+The call itself is binding.Rotary's; the backward pass is the same call the other way round.
+"""
+from __future__ import annotations
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import binding as B
+
+
+def _laid_out(t):
+    """A gradient that arrives broadcast, transposed, or as a part of something larger that starts anywhere."""
+    unit = 16 // t.element_size()
+    if t.stride(3) != 1 or any(s % unit for s in t.stride()[:3]) or t.data_ptr() % 16:
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+class _Rotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, q, k, positions):
+        q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        plan.alsgd_rope(q, k, q_out, k_out, positions=positions)
+        ctx.plan = plan
+        ctx.save_for_backward(positions)
+        return q_out, k_out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        positions, = ctx.saved_tensors
+        dq, dk = _laid_out(dq), _laid_out(dk)
+        dq_in, dk_in = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (dq, dk))
+        ctx.plan.alsgd_rope(dq, dk, dq_in, dk_in, positions=positions, inverse=True)
+        return None, dq_in, dk_in, None
+
+
+def rotate(plan: B.Rotary, q, k, positions=None):
+    """q and k [batch, position, head, dim] at their positions, with gradients; second derivatives raise."""
+    return _Rotate.apply(plan, q, k, positions)
