@@ -57,38 +57,37 @@ __device__ __forceinline__ float teacher_at(const Labels& l, size_t i) {
 constexpr int kCountRows = 256;        // rows of a counting block
 
 // Which rows take part: their number in each block of rows, and each row's place among its block's (-1 - place among those
-// that do not).
-__global__ void __launch_bounds__(kCountRows) count_kernel(Labels l, int padded, int* block_count, int* place) {
+// that do not).  A teacher's entries are read in a row by as many threads as a block may have.
+__global__ void __launch_bounds__(1024) count_kernel(Labels l, int* block_count, int* place) {
     __shared__ int warp_count[kCountRows / 32];
+    __shared__ uint8_t any[kCountRows];
     grid_dependency_sync();
     const int r0 = blockIdx.x * kCountRows, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     bool mine = false;
-    if (!l.teacher) {
+    if (l.teacher) {
+        if (threadIdx.x < kCountRows) any[threadIdx.x] = 0;
+        __syncthreads();
+        const int n = max(0, min(kCountRows, l.rows - r0)) * l.top;
+        const size_t from = (size_t)r0 * l.top;
+#pragma unroll 8
+        for (int i = threadIdx.x; i < n; i += 1024)
+            if (label_at(l, from + i) >= 0 && teacher_at(l, from + i) != -INFINITY) any[i / l.top] = 1;
+        __syncthreads();
+        if (threadIdx.x >= kCountRows) return;
+        mine = any[threadIdx.x];
+    } else {
         const int r = r0 + threadIdx.x;
         mine = r < l.rows && label_at(l, r) >= 0;
-    } else {
-        // a warp looks at its 32 rows one by one
-        for (int i = 0; i < 32; ++i) {
-            const int r = r0 + 32 * warp + i;
-            bool any = false;
-            if (r < l.rows)
-                for (int k = lane; k < l.top; k += 32) {
-                    const size_t at = (size_t)r * l.top + k;
-                    any |= label_at(l, at) >= 0 && teacher_at(l, at) != -INFINITY;
-                }
-            any = __any_sync(~0u, any);
-            if (lane == i) mine = any;
-        }
     }
     const uint32_t votes = __ballot_sync(~0u, mine);
     if (lane == 0) warp_count[warp] = __popc(votes);
-    __syncthreads();
+    asm volatile("bar.sync 1, %0;" ::"n"(kCountRows) : "memory");
     int before = __popc(votes & ((1u << lane) - 1)), total = 0;
     for (int w = 0; w < kCountRows / 32; ++w) {
         if (w < warp) before += warp_count[w];
         total += warp_count[w];
     }
-    if (r0 + (int)threadIdx.x < padded) place[r0 + threadIdx.x] = mine ? before : -1 - ((int)threadIdx.x - before);
+    place[r0 + threadIdx.x] = mine ? before : -1 - ((int)threadIdx.x - before);
     if (threadIdx.x == 0) block_count[blockIdx.x] = total;
 }
 
@@ -100,6 +99,9 @@ struct GatherArgs {
     int64_t dloss_step;
     float scale;
     int padded, blocks, dim, tiles;    // rows in whole tiles; counting blocks; tiles of the vocabulary
+    int direct;                        // where all rows take part, the products read x itself
+    uint16_t* dx;                      // backward only: zeros for the rows that take no part
+    int64_t dx_step;
     const int *block_count, *place;
     int* count;                        // one: rows that take part
     int* slot;                         // [rows]: place among them, or -1
@@ -109,7 +111,7 @@ struct GatherArgs {
     int* index;                        // [padded][top] ascending, then places that take no part; teacher only
     float* weight;                     // [padded][top]
     float* entropy;                    // [padded]: sum t log t
-    uint8_t* first;                    // [padded][tiles + 1]: entries below each tile's first word
+    uint8_t* first;                    // [padded][2 * tiles + 1]: entries below the first word of each half of a tile
     float *lse2, *coef;                // [padded]; backward only
 };
 
@@ -145,13 +147,19 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
     const bool used = place >= 0;
     // rows that do not take part fill the places behind; of those only the last tile's are looked at
     const int slot = used ? before + place : count + (block * kCountRows - before) + (-1 - place);
-    if (lane == 0 && r < a.l.rows) a.slot[r] = used ? slot : -1;
+    if (r < a.l.rows) {
+        if (lane == 0) a.slot[r] = used ? slot : -1;
+        if (!used && a.dx)
+            for (int c = 8 * lane; c < a.dim; c += 256) *reinterpret_cast<uint4*>(a.dx + r * a.dx_step + c) = make_uint4(0, 0, 0, 0);
+    }
     if (slot >= (count + kTile - 1) / kTile * kTile) return;
 
-    uint16_t* to = a.xc + (size_t)slot * a.dim;
-    const uint16_t* from = a.x + r * a.x_step;
-    for (int c = 8 * lane; c < a.dim; c += 256)
-        *reinterpret_cast<uint4*>(to + c) = used ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0, 0, 0, 0);
+    if (!(a.direct && count == a.l.rows)) {
+        uint16_t* to = a.xc + (size_t)slot * a.dim;
+        const uint16_t* from = a.x + r * a.x_step;
+        for (int c = 8 * lane; c < a.dim; c += 256)
+            *reinterpret_cast<uint4*>(to + c) = used ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0, 0, 0, 0);
+    }
     if (lane == 0) {
         a.row[slot] = r;
         if (a.lse) {
@@ -163,9 +171,9 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
     if (a.target) return;
 
     // the teacher's softmax over the entries that take part, then the entries in ascending order of their words
-    uint8_t* first = a.first + (size_t)slot * (a.tiles + 1);
+    uint8_t* first = a.first + (size_t)slot * (2 * a.tiles + 1);
     if (!used) {
-        for (int t = lane; t <= a.tiles; t += 32) first[t] = 0;
+        for (int t = lane; t <= 2 * a.tiles; t += 32) first[t] = 0;
         return;
     }
     constexpr int E = kMaxTop / 32;
@@ -214,8 +222,8 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
     for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
     if (lane == 0) a.entropy[slot] = entropy;
     __syncwarp();
-    for (int t = lane; t <= a.tiles; t += 32) {
-        const int word = min(t * kTile, a.l.vocab);            // places that take no part are behind every word
+    for (int t = lane; t <= 2 * a.tiles; t += 32) {
+        const int word = min(t * (kTile / 2), a.l.vocab);            // places that take no part are behind every word
         int low = 0, high = a.l.top;
         while (low < high) {
             const int mid = (low + high) / 2;
@@ -353,8 +361,9 @@ __device__ __forceinline__ void tile_taken(const Pair<STAGES>& p, int tile, int 
 // ---------------------------------------------------------------------------------------------- logits
 
 struct LogitArgs {
-    CUtensorMap x, w;                  // gathered rows, words: boxes of 64 x 128
+    CUtensorMap x, x_all, w;           // gathered rows, the rows as they are, words: boxes of 64 x 128
     const int* count;
+    int all_rows;                      // with as many rows that take part, x_all is read; -1: never
     int dim, vocab, top;
     int tile0, tiles, all_tiles;       // of the vocabulary: this launch's, all of them
     float scale2;                      // scale * log2 e
@@ -394,6 +403,45 @@ __device__ __forceinline__ float pick(const uint32_t (&z)[32], int at) {
     return v;
 }
 
+// Takes `t` off one of them.
+__device__ __forceinline__ void take_off(uint32_t (&z)[32], int at, float t) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) - (i == at ? t : 0.0f));
+}
+
+// A row's labels within some words, in ascending order, four of them on the way: a list read one by one costs its warp the
+// memory's latency at every label (169 to 222 us against 155 for single labels, 5461 rows x 8192 words x 768).
+struct LabelQueue {
+    static constexpr int kAhead = 4;
+    const int* indices;
+    const float* weights;
+    int at, end;
+    int index[kAhead];                 // INT_MAX behind the last
+    float weight[kAhead];
+    __device__ __forceinline__ void load(int i) {
+        const bool is = at + i < end;
+        index[i] = is ? indices[at + i] : INT_MAX;
+        if (weights) weight[i] = is ? weights[at + i] : 0.0f;
+    }
+    __device__ __forceinline__ void start(const int* all_indices, const float* all_weights, int first, int last) {
+        indices = all_indices;
+        weights = all_weights;
+        at = first;
+        end = last;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(i);
+    }
+    __device__ __forceinline__ void next() {
+        ++at;
+#pragma unroll
+        for (int i = 0; i + 1 < kAhead; ++i) {
+            index[i] = index[i + 1];
+            weight[i] = weight[i + 1];
+        }
+        load(kAhead - 1);
+    }
+};
+
 template <bool BACKWARD, bool TOP>
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_kernel(const __grid_constant__ LogitArgs a) {
     extern __shared__ uint8_t raw[];
@@ -410,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
 
     if (warp == 0) {
         if (elect_one()) {
+            const CUtensorMap* x = count == a.all_rows ? &a.x_all : &a.x;
             Ring ring;
             for (int i = first; i < tiles; i += pairs) {
                 int rt, ct;
@@ -419,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                     wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
                     if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * kStageBytes);
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
-                    tma_load2_pair(p.a(ring.stage), &a.x, full, k * kStep, row);
+                    tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
                     tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
                     ring.next<kLogitStages>();
                 }
@@ -445,19 +494,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             tile_at(i, row_tiles, a.tiles, rt, ct);
             const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
             const int c0 = (a.tile0 + ct) * kTile + half * 128;    // first word
-            int label = -1, e = 0, e_end = 0;
-            float weight = 1.0f;
+            int label = -1;
+            LabelQueue queue;
             const size_t list = (size_t)row * a.top;
             if (TOP) {
-                const uint8_t* f = a.first + (size_t)row * (a.all_tiles + 1) + a.tile0 + ct;
-                e = f[0];
-                e_end = f[1];
-                // the other half's entries are its own
-                while (e < e_end && a.index[list + e] < c0) ++e;
-                if (e < e_end) {
-                    label = a.index[list + e];
-                    weight = a.weight[list + e];
-                }
+                const uint8_t* f = a.first + (size_t)row * (2 * a.all_tiles + 1) + 2 * (a.tile0 + ct) + half;
+                queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, f[0], f[1]);
             } else {
                 label = a.target[row];
             }
@@ -485,9 +527,9 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                         for (int j = 0; j < 32; ++j) z[j] = w0 + j < a.vocab ? z[j] : 0xFF800000u;
                     }
                     if (TOP) {
-                        while (e < e_end && label < w0 + 32) {
-                            a.label_z[list + e] = pick(z, label - w0);
-                            if (++e < e_end) label = a.index[list + e];
+                        while (queue.index[0] < w0 + 32) {
+                            a.label_z[list + queue.at] = pick(z, queue.index[0] - w0);
+                            queue.next();
                         }
                     } else if ((uint32_t)(label - w0) < 32u) {
                         a.label_z[row] = pick(z, label - w0);
@@ -505,20 +547,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
 #pragma unroll
                     for (int j = 0; j < 32; ++j) z[j] = __float_as_uint(coef * exp2_fast(fmaf(__uint_as_float(z[j]), a.scale2, -lse2)));
                     if (TOP) {
-                        while (e < e_end && label < w0 + 32) {
-                            const float t = coef * weight;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j == label - w0) z[j] = __float_as_uint(__uint_as_float(z[j]) - t);
-                            if (++e < e_end) {
-                                label = a.index[list + e];
-                                weight = a.weight[list + e];
-                            }
+                        while (queue.index[0] < w0 + 32) {
+                            take_off(z, queue.index[0] - w0, coef * queue.weight[0]);
+                            queue.next();
                         }
                     } else if ((uint32_t)(label - w0) < 32u) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j == label - w0) z[j] = __float_as_uint(__uint_as_float(z[j]) - coef);
+                        take_off(z, label - w0, coef);
                     }
                     __syncwarp();
                     if (dead) z[0] = 0x7FC00000u;
@@ -571,9 +605,9 @@ struct LossArgs {
     float *loss, *lse;
 };
 
-constexpr int kLossRows = 32, kLossParts = 8;
+constexpr int kLossRows = 32, kLossParts = 16;
 
-// 32 rows in gathered order, eight threads for each.  The rows that take no part get zeros.
+// 32 rows in gathered order, sixteen threads for each.  The rows that take no part get zeros.
 __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a, const int* row_of) {
     __shared__ float s_top[kLossParts][kLossRows], s_sum[kLossParts][kLossRows], s_z[kLossParts][kLossRows], s_weight[kLossParts][kLossRows];
     grid_dependency_sync();
@@ -581,19 +615,29 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
     if (threadIdx.x < kLossRows && row < a.rows && a.slot[row] < 0) a.loss[row] = a.lse[row] = 0.0f;
     if (blockIdx.x * kLossRows >= count) return;
     float top = -INFINITY, sum = 0.0f;
-    for (int t = part; t < a.parts; t += kLossParts) {
-        const float2 s = a.stats[(size_t)t * a.padded + row];
-        const float m = fmaxf(top, s.x), ref = m == -INFINITY ? 0.0f : m * a.scale2;
-        sum = sum * exp2f(fmaf(top, a.scale2, -ref)) + s.y * exp2f(fmaf(s.x, a.scale2, -ref));
+    constexpr int N = 8;                                       // loads on the way
+    for (int t = part; t < a.parts; t += N * kLossParts) {
+        float2 s[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            s[i] = t + i * kLossParts < a.parts ? a.stats[(size_t)(t + i * kLossParts) * a.padded + row] : make_float2(-INFINITY, 0.0f);
+        float m = top;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, s[i].x);
+        const float ref = m == -INFINITY ? 0.0f : m * a.scale2;
+        sum *= exp2f(fmaf(top, a.scale2, -ref));
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += s[i].y * exp2f(fmaf(s[i].x, a.scale2, -ref));
         top = m;
     }
     float z = 0.0f, weight = 0.0f;                             // sum t z, sum t
     if (row < count)
+#pragma unroll 4
         for (int k = part; k < a.top; k += kLossParts) {
             const size_t at = (size_t)row * a.top + k;
-            if (a.index[at] == INT_MAX) break;
-            z = fmaf(a.weight[at], a.label_z[at], z);
-            weight += a.weight[at];
+            const float t = a.index[at] == INT_MAX ? 0.0f : a.weight[at], label = a.label_z[at];
+            z += t == 0.0f ? 0.0f : t * label;                 // nothing was written for the entries that take no part
+            weight += t;
         }
     s_top[part][i] = top;
     s_sum[part][i] = sum;
@@ -617,14 +661,18 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
 // ---------------------------------------------------------------------------------------------- dx += dz w, dw = dz^T x
 
 struct ProductArgs {
-    CUtensorMap dz, x, w;              // boxes of 64 x 64; dz's rows are those of its blocks
+    CUtensorMap dz, x, x_all, w;       // boxes of 64 x 64; dz's rows are those of its blocks; x as for the logits
     const int* count;
+    int all_rows;
     int dim, vocab;
     int tile0, tiles;                  // of the vocabulary: the piece
     int splits, split_steps;           // of dx's inner axis
     int n, dim_tiles;                  // columns of a tile, tiles of dim
-    int padded, add;                   // add: dx's sums so far are read
-    float* dx;                         // [splits][padded][dim]
+    int padded, add, last;             // add: dx's sums so far are read; last: dx is written in place of its sums
+    float* sums;                       // [splits][padded][dim]: dx so far
+    const int* row;                    // of a place
+    uint16_t* dx;
+    int64_t dx_step;
     uint16_t* dw;
     int64_t dw_step;
 };
@@ -725,6 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         }
     } else if (warp == 0) {
         if (elect_one()) {
+            const CUtensorMap* x = count == a.all_rows ? &a.x_all : &a.x;
             Ring ring;
             Item t;
             for (int i = 0; item_at(a, deal, count, i, t); ++i) {
@@ -739,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                         const int y = (int)(block * 128 + (k & 1) * 64);
                         tma_load2_pair(p.a(ring.stage), &a.dz, full, 0, y);
                         tma_load2_pair(p.a(ring.stage) + 8192, &a.dz, full, 0, y + 128);
-                        for (int b = 0; b < boxes; ++b) tma_load2_pair(p.b(ring.stage) + b * 8192, &a.x, full, d0 + 64 * b, k * kStep);
+                        for (int b = 0; b < boxes; ++b) tma_load2_pair(p.b(ring.stage) + b * 8192, x, full, d0 + 64 * b, k * kStep);
                     } else {
                         // 128 rows x 64 words: a whole block
                         const int y = (int)(((int64_t)(t.rt * 2 + p.rank) * half_blocks + k) * 128);
@@ -777,8 +826,9 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             const bool dead = *p.dead != 0;
             const int64_t word = (int64_t)a.tile0 * kTile + row;
             const bool writes = t.is_dw ? word < a.vocab : row < count;
-            uint16_t* dw = a.dw + word * a.dw_step;
-            float* dx = a.dx + ((size_t)t.split * a.padded + row) * a.dim;
+            uint16_t* out = t.is_dw ? a.dw + word * a.dw_step : a.dx;
+            if (!t.is_dw && a.last && writes) out += (int64_t)a.row[row] * a.dx_step;
+            float* sums = a.sums + ((size_t)t.split * a.padded + row) * a.dim;
             for (int c = half; c < a.n / 32; c += 2) {
                 uint32_t v[32];
                 tmem_ld32(v, lanes + (i & 1) * kAccColumns + 32 * c);
@@ -792,26 +842,20 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (!writes || d0 + 8 * j >= a.dim) break;
-                    if (t.is_dw) {
-                        uint32_t o[4];
+                    float o[8];
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) o[h] = pack_bf16(__uint_as_float(v[8 * j + 2 * h]), __uint_as_float(v[8 * j + 2 * h + 1]));
-                        *reinterpret_cast<uint4*>(dw + d0 + 8 * j) = make_uint4(o[0], o[1], o[2], o[3]);
+                    for (int h = 0; h < 8; ++h) o[h] = __uint_as_float(v[8 * j + h]);
+                    float4* at = reinterpret_cast<float4*>(sums + d0 + 8 * j);
+                    if (!t.is_dw && a.add) {
+                        const float4 lo = at[0], hi = at[1];
+                        o[0] += lo.x, o[1] += lo.y, o[2] += lo.z, o[3] += lo.w;
+                        o[4] += hi.x, o[5] += hi.y, o[6] += hi.z, o[7] += hi.w;
+                    }
+                    if (t.is_dw || a.last) {
+                        *reinterpret_cast<uint4*>(out + d0 + 8 * j) = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
                     } else {
-                        float4* to = reinterpret_cast<float4*>(dx + d0 + 8 * j);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float4 o = make_float4(__uint_as_float(v[8 * j + 4 * h]), __uint_as_float(v[8 * j + 4 * h + 1]),
-                                                   __uint_as_float(v[8 * j + 4 * h + 2]), __uint_as_float(v[8 * j + 4 * h + 3]));
-                            if (a.add) {
-                                const float4 s = to[h];
-                                o.x += s.x;
-                                o.y += s.y;
-                                o.z += s.z;
-                                o.w += s.w;
-                            }
-                            to[h] = o;
-                        }
+                        at[0] = make_float4(o[0], o[1], o[2], o[3]);
+                        at[1] = make_float4(o[4], o[5], o[6], o[7]);
                     }
                 }
                 __syncwarp();
@@ -822,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     pair_end(p);
 }
 
-// dx of every row: the splits' sums, rounded; zeros for the rows that take no part.
+// dx from several parts: their sums, rounded.
 __global__ void __launch_bounds__(256) dx_kernel(const float* sums, const int* slot, int rows, int dim, int splits, int64_t split_elems, uint16_t* dx,
                                                  int64_t dx_step) {
     grid_dependency_sync();
@@ -830,15 +874,15 @@ __global__ void __launch_bounds__(256) dx_kernel(const float* sums, const int* s
     const int64_t all = (int64_t)rows * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int row = (int)(i / per_row), d = 8 * (int)(i - (int64_t)row * per_row), s = slot[row];
+        if (s < 0) continue;
         float v[8] = {};
-        if (s >= 0) {
-            const float* from = sums + (int64_t)s * dim + d;
-            for (int k = 0; k < splits; ++k, from += split_elems) {
-                const float4 lo = reinterpret_cast<const float4*>(from)[0], hi = reinterpret_cast<const float4*>(from)[1];
-                const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        const float* from = sums + (int64_t)s * dim + d;
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k, from += split_elems) {
+            const float4 lo = reinterpret_cast<const float4*>(from)[0], hi = reinterpret_cast<const float4*>(from)[1];
+            const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += add[j];
-            }
+            for (int j = 0; j < 8; ++j) v[j] += add[j];
         }
         *reinterpret_cast<uint4*>(dx + row * dx_step + d) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
@@ -896,7 +940,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.index = take(4 * padded * d.top);
         p.weight = take(4 * padded * d.top);
         p.entropy = take(4 * padded);
-        p.first = take(padded * (p.tiles + 1));
+        p.first = take(padded * (2 * p.tiles + 1));
     } else {
         p.target = take(4 * padded);
     }
@@ -956,6 +1000,9 @@ struct Call {
     cudaStream_t stream;
 };
 
+// x as it is can be an operand of the products, unless its rows overlap.
+bool direct_x(const Call& c) { return c.d->rows == 1 || c.x->stride_row >= (int64_t)c.d->dim; }
+
 uint64_t step_of(const alsgd_matrix& m, uint32_t rows, uint32_t dim) {
     return rows == 1 || m.stride_row == 0 ? (uint64_t)dim : (uint64_t)m.stride_row;
 }
@@ -983,7 +1030,7 @@ T* at(const Call& c, uint64_t offset) {
 }
 
 // Rows that take part, their copies and labels.
-int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dloss, int64_t dloss_step) {
+int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx) {
     const alsgd_vocab_desc& d = *c.d;
     GatherArgs g;
     std::memset(&g, 0, sizeof g);
@@ -994,6 +1041,11 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
     g.dloss = dloss;
     g.dloss_step = dloss_step;
     g.scale = d.scale;
+    g.direct = direct_x(c);
+    if (dx) {
+        g.dx = static_cast<uint16_t*>(dx->data);
+        g.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
+    }
     g.padded = p.padded;
     g.blocks = p.count_blocks;
     g.dim = (int)d.dim;
@@ -1016,8 +1068,8 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
         g.lse2 = at<float>(c, p.lse2);
         g.coef = at<float>(c, p.coef);
     }
-    if (launch_dependent(count_kernel, dim3(p.count_blocks), dim3(kCountRows), 0, c.stream, g.l, p.padded, at<int>(c, p.block_count), at<int>(c, p.place)) !=
-        cudaSuccess)
+    if (launch_dependent(count_kernel, dim3(p.count_blocks), dim3(d.top ? 1024 : kCountRows), 0, c.stream, g.l, at<int>(c, p.block_count),
+                         at<int>(c, p.place)) != cudaSuccess)
         return ALSGD_E_CUDA;
     return launch_dependent(gather_kernel, dim3(p.padded / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
@@ -1028,6 +1080,8 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
     int rc;
     if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 128, true, &a->x)) != ALSGD_OK) return rc;
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, true, &a->w)) != ALSGD_OK) return rc;
+    a->all_rows = direct_x(c) ? (int)d.rows : -1;
+    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 128, true, &a->x_all)) != ALSGD_OK) return rc;
     a->count = at<int>(c, p.count);
     a->dim = (int)d.dim;
     a->vocab = (int)d.vocab;
@@ -1068,7 +1122,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     if (!use.ok) return ALSGD_E_CUDA;
     LogitArgs a;
     if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
-    if ((rc = gather_rows(c, p, nullptr, nullptr, 0)) != ALSGD_OK) return rc;
+    if ((rc = gather_rows(c, p, nullptr, nullptr, 0, nullptr)) != ALSGD_OK) return rc;
     a.tiles = p.tiles;
     a.stats = at<float2>(c, p.stats);
     a.label_z = at<float>(c, p.label_z);
@@ -1119,16 +1173,21 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, true, &m.x)) != ALSGD_OK) return rc;
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, true, &m.w)) != ALSGD_OK) return rc;
     if ((rc = make_map(a.dz, (uint64_t)p.padded * p.piece * 4, 64, 128, 64, false, &m.dz)) != ALSGD_OK) return rc;
+    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, true, &m.x_all)) != ALSGD_OK) return rc;
+    m.all_rows = a.all_rows;
     m.count = a.count;
     m.dim = (int)d.dim;
     m.vocab = (int)d.vocab;
     m.n = p.n;
     m.dim_tiles = p.dim_tiles;
     m.padded = p.padded;
-    m.dx = at<float>(c, p.dx);
+    m.sums = at<float>(c, p.dx);
+    m.row = at<int>(c, p.row);
+    m.dx = static_cast<uint16_t*>(dx->data);
+    m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
     m.dw = static_cast<uint16_t*>(dw->data);
     m.dw_step = (int64_t)dw_step;
-    if ((rc = gather_rows(c, p, lse, dloss, dloss_step)) != ALSGD_OK) return rc;
+    if ((rc = gather_rows(c, p, lse, dloss, dloss_step, dx)) != ALSGD_OK) return rc;
     static SmemLimit limit;
     constexpr size_t smem = sizeof(ProductSmem) + 1024;
     if (!limit.raise(product_kernel, d.device, smem)) return ALSGD_E_CUDA;
@@ -1139,14 +1198,15 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         m.split_steps = p.split_steps;
         m.splits = (4 * m.tiles + p.split_steps - 1) / p.split_steps;
         m.add = i > 0;
+        m.last = i + 1 == p.pieces && p.splits == 1;
         if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
         const int64_t items = (int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles;
         if (launch_dependent(product_kernel, dim3(grid_of(items)), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
     }
+    if (p.splits == 1) return ALSGD_OK;
     const int64_t groups = (int64_t)d.rows * (d.dim / 8), blocks = (groups + 255) / 256;
-    return launch_dependent(dx_kernel, dim3((unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs)), dim3(256), 0, c.stream, (const float*)m.dx,
-                            (const int*)at<int>(c, p.slot), (int)d.rows, (int)d.dim, p.splits, (int64_t)p.padded * d.dim, static_cast<uint16_t*>(dx->data),
-                            (int64_t)step_of(*dx, d.rows, d.dim)) == cudaSuccess
+    return launch_dependent(dx_kernel, dim3((unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs)), dim3(256), 0, c.stream, (const float*)m.sums,
+                            (const int*)at<int>(c, p.slot), (int)d.rows, (int)d.dim, p.splits, (int64_t)p.padded * d.dim, m.dx, m.dx_step) == cudaSuccess
                ? ALSGD_OK
                : ALSGD_E_CUDA;
 }
