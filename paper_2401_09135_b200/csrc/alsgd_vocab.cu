@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
 
 constexpr int kThreads = 320;          // copies, products, eight warps that take tiles out
 constexpr int kOutWarps = 8;
-constexpr int kStageBytes = 32768;     // of a block: 128 x 64 of A, up to 128 x 64 of B
+constexpr int kOperandBytes = 16384;   // of a block in a stage: 128 x 64 of A, up to 128 x 64 of B
 constexpr int kAccColumns = 256;
 constexpr int kStagingBytes = 4096;    // of a warp: 32 rows of 64 bf16
 
@@ -248,21 +248,22 @@ struct Bars {
     uint32_t tmem, dead;
 };
 
-// What every warp of a block knows about its pair's shared memory.
-template <int STAGES>
+// What every warp of a block knows about its pair's shared memory: stages of SUBS operands A, one B.
+template <int STAGES, int SUBS>
 struct Pair {
+    static constexpr int kStageBytes = (SUBS + 1) * kOperandBytes;
     uint32_t stage0, full, empty, acc_full, acc_empty, rank, tmem;
     volatile uint32_t* dead;
 
     __device__ __forceinline__ uint32_t a(int s) const { return stage0 + s * kStageBytes; }
-    __device__ __forceinline__ uint32_t b(int s) const { return stage0 + s * kStageBytes + kStageBytes / 2; }
+    __device__ __forceinline__ uint32_t b(int s) const { return stage0 + s * kStageBytes + SUBS * kOperandBytes; }
 };
 
 // Barriers and tensor memory of both blocks.  Full: one arrival (the first block's copying thread, for the bytes of
 // both).  Empty, finished tile: one arrival, by the tensor core, on either block's.  Tile taken out: every warp of both blocks.
-template <int STAGES>
-__device__ __forceinline__ Pair<STAGES> pair_begin(uint8_t* stages, Bars<STAGES>* bars) {
-    Pair<STAGES> p;
+template <int STAGES, int SUBS>
+__device__ __forceinline__ Pair<STAGES, SUBS> pair_begin(uint8_t* stages, Bars<STAGES>* bars) {
+    Pair<STAGES, SUBS> p;
     p.stage0 = smem_u32(stages);
     p.full = smem_u32(bars->full);
     p.empty = smem_u32(bars->empty);
@@ -291,10 +292,9 @@ __device__ __forceinline__ Pair<STAGES> pair_begin(uint8_t* stages, Bars<STAGES>
     return p;
 }
 
-// The blocks leave together: neither's shared memory goes while the other's copies or products may touch it.  `steps`:
-// stages that the copying thread filled in all.
-template <int STAGES>
-__device__ __forceinline__ void pair_end(const Pair<STAGES>& p) {
+// The blocks leave together: neither's shared memory goes while the other's copies or products may touch it.
+template <int STAGES, int SUBS>
+__device__ __forceinline__ void pair_end(const Pair<STAGES, SUBS>& p) {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -322,40 +322,45 @@ struct Ring {
 enum : uint32_t { kWaitEmpty = 1, kWaitFull = 2, kWaitAccEmpty = 4, kWaitAccFull = 8 };
 
 // Before the copying thread leaves, everything that it started has landed and been consumed (at once, unless it gave up).
-template <int STAGES>
-__device__ __forceinline__ void ring_drain(const Pair<STAGES>& p, Ring ring) {
+template <int STAGES, int SUBS>
+__device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS>& p, Ring ring) {
     for (int s = 0; s < STAGES; ++s) {
         drain(p.empty + 8 * ring.stage, ring.phase ^ 1);
         ring.next<STAGES>();
     }
 }
 
-// One tile's products: `steps` stages, each four products of 16 along the inner axis.  a_step / b_step: bytes of shared memory
-// from one to the next.
-template <int STAGES, typename DESC_A, typename DESC_B>
-__device__ __forceinline__ void tile_products(const Pair<STAGES>& p, Ring& ring, int tile, int steps, uint32_t desc, DESC_A a, DESC_B b) {
-    const int buf = tile & 1;
-    wait_cluster(p.acc_empty + 8 * buf, ((tile >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
-    tc_fence_after();
-    const uint32_t d = p.tmem + buf * kAccColumns;
+// The products of `subs` tiles that share B: `steps` stages, each four products of 16 along the inner axis for either tile.
+// a, b: descriptors of the i-th.  acc: tiles before these; tensor memory holds two, in turn.
+template <int STAGES, int SUBS, typename DESC_A, typename DESC_B>
+__device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring& ring, uint32_t acc, int subs, int steps, uint32_t desc, DESC_A a, DESC_B b) {
     for (int k = 0; k < steps; ++k) {
         wait_cluster(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
         tc_fence_after();
         const uint32_t sa = p.a(ring.stage), sb = p.b(ring.stage);
 #pragma unroll
-        for (int i = 0; i < kStep / 16; ++i) mma_ss_pair(d, a(sa, i), b(sb, i), desc, k || i);
+        for (int s = 0; s < SUBS; ++s) {
+            if (s >= subs) break;
+            const uint32_t buf = (acc + s) & 1;
+            if (k == 0) {
+                wait_cluster(p.acc_empty + 8 * buf, (((acc + s) >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
+                tc_fence_after();
+            }
+#pragma unroll
+            for (int i = 0; i < kStep / 16; ++i) mma_ss_pair(p.tmem + buf * kAccColumns, a(sa + s * kOperandBytes, i), b(sb, i), desc, k || i);
+        }
         mma_commit_pair(p.empty + 8 * ring.stage);
         ring.next<STAGES>();
     }
-    mma_commit_pair(p.acc_full + 8 * buf);
+    for (int s = 0; s < subs; ++s) mma_commit_pair(p.acc_full + 8 * ((acc + s) & 1));
 }
 
-// The warp has taken its part of tile `tile` out of tensor memory.
-template <int STAGES>
-__device__ __forceinline__ void tile_taken(const Pair<STAGES>& p, int tile, int lane) {
+// The warp has taken its part of the tile out of tensor memory.
+template <int STAGES, int SUBS>
+__device__ __forceinline__ void tile_taken(const Pair<STAGES, SUBS>& p, uint32_t acc, int lane) {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (tile & 1), 0));
+    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (acc & 1), 0));
 }
 
 // ---------------------------------------------------------------------------------------------- logits
@@ -390,7 +395,7 @@ __device__ __forceinline__ void tile_at(int i, int row_tiles, int tiles, int& rt
 constexpr int kLogitStages = 6;
 
 struct LogitSmem {
-    uint8_t stages[kLogitStages * kStageBytes];
+    uint8_t stages[kLogitStages * 2 * kOperandBytes];
     uint8_t staging[kOutWarps * kStagingBytes];
     Bars<kLogitStages> bars;
 };
@@ -451,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
-    const Pair<kLogitStages> p = pair_begin<kLogitStages>(sm.stages, &sm.bars);
+    const Pair<kLogitStages, 1> p = pair_begin<kLogitStages, 1>(sm.stages, &sm.bars);
     grid_dependency_sync();
     const int count = *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
     const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / 2, pairs = gridDim.x / 2;
@@ -466,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                 const int row = rt * kTile + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
                 for (int k = 0; k < steps; ++k) {
                     wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
-                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * kStageBytes);
+                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * p.kStageBytes);
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
                     tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
                     tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
@@ -478,9 +483,9 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
     } else if (warp == 1) {
         if (p.rank == 0 && elect_one()) {
             Ring ring;
-            int tile = 0;
-            for (int i = first; i < tiles; i += pairs, ++tile)
-                tile_products(p, ring, tile, steps, mma_desc_pair(kTile, false, false), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+            uint32_t acc = 0;
+            for (int i = first; i < tiles; i += pairs, ++acc)
+                tile_products(p, ring, acc, 1, steps, mma_desc_pair(kTile, false, false), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
                               [](uint32_t s, int i) { return desc_k_major(s + 32 * i); });
         }
     } else {
@@ -488,8 +493,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
         const uint32_t staging = smem_u32(sm.staging) + (warp - 2) * kStagingBytes;
         uint8_t* const line = sm.staging + (warp - 2) * kStagingBytes + lane * 128;
-        int tile = 0;
-        for (int i = first; i < tiles; i += pairs, ++tile) {
+        uint32_t acc = 0;
+        for (int i = first; i < tiles; i += pairs, ++acc) {
             int rt, ct;
             tile_at(i, row_tiles, a.tiles, rt, ct);
             const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
@@ -510,16 +515,16 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                 coef = a.coef[row];
             }
             float top = -INFINITY, sum = 0.0f;
-            wait_warp(p.acc_full + 8 * (tile & 1), (tile >> 1) & 1, p.dead, kWaitAccFull);
+            wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t z[32];
-                tmem_ld32(z, lanes + (tile & 1) * kAccColumns + half * 128 + 32 * c);
+                tmem_ld32(z, lanes + (acc & 1) * kAccColumns + half * 128 + 32 * c);
                 tmem_wait_ld();
                 tmem_use(z);
-                if (c == 3) tile_taken(p, tile, lane);
+                if (c == 3) tile_taken(p, acc, lane);
                 const int w0 = c0 + 32 * c;
                 if (!BACKWARD) {
                     if (w0 + 32 > a.vocab) {                       // words behind the last have no logits
@@ -677,24 +682,30 @@ struct ProductArgs {
     int64_t dw_step;
 };
 
-constexpr int kProductStages = 7;
+// Two tiles, one above the other, share every copy of B where the inner axis is long: a step's copies are then 96 KB for
+// two tiles instead of 128, and what a pair can draw from the L2 (about 100 bytes a cycle) is what bounds the steps.  Both
+// halves of tensor memory belong to one item then, which its way out is not hidden behind: not worth it for short inner axes.
+constexpr int kProductStages = 4;
+constexpr int kLongSteps = 16;
 
 struct ProductSmem {
-    uint8_t stages[kProductStages * kStageBytes];
+    uint8_t stages[kProductStages * 3 * kOperandBytes];
     Bars<kProductStages> bars;
 };
 
 struct Item {
     bool is_dw;
-    int rt, dt, split, k0, steps;      // row tile (of rows or of words)
+    int rt, subs, dt, split, k0, steps;        // first tile (of rows or of words), tiles
 };
 
 // A pair's items: the longer kind first, dealt in turn; then the shorter kind, at first to the pairs that got one less of the
-// longer, until they are even.
+// longer, until they are even; what is left over goes out as single tiles where there are pairs for all of them.
 struct Deal {
-    int long_n, short_n, extra, pair, pairs;
+    int long_n, short_n, extra, pair, pairs, dx_subs, dw_subs;
     bool dw_long;
-    __device__ __forceinline__ bool at(int i, bool& is_dw, int& item) const {
+    // only: -1, or the one tile of the item
+    __device__ __forceinline__ bool at(int i, bool& is_dw, int& item, int& only) const {
+        only = -1;
         const int rest = long_n % pairs, mine = long_n / pairs + (pair < rest);
         if (i < mine) {
             is_dw = dw_long;
@@ -711,15 +722,26 @@ struct Deal {
             }
             i -= extra;
         }
-        item = extra * late + pair + i * pairs;
-        return item < short_n;
+        const int from = extra * late, left = max(0, short_n - from), rounds = left / pairs, over = left - rounds * pairs;
+        item = from + pair + i * pairs;
+        if (i < rounds) return true;
+        if (i > rounds) return false;
+        if ((is_dw ? dw_subs : dx_subs) == 2 && 2 * over <= pairs) {
+            item = from + rounds * pairs + pair / 2;
+            only = pair & 1;
+            return pair < 2 * over;
+        }
+        return pair < over;
     }
 };
 
 __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pair, int pairs) {
-    const int dx_n = (count + kTile - 1) / kTile * a.dim_tiles * a.splits, dw_n = a.tiles * a.dim_tiles;
-    const int dx_cost = a.split_steps + 4, dw_cost = (count + kStep - 1) / kStep + 4;
+    const int row_tiles = (count + kTile - 1) / kTile, dw_steps = (count + kStep - 1) / kStep;
     Deal d;
+    d.dx_subs = row_tiles > 1 && a.split_steps >= kLongSteps ? 2 : 1;
+    d.dw_subs = a.tiles > 1 && dw_steps >= kLongSteps ? 2 : 1;
+    const int dx_n = (row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = (a.tiles + d.dw_subs - 1) / d.dw_subs * a.dim_tiles;
+    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (dw_steps + 4) * d.dw_subs;
     d.dw_long = dw_cost >= dx_cost;
     d.long_n = d.dw_long ? dw_n : dx_n;
     d.short_n = d.dw_long ? dx_n : dw_n;
@@ -731,21 +753,28 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
 }
 
 __device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int count, int i, Item& t) {
-    int n;
-    if (!d.at(i, t.is_dw, n)) return false;
+    int n, only;
+    if (!d.at(i, t.is_dw, n, only)) return false;
     t.dt = n % a.dim_tiles;
     n /= a.dim_tiles;
-    if (t.is_dw) {
-        t.rt = n;
-        t.split = 0;
-        t.k0 = 0;
-        t.steps = (count + kStep - 1) / kStep;
-    } else {
+    t.split = 0;
+    t.k0 = 0;
+    t.steps = (count + kStep - 1) / kStep;
+    if (!t.is_dw) {
         t.split = n % a.splits;
-        t.rt = n / a.splits;
+        n /= a.splits;
         t.k0 = t.split * a.split_steps;
         t.steps = min(a.split_steps, a.tiles * 4 - t.k0);
     }
+    t.subs = t.is_dw ? d.dw_subs : d.dx_subs;
+    t.rt = n * t.subs;
+    const int end = t.is_dw ? a.tiles : (count + kTile - 1) / kTile;
+    if (only >= 0) {
+        t.rt += only;
+        t.subs = 1;
+        return t.rt < end;                                         // a pair's last item
+    }
+    t.subs = min(t.subs, end - t.rt);
     return true;
 }
 
@@ -758,7 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
-    const Pair<kProductStages> p = pair_begin<kProductStages>(sm.stages, &sm.bars);
+    const Pair<kProductStages, 2> p = pair_begin<kProductStages, 2>(sm.stages, &sm.bars);
     grid_dependency_sync();
     const int count = *a.count, pairs = gridDim.x / 2;
     const Deal deal = deal_of(a, count, blockIdx.x / 2, pairs);
@@ -777,26 +806,22 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             Ring ring;
             Item t;
             for (int i = 0; item_at(a, deal, count, i, t); ++i) {
-                const int d0 = t.dt * a.n + p.rank * (a.n / 2), half_blocks = a.tiles * 4;
+                const int d0 = t.dt * a.n + p.rank * (a.n / 2), row_blocks = a.tiles * 4;      // of one block's rows
                 for (int k = t.k0; k < t.k0 + t.steps; ++k) {
                     wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
-                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * (16384 + boxes * 8192));
+                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * (t.subs * kOperandBytes + boxes * 8192));
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
-                    if (t.is_dw) {
-                        // 64 rows x 128 words: half of each of two blocks
-                        const int64_t block = (int64_t)(k / 2) * half_blocks + t.rt * 4 + p.rank * 2;
-                        const int y = (int)(block * 128 + (k & 1) * 64);
-                        tma_load2_pair(p.a(ring.stage), &a.dz, full, 0, y);
-                        tma_load2_pair(p.a(ring.stage) + 8192, &a.dz, full, 0, y + 128);
-                        for (int b = 0; b < boxes; ++b) tma_load2_pair(p.b(ring.stage) + b * 8192, x, full, d0 + 64 * b, k * kStep);
-                    } else {
-                        // 128 rows x 64 words: a whole block
-                        const int y = (int)(((int64_t)(t.rt * 2 + p.rank) * half_blocks + k) * 128);
-                        tma_load2_pair(p.a(ring.stage), &a.dz, full, 0, y);
-                        tma_load2_pair(p.a(ring.stage) + 8192, &a.dz, full, 0, y + 64);
-                        for (int b = 0; b < boxes; ++b)
-                            tma_load2_pair(p.b(ring.stage) + b * 8192, &a.w, full, d0 + 64 * b, a.tile0 * kTile + k * kStep);
+                    for (int s = 0; s < t.subs; ++s) {
+                        const uint32_t to = p.a(ring.stage) + s * kOperandBytes;
+                        // dw: 64 rows x 128 words, half of each of two blocks; dx: 128 rows x 64 words, a whole block
+                        const int64_t block = t.is_dw ? (int64_t)(k / 2) * row_blocks + (t.rt + s) * 4 + p.rank * 2
+                                                      : (int64_t)((t.rt + s) * 2 + p.rank) * row_blocks + k;
+                        const int y = (int)(block * 128) + (t.is_dw ? (k & 1) * 64 : 0);
+                        tma_load2_pair(to, &a.dz, full, 0, y);
+                        tma_load2_pair(to + 8192, &a.dz, full, 0, y + (t.is_dw ? 128 : 64));
                     }
+                    for (int b = 0; b < boxes; ++b)
+                        tma_load2_pair(p.b(ring.stage) + b * 8192, t.is_dw ? x : &a.w, full, d0 + 64 * b, t.is_dw ? k * kStep : a.tile0 * kTile + k * kStep);
                     ring.next<kProductStages>();
                 }
             }
@@ -806,22 +831,25 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         if (p.rank == 0 && elect_one()) {
             Ring ring;
             Item t;
+            uint32_t acc = 0;
             for (int i = 0; item_at(a, deal, count, i, t); ++i) {
                 if (t.is_dw)
-                    tile_products(p, ring, i, t.steps, mma_desc_pair(a.n, true, true), [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); },
-                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
+                    tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, true, true),
+                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); }, [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
                 else
-                    tile_products(p, ring, i, t.steps, mma_desc_pair(a.n, false, true), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+                    tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, false, true), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
                                   [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
+                acc += t.subs;
             }
         }
     } else {
         const int quad = warp & 3, half = (warp - 2) / 4;
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
         Item t;
-        for (int i = 0; item_at(a, deal, count, i, t); ++i) {
-            const int row = t.rt * kTile + p.rank * 128 + 32 * quad + lane;
-            wait_warp(p.acc_full + 8 * (i & 1), (i >> 1) & 1, p.dead, kWaitAccFull);
+        uint32_t acc = 0;
+        for (int i = 0, sub = 0; item_at(a, deal, count, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
+            const int row = (t.rt + sub) * kTile + p.rank * 128 + 32 * quad + lane;
+            wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;
             const int64_t word = (int64_t)a.tile0 * kTile + row;
@@ -831,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             float* sums = a.sums + ((size_t)t.split * a.padded + row) * a.dim;
             for (int c = half; c < a.n / 32; c += 2) {
                 uint32_t v[32];
-                tmem_ld32(v, lanes + (i & 1) * kAccColumns + 32 * c);
+                tmem_ld32(v, lanes + (acc & 1) * kAccColumns + 32 * c);
                 tmem_wait_ld();
                 tmem_use(v);
                 const int d0 = t.dt * a.n + 32 * c;
@@ -860,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                 }
                 __syncwarp();
             }
-            tile_taken(p, i, lane);
+            tile_taken(p, acc, lane);
         }
     }
     pair_end(p);
@@ -913,10 +941,12 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     if (piece > (uint64_t)p.tiles) piece = p.tiles;
     p.pieces = (int)((p.tiles + piece - 1) / piece);
     p.piece = (p.tiles + p.pieces - 1) / p.pieces;
+    if (p.pieces > 1) p.piece += p.piece % 2;
     p.pieces = (p.tiles + p.piece - 1) / p.piece;
     // dx's inner axis is split while one of its tiles would take longer than its share of the launch
     const int64_t row_tiles = p.padded / kTile, dx_steps = 4ll * p.piece;
-    const int64_t all = row_tiles * p.dim_tiles * dx_steps + (int64_t)p.piece * p.dim_tiles * (p.padded / kStep);
+    int64_t all = row_tiles * p.dim_tiles * dx_steps + (int64_t)p.piece * p.dim_tiles * (p.padded / kStep);
+    if (row_tiles > 1) all /= 2;                                   // two tiles at a time
     const int64_t share = all / kPairs > 8 ? all / kPairs : 8;
     int64_t splits = (dx_steps + share - 1) / share;
     if (splits > kMaxSplits) splits = kMaxSplits;
