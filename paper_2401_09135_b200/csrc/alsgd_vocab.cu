@@ -667,6 +667,7 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
 
 struct ProductArgs {
     CUtensorMap dz, x, x_all, w;       // boxes of 64 x 64; dz's rows are those of its blocks; x as for the logits
+    CUtensorMap dw_map;                // boxes of 32 x 32
     const int* count;
     int all_rows;
     int dim, vocab;
@@ -674,7 +675,7 @@ struct ProductArgs {
     int splits, split_steps;           // of dx's inner axis
     int n, dim_tiles;                  // columns of a tile, tiles of dim
     int padded, add, last;             // add: dx's sums so far are read; last: dx is written in place of its sums
-    float* sums;                       // [splits][padded][dim]: dx so far
+    float4* sums;                      // [splits][padded / 128][dim / 4][128]: dx so far, four columns of a row in one place
     const int* row;                    // of a place
     uint16_t* dx;
     int64_t dx_step;
@@ -690,6 +691,7 @@ constexpr int kLongSteps = 16;
 
 struct ProductSmem {
     uint8_t stages[kProductStages * 3 * kOperandBytes];
+    uint8_t staging[kOutWarps * kStagingBytes];
     Bars<kProductStages> bars;
 };
 
@@ -846,74 +848,111 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         const int quad = warp & 3, half = (warp - 2) / 4;
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
         Item t;
-        uint32_t acc = 0;
+        uint32_t acc = 0, boxes_out = 0;
         for (int i = 0, sub = 0; item_at(a, deal, count, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
             const int row = (t.rt + sub) * kTile + p.rank * 128 + 32 * quad + lane;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;
-            const int64_t word = (int64_t)a.tile0 * kTile + row;
-            const bool writes = t.is_dw ? word < a.vocab : row < count;
-            uint16_t* out = t.is_dw ? a.dw + word * a.dw_step : a.dx;
-            if (!t.is_dw && a.last && writes) out += (int64_t)a.row[row] * a.dx_step;
-            float* sums = a.sums + ((size_t)t.split * a.padded + row) * a.dim;
+            const int block = (t.rt + sub) * 2 + p.rank, word = (a.tile0 + t.rt + sub) * kTile + p.rank * 128 + 32 * quad;
+            float4* const sums = a.sums + ((size_t)t.split * (a.padded / 128) + block) * (a.dim / 4) * 128 + 32 * quad + lane;
+            const bool out = t.is_dw || a.last, adds = !t.is_dw && a.add && row < count;
+            // the rows that the lane writes in turn: 8 at a time, four lanes for 64 bytes of each
+            int64_t to[4];
+            if (out && !t.is_dw)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int place = row - lane + 8 * r + lane / 4;
+                    to[r] = place < count ? a.row[place] * a.dx_step : -1;
+                }
             for (int c = half; c < a.n / 32; c += 2) {
+                const int d0 = t.dt * a.n + 32 * c;
+                if (d0 >= a.dim) break;
+                float4 before[8];
+                if (adds)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) before[j] = d0 + 4 * j < a.dim ? sums[(size_t)(d0 / 4 + j) * 128] : make_float4(0, 0, 0, 0);
                 uint32_t v[32];
                 tmem_ld32(v, lanes + (acc & 1) * kAccColumns + 32 * c);
                 tmem_wait_ld();
                 tmem_use(v);
-                const int d0 = t.dt * a.n + 32 * c;
                 if (dead) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
                 }
+                if (adds) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (!writes || d0 + 8 * j >= a.dim) break;
-                    float o[8];
-#pragma unroll
-                    for (int h = 0; h < 8; ++h) o[h] = __uint_as_float(v[8 * j + h]);
-                    float4* at = reinterpret_cast<float4*>(sums + d0 + 8 * j);
-                    if (!t.is_dw && a.add) {
-                        const float4 lo = at[0], hi = at[1];
-                        o[0] += lo.x, o[1] += lo.y, o[2] += lo.z, o[3] += lo.w;
-                        o[4] += hi.x, o[5] += hi.y, o[6] += hi.z, o[7] += hi.w;
-                    }
-                    if (t.is_dw || a.last) {
-                        *reinterpret_cast<uint4*>(out + d0 + 8 * j) = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
-                    } else {
-                        at[0] = make_float4(o[0], o[1], o[2], o[3]);
-                        at[1] = make_float4(o[4], o[5], o[6], o[7]);
+                    for (int j = 0; j < 8; ++j) {
+                        v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + before[j].x);
+                        v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + before[j].y);
+                        v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + before[j].z);
+                        v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + before[j].w);
                     }
                 }
+                if (!out) {
+                    if (row < count)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (d0 + 4 * j < a.dim)
+                                sums[(size_t)(d0 / 4 + j) * 128] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
+                                                                               __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
+                    __syncwarp();
+                    continue;
+                }
+                // 32 rows of 64 bytes, in the 64-byte swizzle that the tensor map reads, in one of two places
+                uint8_t* const box = sm.staging + (warp - 2) * kStagingBytes + (boxes_out & 1) * 2048;
+                if (lane == 0) tma_store_wait_read_1();
                 __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) w[h] = pack_bf16(__uint_as_float(v[8 * j + 2 * h]), __uint_as_float(v[8 * j + 2 * h + 1]));
+                    *reinterpret_cast<uint4*>(box + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                if (t.is_dw) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && word < a.vocab) {
+                        tma_store2(&a.dw_map, smem_u32(box), d0, word);
+                        tma_store_commit();
+                    }
+                } else {
+                    __syncwarp();
+                    const int at = 8 * (lane & 3);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int line = 8 * r + lane / 4;
+                        const uint4 w = *reinterpret_cast<const uint4*>(box + line * 64 + (((lane & 3) ^ ((line >> 1) & 3)) << 4));
+                        if (to[r] >= 0 && d0 + at < a.dim) *reinterpret_cast<uint4*>(a.dx + to[r] + d0 + at) = w;
+                    }
+                }
+                ++boxes_out;
             }
             tile_taken(p, acc, lane);
         }
+        if (lane == 0) bulk_store_wait();
     }
     pair_end(p);
 }
 
-// dx from several parts: their sums, rounded.
-__global__ void __launch_bounds__(256) dx_kernel(const float* sums, const int* slot, int rows, int dim, int splits, int64_t split_elems, uint16_t* dx,
+// dx from several parts: their sums, rounded.  A warp takes 32 rows x 8 columns.
+__global__ void __launch_bounds__(256) dx_kernel(const float4* sums, const int* count, const int* row_of, int padded, int dim, int splits, uint16_t* dx,
                                                  int64_t dx_step) {
     grid_dependency_sync();
-    const int per_row = dim / 8;
-    const int64_t all = (int64_t)rows * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int row = (int)(i / per_row), d = 8 * (int)(i - (int64_t)row * per_row), s = slot[row];
-        if (s < 0) continue;
-        float v[8] = {};
-        const float* from = sums + (int64_t)s * dim + d;
+    const int row = blockIdx.x * 32 + threadIdx.x % 32, d = 8 * (blockIdx.y * 8 + threadIdx.x / 32);
+    if (row >= *count || d >= dim) return;
+    const int64_t part = (int64_t)(padded / 128) * (dim / 4) * 128;
+    const float4* from = sums + ((int64_t)(row / 128) * (dim / 4) + d / 4) * 128 + row % 128;
+    float v[8] = {};
 #pragma unroll 4
-        for (int k = 0; k < splits; ++k, from += split_elems) {
-            const float4 lo = reinterpret_cast<const float4*>(from)[0], hi = reinterpret_cast<const float4*>(from)[1];
-            const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    for (int k = 0; k < splits; ++k, from += part) {
+        const float4 lo = from[0], hi = from[128];
+        const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += add[j];
-        }
-        *reinterpret_cast<uint4*>(dx + row * dx_step + d) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        for (int j = 0; j < 8; ++j) v[j] += add[j];
     }
+    *reinterpret_cast<uint4*>(dx + row_of[row] * dx_step + d) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -1009,14 +1048,15 @@ int check_matrix(const alsgd_matrix* m, uint32_t rows, uint32_t dim, bool output
     return ALSGD_OK;
 }
 
-// Boxes of 64 columns x box_rows rows of a bf16 matrix, swizzled over their 128-byte rows, or as they are; zeros outside.
-int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t step_bytes, uint32_t box_rows, bool swizzle, CUtensorMap* out) {
+// Boxes of 64 (or 32) columns x box_rows rows of a bf16 matrix, swizzled over their 128-byte (64-byte) rows, or as they are; zeros
+// outside.
+int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t step_bytes, uint32_t box_rows, bool swizzle, CUtensorMap* out, uint32_t box_cols = 64) {
     EncodeTiled encode = encode_tiled();
     if (!encode) return ALSGD_E_CUDA;
     const cuuint64_t size[2] = {cols, rows}, bytes[1] = {step_bytes};
-    const cuuint32_t box[2] = {64, box_rows}, unit[2] = {1, 1};
+    const cuuint32_t box[2] = {box_cols, box_rows}, unit[2] = {1, 1};
     const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(data), size, bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? ALSGD_OK : ALSGD_E_ARG;
 }
@@ -1203,6 +1243,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, true, &m.x)) != ALSGD_OK) return rc;
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, true, &m.w)) != ALSGD_OK) return rc;
     if ((rc = make_map(a.dz, (uint64_t)p.padded * p.piece * 4, 64, 128, 64, false, &m.dz)) != ALSGD_OK) return rc;
+    if ((rc = make_map(dw->data, d.vocab, d.dim, 2 * dw_step, 32, true, &m.dw_map, 32)) != ALSGD_OK) return rc;
     if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, true, &m.x_all)) != ALSGD_OK) return rc;
     m.all_rows = a.all_rows;
     m.count = a.count;
@@ -1211,7 +1252,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     m.n = p.n;
     m.dim_tiles = p.dim_tiles;
     m.padded = p.padded;
-    m.sums = at<float>(c, p.dx);
+    m.sums = at<float4>(c, p.dx);
     m.row = at<int>(c, p.row);
     m.dx = static_cast<uint16_t*>(dx->data);
     m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
@@ -1234,9 +1275,8 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         if (launch_dependent(product_kernel, dim3(grid_of(items)), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
     }
     if (p.splits == 1) return ALSGD_OK;
-    const int64_t groups = (int64_t)d.rows * (d.dim / 8), blocks = (groups + 255) / 256;
-    return launch_dependent(dx_kernel, dim3((unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs)), dim3(256), 0, c.stream, (const float*)m.sums,
-                            (const int*)at<int>(c, p.slot), (int)d.rows, (int)d.dim, p.splits, (int64_t)p.padded * d.dim, m.dx, m.dx_step) == cudaSuccess
+    return launch_dependent(dx_kernel, dim3(p.padded / 32, (unsigned)((d.dim + 63) / 64)), dim3(256), 0, c.stream, (const float4*)m.sums, m.count, m.row,
+                            p.padded, (int)d.dim, p.splits, m.dx, m.dx_step) == cudaSuccess
                ? ALSGD_OK
                : ALSGD_E_CUDA;
 }
