@@ -9,7 +9,9 @@
 // workspace's size), then dx += dz w and dw = dz^T x in one launch.
 //
 // The rows that take part are gathered first (a padded batch pays for its tokens, not for its padding; what the other rows
-// hold reaches nothing) and everything behind works on their number, which only the device knows.
+// hold reaches nothing) and everything behind works on their number, which only the device knows.  One tile's worth of rows or
+// fewer stay where they are: there is nothing to save, and the two launches in front would cost more than the rest
+// (forward of 77 rows x 32000 words x 384: 16.6 -> 13.1 us).
 //
 // The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
 // of either operand, so that a tile needs half of the shared memory traffic of two single ones.  One warp copies, one
@@ -100,6 +102,7 @@ struct GatherArgs {
     float scale;
     int padded, blocks, dim, tiles;    // rows in whole tiles; counting blocks; tiles of the vocabulary
     int direct;                        // where all rows take part, the products read x itself
+    int plain;                         // rows stay in their places; only the teacher's lists are made
     uint16_t* dx;                      // backward only: zeros for the rows that take no part
     int64_t dx_step;
     const int *block_count, *place;
@@ -107,7 +110,7 @@ struct GatherArgs {
     int* slot;                         // [rows]: place among them, or -1
     int* row;                          // [padded]: the row at a place
     uint16_t* xc;                      // [padded][dim]
-    int* target;                       // [padded]; labels only
+    int* target;                       // [padded]: a label, or -1.  With a teacher and plain rows: 0, or -1
     int* index;                        // [padded][top] ascending, then places that take no part; teacher only
     float* weight;                     // [padded][top]
     float* entropy;                    // [padded]: sum t log t
@@ -117,6 +120,81 @@ struct GatherArgs {
 
 constexpr int kGatherWarps = 4;
 
+// One row's list by one warp: the teacher's softmax over the entries that take part, then the entries in ascending order of
+// their words.
+__device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int slot, bool used, int* words, int* sorted, int lane) {
+    uint8_t* first = a.first + (size_t)slot * (2 * a.tiles + 1);
+    if (!used) {
+        for (int t = lane; t <= 2 * a.tiles; t += 32) first[t] = 0;
+        if (a.plain && lane == 0) a.target[slot] = -1;
+        return;
+    }
+    constexpr int E = kMaxTop / 32;
+    const float c = a.scale * kLog2e;
+    int at[E];
+    float v[E], top = -INFINITY, sum = 0.0f;
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int k = lane + 32 * e;
+        at[e] = INT_MAX;
+        v[e] = -INFINITY;
+        if (k < a.l.top) {
+            const size_t i = (size_t)r * a.l.top + k;
+            const int word = label_at(a.l, i);
+            const float t = teacher_at(a.l, i);
+            if (word >= 0 && t != -INFINITY) {
+                at[e] = word;
+                v[e] = t;
+            }
+            words[k] = at[e];
+        }
+        nan |= v[e] != v[e];
+        top = fmaxf(top, v[e]);
+    }
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    if (__any_sync(~0u, nan)) top = NAN;
+    if (a.plain) {
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) any |= at[e] != INT_MAX;
+        any = __any_sync(~0u, any);
+        if (lane == 0) a.target[slot] = any ? 0 : -1;
+        if (!any) top = 0.0f;                                      // the list is empty; so is everything below
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c);
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    const float inv = 1.0f / sum, log_sum = logf(sum);
+    float entropy = 0.0f;
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int k = lane + 32 * e;
+        if (k >= a.l.top) continue;
+        const float t = at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c) * inv;
+        if (at[e] != INT_MAX) entropy += t * ((v[e] - top) * a.scale - log_sum);
+        int rank = 0;
+        for (int j = 0; j < a.l.top; ++j) rank += words[j] < at[e] || (words[j] == at[e] && j < k);
+        sorted[rank] = at[e];
+        a.index[(size_t)slot * a.l.top + rank] = at[e];
+        a.weight[(size_t)slot * a.l.top + rank] = t;
+    }
+    for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
+    if (lane == 0) a.entropy[slot] = entropy;
+    __syncwarp();
+    for (int t = lane; t <= 2 * a.tiles; t += 32) {
+        const int word = min(t * (kTile / 2), a.l.vocab);            // places that take no part are behind every word
+        int low = 0, high = a.l.top;
+        while (low < high) {
+            const int mid = (low + high) / 2;
+            if (sorted[mid] < word) low = mid + 1;
+            else high = mid;
+        }
+        first[t] = (uint8_t)low;
+    }
+}
+
 // One warp per row: its place, its copy of x, its labels, what the gradient scales by.
 __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_constant__ GatherArgs a) {
     __shared__ int s_index[kGatherWarps][kMaxTop], s_sorted[kGatherWarps][kMaxTop];
@@ -124,6 +202,10 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
     grid_dependency_sync();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int r0 = blockIdx.x * kGatherWarps, r = r0 + warp, block = r0 / kCountRows;     // a block's rows share a counting block
+    if (a.plain) {
+        teacher_lists(a, r, r, r < a.l.rows, s_index[warp], s_sorted[warp], lane);
+        return;
+    }
     int before = 0, total = 0;
     for (int i = threadIdx.x; i < a.blocks; i += 32 * kGatherWarps) {
         const int n = a.block_count[i];
@@ -168,70 +250,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
         }
         if (a.target) a.target[slot] = used ? label_at(a.l, r) : -1;
     }
-    if (a.target) return;
-
-    // the teacher's softmax over the entries that take part, then the entries in ascending order of their words
-    uint8_t* first = a.first + (size_t)slot * (2 * a.tiles + 1);
-    if (!used) {
-        for (int t = lane; t <= 2 * a.tiles; t += 32) first[t] = 0;
-        return;
-    }
-    constexpr int E = kMaxTop / 32;
-    const float c = a.scale * kLog2e;
-    int at[E];
-    float v[E], top = -INFINITY, sum = 0.0f;
-    bool nan = false;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int k = lane + 32 * e;
-        at[e] = INT_MAX;
-        v[e] = -INFINITY;
-        if (k < a.l.top) {
-            const size_t i = (size_t)r * a.l.top + k;
-            const int word = label_at(a.l, i);
-            const float t = teacher_at(a.l, i);
-            if (word >= 0 && t != -INFINITY) {
-                at[e] = word;
-                v[e] = t;
-            }
-            s_index[warp][k] = at[e];
-        }
-        nan |= v[e] != v[e];
-        top = fmaxf(top, v[e]);
-    }
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-    if (__any_sync(~0u, nan)) top = NAN;
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c);
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-    const float inv = 1.0f / sum, log_sum = logf(sum);
-    float entropy = 0.0f;
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int k = lane + 32 * e;
-        if (k >= a.l.top) continue;
-        const float t = at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c) * inv;
-        if (at[e] != INT_MAX) entropy += t * ((v[e] - top) * a.scale - log_sum);
-        int rank = 0;
-        for (int j = 0; j < a.l.top; ++j) rank += s_index[warp][j] < at[e] || (s_index[warp][j] == at[e] && j < k);
-        s_sorted[warp][rank] = at[e];
-        a.index[(size_t)slot * a.l.top + rank] = at[e];
-        a.weight[(size_t)slot * a.l.top + rank] = t;
-    }
-    for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
-    if (lane == 0) a.entropy[slot] = entropy;
-    __syncwarp();
-    for (int t = lane; t <= 2 * a.tiles; t += 32) {
-        const int word = min(t * (kTile / 2), a.l.vocab);            // places that take no part are behind every word
-        int low = 0, high = a.l.top;
-        while (low < high) {
-            const int mid = (low + high) / 2;
-            if (s_sorted[warp][mid] < word) low = mid + 1;
-            else high = mid;
-        }
-        first[t] = (uint8_t)low;
-    }
+    if (a.l.teacher) teacher_lists(a, r, slot, used, s_index[warp], s_sorted[warp], lane);
 }
 
 // ---------------------------------------------------------------------------------------------- the pair's machinery
@@ -369,6 +388,15 @@ struct LogitArgs {
     CUtensorMap x, x_all, w;           // gathered rows, the rows as they are, words: boxes of 64 x 128
     const int* count;
     int all_rows;                      // with as many rows that take part, x_all is read; -1: never
+    int plain, rows;                   // rows stay in their places
+    Labels l;
+    const float *lse, *dloss;          // backward, plain
+    int64_t dloss_step;
+    float scale;
+    const uint16_t* x_rows;
+    int64_t x_step;
+    uint16_t* xc;
+    int* row;
     int dim, vocab, top;
     int tile0, tiles, all_tiles;       // of the vocabulary: this launch's, all of them
     float scale2;                      // scale * log2 e
@@ -458,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
     }
     const Pair<kLogitStages, 1> p = pair_begin<kLogitStages, 1>(sm.stages, &sm.bars);
     grid_dependency_sync();
-    const int count = *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
+    const int count = a.plain ? a.rows : *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
     const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / 2, pairs = gridDim.x / 2;
 
     if (warp == 0) {
@@ -494,6 +522,15 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         const uint32_t staging = smem_u32(sm.staging) + (warp - 2) * kStagingBytes;
         uint8_t* const line = sm.staging + (warp - 2) * kStagingBytes + lane * 128;
         uint32_t acc = 0;
+        if (BACKWARD && a.plain) {
+            // for the products behind: zeros in the rows that take no part
+            for (int r = (warp - 2) * gridDim.x + blockIdx.x; r < a.padded; r += kOutWarps * gridDim.x) {
+                const bool used = r < a.rows && (TOP ? a.target[r] : label_at(a.l, r)) >= 0;
+                for (int c = 8 * lane; c < a.dim; c += 256)
+                    *reinterpret_cast<uint4*>(a.xc + (size_t)r * a.dim + c) = used ? *reinterpret_cast<const uint4*>(a.x_rows + r * a.x_step + c) : make_uint4(0, 0, 0, 0);
+                if (lane == 0) a.row[r] = used ? r : ~r;
+            }
+        }
         for (int i = first; i < tiles; i += pairs, ++acc) {
             int rt, ct;
             tile_at(i, row_tiles, a.tiles, rt, ct);
@@ -504,15 +541,24 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             const size_t list = (size_t)row * a.top;
             if (TOP) {
                 const uint8_t* f = a.first + (size_t)row * (2 * a.all_tiles + 1) + 2 * (a.tile0 + ct) + half;
-                queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, f[0], f[1]);
-            } else {
-                label = a.target[row];
+                const bool listed = row < count;                   // what fills the tile up has no list
+                queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, listed ? f[0] : 0, listed ? f[1] : 0);
             }
-            const bool used = row < count;
             float lse2 = 0.0f, coef = 0.0f;
-            if (BACKWARD) {
-                lse2 = a.lse2[row];
-                coef = a.coef[row];
+            bool used = row < count;
+            if (a.plain) {
+                if (used) label = TOP ? a.target[row] : label_at(a.l, row);
+                used = label >= 0;
+                if (BACKWARD && used) {
+                    lse2 = a.lse[row] * kLog2e;
+                    coef = a.dloss[row * a.dloss_step] * a.scale;
+                }
+            } else {
+                if (!TOP) label = a.target[row];
+                if (BACKWARD) {
+                    lse2 = a.lse2[row];
+                    coef = a.coef[row];
+                }
             }
             float top = -INFINITY, sum = 0.0f;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
@@ -605,6 +651,9 @@ struct LossArgs {
     const float *weight, *entropy;     // teacher only
     const int *index;
     const int *slot, *count;
+    int plain;                         // rows stay in their places
+    Labels l;
+    const int* target;
     int rows, padded, parts, top;      // parts: 2 * tiles
     float scale, scale2;
     float *loss, *lse;
@@ -616,8 +665,8 @@ constexpr int kLossRows = 32, kLossParts = 16;
 __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a, const int* row_of) {
     __shared__ float s_top[kLossParts][kLossRows], s_sum[kLossParts][kLossRows], s_z[kLossParts][kLossRows], s_weight[kLossParts][kLossRows];
     grid_dependency_sync();
-    const int count = *a.count, i = threadIdx.x % kLossRows, part = threadIdx.x / kLossRows, row = blockIdx.x * kLossRows + i;
-    if (threadIdx.x < kLossRows && row < a.rows && a.slot[row] < 0) a.loss[row] = a.lse[row] = 0.0f;
+    const int count = a.plain ? a.rows : *a.count, i = threadIdx.x % kLossRows, part = threadIdx.x / kLossRows, row = blockIdx.x * kLossRows + i;
+    if (!a.plain && threadIdx.x < kLossRows && row < a.rows && a.slot[row] < 0) a.loss[row] = a.lse[row] = 0.0f;
     if (blockIdx.x * kLossRows >= count) return;
     float top = -INFINITY, sum = 0.0f;
     constexpr int N = 8;                                       // loads on the way
@@ -636,7 +685,7 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
         top = m;
     }
     float z = 0.0f, weight = 0.0f;                             // sum t z, sum t
-    if (row < count)
+    if (row < count && !(a.plain && a.top && a.target[row] < 0))
 #pragma unroll 4
         for (int k = part; k < a.top; k += kLossParts) {
             const size_t at = (size_t)row * a.top + k;
@@ -658,7 +707,11 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
         weight += s_weight[q][i];
     }
     const float lse = fmaf(top, a.scale, logf(sum));
-    const int r = row_of[row];
+    if (a.plain && (a.top ? a.target[row] : label_at(a.l, row)) < 0) {
+        a.loss[row] = a.lse[row] = 0.0f;
+        return;
+    }
+    const int r = a.plain ? row : row_of[row];
     a.loss[r] = a.top ? a.entropy[row] - a.scale * z + lse * weight : lse - a.scale * a.label_z[row];
     a.lse[r] = lse;
 }
@@ -670,13 +723,14 @@ struct ProductArgs {
     CUtensorMap dw_map;                // boxes of 32 x 32
     const int* count;
     int all_rows;
+    int plain, rows;                   // rows stay in their places
     int dim, vocab;
     int tile0, tiles;                  // of the vocabulary: the piece
     int splits, split_steps;           // of dx's inner axis
     int n, dim_tiles;                  // columns of a tile, tiles of dim
     int padded, add, last;             // add: dx's sums so far are read; last: dx is written in place of its sums
     float4* sums;                      // [splits][padded / 128][dim / 4][128]: dx so far, four columns of a row in one place
-    const int* row;                    // of a place
+    const int* row;                    // of a place; ~row: its dx is zero
     uint16_t* dx;
     int64_t dx_step;
     uint16_t* dw;
@@ -791,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     }
     const Pair<kProductStages, 2> p = pair_begin<kProductStages, 2>(sm.stages, &sm.bars);
     grid_dependency_sync();
-    const int count = *a.count, pairs = gridDim.x / 2;
+    const int count = a.plain ? a.rows : *a.count, pairs = gridDim.x / 2;
     const Deal deal = deal_of(a, count, blockIdx.x / 2, pairs);
     const int boxes = (a.n / 2 + 63) / 64;                         // of B in either block
 
@@ -859,11 +913,13 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             const bool out = t.is_dw || a.last, adds = !t.is_dw && a.add && row < count;
             // the rows that the lane writes in turn: 8 at a time, four lanes for 64 bytes of each
             int64_t to[4];
+            bool zero[4] = {};
             if (out && !t.is_dw)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int place = row - lane + 8 * r + lane / 4;
-                    to[r] = place < count ? a.row[place] * a.dx_step : -1;
+                    const int place = row - lane + 8 * r + lane / 4, at = place < count ? a.row[place] : 0;
+                    zero[r] = at < 0;
+                    to[r] = place < count ? (at < 0 ? ~at : at) * a.dx_step : -1;
                 }
             for (int c = half; c < a.n / 32; c += 2) {
                 const int d0 = t.dt * a.n + 32 * c;
@@ -924,7 +980,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                     for (int r = 0; r < 4; ++r) {
                         const int line = 8 * r + lane / 4;
                         const uint4 w = *reinterpret_cast<const uint4*>(box + line * 64 + (((lane & 3) ^ ((line >> 1) & 3)) << 4));
-                        if (to[r] >= 0 && d0 + at < a.dim) *reinterpret_cast<uint4*>(a.dx + to[r] + d0 + at) = w;
+                        if (to[r] >= 0 && d0 + at < a.dim) *reinterpret_cast<uint4*>(a.dx + to[r] + d0 + at) = zero[r] ? make_uint4(0, 0, 0, 0) : w;
                     }
                 }
                 ++boxes_out;
@@ -936,23 +992,36 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     pair_end(p);
 }
 
-// dx from several parts: their sums, rounded.  A warp takes 32 rows x 8 columns.
-__global__ void __launch_bounds__(256) dx_kernel(const float4* sums, const int* count, const int* row_of, int padded, int dim, int splits, uint16_t* dx,
+// dx from several parts: their sums, rounded.  A block takes 32 rows x 8 columns, a warp every eighth part; the warps' sums are
+// added in their order.
+__global__ void __launch_bounds__(256) dx_kernel(const float4* sums, const int* count, int rows, const int* row_of, int padded, int dim, int splits, uint16_t* dx,
                                                  int64_t dx_step) {
+    __shared__ float s[8][8][32];
     grid_dependency_sync();
-    const int row = blockIdx.x * 32 + threadIdx.x % 32, d = 8 * (blockIdx.y * 8 + threadIdx.x / 32);
-    if (row >= *count || d >= dim) return;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, row = blockIdx.x * 32 + lane, d = 8 * blockIdx.y;
+    const int n = count ? *count : rows;
+    if ((int)blockIdx.x * 32 >= n) return;
     const int64_t part = (int64_t)(padded / 128) * (dim / 4) * 128;
     const float4* from = sums + ((int64_t)(row / 128) * (dim / 4) + d / 4) * 128 + row % 128;
+    const int to = row < n && warp == 0 ? row_of[row] : 0;
     float v[8] = {};
+    if (row < n)
 #pragma unroll 4
-    for (int k = 0; k < splits; ++k, from += part) {
-        const float4 lo = from[0], hi = from[128];
-        const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        for (int k = warp; k < splits; k += 8) {
+            const float4 lo = from[k * part], hi = from[k * part + 128];
+            const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += add[j];
-    }
-    *reinterpret_cast<uint4*>(dx + row_of[row] * dx_step + d) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            for (int j = 0; j < 8; ++j) v[j] += add[j];
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[warp][j][lane] = v[j];
+    __syncthreads();
+    if (warp || row >= n) return;
+    for (int w = 1; w < 8; ++w)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += s[w][j][lane];
+    const uint4 out = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    *reinterpret_cast<uint4*>(dx + (to < 0 ? ~to : to) * dx_step + d) = to < 0 ? make_uint4(0, 0, 0, 0) : out;
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -1010,9 +1079,8 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.weight = take(4 * padded * d.top);
         p.entropy = take(4 * padded);
         p.first = take(padded * (2 * p.tiles + 1));
-    } else {
-        p.target = take(4 * padded);
     }
+    p.target = take(4 * padded);
     if (backward) {
         p.lse2 = take(4 * padded);
         p.coef = take(4 * padded);
@@ -1073,6 +1141,9 @@ struct Call {
 // x as it is can be an operand of the products, unless its rows overlap.
 bool direct_x(const Call& c) { return c.d->rows == 1 || c.x->stride_row >= (int64_t)c.d->dim; }
 
+// Rows that fit one tile stay in their places.
+bool plain_rows(const Call& c) { return c.d->rows <= kTile && direct_x(c); }
+
 uint64_t step_of(const alsgd_matrix& m, uint32_t rows, uint32_t dim) {
     return rows == 1 || m.stride_row == 0 ? (uint64_t)dim : (uint64_t)m.stride_row;
 }
@@ -1099,12 +1170,19 @@ T* at(const Call& c, uint64_t offset) {
     return reinterpret_cast<T*>(static_cast<uint8_t*>(c.work) + offset);
 }
 
+Labels labels_of(const Call& c) {
+    const alsgd_vocab_desc& d = *c.d;
+    return {c.index, c.teacher, d.index_dtype == ALSGD_I64, d.teacher_dtype == ALSGD_BF16, (int)d.rows, (int)d.top, (int)d.vocab};
+}
+
 // Rows that take part, their copies and labels.
 int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx) {
     const alsgd_vocab_desc& d = *c.d;
     GatherArgs g;
     std::memset(&g, 0, sizeof g);
-    g.l = {c.index, c.teacher, d.index_dtype == ALSGD_I64, d.teacher_dtype == ALSGD_BF16, (int)d.rows, (int)d.top, (int)d.vocab};
+    g.l = labels_of(c);
+    g.plain = plain_rows(c);
+    if (g.plain && !d.top) return ALSGD_OK;                        // nothing to do
     g.x = static_cast<const uint16_t*>(c.x->data);
     g.x_step = d.rows == 1 ? 0 : c.x->stride_row;
     g.lse = lse;
@@ -1131,17 +1209,17 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
         g.weight = at<float>(c, p.weight);
         g.entropy = at<float>(c, p.entropy);
         g.first = at<uint8_t>(c, p.first);
-    } else {
-        g.target = at<int>(c, p.target);
     }
+    if (!d.top || g.plain) g.target = at<int>(c, p.target);
     if (lse) {
         g.lse2 = at<float>(c, p.lse2);
         g.coef = at<float>(c, p.coef);
     }
-    if (launch_dependent(count_kernel, dim3(p.count_blocks), dim3(d.top ? 1024 : kCountRows), 0, c.stream, g.l, at<int>(c, p.block_count),
-                         at<int>(c, p.place)) != cudaSuccess)
+    if (!g.plain && launch_dependent(count_kernel, dim3(p.count_blocks), dim3(d.top ? 1024 : kCountRows), 0, c.stream, g.l, at<int>(c, p.block_count),
+                                     at<int>(c, p.place)) != cudaSuccess)
         return ALSGD_E_CUDA;
-    return launch_dependent(gather_kernel, dim3(p.padded / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    const int rows = g.plain ? ((int)d.rows + kGatherWarps - 1) / kGatherWarps * kGatherWarps : p.padded;
+    return launch_dependent(gather_kernel, dim3(rows / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
 int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
@@ -1152,6 +1230,14 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, true, &a->w)) != ALSGD_OK) return rc;
     a->all_rows = direct_x(c) ? (int)d.rows : -1;
     if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 128, true, &a->x_all)) != ALSGD_OK) return rc;
+    a->plain = plain_rows(c);
+    a->rows = (int)d.rows;
+    a->l = labels_of(c);
+    a->scale = d.scale;
+    a->x_rows = static_cast<const uint16_t*>(c.x->data);
+    a->x_step = d.rows == 1 ? 0 : c.x->stride_row;
+    a->xc = at<uint16_t>(c, p.xc);
+    a->row = at<int>(c, p.row);
     a->count = at<int>(c, p.count);
     a->dim = (int)d.dim;
     a->vocab = (int)d.vocab;
@@ -1163,9 +1249,8 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
         a->index = at<int>(c, p.index);
         a->weight = at<float>(c, p.weight);
         a->first = at<uint8_t>(c, p.first);
-    } else {
-        a->target = at<int>(c, p.target);
     }
+    a->target = at<int>(c, p.target);
     return ALSGD_OK;
 }
 
@@ -1206,6 +1291,9 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
         l.entropy = at<float>(c, p.entropy);
         l.index = a.index;
     }
+    l.plain = a.plain;
+    l.l = a.l;
+    l.target = a.target;
     l.slot = at<int>(c, p.slot);
     l.count = a.count;
     l.rows = (int)d.rows;
@@ -1240,12 +1328,17 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     a.lse2 = at<float>(c, p.lse2);
     a.coef = at<float>(c, p.coef);
     a.dz = at<uint8_t>(c, p.dz);
+    a.lse = lse;
+    a.dloss = dloss;
+    a.dloss_step = dloss_step;
     if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, true, &m.x)) != ALSGD_OK) return rc;
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, true, &m.w)) != ALSGD_OK) return rc;
     if ((rc = make_map(a.dz, (uint64_t)p.padded * p.piece * 4, 64, 128, 64, false, &m.dz)) != ALSGD_OK) return rc;
     if ((rc = make_map(dw->data, d.vocab, d.dim, 2 * dw_step, 32, true, &m.dw_map, 32)) != ALSGD_OK) return rc;
     if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, true, &m.x_all)) != ALSGD_OK) return rc;
-    m.all_rows = a.all_rows;
+    m.plain = a.plain;
+    m.rows = a.rows;
+    m.all_rows = a.plain ? -1 : a.all_rows;
     m.count = a.count;
     m.dim = (int)d.dim;
     m.vocab = (int)d.vocab;
@@ -1275,8 +1368,8 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         if (launch_dependent(product_kernel, dim3(grid_of(items)), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
     }
     if (p.splits == 1) return ALSGD_OK;
-    return launch_dependent(dx_kernel, dim3(p.padded / 32, (unsigned)((d.dim + 63) / 64)), dim3(256), 0, c.stream, (const float4*)m.sums, m.count, m.row,
-                            p.padded, (int)d.dim, p.splits, m.dx, m.dx_step) == cudaSuccess
+    return launch_dependent(dx_kernel, dim3((a.plain ? (int)d.rows + 31 : p.padded) / 32, d.dim / 8), dim3(256), 0, c.stream, (const float4*)m.sums,
+                            a.plain ? (const int*)nullptr : m.count, (int)d.rows, m.row, p.padded, (int)d.dim, p.splits, m.dx, m.dx_step) == cudaSuccess
                ? ALSGD_OK
                : ALSGD_E_CUDA;
 }
