@@ -18,18 +18,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMaskedOut = -1e30f;   // a table entry at or below this takes its bucket out
 
-// Division of 0 <= n < 2^31 by a divisor known at the launch: n * ceil(2^shift / d) >> shift with 2^(shift - 31) >= d, which
-// is exact for those n.  A kernel's walk over its items divides in every warp.
-struct Divide {
-    uint32_t factor, shift;
-    __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * factor >> shift); }
-};
-
-inline Divide divide_by(int d) {
-    uint32_t shift = 31;
-    while ((1ull << (shift - 31)) < (uint64_t)d) ++shift;
-    return {(uint32_t)(((1ull << shift) + d - 1) / d), shift};
-}
+using alsgd_ops::Divide;
+using alsgd_ops::divide_by;
 
 struct Shape {
     int batch, heads_q, heads_kv, group, len_q, len_kv, dim;

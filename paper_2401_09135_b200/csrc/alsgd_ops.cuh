@@ -70,6 +70,19 @@ __device__ __forceinline__ void grid_dependency_sync() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// Division of 0 <= n < 2^31 by a divisor known at the launch: n * ceil(2^shift / d) >> shift with 2^(shift - 31) >= d, which
+// is exact for those n.  A kernel's walk over its items divides in every warp.
+struct Divide {
+    uint32_t factor, shift;
+    __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * factor >> shift); }
+};
+
+inline Divide divide_by(int d) {
+    uint32_t shift = 31;
+    while ((1ull << (shift - 31)) < (uint64_t)d) ++shift;
+    return {(uint32_t)(((1ull << shift) + d - 1) / d), shift};
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 

@@ -21,28 +21,10 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// `bar` as at_rank gives it.
+// `bar` as at_rank gives it.  What it announces is tensor memory that has been read (the reads have completed, a
+// tc_fence_before behind them): ordering wider than the block's own would wait for every store in flight, most of a microsecond.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// A wait for arrivals of the other block, bounded as wait() is.
-__device__ __forceinline__ bool bar_test_cluster(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-__device__ __forceinline__ void wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
-    for (uint32_t i = 1; !bar_test_cluster(bar, parity); ++i) {
-        if ((i & 63) != 0) continue;
-        if (*dead) return;
-        if (i >= kWaitTries) {
-            *dead = 1;
-            atomicOr(&g_wait_error, code);
-            return;
-        }
-    }
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tma_load2_pair(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
     asm volatile(

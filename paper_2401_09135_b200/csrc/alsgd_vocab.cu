@@ -354,7 +354,7 @@ __device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS>& p, Ring rin
 template <int STAGES, int SUBS, typename DESC_A, typename DESC_B>
 __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring& ring, uint32_t acc, int subs, int steps, uint32_t desc, DESC_A a, DESC_B b) {
     for (int k = 0; k < steps; ++k) {
-        wait_cluster(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
+        wait(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
         tc_fence_after();
         const uint32_t sa = p.a(ring.stage), sb = p.b(ring.stage);
 #pragma unroll
@@ -362,7 +362,7 @@ __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring&
             if (s >= subs) break;
             const uint32_t buf = (acc + s) & 1;
             if (k == 0) {
-                wait_cluster(p.acc_empty + 8 * buf, (((acc + s) >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
+                wait(p.acc_empty + 8 * buf, (((acc + s) >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
                 tc_fence_after();
             }
 #pragma unroll
@@ -399,6 +399,7 @@ struct LogitArgs {
     int* row;
     int dim, vocab, top;
     int tile0, tiles, all_tiles;       // of the vocabulary: this launch's, all of them
+    Divide by_group;                   // tiles of a group of row tiles
     float scale2;                      // scale * log2 e
     const int* target;
     const int* index;
@@ -414,9 +415,9 @@ struct LogitArgs {
 constexpr int kGroup = 8;              // row tiles whose x stays in the L2 while the words go by
 
 // Tiles in an order that lets the blocks at work share operands: the words' tiles in turn for a group of row tiles.
-__device__ __forceinline__ void tile_at(int i, int row_tiles, int tiles, int& rt, int& ct) {
-    const int group = i / (kGroup * tiles), g0 = group * kGroup, n = min(kGroup, row_tiles - g0), rest = i - g0 * tiles;
-    ct = rest / n;
+__device__ __forceinline__ void tile_at(const LogitArgs& a, int i, int row_tiles, int& rt, int& ct) {
+    const int group = a.by_group(i), g0 = group * kGroup, n = min(kGroup, row_tiles - g0), rest = i - g0 * a.tiles;
+    ct = n == kGroup ? rest / kGroup : n == 1 ? rest : rest / n;
     rt = g0 + rest - ct * n;
 }
 
@@ -495,10 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             Ring ring;
             for (int i = first; i < tiles; i += pairs) {
                 int rt, ct;
-                tile_at(i, row_tiles, a.tiles, rt, ct);
+                tile_at(a, i, row_tiles, rt, ct);
                 const int row = rt * kTile + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
                 for (int k = 0; k < steps; ++k) {
-                    wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    wait(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
                     if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * p.kStageBytes);
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
                     tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
@@ -524,6 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         uint32_t acc = 0;
         if (BACKWARD && a.plain) {
             // for the products behind: zeros in the rows that take no part
+#pragma unroll 4
             for (int r = (warp - 2) * gridDim.x + blockIdx.x; r < a.padded; r += kOutWarps * gridDim.x) {
                 const bool used = r < a.rows && (TOP ? a.target[r] : label_at(a.l, r)) >= 0;
                 for (int c = 8 * lane; c < a.dim; c += 256)
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         }
         for (int i = first; i < tiles; i += pairs, ++acc) {
             int rt, ct;
-            tile_at(i, row_tiles, a.tiles, rt, ct);
+            tile_at(a, i, row_tiles, rt, ct);
             const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
             const int c0 = (a.tile0 + ct) * kTile + half * 128;    // first word
             int label = -1;
@@ -728,6 +730,7 @@ struct ProductArgs {
     int tile0, tiles;                  // of the vocabulary: the piece
     int splits, split_steps;           // of dx's inner axis
     int n, dim_tiles;                  // columns of a tile, tiles of dim
+    Divide by_pairs, by_dim_tiles, by_splits;
     int padded, add, last;             // add: dx's sums so far are read; last: dx is written in place of its sums
     float4* sums;                      // [splits][padded / 128][dim / 4][128]: dx so far, four columns of a row in one place
     const int* row;                    // of a place; ~row: its dx is zero
@@ -757,74 +760,84 @@ struct Item {
 // A pair's items: the longer kind first, dealt in turn; then the shorter kind, at first to the pairs that got one less of the
 // longer, until they are even; what is left over goes out as single tiles where there are pairs for all of them.
 struct Deal {
-    int long_n, short_n, extra, pair, pairs, dx_subs, dw_subs;
     bool dw_long;
-    // only: -1, or the one tile of the item
-    __device__ __forceinline__ bool at(int i, bool& is_dw, int& item, int& only) const {
-        only = -1;
-        const int rest = long_n % pairs, mine = long_n / pairs + (pair < rest);
-        if (i < mine) {
-            is_dw = dw_long;
-            item = pair + i * pairs;
-            return true;
-        }
-        is_dw = !dw_long;
-        i -= mine;
-        const int late = pairs - rest;                             // pairs with one less
-        if (pair >= rest) {
-            if (i < extra) {
-                item = pair - rest + i * late;
-                return item < short_n;
-            }
-            i -= extra;
-        }
-        const int from = extra * late, left = max(0, short_n - from), rounds = left / pairs, over = left - rounds * pairs;
-        item = from + pair + i * pairs;
-        if (i < rounds) return true;
-        if (i > rounds) return false;
-        if ((is_dw ? dw_subs : dx_subs) == 2 && 2 * over <= pairs) {
-            item = from + rounds * pairs + pair / 2;
-            only = pair & 1;
-            return pair < 2 * over;
-        }
-        return pair < over;
-    }
+    int dx_subs, dw_subs, dw_steps, row_tiles, pair, pairs;
+    int longs;                                 // of the longer kind, this pair's
+    int short_n, extra, late, extra_from;      // extra for each of the `late` pairs from extra_from on
+    int from, rounds, over;                    // then these rounds for all pairs, and some left over
+    bool halves;                               // which go out as single tiles
 };
 
-__device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pair, int pairs) {
-    const int row_tiles = (count + kTile - 1) / kTile, dw_steps = (count + kStep - 1) / kStep;
+__device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pair) {
     Deal d;
-    d.dx_subs = row_tiles > 1 && a.split_steps >= kLongSteps ? 2 : 1;
-    d.dw_subs = a.tiles > 1 && dw_steps >= kLongSteps ? 2 : 1;
-    const int dx_n = (row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = (a.tiles + d.dw_subs - 1) / d.dw_subs * a.dim_tiles;
-    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (dw_steps + 4) * d.dw_subs;
-    d.dw_long = dw_cost >= dx_cost;
-    d.long_n = d.dw_long ? dw_n : dx_n;
-    d.short_n = d.dw_long ? dx_n : dw_n;
     d.pair = pair;
-    d.pairs = pairs;
-    const int more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
-    d.extra = d.long_n % pairs ? (more + less / 2) / less : 0;
+    d.pairs = gridDim.x / 2;
+    d.row_tiles = (count + kTile - 1) / kTile;
+    d.dw_steps = (count + kStep - 1) / kStep;
+    d.dx_subs = d.row_tiles > 1 && a.split_steps >= kLongSteps ? 2 : 1;
+    d.dw_subs = a.tiles > 1 && d.dw_steps >= kLongSteps ? 2 : 1;
+    const int dx_n = (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = (a.tiles + d.dw_subs - 1) / d.dw_subs * a.dim_tiles;
+    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (d.dw_steps + 4) * d.dw_subs;
+    d.dw_long = dw_cost >= dx_cost;
+    const int long_n = d.dw_long ? dw_n : dx_n, more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
+    d.short_n = d.dw_long ? dx_n : dw_n;
+    d.longs = a.by_pairs(long_n);
+    const int rest = long_n - d.longs * d.pairs;
+    d.longs += pair < rest;
+    d.extra = rest ? (more + less / 2) / less : 0;
+    d.extra_from = rest;
+    d.late = d.pairs - rest;
+    d.from = d.extra * d.late;
+    const int left = max(0, d.short_n - d.from);
+    d.rounds = a.by_pairs(left);
+    d.over = left - d.rounds * d.pairs;
+    d.halves = (d.dw_long ? d.dx_subs : d.dw_subs) == 2 && 2 * d.over <= d.pairs;
     return d;
 }
 
-__device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int count, int i, Item& t) {
-    int n, only;
-    if (!d.at(i, t.is_dw, n, only)) return false;
-    t.dt = n % a.dim_tiles;
-    n /= a.dim_tiles;
+// The pair's i-th item; false behind its last.
+__device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int i, Item& t) {
+    int n, only = -1;                                              // only: one tile of the item
+    t.is_dw = d.dw_long;
+    if (i < d.longs) {
+        n = d.pair + i * d.pairs;
+    } else {
+        t.is_dw = !d.dw_long;
+        i -= d.longs;
+        const bool late = d.pair >= d.extra_from;
+        if (late && i < d.extra) {
+            n = d.pair - d.extra_from + i * d.late;
+            if (n >= d.short_n) return false;
+        } else {
+            if (late) i -= d.extra;
+            n = d.from + d.pair + i * d.pairs;
+            if (i > d.rounds) return false;
+            if (i == d.rounds) {
+                if (d.halves) {
+                    if (d.pair >= 2 * d.over) return false;
+                    n = d.from + d.rounds * d.pairs + d.pair / 2;
+                    only = d.pair & 1;
+                } else if (d.pair >= d.over) {
+                    return false;
+                }
+            }
+        }
+    }
+    const int m = a.by_dim_tiles(n);
+    t.dt = n - m * a.dim_tiles;
+    n = m;
     t.split = 0;
     t.k0 = 0;
-    t.steps = (count + kStep - 1) / kStep;
+    t.steps = d.dw_steps;
     if (!t.is_dw) {
-        t.split = n % a.splits;
-        n /= a.splits;
+        n = a.by_splits(m);
+        t.split = m - n * a.splits;
         t.k0 = t.split * a.split_steps;
         t.steps = min(a.split_steps, a.tiles * 4 - t.k0);
     }
     t.subs = t.is_dw ? d.dw_subs : d.dx_subs;
     t.rt = n * t.subs;
-    const int end = t.is_dw ? a.tiles : (count + kTile - 1) / kTile;
+    const int end = t.is_dw ? a.tiles : d.row_tiles;
     if (only >= 0) {
         t.rt += only;
         t.subs = 1;
@@ -845,8 +858,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     }
     const Pair<kProductStages, 2> p = pair_begin<kProductStages, 2>(sm.stages, &sm.bars);
     grid_dependency_sync();
-    const int count = a.plain ? a.rows : *a.count, pairs = gridDim.x / 2;
-    const Deal deal = deal_of(a, count, blockIdx.x / 2, pairs);
+    const int count = a.plain ? a.rows : *a.count;
+    const Deal deal = deal_of(a, count, blockIdx.x / 2);
     const int boxes = (a.n / 2 + 63) / 64;                         // of B in either block
 
     if (count == 0) {
@@ -861,10 +874,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             const CUtensorMap* x = count == a.all_rows ? &a.x_all : &a.x;
             Ring ring;
             Item t;
-            for (int i = 0; item_at(a, deal, count, i, t); ++i) {
+            for (int i = 0; item_at(a, deal, i, t); ++i) {
                 const int d0 = t.dt * a.n + p.rank * (a.n / 2), row_blocks = a.tiles * 4;      // of one block's rows
                 for (int k = t.k0; k < t.k0 + t.steps; ++k) {
-                    wait_cluster(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    wait(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
                     if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * (t.subs * kOperandBytes + boxes * 8192));
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
                     for (int s = 0; s < t.subs; ++s) {
@@ -888,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             Ring ring;
             Item t;
             uint32_t acc = 0;
-            for (int i = 0; item_at(a, deal, count, i, t); ++i) {
+            for (int i = 0; item_at(a, deal, i, t); ++i) {
                 if (t.is_dw)
                     tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, true, true),
                                   [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); }, [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
@@ -903,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
         Item t;
         uint32_t acc = 0, boxes_out = 0;
-        for (int i = 0, sub = 0; item_at(a, deal, count, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
+        for (int i = 0, sub = 0; item_at(a, deal, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
             const int row = (t.rt + sub) * kTile + p.rank * 128 + 32 * quad + lane;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
@@ -932,6 +945,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                 tmem_ld32(v, lanes + (acc & 1) * kAccColumns + 32 * c);
                 tmem_wait_ld();
                 tmem_use(v);
+                if (c + 2 >= a.n / 32 || d0 + 64 >= a.dim) tile_taken(p, acc, lane);
                 if (dead) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
@@ -985,7 +999,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                 }
                 ++boxes_out;
             }
-            tile_taken(p, acc, lane);
+            if (half >= a.n / 32 || t.dt * a.n + 32 * half >= a.dim) tile_taken(p, acc, lane);     // nothing was this warp's
         }
         if (lane == 0) bulk_store_wait();
     }
@@ -1279,6 +1293,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
     if ((rc = gather_rows(c, p, nullptr, nullptr, 0, nullptr)) != ALSGD_OK) return rc;
     a.tiles = p.tiles;
+    a.by_group = divide_by(kGroup * a.tiles);
     a.stats = at<float2>(c, p.stats);
     a.label_z = at<float>(c, p.label_z);
     if ((rc = d.top ? launch_logits<false, true>(a, d.device, c.stream) : launch_logits<false, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
@@ -1344,6 +1359,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     m.vocab = (int)d.vocab;
     m.n = p.n;
     m.dim_tiles = p.dim_tiles;
+    m.by_dim_tiles = divide_by(p.dim_tiles);
     m.padded = p.padded;
     m.sums = at<float4>(c, p.dx);
     m.row = at<int>(c, p.row);
@@ -1358,14 +1374,17 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     for (int i = 0; i < p.pieces; ++i) {
         a.tile0 = m.tile0 = i * p.piece;
         a.tiles = m.tiles = p.tiles - a.tile0 < p.piece ? p.tiles - a.tile0 : p.piece;
+        a.by_group = divide_by(kGroup * a.tiles);
         // the first piece writes all of dx's sums; a shorter last one adds to as many as it has steps for
         m.split_steps = p.split_steps;
         m.splits = (4 * m.tiles + p.split_steps - 1) / p.split_steps;
         m.add = i > 0;
         m.last = i + 1 == p.pieces && p.splits == 1;
         if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
-        const int64_t items = (int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles;
-        if (launch_dependent(product_kernel, dim3(grid_of(items)), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
+        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles);
+        m.by_pairs = divide_by(grid / 2);
+        m.by_splits = divide_by(m.splits);
+        if (launch_dependent(product_kernel, dim3(grid), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
     }
     if (p.splits == 1) return ALSGD_OK;
     return launch_dependent(dx_kernel, dim3((a.plain ? (int)d.rows + 31 : p.padded) / 32, d.dim / 8), dim3(256), 0, c.stream, (const float4*)m.sums,
