@@ -437,6 +437,52 @@ __device__ __forceinline__ float pick(const uint32_t (&z)[32], int at) {
     return v;
 }
 
+// The arithmetic on a thread's 32 logits, two at a time where there is an instruction for it.
+__device__ __forceinline__ float largest(const uint32_t (&z)[32], float m) {
+    float part[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        part[g] = max3(__uint_as_float(z[8 * g]), __uint_as_float(z[8 * g + 1]), __uint_as_float(z[8 * g + 2]));
+        part[g] = max3(part[g], __uint_as_float(z[8 * g + 3]), __uint_as_float(z[8 * g + 4]));
+        part[g] = max3(part[g], __uint_as_float(z[8 * g + 5]), __uint_as_float(z[8 * g + 6]));
+    }
+    return max3(max3(part[0], part[1], part[2]), max3(part[3], __uint_as_float(z[7]), __uint_as_float(z[15])),
+                max3(__uint_as_float(z[23]), __uint_as_float(z[31]), m));
+}
+// z <- 2^(z scale + shift)
+__device__ __forceinline__ void exponentials(uint32_t (&z)[32], float scale, float shift) {
+    const uint64_t scale_2 = pack2(scale, scale), shift_2 = pack2(shift, shift);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float lo, hi;
+        unpack2(fma2(pack2(__uint_as_float(z[2 * j]), __uint_as_float(z[2 * j + 1])), scale_2, shift_2), lo, hi);
+        z[2 * j] = __float_as_uint(exp2_fast(lo));
+        z[2 * j + 1] = __float_as_uint(exp2_fast(hi));
+    }
+}
+__device__ __forceinline__ float total(const uint32_t (&z)[32]) {
+    uint64_t part[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        part[g] = pack2(__uint_as_float(z[2 * g]), __uint_as_float(z[2 * g + 1]));
+#pragma unroll
+        for (int j = 1; j < 4; ++j) part[g] = add2(part[g], pack2(__uint_as_float(z[8 * j + 2 * g]), __uint_as_float(z[8 * j + 2 * g + 1])));
+    }
+    float lo, hi;
+    unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), lo, hi);
+    return lo + hi;
+}
+__device__ __forceinline__ void times(uint32_t (&z)[32], float c) {
+    const uint64_t c_2 = pack2(c, c);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float lo, hi;
+        unpack2(mul2(pack2(__uint_as_float(z[2 * j]), __uint_as_float(z[2 * j + 1])), c_2), lo, hi);
+        z[2 * j] = __float_as_uint(lo);
+        z[2 * j + 1] = __float_as_uint(hi);
+    }
+}
+
 // Takes `t` off one of them.
 __device__ __forceinline__ void take_off(uint32_t (&z)[32], int at, float t) {
 #pragma unroll
@@ -562,6 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                     coef = a.coef[row];
                 }
             }
+            const bool all_used = __all_sync(~0u, used);
             float top = -INFINITY, sum = 0.0f;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
@@ -588,17 +635,14 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                         a.label_z[row] = pick(z, label - w0);
                     }
                     __syncwarp();
-                    float m = top;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) m = fmaxf(m, __uint_as_float(z[j]));
-                    const float ref = m == -INFINITY ? 0.0f : m * a.scale2;
+                    const float m = largest(z, top), ref = m == -INFINITY ? 0.0f : m * a.scale2;
                     sum *= exp2_fast(fmaf(top, a.scale2, -ref));
                     top = m;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum += exp2_fast(fmaf(__uint_as_float(z[j]), a.scale2, -ref));
+                    exponentials(z, a.scale2, -ref);
+                    sum += total(z);
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) z[j] = __float_as_uint(coef * exp2_fast(fmaf(__uint_as_float(z[j]), a.scale2, -lse2)));
+                    exponentials(z, a.scale2, -lse2);
+                    times(z, coef);
                     if (TOP) {
                         while (queue.index[0] < w0 + 32) {
                             take_off(z, queue.index[0] - w0, coef * queue.weight[0]);
@@ -609,6 +653,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                     }
                     __syncwarp();
                     if (dead) z[0] = 0x7FC00000u;
+                    // rows that fill the last tile, words behind the last: zeros, whatever the operands hold
+                    if (w0 + 32 > a.vocab || !all_used) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = used && w0 + j < a.vocab ? z[j] : 0;
+                    }
                     if ((c & 1) == 0) {                            // the staged block before this one has left
                         if (lane == 0) tma_store_wait_read();
                         __syncwarp();
@@ -617,13 +666,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                     for (int j = 0; j < 4; ++j) {
                         uint32_t v[4];
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
-                            // rows that fill the last tile, words behind the last: zeros, whatever the operands hold
-                            const int word = w0 + 8 * j + 2 * h;
-                            if (!used || word >= a.vocab) v[h] = 0;
-                            else if (word + 1 >= a.vocab) v[h] &= 0xFFFFu;
-                        }
+                        for (int h = 0; h < 4; ++h) v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
                         const int chunk = 4 * (c & 1) + j;
                         *reinterpret_cast<uint4*>(line + ((chunk ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
