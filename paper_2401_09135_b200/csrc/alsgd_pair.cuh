@@ -31,11 +31,13 @@ __device__ __forceinline__ void tma_load2_pair(uint32_t dst, const CUtensorMap* 
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(dst), "l"(m), "r"(bar), "r"(x), "r"(y) : "memory");
 }
-// 16-byte aligned on both sides, a multiple of 16 bytes.
-__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void tma_load3_pair(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(m), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// Every store of the thread has been written.
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t columns) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(columns) : "memory");
@@ -48,6 +50,11 @@ __device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t columns) 
 __host__ __device__ constexpr uint32_t mma_desc_pair(uint32_t n, bool a_m_major, bool b_n_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((a_m_major ? 1u : 0u) << 15) | ((b_n_major ? 1u : 0u) << 16) | ((n >> 3) << 17) |
            ((256u >> 4) << 24);
+}
+// Shared-memory operands without a swizzle, in groups of 8 x 16 bytes, each 128 bytes in a row: 8 rows of the operand with 8
+// of K each, or 8 of K with 8 rows each (mma_desc_pair's a_m_major).  Bytes to the next 8 of K, to the next 8 rows.
+__device__ __forceinline__ uint64_t desc_plain(uint32_t addr, uint32_t k_step, uint32_t row_step) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(k_step >> 4) << 16) | ((uint64_t)(row_step >> 4) << 32) | (1ull << 46);
 }
 // D (+)= A B; issued by one thread of the first block.
 __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool accumulate) {

@@ -15,7 +15,7 @@
 //
 // The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
 // of either operand, so that a tile needs half of the shared memory traffic of two single ones.  One warp copies, one
-// issues products, eight take the finished tile out of tensor memory while the next one is formed in its other half.
+// issues products, sixteen take the finished tile out of tensor memory while the next one is formed in its other half.
 #include "../../include/alsgd.h"
 #include "alsgd_ops.cuh"
 #include "alsgd_pair.cuh"
@@ -114,7 +114,7 @@ struct GatherArgs {
     int* index;                        // [padded][top] ascending, then places that take no part; teacher only
     float* weight;                     // [padded][top]
     float* entropy;                    // [padded]: sum t log t
-    uint8_t* first;                    // [padded][2 * tiles + 1]: entries below the first word of each half of a tile
+    uint8_t* first;                    // [padded][4 * tiles + 1]: entries below the first word of each quarter of a tile
     float *lse2, *coef;                // [padded]; backward only
 };
 
@@ -123,9 +123,9 @@ constexpr int kGatherWarps = 4;
 // One row's list by one warp: the teacher's softmax over the entries that take part, then the entries in ascending order of
 // their words.
 __device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int slot, bool used, int* words, int* sorted, int lane) {
-    uint8_t* first = a.first + (size_t)slot * (2 * a.tiles + 1);
+    uint8_t* first = a.first + (size_t)slot * (4 * a.tiles + 1);
     if (!used) {
-        for (int t = lane; t <= 2 * a.tiles; t += 32) first[t] = 0;
+        for (int t = lane; t <= 4 * a.tiles; t += 32) first[t] = 0;
         if (a.plain && lane == 0) a.target[slot] = -1;
         return;
     }
@@ -183,8 +183,8 @@ __device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int sl
     for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
     if (lane == 0) a.entropy[slot] = entropy;
     __syncwarp();
-    for (int t = lane; t <= 2 * a.tiles; t += 32) {
-        const int word = min(t * (kTile / 2), a.l.vocab);            // places that take no part are behind every word
+    for (int t = lane; t <= 4 * a.tiles; t += 32) {
+        const int word = min(t * (kTile / 4), a.l.vocab);            // places that take no part are behind every word
         int low = 0, high = a.l.top;
         while (low < high) {
             const int mid = (low + high) / 2;
@@ -255,11 +255,11 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
 
 // ---------------------------------------------------------------------------------------------- the pair's machinery
 
-constexpr int kThreads = 320;          // copies, products, eight warps that take tiles out
-constexpr int kOutWarps = 8;
+constexpr int kOutWarps = 16;          // that take tiles out, four for each quarter of the columns
+constexpr int kThreads = 64 + 32 * kOutWarps;                 // and one that copies, one that issues products
 constexpr int kOperandBytes = 16384;   // of a block in a stage: 128 x 64 of A, up to 128 x 64 of B
 constexpr int kAccColumns = 256;
-constexpr int kStagingBytes = 4096;    // of a warp: 32 rows of 64 bf16
+constexpr int kPart = kTile / 4;       // columns of a warp
 
 template <int STAGES>
 struct Bars {
@@ -406,10 +406,11 @@ struct LogitArgs {
     const float* weight;
     const uint8_t* first;
     int padded;
-    float2* stats;                     // forward: [2 * all_tiles][padded]: maximum of z / scale, sum of exponentials
+    float2* stats;                     // forward: [all_tiles][padded]: maximum of z / scale, sum of exponentials
     float* label_z;                    // forward: [padded][max(1, top)]: z / scale at the labels
     const float *lse2, *coef;          // backward
-    uint8_t* dz;                       // backward: blocks of 128 rows x 64 words, [row block][word block]
+    uint8_t* dz;                       // backward: blocks of 128 rows x 64 words, [row block][word block][8 words][row]: a warp's
+                                       // stores, the copies and the products of either direction all see 16-byte pieces in a row
 };
 
 constexpr int kGroup = 8;              // row tiles whose x stays in the L2 while the words go by
@@ -421,12 +422,12 @@ __device__ __forceinline__ void tile_at(const LogitArgs& a, int i, int row_tiles
     rt = g0 + rest - ct * n;
 }
 
-constexpr int kLogitStages = 6;
-
+template <bool BACKWARD>
 struct LogitSmem {
-    uint8_t stages[kLogitStages * 2 * kOperandBytes];
-    uint8_t staging[kOutWarps * kStagingBytes];
-    Bars<kLogitStages> bars;
+    static constexpr int kStages = BACKWARD ? 7 : 6;
+    uint8_t stages[kStages * 2 * kOperandBytes];
+    float2 stats[BACKWARD ? 1 : 2 * 4 * 128];                      // forward: of a tile, in turn: by part, by row
+    Bars<kStages> bars;
 };
 
 // Replaces / reads the value of one of 32 registers, chosen at run time.
@@ -525,13 +526,15 @@ struct LabelQueue {
 template <bool BACKWARD, bool TOP>
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_kernel(const __grid_constant__ LogitArgs a) {
     extern __shared__ uint8_t raw[];
-    LogitSmem& sm = *reinterpret_cast<LogitSmem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    using Smem = LogitSmem<BACKWARD>;
+    constexpr int STAGES = Smem::kStages;
+    Smem& sm = *reinterpret_cast<Smem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
-    const Pair<kLogitStages, 1> p = pair_begin<kLogitStages, 1>(sm.stages, &sm.bars);
+    const Pair<STAGES, 1> p = pair_begin<STAGES, 1>(sm.stages, &sm.bars);
     grid_dependency_sync();
     const int count = a.plain ? a.rows : *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
     const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / 2, pairs = gridDim.x / 2;
@@ -550,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
                     tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
                     tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
-                    ring.next<kLogitStages>();
+                    ring.next<STAGES>();
                 }
             }
             ring_drain(p, ring);
@@ -564,10 +567,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                               [](uint32_t s, int i) { return desc_k_major(s + 32 * i); });
         }
     } else {
-        const int quad = warp & 3, half = (warp - 2) / 4;          // tensor memory's lanes that the warp may read; the tile's columns
+        const int quad = warp & 3, part = (warp - 2) / 4;          // tensor memory's lanes that the warp may read; the tile's columns
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
-        const uint32_t staging = smem_u32(sm.staging) + (warp - 2) * kStagingBytes;
-        uint8_t* const line = sm.staging + (warp - 2) * kStagingBytes + lane * 128;
         uint32_t acc = 0;
         if (BACKWARD && a.plain) {
             // for the products behind: zeros in the rows that take no part
@@ -583,12 +584,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             int rt, ct;
             tile_at(a, i, row_tiles, rt, ct);
             const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
-            const int c0 = (a.tile0 + ct) * kTile + half * 128;    // first word
+            const int c0 = (a.tile0 + ct) * kTile + part * kPart;  // first word
             int label = -1;
             LabelQueue queue;
             const size_t list = (size_t)row * a.top;
             if (TOP) {
-                const uint8_t* f = a.first + (size_t)row * (2 * a.all_tiles + 1) + 2 * (a.tile0 + ct) + half;
+                const uint8_t* f = a.first + (size_t)row * (4 * a.all_tiles + 1) + 4 * (a.tile0 + ct) + part;
                 const bool listed = row < count;                   // what fills the tile up has no list
                 queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, listed ? f[0] : 0, listed ? f[1] : 0);
             }
@@ -614,12 +615,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             tc_fence_after();
             const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
                 uint32_t z[32];
-                tmem_ld32(z, lanes + (acc & 1) * kAccColumns + half * 128 + 32 * c);
+                tmem_ld32(z, lanes + (acc & 1) * kAccColumns + part * kPart + 32 * c);
                 tmem_wait_ld();
                 tmem_use(z);
-                if (c == 3) tile_taken(p, acc, lane);
+                if (c == 1) tile_taken(p, acc, lane);
                 const int w0 = c0 + 32 * c;
                 if (!BACKWARD) {
                     if (w0 + 32 > a.vocab) {                       // words behind the last have no logits
@@ -658,32 +659,31 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z[j] = used && w0 + j < a.vocab ? z[j] : 0;
                     }
-                    if ((c & 1) == 0) {                            // the staged block before this one has left
-                        if (lane == 0) tma_store_wait_read();
-                        __syncwarp();
-                    }
+                    uint8_t* const to = a.dz + ((size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4 + part) * 16384 + block_row * 16;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t v[4];
 #pragma unroll
                         for (int h = 0; h < 4; ++h) v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
-                        const int chunk = 4 * (c & 1) + j;
-                        *reinterpret_cast<uint4*>(line + ((chunk ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                    }
-                    if (c & 1) {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            const size_t block = (size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4 + half * 2 + c / 2;
-                            bulk_store(a.dz + block * 16384 + quad * 4096, staging, kStagingBytes);
-                            tma_store_commit();
-                        }
+                        *reinterpret_cast<uint4*>(to + (4 * c + j) * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
-            if (!BACKWARD) a.stats[(size_t)(2 * (a.tile0 + ct) + half) * a.padded + row] = make_float2(top, dead ? NAN : sum);
+            if (!BACKWARD) {
+                // the parts' sums of a row become one
+                float2* const stats = sm.stats + (acc & 1) * 512 + block_row;
+                stats[128 * part] = make_float2(top, dead ? NAN : sum);
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + quad) : "memory");
+                if (part == 0) {
+                    const float2 o[3] = {stats[128], stats[256], stats[384]};
+                    const float m = max3(top, o[0].x, fmaxf(o[1].x, o[2].x)), ref = m == -INFINITY ? 0.0f : m * a.scale2;
+                    sum *= exp2_fast(fmaf(top, a.scale2, -ref));
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) sum += o[q].y * exp2_fast(fmaf(o[q].x, a.scale2, -ref));
+                    a.stats[(size_t)(a.tile0 + ct) * a.padded + row] = make_float2(m, dead ? NAN : sum);
+                }
+            }
         }
-        if (BACKWARD && lane == 0) bulk_store_wait();
     }
     pair_end(p);
 }
@@ -699,7 +699,7 @@ struct LossArgs {
     int plain;                         // rows stay in their places
     Labels l;
     const int* target;
-    int rows, padded, parts, top;      // parts: 2 * tiles
+    int rows, padded, parts, top;      // parts: tiles of the vocabulary
     float scale, scale2;
     float *loss, *lse;
 };
@@ -764,7 +764,8 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
 // ---------------------------------------------------------------------------------------------- dx += dz w, dw = dz^T x
 
 struct ProductArgs {
-    CUtensorMap dz, x, x_all, w;       // boxes of 64 x 64; dz's rows are those of its blocks; x as for the logits
+    CUtensorMap dz_block, dz_half;     // dz's blocks: all of one, or half of its rows
+    CUtensorMap x, x_all, w;           // boxes of 64 x 64; x as for the logits
     CUtensorMap dw_map;                // boxes of 32 x 32
     const int* count;
     int all_rows;
@@ -791,7 +792,7 @@ constexpr int kLongSteps = 16;
 
 struct ProductSmem {
     uint8_t stages[kProductStages * 3 * kOperandBytes];
-    uint8_t staging[kOutWarps * kStagingBytes];
+    uint8_t staging[kOutWarps * 2048];
     Bars<kProductStages> bars;
 };
 
@@ -895,7 +896,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     ProductSmem& sm = *reinterpret_cast<ProductSmem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
-        tma_prefetch(&a.dz);
+        tma_prefetch(&a.dz_block);
+        tma_prefetch(&a.dz_half);
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
@@ -926,11 +928,14 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                     for (int s = 0; s < t.subs; ++s) {
                         const uint32_t to = p.a(ring.stage) + s * kOperandBytes;
                         // dw: 64 rows x 128 words, half of each of two blocks; dx: 128 rows x 64 words, a whole block
-                        const int64_t block = t.is_dw ? (int64_t)(k / 2) * row_blocks + (t.rt + s) * 4 + p.rank * 2
-                                                      : (int64_t)((t.rt + s) * 2 + p.rank) * row_blocks + k;
-                        const int y = (int)(block * 128) + (t.is_dw ? (k & 1) * 64 : 0);
-                        tma_load2_pair(to, &a.dz, full, 0, y);
-                        tma_load2_pair(to + 8192, &a.dz, full, 0, y + (t.is_dw ? 128 : 64));
+                        if (t.is_dw) {
+                            const int block = (k / 2) * row_blocks + (t.rt + s) * 4 + p.rank * 2;
+                            tma_load3_pair(to, &a.dz_half, full, 0, (k & 1) * 8, block * 8);
+                            tma_load3_pair(to + 8192, &a.dz_half, full, 0, (k & 1) * 8, block * 8 + 8);
+                        } else {
+                            const int block = ((t.rt + s) * 2 + p.rank) * row_blocks + k;
+                            tma_load3_pair(to, &a.dz_block, full, 0, 0, block * 8);
+                        }
                     }
                     for (int b = 0; b < boxes; ++b)
                         tma_load2_pair(p.b(ring.stage) + b * 8192, t.is_dw ? x : &a.w, full, d0 + 64 * b, t.is_dw ? k * kStep : a.tile0 * kTile + k * kStep);
@@ -947,18 +952,21 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             for (int i = 0; item_at(a, deal, i, t); ++i) {
                 if (t.is_dw)
                     tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, true, true),
-                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); }, [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
+                                  [](uint32_t s, int i) { return desc_plain(s + 256 * i, 128, 1024); },
+                                  [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
                 else
-                    tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, false, true), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+                    tile_products(p, ring, acc, t.subs, t.steps, mma_desc_pair(a.n, false, true),
+                                  [](uint32_t s, int i) { return desc_plain(s + 4096 * i, 2048, 128); },
                                   [](uint32_t s, int i) { return desc_n_major(s + 2048 * i, 8192); });
                 acc += t.subs;
             }
         }
     } else {
-        const int quad = warp & 3, half = (warp - 2) / 4;
+        const int quad = warp & 3, part = (warp - 2) / 4;
+        uint8_t* const box = sm.staging + (warp - 2) * 2048;
         const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
         Item t;
-        uint32_t acc = 0, boxes_out = 0;
+        uint32_t acc = 0;
         for (int i = 0, sub = 0; item_at(a, deal, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
             const int row = (t.rt + sub) * kTile + p.rank * 128 + 32 * quad + lane;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
@@ -977,7 +985,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                     zero[r] = at < 0;
                     to[r] = place < count ? (at < 0 ? ~at : at) * a.dx_step : -1;
                 }
-            for (int c = half; c < a.n / 32; c += 2) {
+            for (int c = part; c < a.n / 32; c += 4) {
                 const int d0 = t.dt * a.n + 32 * c;
                 if (d0 >= a.dim) break;
                 float4 before[8];
@@ -988,7 +996,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                 tmem_ld32(v, lanes + (acc & 1) * kAccColumns + 32 * c);
                 tmem_wait_ld();
                 tmem_use(v);
-                if (c + 2 >= a.n / 32 || d0 + 64 >= a.dim) tile_taken(p, acc, lane);
+                if (c + 4 >= a.n / 32 || d0 + 128 >= a.dim) tile_taken(p, acc, lane);
                 if (dead) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
@@ -1012,9 +1020,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                     __syncwarp();
                     continue;
                 }
-                // 32 rows of 64 bytes, in the 64-byte swizzle that the tensor map reads, in one of two places
-                uint8_t* const box = sm.staging + (warp - 2) * kStagingBytes + (boxes_out & 1) * 2048;
-                if (lane == 0) tma_store_wait_read_1();
+                // 32 rows of 64 bytes, in the 64-byte swizzle that the tensor map reads, when those before have left
+                if (lane == 0) tma_store_wait_read();
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -1040,11 +1047,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                         if (to[r] >= 0 && d0 + at < a.dim) *reinterpret_cast<uint4*>(a.dx + to[r] + d0 + at) = zero[r] ? make_uint4(0, 0, 0, 0) : w;
                     }
                 }
-                ++boxes_out;
             }
-            if (half >= a.n / 32 || t.dt * a.n + 32 * half >= a.dim) tile_taken(p, acc, lane);     // nothing was this warp's
+            if (part >= a.n / 32 || t.dt * a.n + 32 * part >= a.dim) tile_taken(p, acc, lane);     // nothing was this warp's
         }
-        if (lane == 0) bulk_store_wait();
+        if (lane == 0) tma_store_wait();
     }
     pair_end(p);
 }
@@ -1135,7 +1141,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.index = take(4 * padded * d.top);
         p.weight = take(4 * padded * d.top);
         p.entropy = take(4 * padded);
-        p.first = take(padded * (2 * p.tiles + 1));
+        p.first = take(padded * (4 * p.tiles + 1));
     }
     p.target = take(4 * padded);
     if (backward) {
@@ -1144,7 +1150,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.dz = take(tile_bytes * p.piece);
         p.dx = take(4ull * p.splits * padded * d.dim);
     } else {
-        p.stats = take(16 * padded * p.tiles);
+        p.stats = take(8 * padded * p.tiles);
         p.label_z = take(4 * padded * p.labels);
     }
     p.bytes = at;
@@ -1173,17 +1179,27 @@ int check_matrix(const alsgd_matrix* m, uint32_t rows, uint32_t dim, bool output
     return ALSGD_OK;
 }
 
-// Boxes of 64 (or 32) columns x box_rows rows of a bf16 matrix, swizzled over their 128-byte (64-byte) rows, or as they are; zeros
-// outside.
-int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t step_bytes, uint32_t box_rows, bool swizzle, CUtensorMap* out, uint32_t box_cols = 64) {
+int encode_map(uint32_t rank, const void* data, const cuuint64_t* size, const cuuint64_t* step_bytes, const cuuint32_t* box, CUtensorMapSwizzle swizzle, CUtensorMap* out) {
     EncodeTiled encode = encode_tiled();
     if (!encode) return ALSGD_E_CUDA;
-    const cuuint64_t size[2] = {cols, rows}, bytes[1] = {step_bytes};
-    const cuuint32_t box[2] = {box_cols, box_rows}, unit[2] = {1, 1};
-    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(data), size, bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint32_t unit[3] = {1, 1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(data), size, step_bytes, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? ALSGD_OK : ALSGD_E_ARG;
+}
+
+// Boxes of 64 columns x box_rows rows of a bf16 matrix, swizzled over their 128-byte rows; zeros outside.
+int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t step_bytes, uint32_t box_rows, CUtensorMap* out) {
+    const cuuint64_t size[2] = {cols, rows};
+    const cuuint32_t box[2] = {64, box_rows};
+    return encode_map(2, data, size, &step_bytes, box, CU_TENSOR_MAP_SWIZZLE_128B, out);
+}
+
+// dz's blocks as [block * 8 words][8 rows][64 values]: `groups` of the 16 groups of rows of a block.
+int make_dz_map(const void* data, uint64_t blocks, uint32_t groups, CUtensorMap* out) {
+    const cuuint64_t size[3] = {64, 16, 8 * blocks}, step_bytes[2] = {128, 2048};
+    const cuuint32_t box[3] = {64, groups, 8};
+    return encode_map(3, data, size, step_bytes, box, CU_TENSOR_MAP_SWIZZLE_NONE, out);
 }
 
 struct Call {
@@ -1283,10 +1299,10 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
     const alsgd_vocab_desc& d = *c.d;
     std::memset(a, 0, sizeof *a);
     int rc;
-    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 128, true, &a->x)) != ALSGD_OK) return rc;
-    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, true, &a->w)) != ALSGD_OK) return rc;
+    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 128, &a->x)) != ALSGD_OK) return rc;
+    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, &a->w)) != ALSGD_OK) return rc;
     a->all_rows = direct_x(c) ? (int)d.rows : -1;
-    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 128, true, &a->x_all)) != ALSGD_OK) return rc;
+    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 128, &a->x_all)) != ALSGD_OK) return rc;
     a->plain = plain_rows(c);
     a->rows = (int)d.rows;
     a->l = labels_of(c);
@@ -1316,7 +1332,7 @@ int grid_of(int64_t tiles) { return 2 * (int)(tiles < kPairs ? tiles : kPairs); 
 template <bool BACKWARD, bool TOP>
 int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
     static SmemLimit limit;
-    constexpr size_t smem = sizeof(LogitSmem) + 1024;
+    constexpr size_t smem = sizeof(LogitSmem<BACKWARD>) + 1024;
     if (!limit.raise(logit_kernel<BACKWARD, TOP>, device, smem)) return ALSGD_E_CUDA;
     const int64_t tiles = (int64_t)(a.padded / kTile) * a.tiles;
     return launch_dependent(logit_kernel<BACKWARD, TOP>, dim3(grid_of(tiles)), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
@@ -1356,7 +1372,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     l.count = a.count;
     l.rows = (int)d.rows;
     l.padded = p.padded;
-    l.parts = 2 * p.tiles;
+    l.parts = p.tiles;
     l.top = (int)d.top;
     l.scale = d.scale;
     l.scale2 = a.scale2;
@@ -1389,11 +1405,16 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     a.lse = lse;
     a.dloss = dloss;
     a.dloss_step = dloss_step;
-    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, true, &m.x)) != ALSGD_OK) return rc;
-    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, true, &m.w)) != ALSGD_OK) return rc;
-    if ((rc = make_map(a.dz, (uint64_t)p.padded * p.piece * 4, 64, 128, 64, false, &m.dz)) != ALSGD_OK) return rc;
-    if ((rc = make_map(dw->data, d.vocab, d.dim, 2 * dw_step, 32, true, &m.dw_map, 32)) != ALSGD_OK) return rc;
-    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, true, &m.x_all)) != ALSGD_OK) return rc;
+    if ((rc = make_map(at<void>(c, p.xc), p.padded, d.dim, 2ull * d.dim, 64, &m.x)) != ALSGD_OK) return rc;
+    if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, &m.w)) != ALSGD_OK) return rc;
+    const uint64_t blocks = (uint64_t)(p.padded / 128) * p.piece * 4;
+    if ((rc = make_dz_map(a.dz, blocks, 16, &m.dz_block)) != ALSGD_OK || (rc = make_dz_map(a.dz, blocks, 8, &m.dz_half)) != ALSGD_OK) return rc;
+    {
+        const cuuint64_t size[2] = {d.dim, d.vocab}, step_bytes = 2 * dw_step;
+        const cuuint32_t box[2] = {32, 32};
+        if ((rc = encode_map(2, dw->data, size, &step_bytes, box, CU_TENSOR_MAP_SWIZZLE_64B, &m.dw_map)) != ALSGD_OK) return rc;
+    }
+    if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, &m.x_all)) != ALSGD_OK) return rc;
     m.plain = a.plain;
     m.rows = a.rows;
     m.all_rows = a.plain ? -1 : a.all_rows;
