@@ -18,7 +18,9 @@ using namespace alsgd_ops;
 
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
-constexpr int kUnits = 4;              // units of 16 elements that a thread has in flight
+// Units of 16 elements that a thread has in flight, with five blocks per SM: 23.0 us at 64 x 256 tokens and 32 heads of 64, 33.3 at
+// 4 x 4099 tokens and 20 heads of 128 (5.8 and 5.0 TB/s).  Four units, four blocks: 24.2 and 35.0; two and six: 25.9 and 33.0 (spills).
+constexpr int kUnits = 2;
 constexpr int kMaxTokens = 16;         // of a block
 
 struct RopeArgs {
@@ -30,6 +32,7 @@ struct RopeArgs {
     int64_t pos0;
     int len, heads_q, heads, dim, rot, interleaved, tokens, per_block;
     int units, angles;                 // of a head
+    Divide by_token, by_units, by_len, by_angles;                  // units of a token, of a head; tokens of a sequence; angles
     float amplitude, turn;             // turn: 1, or -1 for the inverse
     double turns[kMaxDim / 2];         // f_i / (2 pi)
 };
@@ -81,9 +84,9 @@ __device__ __forceinline__ void turn_pair(float2 cs, float& a, float& b) {
 // Cosine and sine (times the amplitude) of the block's tokens, [token][angle].
 __device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, int token0, int tokens) {
     for (int i = threadIdx.x; i < tokens * a.angles; i += kThreads) {
-        const int t = i / a.angles, n = i - t * a.angles, token = token0 + t;
+        const int t = a.by_angles(i), n = i - t * a.angles, token = token0 + t;
         int64_t pos;
-        if (!a.positions) pos = a.pos0 + token % a.len;
+        if (!a.positions) pos = a.pos0 + token - a.by_len(token) * a.len;
         else pos = a.wide_positions ? static_cast<const int64_t*>(a.positions)[token] : static_cast<const int32_t*>(a.positions)[token];
         const double turns = (double)pos * a.turns[n];
         float s, c;
@@ -93,36 +96,41 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, in
 }
 
 // Where a unit's two groups of eight elements start; one that starts at dim or beyond does not exist.
-//   interleaved: 16 elements in a row.  half: eight of either half of the turned part, then the rest in a row.
+//   half: eight of either half of the turned part, then eight of either half of the rest.  interleaved: of either half of the
+//   head.  Neighbouring threads take neighbouring groups: 32 bytes a thread in a row took 39 us in place of 35.5 (4 x 4099
+//   tokens, 20 heads of 128, half of each turned).
 struct Unit {
-    int64_t from, to;                  // of the head's first element
+    int64_t batch, pos, head;          // to be multiplied by steps
     int at[2];
     int token, n;                      // token of the block, unit of the head
     bool is_q;
+    __device__ __forceinline__ int64_t offset(const int64_t (&step)[3]) const { return batch * step[0] + pos * step[1] + head * step[2]; }
 };
+// (Plain divisions and remainders here bounded the kernel by its instructions: 33 us at 64 x 256 tokens against 26 with
+// reciprocals.)
 __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
     Unit u;
-    const int per_token = a.heads * a.units;
-    u.token = i / per_token;
-    const int rest = i - u.token * per_token;
-    int head = rest / a.units;
+    u.token = a.by_token(i);
+    const int rest = i - u.token * (a.heads * a.units), head = a.by_units(rest);
     u.n = rest - head * a.units;
-    const int token = token0 + u.token, b = token / a.len, s = token - b * a.len;
+    const int token = token0 + u.token, b = a.by_len(token);
+    u.batch = b;
+    u.pos = token - b * a.len;
     u.is_q = head < a.heads_q;
-    const int64_t* from = u.is_q ? a.q_step : a.k_step;
-    const int64_t* to = u.is_q ? a.q_out_step : a.k_out_step;
-    if (!u.is_q) head -= a.heads_q;
-    u.from = b * from[0] + s * from[1] + head * from[2];
-    u.to = b * to[0] + s * to[1] + head * to[2];
-    const int turned = a.rot / 16;
-    const bool halves = !a.interleaved && u.n < turned;
-    u.at[0] = halves ? 8 * u.n : 16 * u.n;
-    u.at[1] = halves ? a.rot / 2 + 8 * u.n : u.at[0] + 8;
+    u.head = u.is_q ? head : head - a.heads_q;
+    const int turned = a.interleaved ? 0 : a.rot / 16;
+    if (u.n < turned) {
+        u.at[0] = 8 * u.n;
+        u.at[1] = a.rot / 2 + u.at[0];
+    } else {
+        u.at[0] = 8 * (u.n + turned);                              // behind 2 * turned groups
+        u.at[1] = u.at[0] + 8 * (a.units - turned);
+    }
     return u;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
     extern __shared__ float2 table[];
     grid_dependency_sync();
     const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
@@ -136,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
             const Unit u = unit_of(a, token0, i);
-            const T* p = static_cast<const T*>(u.is_q ? a.q : a.k) + u.from;
+            const T* p = u.is_q ? static_cast<const T*>(a.q) + u.offset(a.q_step) : static_cast<const T*>(a.k) + u.offset(a.k_step);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (u.at[h] < a.dim) load8(p + u.at[h], raw[j][h]);
@@ -151,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
             const Unit u = unit_of(a, token0, i);
-            T* p = static_cast<T*>(u.is_q ? a.q_out : a.k_out) + u.to;
+            T* p = u.is_q ? static_cast<T*>(a.q_out) + u.offset(a.q_out_step) : static_cast<T*>(a.k_out) + u.offset(a.k_out_step);
             const float2* cs = table + u.token * a.angles;
             Eight e[2] = {widen(p, raw[j][0]), widen(p, raw[j][1])};
             if (a.interleaved) {
@@ -162,7 +170,6 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
                         const int pair = u.at[h] / 2 + x;
                         if (pair < a.angles) turn_pair(cs[pair], e[h].v[2 * x], e[h].v[2 * x + 1]);
                     }
-                if (!copies && u.at[0] >= a.rot) continue;
             } else if (u.n < a.rot / 16) {
 #pragma unroll
                 for (int x = 0; x < 8; ++x) turn_pair(cs[8 * u.n + x], e[0].v[x], e[1].v[x]);
@@ -317,9 +324,13 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     for (int i = 0; i < a.angles; ++i) a.turns[i] *= 1.0 / 6.283185307179586476925;
     const bool by_element = !a.interleaved && a.rot % 16;
     a.units = (a.dim + 15) / 16;
+    a.by_token = divide_by(a.heads * a.units);
+    a.by_units = divide_by(a.units);
+    a.by_len = divide_by(a.len);
+    a.by_angles = divide_by(a.angles);
     // enough tokens for every thread's kUnits, but no fewer than two blocks per SM as long as there are tokens for them
     const int per_token = a.heads * a.units;
-    a.per_block = (kThreads * kUnits + per_token - 1) / per_token;
+    a.per_block = kThreads * kUnits / per_token;
     if (a.per_block > a.tokens / (2 * kSMs)) a.per_block = a.tokens / (2 * kSMs);
     if (a.per_block > kMaxTokens) a.per_block = kMaxTokens;
     if (a.per_block < 1) a.per_block = 1;
