@@ -549,7 +549,8 @@ int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out);
  *     dx_i = sum_j dz[i][j] w_j,   dw_j = sum_i dz[i][j] x_i
  * Logits, sums and statistics are binary32; dz is rounded to bf16 before the products with w and x.  Results are written, not
  * added to, and do not depend on the order in which blocks run.  The workspace holds a copy of the rows that take part and,
- * backward, dz of a piece of the vocabulary: 256 MiB, or 8 KiB a row where that is more, and sums of dx.
+ * backward, dz of a piece of the vocabulary (256 MiB, or 8 KiB a row where that is more) and sums of dx and dw (256 MiB of
+ * either, or one of dx where that is more).
  * A NaN or infinity in w or in the x of a row that takes part reaches what is computed from it: the row's loss, all of dw. */
 typedef struct alsgd_vocab_desc {
     uint32_t rows;                     /* up to 2^22; may be 0 */

@@ -9,7 +9,7 @@
 // workspace's size), then dx += dz w and dw = dz^T x in one launch.
 //
 // The rows that take part are gathered first (a padded batch pays for its tokens, not for its padding; what the other rows
-// hold reaches nothing) and everything behind works on their number, which only the device knows.  One tile's worth of rows or
+// hold reaches nothing) and everything behind works on their number, which only the device knows.  Two tiles' worth of rows or
 // fewer stay where they are: there is nothing to save, and the two launches in front would cost more than the rest
 // (forward of 77 rows x 32000 words x 384: 16.6 -> 13.1 us).
 //
@@ -20,7 +20,7 @@
 #include "alsgd_ops.cuh"
 #include "alsgd_pair.cuh"
 
-#include <cfloat>
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(1024) count_kernel(Labels l, int* block_count,
         const size_t from = (size_t)r0 * l.top;
 #pragma unroll 8
         for (int i = threadIdx.x; i < n; i += 1024)
-            if (label_at(l, from + i) >= 0 && teacher_at(l, from + i) != -INFINITY) any[i / l.top] = 1;
+            if ((label_at(l, from + i) >= 0) & (teacher_at(l, from + i) != -INFINITY)) any[i / l.top] = 1;
         __syncthreads();
         if (threadIdx.x >= kCountRows) return;
         mine = any[threadIdx.x];
@@ -183,14 +183,14 @@ __device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int sl
     for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
     if (lane == 0) a.entropy[slot] = entropy;
     __syncwarp();
+#pragma unroll 4
     for (int t = lane; t <= 4 * a.tiles; t += 32) {
-        const int word = min(t * (kTile / 4), a.l.vocab);            // places that take no part are behind every word
-        int low = 0, high = a.l.top;
-        while (low < high) {
-            const int mid = (low + high) / 2;
-            if (sorted[mid] < word) low = mid + 1;
-            else high = mid;
-        }
+        const int word = min(t * (kTile / 4), a.l.vocab);          // places that take no part are behind every word
+        int low = 0;
+#pragma unroll
+        for (int step = kMaxTop / 2; step; step /= 2)
+            if (low + step <= a.l.top && sorted[low + step - 1] < word) low += step;
+        if (low < a.l.top && sorted[low] < word) ++low;            // the steps add up to one less than the longest list
         first[t] = (uint8_t)low;
     }
 }
@@ -772,11 +772,13 @@ struct ProductArgs {
     int plain, rows;                   // rows stay in their places
     int dim, vocab;
     int tile0, tiles;                  // of the vocabulary: the piece
-    int splits, split_steps;           // of dx's inner axis
+    int dx_subs, splits, split_steps;  // dx: tiles of an item (where there are as many), parts of the inner axis
+    int dw_subs, dw_splits, dw_split_steps, dw_groups;             // dw: the same; items of one part and column
     int n, dim_tiles;                  // columns of a tile, tiles of dim
-    Divide by_pairs, by_dim_tiles, by_splits;
+    Divide by_pairs, by_dim_tiles, by_splits, by_dw_groups;
     int padded, add, last;             // add: dx's sums so far are read; last: dx is written in place of its sums
     float4* sums;                      // [splits][padded / 128][dim / 4][128]: dx so far, four columns of a row in one place
+    float4* dw_sums;                   // [dw_splits][2 * tiles][dim / 4][128], where dw has several parts
     const int* row;                    // of a place; ~row: its dx is zero
     uint16_t* dx;
     int64_t dx_step;
@@ -788,7 +790,7 @@ struct ProductArgs {
 // two tiles instead of 128, and what a pair can draw from the L2 (about 100 bytes a cycle) is what bounds the steps.  Both
 // halves of tensor memory belong to one item then, which its way out is not hidden behind: not worth it for short inner axes.
 constexpr int kProductStages = 4;
-constexpr int kLongSteps = 16;
+constexpr int kLongSteps = 16;          // fewer: one tile
 
 struct ProductSmem {
     uint8_t stages[kProductStages * 3 * kOperandBytes];
@@ -805,7 +807,7 @@ struct Item {
 // longer, until they are even; what is left over goes out as single tiles where there are pairs for all of them.
 struct Deal {
     bool dw_long;
-    int dx_subs, dw_subs, dw_steps, row_tiles, pair, pairs;
+    int dx_subs, dw_steps, row_tiles, pair, pairs;
     int longs;                                 // of the longer kind, this pair's
     int short_n, extra, late, extra_from;      // extra for each of the `late` pairs from extra_from on
     int from, rounds, over;                    // then these rounds for all pairs, and some left over
@@ -818,10 +820,11 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
     d.pairs = gridDim.x / 2;
     d.row_tiles = (count + kTile - 1) / kTile;
     d.dw_steps = (count + kStep - 1) / kStep;
-    d.dx_subs = d.row_tiles > 1 && a.split_steps >= kLongSteps ? 2 : 1;
-    d.dw_subs = a.tiles > 1 && d.dw_steps >= kLongSteps ? 2 : 1;
-    const int dx_n = (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = (a.tiles + d.dw_subs - 1) / d.dw_subs * a.dim_tiles;
-    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (d.dw_steps + 4) * d.dw_subs;
+    d.dx_subs = d.row_tiles > 1 ? a.dx_subs : 1;
+    // parts of dw that have steps
+    const int dw_parts = a.dw_splits == 1 ? 1 : (d.dw_steps + a.dw_split_steps - 1) / a.dw_split_steps;
+    const int dx_n = (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = dw_parts * a.dw_groups * a.dim_tiles;
+    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (min(d.dw_steps, a.dw_split_steps) + 4) * a.dw_subs;
     d.dw_long = dw_cost >= dx_cost;
     const int long_n = d.dw_long ? dw_n : dx_n, more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
     d.short_n = d.dw_long ? dx_n : dw_n;
@@ -835,7 +838,7 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
     const int left = max(0, d.short_n - d.from);
     d.rounds = a.by_pairs(left);
     d.over = left - d.rounds * d.pairs;
-    d.halves = (d.dw_long ? d.dx_subs : d.dw_subs) == 2 && 2 * d.over <= d.pairs;
+    d.halves = (d.dw_long ? d.dx_subs : a.dw_subs) == 2 && 2 * d.over <= d.pairs;
     return d;
 }
 
@@ -869,17 +872,19 @@ __device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int
     }
     const int m = a.by_dim_tiles(n);
     t.dt = n - m * a.dim_tiles;
-    n = m;
-    t.split = 0;
-    t.k0 = 0;
-    t.steps = d.dw_steps;
-    if (!t.is_dw) {
+    if (t.is_dw) {
+        t.split = a.by_dw_groups(m);
+        n = m - t.split * a.dw_groups;
+        t.k0 = t.split * a.dw_split_steps;
+        t.steps = min(a.dw_split_steps, d.dw_steps - t.k0);
+        t.subs = a.dw_subs;
+    } else {
         n = a.by_splits(m);
         t.split = m - n * a.splits;
         t.k0 = t.split * a.split_steps;
         t.steps = min(a.split_steps, a.tiles * 4 - t.k0);
+        t.subs = d.dx_subs;
     }
-    t.subs = t.is_dw ? d.dw_subs : d.dx_subs;
     t.rt = n * t.subs;
     const int end = t.is_dw ? a.tiles : d.row_tiles;
     if (only >= 0) {
@@ -973,8 +978,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             tc_fence_after();
             const bool dead = *p.dead != 0;
             const int block = (t.rt + sub) * 2 + p.rank, word = (a.tile0 + t.rt + sub) * kTile + p.rank * 128 + 32 * quad;
-            float4* const sums = a.sums + ((size_t)t.split * (a.padded / 128) + block) * (a.dim / 4) * 128 + 32 * quad + lane;
-            const bool out = t.is_dw || a.last, adds = !t.is_dw && a.add && row < count;
+            float4* const sums = (t.is_dw ? a.dw_sums + ((size_t)t.split * (2 * a.tiles) + block) * (a.dim / 4) * 128
+                                          : a.sums + ((size_t)t.split * (a.padded / 128) + block) * (a.dim / 4) * 128) + 32 * quad + lane;
+            const bool out = t.is_dw ? a.dw_splits == 1 : a.last, adds = !t.is_dw && a.add && row < count;
+            const bool writes = t.is_dw ? word + lane < a.vocab : row < count;
             // the rows that the lane writes in turn: 8 at a time, four lanes for 64 bytes of each
             int64_t to[4];
             bool zero[4] = {};
@@ -1011,7 +1018,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
                     }
                 }
                 if (!out) {
-                    if (row < count)
+                    if (writes)
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             if (d0 + 4 * j < a.dim)
@@ -1055,36 +1062,54 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
     pair_end(p);
 }
 
-// dx from several parts: their sums, rounded.  A block takes 32 rows x 8 columns, a warp every eighth part; the warps' sums are
-// added in their order.
-__global__ void __launch_bounds__(256) dx_kernel(const float4* sums, const int* count, int rows, const int* row_of, int padded, int dim, int splits, uint16_t* dx,
-                                                 int64_t dx_step) {
+// dx and dw from several parts: their sums, rounded.
+struct Parts {
+    const float4* sums;
+    int parts, part_steps;             // dw: parts that begin behind the rows' last step hold nothing
+    int blocks;                        // of this launch: 32 rows each
+    int rows, padded;
+    const int* row;                    // of a place; null: the place itself
+    uint16_t* out;
+    int64_t step;
+    int ways;                          // warps that share the parts: 1, 2, 4 or 8
+};
+
+// A block takes 32 rows x 64 / ways columns; the warps that share a column's parts add their sums in order.
+__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Parts dx, const __grid_constant__ Parts dw, const int* count, int rows, int dim) {
     __shared__ float s[8][8][32];
     grid_dependency_sync();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, row = blockIdx.x * 32 + lane, d = 8 * blockIdx.y;
-    const int n = count ? *count : rows;
-    if ((int)blockIdx.x * 32 >= n) return;
-    const int64_t part = (int64_t)(padded / 128) * (dim / 4) * 128;
-    const float4* from = sums + ((int64_t)(row / 128) * (dim / 4) + d / 4) * 128 + row % 128;
-    const int to = row < n && warp == 0 ? row_of[row] : 0;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n = count ? *count : rows;
+    const bool is_dw = (int)blockIdx.x >= dx.blocks;
+    const Parts& p = is_dw ? dw : dx;
+    const int row0 = (blockIdx.x - (is_dw ? dx.blocks : 0)) * 32, row = row0 + lane, end = is_dw ? p.rows : n;
+    const int parts = is_dw ? min(p.parts, ((n + kStep - 1) / kStep + p.part_steps - 1) / p.part_steps) : p.parts;
+    const int columns = 8 / p.ways, way = warp % p.ways, groups = dim / 8, group0 = blockIdx.y * columns;
+    if (row0 >= end || group0 >= groups) return;
+    const int group = group0 + warp / p.ways;
+    const int64_t part = (int64_t)(p.padded / 128) * (dim / 4) * 128;
+    const float4* from = p.sums + ((int64_t)(row / 128) * (dim / 4) + 2 * group) * 128 + row % 128;
+    const int to = row < end && p.row && way == 0 ? p.row[row] : row;
+    const bool mine = row < end && group < groups;
     float v[8] = {};
-    if (row < n)
+    if (mine)
 #pragma unroll 4
-        for (int k = warp; k < splits; k += 8) {
+        for (int k = way; k < parts; k += p.ways) {
             const float4 lo = from[k * part], hi = from[k * part + 128];
             const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += add[j];
         }
+    if (p.ways > 1) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[warp][j][lane] = v[j];
-    __syncthreads();
-    if (warp || row >= n) return;
-    for (int w = 1; w < 8; ++w)
+        for (int j = 0; j < 8; ++j) s[warp][j][lane] = v[j];
+        __syncthreads();
+        for (int w = 1; w < p.ways; ++w)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += s[w][j][lane];
+            for (int j = 0; j < 8; ++j) v[j] += s[(warp + w) & 7][j][lane];
+    }
+    if (!mine || way) return;
     const uint4 out = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    *reinterpret_cast<uint4*>(dx + (to < 0 ? ~to : to) * dx_step + d) = to < 0 ? make_uint4(0, 0, 0, 0) : out;
+    *reinterpret_cast<uint4*>(p.out + (to < 0 ? ~to : to) * p.step + 8 * group) = to < 0 ? make_uint4(0, 0, 0, 0) : out;
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -1092,9 +1117,20 @@ __global__ void __launch_bounds__(256) dx_kernel(const float4* sums, const int* 
 // Sizes and places in the workspace.
 struct Plan {
     int padded, count_blocks, tiles, labels;
-    int piece, pieces, splits, split_steps, n, dim_tiles;
-    uint64_t block_count, place, count, slot, row, xc, target, index, weight, entropy, first, stats, label_z, lse2, coef, dz, dx, bytes;
+    int piece, pieces, dx_subs, splits, split_steps, dw_subs, dw_splits, dw_split_steps, n, dim_tiles;
+    uint64_t block_count, place, count, slot, row, xc, target, index, weight, entropy, first, stats, label_z, lse2, coef, dz, dx, dw, bytes;
 };
+
+// Parts of an inner axis, so that an item of one tile, or of two that share an operand where the parts stay long, takes no longer
+// than `share` steps.
+void split_axis(int64_t steps, int64_t share, bool pairs, int most, int* subs, int* splits, int* split_steps) {
+    for (*subs = pairs ? 2 : 1;; *subs = 1) {
+        const int64_t n = std::max<int64_t>(1, std::min<int64_t>(most, (steps * *subs + share - 1) / share));
+        *split_steps = (int)std::max<int64_t>(1, (steps + n - 1) / n);
+        *splits = (int)std::max<int64_t>(1, (steps + *split_steps - 1) / *split_steps);
+        if (*subs == 1 || *split_steps >= kLongSteps) return;
+    }
+}
 
 Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     Plan p;
@@ -1114,15 +1150,15 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     p.piece = (p.tiles + p.pieces - 1) / p.pieces;
     if (p.pieces > 1) p.piece += p.piece % 2;
     p.pieces = (p.tiles + p.piece - 1) / p.piece;
-    // dx's inner axis is split while one of its tiles would take longer than its share of the launch
-    const int64_t row_tiles = p.padded / kTile, dx_steps = 4ll * p.piece;
-    int64_t all = row_tiles * p.dim_tiles * dx_steps + (int64_t)p.piece * p.dim_tiles * (p.padded / kStep);
-    if (row_tiles > 1) all /= 2;                                   // two tiles at a time
+    // an inner axis is split while an item would take longer than a pair's share of the launch; dw's only where the piece is the
+    // whole vocabulary, which with few rows or words it is
+    const int64_t row_tiles = p.padded / kTile, dx_steps = 4ll * p.piece, dw_steps = p.padded / kStep;
+    const int64_t all = p.dim_tiles * (row_tiles * dx_steps + p.piece * dw_steps);
     const int64_t share = all / kPairs > 8 ? all / kPairs : 8;
-    int64_t splits = (dx_steps + share - 1) / share;
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    p.split_steps = (int)((dx_steps + splits - 1) / splits);
-    p.splits = (int)((dx_steps + p.split_steps - 1) / p.split_steps);
+    const uint64_t dx_bytes = 4ull * p.padded * d.dim, dw_bytes = 4ull * p.tiles * kTile * d.dim;      // of a part's sums
+    auto most = [](uint64_t bytes) { return (int)std::min<uint64_t>(kMaxSplits, std::max<uint64_t>(1, kPieceBytes / (bytes + 1))); };
+    split_axis(dx_steps, share, row_tiles > 1, most(dx_bytes), &p.dx_subs, &p.splits, &p.split_steps);
+    split_axis(dw_steps, share, p.piece > 1, p.pieces > 1 ? 1 : most(dw_bytes), &p.dw_subs, &p.dw_splits, &p.dw_split_steps);
 
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
@@ -1149,6 +1185,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.coef = take(4 * padded);
         p.dz = take(tile_bytes * p.piece);
         p.dx = take(4ull * p.splits * padded * d.dim);
+        if (p.dw_splits > 1) p.dw = take(p.dw_splits * dw_bytes);
     } else {
         p.stats = take(8 * padded * p.tiles);
         p.label_z = take(4 * padded * p.labels);
@@ -1214,8 +1251,8 @@ struct Call {
 // x as it is can be an operand of the products, unless its rows overlap.
 bool direct_x(const Call& c) { return c.d->rows == 1 || c.x->stride_row >= (int64_t)c.d->dim; }
 
-// Rows that fit one tile stay in their places.
-bool plain_rows(const Call& c) { return c.d->rows <= kTile && direct_x(c); }
+// Rows that fit two tiles stay in their places.
+bool plain_rows(const Call& c) { return c.d->rows <= 2 * kTile && direct_x(c); }
 
 uint64_t step_of(const alsgd_matrix& m, uint32_t rows, uint32_t dim) {
     return rows == 1 || m.stride_row == 0 ? (uint64_t)dim : (uint64_t)m.stride_row;
@@ -1425,7 +1462,12 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     m.dim_tiles = p.dim_tiles;
     m.by_dim_tiles = divide_by(p.dim_tiles);
     m.padded = p.padded;
+    m.dx_subs = p.dx_subs;
+    m.dw_subs = p.dw_subs;
+    m.dw_splits = p.dw_splits;
+    m.dw_split_steps = p.dw_split_steps;
     m.sums = at<float4>(c, p.dx);
+    m.dw_sums = at<float4>(c, p.dw);
     m.row = at<int>(c, p.row);
     m.dx = static_cast<uint16_t*>(dx->data);
     m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
@@ -1445,14 +1487,24 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         m.add = i > 0;
         m.last = i + 1 == p.pieces && p.splits == 1;
         if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
-        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles);
+        m.dw_groups = (m.tiles + p.dw_subs - 1) / p.dw_subs;
+        m.by_dw_groups = divide_by(m.dw_groups);
+        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles * p.dw_splits);
         m.by_pairs = divide_by(grid / 2);
         m.by_splits = divide_by(m.splits);
         if (launch_dependent(product_kernel, dim3(grid), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
     }
-    if (p.splits == 1) return ALSGD_OK;
-    return launch_dependent(dx_kernel, dim3((a.plain ? (int)d.rows + 31 : p.padded) / 32, d.dim / 8), dim3(256), 0, c.stream, (const float4*)m.sums,
-                            a.plain ? (const int*)nullptr : m.count, (int)d.rows, m.row, p.padded, (int)d.dim, p.splits, m.dx, m.dx_step) == cudaSuccess
+    if (p.splits == 1 && p.dw_splits == 1) return ALSGD_OK;
+    Parts dx_parts, dw_parts;
+    std::memset(&dx_parts, 0, sizeof dx_parts);
+    std::memset(&dw_parts, 0, sizeof dw_parts);
+    auto ways = [](int parts) { return parts >= 8 ? 8 : parts >= 4 ? 4 : parts >= 2 ? 2 : 1; };
+    if (p.splits > 1) dx_parts = {m.sums, p.splits, p.split_steps, (int)((d.rows + 31) / 32), (int)d.rows, p.padded, m.row, m.dx, m.dx_step, ways(p.splits)};
+    if (p.dw_splits > 1)
+        dw_parts = {m.dw_sums, p.dw_splits, p.dw_split_steps, (int)((d.vocab + 31) / 32), (int)d.vocab, p.tiles * kTile, nullptr, m.dw, m.dw_step, ways(p.dw_splits)};
+    const int columns = 8 / std::max(dx_parts.ways, dw_parts.ways), groups = (int)d.dim / 8;
+    return launch_dependent(parts_kernel, dim3(dx_parts.blocks + dw_parts.blocks, (groups + columns - 1) / columns), dim3(256), 0, c.stream, dx_parts, dw_parts,
+                            a.plain ? (const int*)nullptr : m.count, (int)d.rows, (int)d.dim) == cudaSuccess
                ? ALSGD_OK
                : ALSGD_E_CUDA;
 }
