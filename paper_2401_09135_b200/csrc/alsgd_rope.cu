@@ -18,7 +18,7 @@ using namespace alsgd_ops;
 
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
-// Units of 16 elements that a thread has in flight, with five blocks per SM: 23.0 us at 64 x 256 tokens and 32 heads of 64, 33.3 at
+// Units of two groups that a thread has in flight, with five blocks per SM: 23.0 us at 64 x 256 tokens and 32 heads of 64, 33.3 at
 // 4 x 4099 tokens and 20 heads of 128 (5.8 and 5.0 TB/s).  Four units, four blocks: 24.2 and 35.0; two and six: 25.9 and 33.0 (spills).
 constexpr int kUnits = 2;
 constexpr int kMaxTokens = 16;         // of a block
@@ -31,49 +31,60 @@ struct RopeArgs {
     int wide_positions;                // binary64 whole numbers
     int64_t pos0;
     int len, heads_q, heads, dim, rot, interleaved, tokens, per_block;
-    int units, angles;                 // of a head
+    int units, turned, angles;         // of a head; turned: units that begin the two halves
     Divide by_token, by_units, by_len, by_angles;                  // units of a token, of a head; tokens of a sequence; angles
     float amplitude, turn;             // turn: 1, or -1 for the inverse
     double turns[kMaxDim / 2];         // f_i / (2 pi)
 };
 
-// Eight elements as 32-bit floats.
-struct Eight {
-    float v[8];
-};
-__device__ __forceinline__ void load8(const uint16_t* p, uint4 (&raw)[2]) { raw[0] = *reinterpret_cast<const uint4*>(p); }
-__device__ __forceinline__ void load8(const float* p, uint4 (&raw)[2]) {
-    raw[0] = reinterpret_cast<const uint4*>(p)[0];
-    raw[1] = reinterpret_cast<const uint4*>(p)[1];
-}
-__device__ __forceinline__ Eight widen(const uint16_t*, const uint4 (&raw)[2]) {
-    const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
-    Eight e;
+// N elements in a row, as they lie and as 32-bit floats.
+template <typename T, int N>
+struct Group {
+    static constexpr int kBytes = N * sizeof(T);
+    uint32_t w[(kBytes + 3) / 4];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kBytes >= 16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        e.v[2 * i] = bf16_lo(w[i]);
-        e.v[2 * i + 1] = bf16_hi(w[i]);
+            for (int i = 0; i < kBytes / 16; ++i) {
+                const uint4 x = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+            }
+        } else if constexpr (kBytes == 8) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x, w[1] = x.y;
+        } else if constexpr (kBytes == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
+        }
     }
-    return e;
-}
-__device__ __forceinline__ Eight widen(const float*, const uint4 (&raw)[2]) {
-    Eight e;
-    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+    __device__ __forceinline__ void widen(float (&v)[N]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = __uint_as_float(w[i]);
-    return e;
-}
-__device__ __forceinline__ void store8(uint16_t* p, const Eight& e) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(e.v[0], e.v[1]), pack_bf16(e.v[2], e.v[3]), pack_bf16(e.v[4], e.v[5]), pack_bf16(e.v[6], e.v[7]));
-}
-__device__ __forceinline__ void store8(float* p, const Eight& e) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(e.v[0], e.v[1], e.v[2], e.v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(e.v[4], e.v[5], e.v[6], e.v[7]);
-}
-__device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)pack_bf16(v, 0.0f); }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+        for (int i = 0; i < N; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
+            else v[i] = i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+        }
+    }
+    __device__ __forceinline__ static void store(T* p, const float (&v)[N]) {
+        Group g;
+#pragma unroll
+        for (int i = 0; i < (kBytes + 3) / 4; ++i) {
+            if constexpr (sizeof(T) == 4) g.w[i] = __float_as_uint(v[i]);
+            else if constexpr (N > 1) g.w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            else g.w[i] = pack_bf16(v[0], 0.0f);
+        }
+        if constexpr (kBytes >= 16) {
+#pragma unroll
+            for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(g.w[4 * i], g.w[4 * i + 1], g.w[4 * i + 2], g.w[4 * i + 3]);
+        } else if constexpr (kBytes == 8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(g.w[0], g.w[1]);
+        } else if constexpr (kBytes == 4) {
+            *reinterpret_cast<uint32_t*>(p) = g.w[0];
+        } else {
+            *reinterpret_cast<uint16_t*>(p) = (uint16_t)g.w[0];
+        }
+    }
+};
 
 __device__ __forceinline__ void turn_pair(float2 cs, float& a, float& b) {
     const float x = a, y = b;
@@ -95,8 +106,8 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, in
     }
 }
 
-// Where a unit's two groups of eight elements start; one that starts at dim or beyond does not exist.
-//   half: eight of either half of the turned part, then eight of either half of the rest.  interleaved: of either half of the
+// Where a unit's two groups of N elements start; one that starts at dim or beyond does not exist.
+//   half: a group of either half of the turned part, then of either half of the rest.  interleaved: of either half of the
 //   head.  Neighbouring threads take neighbouring groups: 32 bytes a thread in a row took 39 us in place of 35.5 (4 x 4099
 //   tokens, 20 heads of 128, half of each turned).
 struct Unit {
@@ -108,6 +119,7 @@ struct Unit {
 };
 // (Plain divisions and remainders here bounded the kernel by its instructions: 33 us at 64 x 256 tokens against 26 with
 // reciprocals.)
+template <int N>
 __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
     Unit u;
     u.token = a.by_token(i);
@@ -118,18 +130,18 @@ __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
     u.pos = token - b * a.len;
     u.is_q = head < a.heads_q;
     u.head = u.is_q ? head : head - a.heads_q;
-    const int turned = a.interleaved ? 0 : a.rot / 16;
-    if (u.n < turned) {
-        u.at[0] = 8 * u.n;
+    if (u.n < a.turned) {
+        u.at[0] = N * u.n;
         u.at[1] = a.rot / 2 + u.at[0];
     } else {
-        u.at[0] = 8 * (u.n + turned);                              // behind 2 * turned groups
-        u.at[1] = u.at[0] + 8 * (a.units - turned);
+        u.at[0] = N * (u.n + a.turned);                            // behind 2 * turned groups
+        u.at[1] = u.at[0] + N * (a.units - a.turned);
     }
     return u;
 }
 
-template <typename T>
+// N: 8, or what divides half of the turned part where the halves are apart (every group then lies where a load of its size may).
+template <typename T, int N>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
     extern __shared__ float2 table[];
     grid_dependency_sync();
@@ -138,16 +150,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(
     const bool copies = a.q != a.q_out || a.k != a.k_out;              // in place, what is not turned stays
     bool angles = false;
     for (int u0 = threadIdx.x; u0 < units || !angles; u0 += kThreads * kUnits) {
-        uint4 raw[kUnits][2][2];
+        Group<T, N> raw[kUnits][2];
 #pragma unroll
         for (int j = 0; j < kUnits; ++j) {
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
-            const Unit u = unit_of(a, token0, i);
+            const Unit u = unit_of<N>(a, token0, i);
             const T* p = u.is_q ? static_cast<const T*>(a.q) + u.offset(a.q_step) : static_cast<const T*>(a.k) + u.offset(a.k_step);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                if (u.at[h] < a.dim) load8(p + u.at[h], raw[j][h]);
+                if (u.at[h] < a.dim) raw[j][h].load(p + u.at[h]);
         }
         if (!angles) {
             fill_angles(a, table, token0, tokens);
@@ -158,60 +170,30 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(
         for (int j = 0; j < kUnits; ++j) {
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
-            const Unit u = unit_of(a, token0, i);
+            const Unit u = unit_of<N>(a, token0, i);
             T* p = u.is_q ? static_cast<T*>(a.q_out) + u.offset(a.q_out_step) : static_cast<T*>(a.k_out) + u.offset(a.k_out_step);
             const float2* cs = table + u.token * a.angles;
-            Eight e[2] = {widen(p, raw[j][0]), widen(p, raw[j][1])};
-            if (a.interleaved) {
+            float e[2][N];
+            raw[j][0].widen(e[0]);
+            raw[j][1].widen(e[1]);
+            if (u.n < a.turned) {
+#pragma unroll
+                for (int x = 0; x < N; ++x) turn_pair(cs[N * u.n + x], e[0][x], e[1][x]);
+            } else if (N == 8 && a.interleaved) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
+                    for (int x = 0; x < N / 2; ++x) {
                         const int pair = u.at[h] / 2 + x;
-                        if (pair < a.angles) turn_pair(cs[pair], e[h].v[2 * x], e[h].v[2 * x + 1]);
+                        if (pair < a.angles) turn_pair(cs[pair], e[h][2 * x], e[h][2 * x + 1]);
                     }
-            } else if (u.n < a.rot / 16) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) turn_pair(cs[8 * u.n + x], e[0].v[x], e[1].v[x]);
             } else if (!copies) {
                 continue;
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                if (u.at[h] < a.dim) store8(p + u.at[h], e[h]);
+                if (u.at[h] < a.dim) Group<T, N>::store(p + u.at[h], e[h]);
         }
-    }
-}
-
-// Halves that do not begin on 16 bytes (a turned part that is no multiple of 16): element by element, a unit is a pair or an
-// element of the rest.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rope_elements_kernel(const __grid_constant__ RopeArgs a) {
-    extern __shared__ float2 table[];
-    grid_dependency_sync();
-    const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
-    fill_angles(a, table, token0, tokens);
-    __syncthreads();
-    const int per_head = a.angles + a.dim - a.rot, per_token = a.heads * per_head;
-    for (int i = threadIdx.x; i < tokens * per_token; i += kThreads) {
-        const int t = i / per_token, rest = i - t * per_token, token = token0 + t, b = token / a.len, s = token - b * a.len;
-        int head = rest / per_head;
-        const int n = rest - head * per_head;
-        const bool is_q = head < a.heads_q;
-        const int64_t* from = is_q ? a.q_step : a.k_step;
-        const int64_t* to = is_q ? a.q_out_step : a.k_out_step;
-        if (!is_q) head -= a.heads_q;
-        const T* x = static_cast<const T*>(is_q ? a.q : a.k) + b * from[0] + s * from[1] + head * from[2];
-        T* y = static_cast<T*>(is_q ? a.q_out : a.k_out) + b * to[0] + s * to[1] + head * to[2];
-        if (n >= a.angles) {
-            const int at = n + a.angles;
-            y[at] = x[at];
-            continue;
-        }
-        float lo = load1(x + n), hi = load1(x + n + a.angles);
-        turn_pair(table[t * a.angles + n], lo, hi);
-        store1(y + n, lo);
-        store1(y + n + a.angles, hi);
     }
 }
 
@@ -269,6 +251,16 @@ void frequencies(const alsgd_rope_desc& d, double* f) {
     }
 }
 
+template <typename T>
+cudaError_t launch(int group, dim3 grid, dim3 block, size_t smem, cudaStream_t s, const RopeArgs& a) {
+    switch (group) {
+        case 8: return launch_dependent(rope_kernel<T, 8>, grid, block, smem, s, a);
+        case 4: return launch_dependent(rope_kernel<T, 4>, grid, block, smem, s, a);
+        case 2: return launch_dependent(rope_kernel<T, 2>, grid, block, smem, s, a);
+        default: return launch_dependent(rope_kernel<T, 1>, grid, block, smem, s, a);
+    }
+}
+
 }  // namespace
 
 extern "C" int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out) {
@@ -322,8 +314,11 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     a.turn = d.flags & ALSGD_ROPE_INVERSE ? -1.0f : 1.0f;
     frequencies(d, a.turns);
     for (int i = 0; i < a.angles; ++i) a.turns[i] *= 1.0 / 6.283185307179586476925;
-    const bool by_element = !a.interleaved && a.rot % 16;
-    a.units = (a.dim + 15) / 16;
+    int group = 8;
+    if (!a.interleaved)
+        while (a.angles % group) group /= 2;
+    a.turned = a.interleaved ? 0 : a.angles / group;
+    a.units = a.turned + ((a.interleaved ? a.dim : a.dim - a.rot) / group + 1) / 2;
     a.by_token = divide_by(a.heads * a.units);
     a.by_units = divide_by(a.units);
     a.by_len = divide_by(a.len);
@@ -337,8 +332,6 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kThreads);
     const size_t smem = (size_t)a.per_block * a.angles * sizeof(float2);       // at most 16 KB
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (d.dtype == ALSGD_F32) e = launch_dependent(by_element ? rope_elements_kernel<float> : rope_kernel<float>, grid, block, smem, s, a);
-    else e = launch_dependent(by_element ? rope_elements_kernel<uint16_t> : rope_kernel<uint16_t>, grid, block, smem, s, a);
+    const cudaError_t e = d.dtype == ALSGD_F32 ? launch<float>(group, grid, block, smem, s, a) : launch<uint16_t>(group, grid, block, smem, s, a);
     return e == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
