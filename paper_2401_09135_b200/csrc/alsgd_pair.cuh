@@ -23,8 +23,8 @@ __device__ __forceinline__ void cluster_sync() {
 }
 // `bar` as at_rank gives it.  What it announces is tensor memory that has been read (the reads have completed, a
 // tc_fence_before behind them): ordering wider than the block's own would wait for every store in flight, most of a microsecond.
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar, uint32_t times) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(times) : "memory");
 }
 __device__ __forceinline__ void tma_load2_pair(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
     asm volatile(

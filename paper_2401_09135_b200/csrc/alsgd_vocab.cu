@@ -255,11 +255,10 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
 
 // ---------------------------------------------------------------------------------------------- the pair's machinery
 
-constexpr int kOutWarps = 16;          // that take tiles out, four for each quarter of the columns
+constexpr int kOutWarps = 16;          // that take tiles out, four for each quarter of the columns (or eight for every other tile)
 constexpr int kThreads = 64 + 32 * kOutWarps;                 // and one that copies, one that issues products
 constexpr int kOperandBytes = 16384;   // of a block in a stage: 128 x 64 of A, up to 128 x 64 of B
 constexpr int kAccColumns = 256;
-constexpr int kPart = kTile / 4;       // columns of a warp
 
 template <int STAGES>
 struct Bars {
@@ -374,12 +373,12 @@ __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring&
     for (int s = 0; s < subs; ++s) mma_commit_pair(p.acc_full + 8 * ((acc + s) & 1));
 }
 
-// The warp has taken its part of the tile out of tensor memory.
+// The warp has taken its part of the tile out of tensor memory: of its columns a quarter, or a half, which counts twice.
 template <int STAGES, int SUBS>
-__device__ __forceinline__ void tile_taken(const Pair<STAGES, SUBS>& p, uint32_t acc, int lane) {
+__device__ __forceinline__ void tile_taken(const Pair<STAGES, SUBS>& p, uint32_t acc, int lane, uint32_t quarters = 1) {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (acc & 1), 0));
+    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (acc & 1), 0), quarters);
 }
 
 // ---------------------------------------------------------------------------------------------- logits
@@ -422,11 +421,13 @@ __device__ __forceinline__ void tile_at(const LogitArgs& a, int i, int row_tiles
     rt = g0 + rest - ct * n;
 }
 
+constexpr int kTurnTiles = 2;          // tiles of a pair from which on warps take turns
+
 template <bool BACKWARD>
 struct LogitSmem {
     static constexpr int kStages = BACKWARD ? 7 : 6;
     uint8_t stages[kStages * 2 * kOperandBytes];
-    float2 stats[BACKWARD ? 1 : 2 * 4 * 128];                      // forward: of a tile, in turn: by part, by row
+    float2 stats[BACKWARD ? 1 : 2 * 4 * 128];                      // forward, of two tiles: by part of the columns, by row
     Bars<kStages> bars;
 };
 
@@ -567,9 +568,15 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                               [](uint32_t s, int i) { return desc_k_major(s + 32 * i); });
         }
     } else {
-        const int quad = warp & 3, part = (warp - 2) / 4;          // tensor memory's lanes that the warp may read; the tile's columns
-        const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16);
-        uint32_t acc = 0;
+        // Tensor memory's lanes that the warp may read; its columns.  Either all sixteen warps share every tile, a quarter each,
+        // or, where many tiles follow one another, eight take every other one, a half each: one half's latencies then lie under the
+        // other's exponentials (forward of 3420 rows x 74768 words x 72: 118 -> 99 us; of 333 rows x 32000 x 384, 3.4 tiles a pair:
+        // 23.6 -> 22.6).
+        const int quad = warp & 3, part = (warp - 2) / 4;
+        const bool turns = tiles >= kTurnTiles * pairs;
+        const int chunks = turns ? 4 : 2, column0 = turns ? 128 * (part & 1) : 64 * part, every = turns ? 2 : 1;
+        const uint32_t lanes = p.tmem + ((uint32_t)(32 * quad) << 16) + column0;
+        uint32_t acc = turns ? part >> 1 : 0;
         if (BACKWARD && a.plain) {
             // for the products behind: zeros in the rows that take no part
 #pragma unroll 4
@@ -580,18 +587,18 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
                 if (lane == 0) a.row[r] = used ? r : ~r;
             }
         }
-        for (int i = first; i < tiles; i += pairs, ++acc) {
+        for (int i = first + acc * pairs; i < tiles; i += every * pairs, acc += every) {
             int rt, ct;
             tile_at(a, i, row_tiles, rt, ct);
             const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
-            const int c0 = (a.tile0 + ct) * kTile + part * kPart;  // first word
+            const int c0 = (a.tile0 + ct) * kTile + column0;       // first word
             int label = -1;
             LabelQueue queue;
             const size_t list = (size_t)row * a.top;
             if (TOP) {
-                const uint8_t* f = a.first + (size_t)row * (4 * a.all_tiles + 1) + 4 * (a.tile0 + ct) + part;
+                const uint8_t* f = a.first + (size_t)row * (4 * a.all_tiles + 1) + 4 * (a.tile0 + ct) + column0 / 64;
                 const bool listed = row < count;                   // what fills the tile up has no list
-                queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, listed ? f[0] : 0, listed ? f[1] : 0);
+                queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, listed ? f[0] : 0, listed ? f[chunks / 2] : 0);
             }
             float lse2 = 0.0f, coef = 0.0f;
             bool used = row < count;
@@ -614,13 +621,13 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
                 uint32_t z[32];
-                tmem_ld32(z, lanes + (acc & 1) * kAccColumns + part * kPart + 32 * c);
+                tmem_ld32(z, lanes + (acc & 1) * kAccColumns + 32 * c);
                 tmem_wait_ld();
                 tmem_use(z);
-                if (c == 1) tile_taken(p, acc, lane);
+                if (c + 1 == chunks) tile_taken(p, acc, lane, every);
                 const int w0 = c0 + 32 * c;
                 if (!BACKWARD) {
                     if (w0 + 32 > a.vocab) {                       // words behind the last have no logits
@@ -659,23 +666,24 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z[j] = used && w0 + j < a.vocab ? z[j] : 0;
                     }
-                    uint8_t* const to = a.dz + ((size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4 + part) * 16384 + block_row * 16;
+                    uint8_t* const to = a.dz + ((size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4) * 16384 + (column0 / 8 + 4 * c) * 2048 + block_row * 16;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t v[4];
 #pragma unroll
                         for (int h = 0; h < 4; ++h) v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
-                        *reinterpret_cast<uint4*>(to + (4 * c + j) * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4*>(to + j * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
             if (!BACKWARD) {
-                // the parts' sums of a row become one
-                float2* const stats = sm.stats + (acc & 1) * 512 + block_row;
-                stats[128 * part] = make_float2(top, dead ? NAN : sum);
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + quad) : "memory");
-                if (part == 0) {
-                    const float2 o[3] = {stats[128], stats[256], stats[384]};
+                // the parts' sums of a row become one; a part's place is free again two tiles (of these warps) later
+                float2* const stats = sm.stats + (turns ? (part >> 1) * 512 + ((acc >> 1) & 1) * 256 : (acc & 1) * 512) + block_row;
+                stats[column0 / (turns ? 128 : 64) * 128] = make_float2(top, dead ? NAN : sum);
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + quad + (turns ? 4 * (part >> 1) : 0)), "r"(turns ? 64 : 128) : "memory");
+                if (column0 == 0) {
+                    const float2 none = make_float2(-INFINITY, 0.0f);
+                    const float2 o[3] = {stats[128], turns ? none : stats[256], turns ? none : stats[384]};
                     const float m = max3(top, o[0].x, fmaxf(o[1].x, o[2].x)), ref = m == -INFINITY ? 0.0f : m * a.scale2;
                     sum *= exp2_fast(fmaf(top, a.scale2, -ref));
 #pragma unroll
@@ -791,6 +799,7 @@ struct ProductArgs {
 // halves of tensor memory belong to one item then, which its way out is not hidden behind: not worth it for short inner axes.
 constexpr int kProductStages = 4;
 constexpr int kLongSteps = 16;          // fewer: one tile
+constexpr int kOutSteps = 4;            // what a tile's way out costs, in steps
 
 struct ProductSmem {
     uint8_t stages[kProductStages * 3 * kOperandBytes];
@@ -824,7 +833,7 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
     // parts of dw that have steps
     const int dw_parts = a.dw_splits == 1 ? 1 : (d.dw_steps + a.dw_split_steps - 1) / a.dw_split_steps;
     const int dx_n = (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = dw_parts * a.dw_groups * a.dim_tiles;
-    const int dx_cost = (a.split_steps + 4) * d.dx_subs, dw_cost = (min(d.dw_steps, a.dw_split_steps) + 4) * a.dw_subs;
+    const int dx_cost = (a.split_steps + kOutSteps) * d.dx_subs, dw_cost = (min(d.dw_steps, a.dw_split_steps) + kOutSteps) * a.dw_subs;
     d.dw_long = dw_cost >= dx_cost;
     const int long_n = d.dw_long ? dw_n : dx_n, more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
     d.short_n = d.dw_long ? dx_n : dw_n;
@@ -1114,23 +1123,40 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Part
 
 // ---------------------------------------------------------------------------------------------- host
 
+// Parts of an inner axis, so that an item of one tile, or of two that share an operand where the parts stay long, takes no longer
+// than `share` steps.
+struct Axis {
+    int subs, splits, split_steps;
+};
+Axis split_axis(int64_t steps, int64_t share, bool pairs, int most) {
+    Axis a;
+    for (a.subs = pairs ? 2 : 1;; a.subs = 1) {
+        const int64_t n = std::max<int64_t>(1, std::min<int64_t>(most, (steps * a.subs + share - 1) / share));
+        a.split_steps = (int)std::max<int64_t>(1, (steps + n - 1) / n);
+        a.splits = (int)std::max<int64_t>(1, (steps + a.split_steps - 1) / a.split_steps);
+        if (a.subs == 1 || a.split_steps >= kLongSteps) return a;
+    }
+}
+
+// Steps until the last pair is done, as deal_of deals the items.
+int64_t steps_until_done(int64_t dx_n, const Axis& dx, int64_t dw_n, const Axis& dw) {
+    const int64_t dx_cost = (int64_t)(dx.split_steps + kOutSteps) * dx.subs, dw_cost = (int64_t)(dw.split_steps + kOutSteps) * dw.subs;
+    const bool dw_long = dw_cost >= dx_cost;
+    const int64_t long_n = dw_long ? dw_n : dx_n, short_n = dw_long ? dx_n : dw_n, more = dw_long ? dw_cost : dx_cost, less = dw_long ? dx_cost : dw_cost;
+    const int64_t rest = long_n % kPairs, late = kPairs - rest, extra = rest ? (more + less / 2) / less : 0;
+    const int64_t left = std::max<int64_t>(0, short_n - extra * late), rounds = left / kPairs, over = left % kPairs;
+    const int64_t early_end = (long_n / kPairs + (rest > 0)) * more, late_end = long_n / kPairs * more + std::min(extra, (short_n + late - 1) / late) * less;
+    const bool halves = (dw_long ? dx.subs : dw.subs) == 2 && 2 * over <= kPairs;
+    return std::max(early_end, late_end) + rounds * less + (over == 0 ? 0 : halves ? less * 5 / 8 : less);
+}
+
 // Sizes and places in the workspace.
 struct Plan {
     int padded, count_blocks, tiles, labels;
-    int piece, pieces, dx_subs, splits, split_steps, dw_subs, dw_splits, dw_split_steps, n, dim_tiles;
-    uint64_t block_count, place, count, slot, row, xc, target, index, weight, entropy, first, stats, label_z, lse2, coef, dz, dx, dw, bytes;
+    int piece, pieces, n, dim_tiles;
+    Axis dx, dw;                       // how the products' inner axes are split
+    uint64_t block_count, place, count, slot, row, xc, target, index, weight, entropy, first, stats, label_z, lse2, coef, dz, sums, dw_sums, bytes;
 };
-
-// Parts of an inner axis, so that an item of one tile, or of two that share an operand where the parts stay long, takes no longer
-// than `share` steps.
-void split_axis(int64_t steps, int64_t share, bool pairs, int most, int* subs, int* splits, int* split_steps) {
-    for (*subs = pairs ? 2 : 1;; *subs = 1) {
-        const int64_t n = std::max<int64_t>(1, std::min<int64_t>(most, (steps * *subs + share - 1) / share));
-        *split_steps = (int)std::max<int64_t>(1, (steps + n - 1) / n);
-        *splits = (int)std::max<int64_t>(1, (steps + *split_steps - 1) / *split_steps);
-        if (*subs == 1 || *split_steps >= kLongSteps) return;
-    }
-}
 
 Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     Plan p;
@@ -1150,15 +1176,26 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     p.piece = (p.tiles + p.pieces - 1) / p.pieces;
     if (p.pieces > 1) p.piece += p.piece % 2;
     p.pieces = (p.tiles + p.piece - 1) / p.piece;
-    // an inner axis is split while an item would take longer than a pair's share of the launch; dw's only where the piece is the
-    // whole vocabulary, which with few rows or words it is
+    // an inner axis is split while an item would take longer than a pair's share of the launch, or a half, a third, a quarter of
+    // it, whichever leaves the pairs done first.  (One part where two were better: 10598 rows x 10748 words x 360 are 84 equal items for
+    // 74 pairs.)
     const int64_t row_tiles = p.padded / kTile, dx_steps = 4ll * p.piece, dw_steps = p.padded / kStep;
-    const int64_t all = p.dim_tiles * (row_tiles * dx_steps + p.piece * dw_steps);
-    const int64_t share = all / kPairs > 8 ? all / kPairs : 8;
-    const uint64_t dx_bytes = 4ull * p.padded * d.dim, dw_bytes = 4ull * p.tiles * kTile * d.dim;      // of a part's sums
+    const int64_t all = p.dim_tiles * (row_tiles * dx_steps + p.piece * dw_steps), share = std::max<int64_t>(8, all / kPairs);
+    const uint64_t dx_bytes = 4ull * p.padded * d.dim, dw_bytes = 4ull * p.piece * kTile * d.dim;      // of a part's sums
     auto most = [](uint64_t bytes) { return (int)std::min<uint64_t>(kMaxSplits, std::max<uint64_t>(1, kPieceBytes / (bytes + 1))); };
-    split_axis(dx_steps, share, row_tiles > 1, most(dx_bytes), &p.dx_subs, &p.splits, &p.split_steps);
-    split_axis(dw_steps, share, p.piece > 1, p.pieces > 1 ? 1 : most(dw_bytes), &p.dw_subs, &p.dw_splits, &p.dw_split_steps);
+    int64_t best = INT64_MAX;
+    for (int i = 0; i < 16 && p.padded; ++i) {
+        const Axis dx = split_axis(dx_steps, std::max<int64_t>(8, share / (1 + i % 4)), row_tiles > 1, most(dx_bytes));
+        const Axis dw = split_axis(dw_steps, std::max<int64_t>(8, share / (1 + i / 4)), p.piece > 1, most(dw_bytes));
+        const int64_t dx_n = (row_tiles + dx.subs - 1) / dx.subs * p.dim_tiles * dx.splits, dw_n = (p.piece + dw.subs - 1) / dw.subs * p.dim_tiles * dw.splits;
+        // parts are written and read again (a step's time moves about 1 MB) by one more launch (about 12 steps)
+        const int64_t sums = ((dx.splits > 1 ? dx.splits * dx_bytes : 0) + (dw.splits > 1 ? dw.splits * dw_bytes : 0)) >> 19;
+        const int64_t t = steps_until_done(dx_n, dx, dw_n, dw) + sums + (dx.splits > 1 || dw.splits > 1 ? 12 : 0);
+        if (t >= best) continue;
+        best = t;
+        p.dx = dx;
+        p.dw = dw;
+    }
 
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
@@ -1184,8 +1221,8 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.lse2 = take(4 * padded);
         p.coef = take(4 * padded);
         p.dz = take(tile_bytes * p.piece);
-        p.dx = take(4ull * p.splits * padded * d.dim);
-        if (p.dw_splits > 1) p.dw = take(p.dw_splits * dw_bytes);
+        if (p.pieces > 1 || p.dx.splits > 1) p.sums = take(p.dx.splits * dx_bytes);
+        if (p.dw.splits > 1) p.dw_sums = take(p.dw.splits * dw_bytes);
     } else {
         p.stats = take(8 * padded * p.tiles);
         p.label_z = take(4 * padded * p.labels);
@@ -1419,6 +1456,26 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     return launch_dependent(loss_kernel, dim3(p.padded / kLossRows), dim3(kLossRows * kLossParts), 0, c.stream, l, row_of) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
+// What a piece leaves in parts: dw of its words, with the last piece dx.
+int add_parts(const Plan& p, const ProductArgs& m, cudaStream_t stream) {
+    const bool dx = p.dx.splits > 1 && m.tile0 + m.tiles == p.tiles, dw = p.dw.splits > 1;
+    if (!dx && !dw) return ALSGD_OK;
+    Parts of_dx, of_dw;
+    std::memset(&of_dx, 0, sizeof of_dx);
+    std::memset(&of_dw, 0, sizeof of_dw);
+    auto ways = [](int parts) { return parts >= 8 ? 8 : parts >= 4 ? 4 : parts >= 2 ? 2 : 1; };
+    const int words = std::min(m.vocab - m.tile0 * kTile, m.tiles * kTile);
+    if (dx) of_dx = {m.sums, p.dx.splits, p.dx.split_steps, (m.rows + 31) / 32, m.rows, p.padded, m.row, m.dx, m.dx_step, ways(p.dx.splits)};
+    if (dw)
+        of_dw = {m.dw_sums, p.dw.splits, p.dw.split_steps, (words + 31) / 32, words, m.tiles * kTile, nullptr, m.dw + (int64_t)m.tile0 * kTile * m.dw_step, m.dw_step,
+                 ways(p.dw.splits)};
+    const int columns = 8 / std::max(of_dx.ways, of_dw.ways), groups = m.dim / 8;
+    return launch_dependent(parts_kernel, dim3(of_dx.blocks + of_dw.blocks, (groups + columns - 1) / columns), dim3(256), 0, stream, of_dx, of_dw,
+                            m.plain ? (const int*)nullptr : m.count, m.rows, m.dim) == cudaSuccess
+               ? ALSGD_OK
+               : ALSGD_E_CUDA;
+}
+
 int backward(const Call& c, bool teacher, const float* lse, const float* dloss, int64_t dloss_step, const alsgd_matrix* dx, const alsgd_matrix* dw) {
     int rc = check_call(c, teacher);
     if (rc != ALSGD_OK) return rc;
@@ -1462,12 +1519,12 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     m.dim_tiles = p.dim_tiles;
     m.by_dim_tiles = divide_by(p.dim_tiles);
     m.padded = p.padded;
-    m.dx_subs = p.dx_subs;
-    m.dw_subs = p.dw_subs;
-    m.dw_splits = p.dw_splits;
-    m.dw_split_steps = p.dw_split_steps;
-    m.sums = at<float4>(c, p.dx);
-    m.dw_sums = at<float4>(c, p.dw);
+    m.dx_subs = p.dx.subs;
+    m.dw_subs = p.dw.subs;
+    m.dw_splits = p.dw.splits;
+    m.dw_split_steps = p.dw.split_steps;
+    m.sums = at<float4>(c, p.sums);
+    m.dw_sums = at<float4>(c, p.dw_sums);
     m.row = at<int>(c, p.row);
     m.dx = static_cast<uint16_t*>(dx->data);
     m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
@@ -1482,31 +1539,20 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         a.tiles = m.tiles = p.tiles - a.tile0 < p.piece ? p.tiles - a.tile0 : p.piece;
         a.by_group = divide_by(kGroup * a.tiles);
         // the first piece writes all of dx's sums; a shorter last one adds to as many as it has steps for
-        m.split_steps = p.split_steps;
-        m.splits = (4 * m.tiles + p.split_steps - 1) / p.split_steps;
+        m.split_steps = p.dx.split_steps;
+        m.splits = (4 * m.tiles + p.dx.split_steps - 1) / p.dx.split_steps;
         m.add = i > 0;
-        m.last = i + 1 == p.pieces && p.splits == 1;
+        m.last = i + 1 == p.pieces && p.dx.splits == 1;
         if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
-        m.dw_groups = (m.tiles + p.dw_subs - 1) / p.dw_subs;
+        m.dw_groups = (m.tiles + p.dw.subs - 1) / p.dw.subs;
         m.by_dw_groups = divide_by(m.dw_groups);
-        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.splits + (int64_t)m.tiles * p.dim_tiles * p.dw_splits);
+        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.dx.splits + (int64_t)m.tiles * p.dim_tiles * p.dw.splits);
         m.by_pairs = divide_by(grid / 2);
         m.by_splits = divide_by(m.splits);
         if (launch_dependent(product_kernel, dim3(grid), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;
+        if ((rc = add_parts(p, m, c.stream)) != ALSGD_OK) return rc;
     }
-    if (p.splits == 1 && p.dw_splits == 1) return ALSGD_OK;
-    Parts dx_parts, dw_parts;
-    std::memset(&dx_parts, 0, sizeof dx_parts);
-    std::memset(&dw_parts, 0, sizeof dw_parts);
-    auto ways = [](int parts) { return parts >= 8 ? 8 : parts >= 4 ? 4 : parts >= 2 ? 2 : 1; };
-    if (p.splits > 1) dx_parts = {m.sums, p.splits, p.split_steps, (int)((d.rows + 31) / 32), (int)d.rows, p.padded, m.row, m.dx, m.dx_step, ways(p.splits)};
-    if (p.dw_splits > 1)
-        dw_parts = {m.dw_sums, p.dw_splits, p.dw_split_steps, (int)((d.vocab + 31) / 32), (int)d.vocab, p.tiles * kTile, nullptr, m.dw, m.dw_step, ways(p.dw_splits)};
-    const int columns = 8 / std::max(dx_parts.ways, dw_parts.ways), groups = (int)d.dim / 8;
-    return launch_dependent(parts_kernel, dim3(dx_parts.blocks + dw_parts.blocks, (groups + columns - 1) / columns), dim3(256), 0, c.stream, dx_parts, dw_parts,
-                            a.plain ? (const int*)nullptr : m.count, (int)d.rows, (int)d.dim) == cudaSuccess
-               ? ALSGD_OK
-               : ALSGD_E_CUDA;
+    return ALSGD_OK;
 }
 
 }  // namespace
