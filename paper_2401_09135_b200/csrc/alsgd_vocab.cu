@@ -14,7 +14,8 @@
 // (forward of 77 rows x 32000 words x 384: 16.6 -> 13.1 us).
 //
 // The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
-// of either operand, so that a tile needs half of the shared memory traffic of two single ones.  One warp copies, one
+// of either operand, so that a tile needs half of the shared memory traffic of two single ones.  (Up to 128 rows there is no
+// second half of the rows: every block then forms logits by itself, 128 x 256.)  One warp copies, one
 // issues products, sixteen take the finished tile out of tensor memory while the next one is formed in its other half.
 #include "../../include/alsgd.h"
 #include "alsgd_ops.cuh"
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
 
 constexpr int kOutWarps = 16;          // that take tiles out, four for each quarter of the columns (or eight for every other tile)
 constexpr int kThreads = 64 + 32 * kOutWarps;                 // and one that copies, one that issues products
-constexpr int kOperandBytes = 16384;   // of a block in a stage: 128 x 64 of A, up to 128 x 64 of B
+constexpr int kOperandBytes = 16384;   // 128 x 64 values of an operand
 constexpr int kAccColumns = 256;
 
 template <int STAGES>
@@ -266,10 +267,11 @@ struct Bars {
     uint32_t tmem, dead;
 };
 
-// What every warp of a block knows about its pair's shared memory: stages of SUBS operands A, one B.
-template <int STAGES, int SUBS>
+// What every warp of a block knows about the shared memory that it works on with the other block of its pair, or alone (TWO
+// false): stages of SUBS operands A and one B, half of which the other block of a pair holds.
+template <int STAGES, int SUBS, bool TWO>
 struct Pair {
-    static constexpr int kStageBytes = (SUBS + 1) * kOperandBytes;
+    static constexpr int kStageBytes = (SUBS + (TWO ? 1 : 2)) * kOperandBytes;
     uint32_t stage0, full, empty, acc_full, acc_empty, rank, tmem;
     volatile uint32_t* dead;
 
@@ -279,15 +281,15 @@ struct Pair {
 
 // Barriers and tensor memory of both blocks.  Full: one arrival (the first block's copying thread, for the bytes of
 // both).  Empty, finished tile: one arrival, by the tensor core, on either block's.  Tile taken out: every warp of both blocks.
-template <int STAGES, int SUBS>
-__device__ __forceinline__ Pair<STAGES, SUBS> pair_begin(uint8_t* stages, Bars<STAGES>* bars) {
-    Pair<STAGES, SUBS> p;
+template <int STAGES, int SUBS, bool TWO>
+__device__ __forceinline__ Pair<STAGES, SUBS, TWO> pair_begin(uint8_t* stages, Bars<STAGES>* bars) {
+    Pair<STAGES, SUBS, TWO> p;
     p.stage0 = smem_u32(stages);
     p.full = smem_u32(bars->full);
     p.empty = smem_u32(bars->empty);
     p.acc_full = smem_u32(bars->acc_full);
     p.acc_empty = smem_u32(bars->acc_empty);
-    p.rank = cluster_rank();
+    p.rank = TWO ? cluster_rank() : 0;
     p.dead = &bars->dead;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -296,30 +298,34 @@ __device__ __forceinline__ Pair<STAGES, SUBS> pair_begin(uint8_t* stages, Bars<S
         }
         for (int b = 0; b < 2; ++b) {
             bar_init(p.acc_full + 8 * b, 1);
-            bar_init(p.acc_empty + 8 * b, 2 * kOutWarps);
+            bar_init(p.acc_empty + 8 * b, (TWO ? 2 : 1) * kOutWarps);
         }
         bars->dead = 0;
         bar_init_fence();
     }
-    if (threadIdx.x / 32 == 1) tmem_alloc_pair(smem_u32(&bars->tmem), 2 * kAccColumns);
+    if (threadIdx.x / 32 == 1) {
+        if (TWO) tmem_alloc_pair(smem_u32(&bars->tmem), 2 * kAccColumns);
+        else tmem_alloc(smem_u32(&bars->tmem), 2 * kAccColumns);
+    }
     tc_fence_before();
     __syncthreads();
-    cluster_sync();
+    if (TWO) cluster_sync();
     tc_fence_after();
     p.tmem = bars->tmem;
     return p;
 }
 
 // The blocks leave together: neither's shared memory goes while the other's copies or products may touch it.
-template <int STAGES, int SUBS>
-__device__ __forceinline__ void pair_end(const Pair<STAGES, SUBS>& p) {
+template <int STAGES, int SUBS, bool TWO>
+__device__ __forceinline__ void pair_end(const Pair<STAGES, SUBS, TWO>& p) {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    cluster_sync();
+    if (TWO) cluster_sync();
     if (threadIdx.x / 32 == 1) {
         tc_fence_after();
-        tmem_free_pair(p.tmem, 2 * kAccColumns);
+        if (TWO) tmem_free_pair(p.tmem, 2 * kAccColumns);
+        else tmem_free(p.tmem, 2 * kAccColumns);
     }
 }
 
@@ -340,8 +346,8 @@ struct Ring {
 enum : uint32_t { kWaitEmpty = 1, kWaitFull = 2, kWaitAccEmpty = 4, kWaitAccFull = 8 };
 
 // Before the copying thread leaves, everything that it started has landed and been consumed (at once, unless it gave up).
-template <int STAGES, int SUBS>
-__device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS>& p, Ring ring) {
+template <int STAGES, int SUBS, bool TWO>
+__device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS, TWO>& p, Ring ring) {
     for (int s = 0; s < STAGES; ++s) {
         drain(p.empty + 8 * ring.stage, ring.phase ^ 1);
         ring.next<STAGES>();
@@ -350,8 +356,8 @@ __device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS>& p, Ring rin
 
 // The products of `subs` tiles that share B: `steps` stages, each four products of 16 along the inner axis for either tile.
 // a, b: descriptors of the i-th.  acc: tiles before these; tensor memory holds two, in turn.
-template <int STAGES, int SUBS, typename DESC_A, typename DESC_B>
-__device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring& ring, uint32_t acc, int subs, int steps, uint32_t desc, DESC_A a, DESC_B b) {
+template <int STAGES, int SUBS, bool TWO, typename DESC_A, typename DESC_B>
+__device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS, TWO>& p, Ring& ring, uint32_t acc, int subs, int steps, uint32_t desc, DESC_A a, DESC_B b) {
     for (int k = 0; k < steps; ++k) {
         wait(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
         tc_fence_after();
@@ -365,20 +371,30 @@ __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS>& p, Ring&
                 tc_fence_after();
             }
 #pragma unroll
-            for (int i = 0; i < kStep / 16; ++i) mma_ss_pair(p.tmem + buf * kAccColumns, a(sa + s * kOperandBytes, i), b(sb, i), desc, k || i);
+            for (int i = 0; i < kStep / 16; ++i) {
+                if (TWO) mma_ss_pair(p.tmem + buf * kAccColumns, a(sa + s * kOperandBytes, i), b(sb, i), desc, k || i);
+                else mma_ss(p.tmem + buf * kAccColumns, a(sa + s * kOperandBytes, i), b(sb, i), desc, k || i);
+            }
         }
-        mma_commit_pair(p.empty + 8 * ring.stage);
+        if (TWO) mma_commit_pair(p.empty + 8 * ring.stage);
+        else mma_commit(p.empty + 8 * ring.stage);
         ring.next<STAGES>();
     }
-    for (int s = 0; s < subs; ++s) mma_commit_pair(p.acc_full + 8 * ((acc + s) & 1));
+    for (int s = 0; s < subs; ++s) {
+        if (TWO) mma_commit_pair(p.acc_full + 8 * ((acc + s) & 1));
+        else mma_commit(p.acc_full + 8 * ((acc + s) & 1));
+    }
 }
 
 // The warp has taken its part of the tile out of tensor memory: of its columns a quarter, or a half, which counts twice.
-template <int STAGES, int SUBS>
-__device__ __forceinline__ void tile_taken(const Pair<STAGES, SUBS>& p, uint32_t acc, int lane, uint32_t quarters = 1) {
+template <int STAGES, int SUBS, bool TWO>
+__device__ __forceinline__ void tile_taken(const Pair<STAGES, SUBS, TWO>& p, uint32_t acc, int lane, uint32_t quarters = 1) {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (acc & 1), 0), quarters);
+    if (lane == 0) {
+        if (TWO) bar_arrive_cluster(at_rank(p.acc_empty + 8 * (acc & 1), 0), quarters);
+        else bar_arrive(p.acc_empty + 8 * (acc & 1), quarters);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- logits
@@ -423,10 +439,10 @@ __device__ __forceinline__ void tile_at(const LogitArgs& a, int i, int row_tiles
 
 constexpr int kTurnTiles = 2;          // tiles of a pair from which on warps take turns
 
-template <bool BACKWARD>
+template <bool BACKWARD, bool TWO>
 struct LogitSmem {
-    static constexpr int kStages = BACKWARD ? 7 : 6;
-    uint8_t stages[kStages * 2 * kOperandBytes];
+    static constexpr int kStages = !TWO ? 4 : BACKWARD ? 7 : 6;
+    uint8_t stages[kStages * (TWO ? 2 : 3) * kOperandBytes];
     float2 stats[BACKWARD ? 1 : 2 * 4 * 128];                      // forward, of two tiles: by part of the columns, by row
     Bars<kStages> bars;
 };
@@ -524,21 +540,21 @@ struct LabelQueue {
     }
 };
 
-template <bool BACKWARD, bool TOP>
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_kernel(const __grid_constant__ LogitArgs a) {
+template <bool BACKWARD, bool TOP, bool TWO>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 1) logit_kernel(const __grid_constant__ LogitArgs a) {
     extern __shared__ uint8_t raw[];
-    using Smem = LogitSmem<BACKWARD>;
-    constexpr int STAGES = Smem::kStages;
+    using Smem = LogitSmem<BACKWARD, TWO>;
+    constexpr int STAGES = Smem::kStages, ROWS = TWO ? kTile : kTile / 2, BLOCKS = TWO ? 2 : 1;      // rows of a tile; blocks that form it
     Smem& sm = *reinterpret_cast<Smem*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
-    const Pair<STAGES, 1> p = pair_begin<STAGES, 1>(sm.stages, &sm.bars);
+    const Pair<STAGES, 1, TWO> p = pair_begin<STAGES, 1, TWO>(sm.stages, &sm.bars);
     grid_dependency_sync();
-    const int count = a.plain ? a.rows : *a.count, row_tiles = (count + kTile - 1) / kTile, tiles = row_tiles * a.tiles;
-    const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int count = a.plain ? a.rows : *a.count, row_tiles = (count + ROWS - 1) / ROWS, tiles = row_tiles * a.tiles;
+    const int steps = (a.dim + kStep - 1) / kStep, first = blockIdx.x / BLOCKS, pairs = gridDim.x / BLOCKS;
 
     if (warp == 0) {
         if (elect_one()) {
@@ -547,13 +563,20 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             for (int i = first; i < tiles; i += pairs) {
                 int rt, ct;
                 tile_at(a, i, row_tiles, rt, ct);
-                const int row = rt * kTile + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
+                const int row = rt * ROWS + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
                 for (int k = 0; k < steps; ++k) {
                     wait(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
-                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * p.kStageBytes);
-                    const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
-                    tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
-                    tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
+                    if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, BLOCKS * p.kStageBytes);
+                    if (TWO) {
+                        const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
+                        tma_load2_pair(p.a(ring.stage), x, full, k * kStep, row);
+                        tma_load2_pair(p.b(ring.stage), &a.w, full, k * kStep, word);
+                    } else {
+                        const uint32_t full = p.full + 8 * ring.stage;
+                        tma_load2(p.a(ring.stage), x, full, k * kStep, row);
+                        tma_load2(p.b(ring.stage), &a.w, full, k * kStep, word);
+                        tma_load2(p.b(ring.stage) + kOperandBytes, &a.w, full, k * kStep, word + 128);
+                    }
                     ring.next<STAGES>();
                 }
             }
@@ -564,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
             Ring ring;
             uint32_t acc = 0;
             for (int i = first; i < tiles; i += pairs, ++acc)
-                tile_products(p, ring, acc, 1, steps, mma_desc_pair(kTile, false, false), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
+                tile_products(p, ring, acc, 1, steps, TWO ? mma_desc_pair(kTile, false, false) : mma_desc(kTile, false), [](uint32_t s, int i) { return desc_k_major(s + 32 * i); },
                               [](uint32_t s, int i) { return desc_k_major(s + 32 * i); });
         }
     } else {
@@ -590,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
         for (int i = first + acc * pairs; i < tiles; i += every * pairs, acc += every) {
             int rt, ct;
             tile_at(a, i, row_tiles, rt, ct);
-            const int block_row = 32 * quad + lane, row = rt * kTile + p.rank * 128 + block_row;
+            const int block_row = 32 * quad + lane, row = rt * ROWS + p.rank * 128 + block_row;
             const int c0 = (a.tile0 + ct) * kTile + column0;       // first word
             int label = -1;
             LabelQueue queue;
@@ -666,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) logit_k
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z[j] = used && w0 + j < a.vocab ? z[j] : 0;
                     }
-                    uint8_t* const to = a.dz + ((size_t)(rt * 2 + p.rank) * (a.tiles * 4) + ct * 4) * 16384 + (column0 / 8 + 4 * c) * 2048 + block_row * 16;
+                    uint8_t* const to = a.dz + ((size_t)(rt * BLOCKS + p.rank) * (a.tiles * 4) + ct * 4) * 16384 + (column0 / 8 + 4 * c) * 2048 + block_row * 16;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t v[4];
@@ -915,7 +938,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         tma_prefetch(&a.x);
         tma_prefetch(&a.w);
     }
-    const Pair<kProductStages, 2> p = pair_begin<kProductStages, 2>(sm.stages, &sm.bars);
+    const Pair<kProductStages, 2, true> p = pair_begin<kProductStages, 2, true>(sm.stages, &sm.bars);
     grid_dependency_sync();
     const int count = a.plain ? a.rows : *a.count;
     const Deal deal = deal_of(a, count, blockIdx.x / 2);
@@ -1403,13 +1426,22 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
 
 int grid_of(int64_t tiles) { return 2 * (int)(tiles < kPairs ? tiles : kPairs); }
 
-template <bool BACKWARD, bool TOP>
+template <bool BACKWARD, bool TOP, bool TWO>
 int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
     static SmemLimit limit;
-    constexpr size_t smem = sizeof(LogitSmem<BACKWARD>) + 1024;
-    if (!limit.raise(logit_kernel<BACKWARD, TOP>, device, smem)) return ALSGD_E_CUDA;
+    constexpr size_t smem = sizeof(LogitSmem<BACKWARD, TWO>) + 1024;
+    if (!limit.raise(logit_kernel<BACKWARD, TOP, TWO>, device, smem)) return ALSGD_E_CUDA;
     const int64_t tiles = (int64_t)(a.padded / kTile) * a.tiles;
-    return launch_dependent(logit_kernel<BACKWARD, TOP>, dim3(grid_of(tiles)), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+    const int grid = TWO ? grid_of(tiles) : std::min(a.tiles, kSMs);
+    return launch_dependent(logit_kernel<BACKWARD, TOP, TWO>, dim3(grid), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+}
+
+// Up to 128 rows every block forms logits by itself.  (RULE)
+template <bool BACKWARD>
+int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
+    if (a.plain && a.rows <= kTile / 2)
+        return a.top ? launch_logits<BACKWARD, true, false>(a, device, s) : launch_logits<BACKWARD, false, false>(a, device, s);
+    return a.top ? launch_logits<BACKWARD, true, true>(a, device, s) : launch_logits<BACKWARD, false, true>(a, device, s);
 }
 
 int forward(const Call& c, bool teacher, float* loss, float* lse) {
@@ -1429,7 +1461,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     a.by_group = divide_by(kGroup * a.tiles);
     a.stats = at<float2>(c, p.stats);
     a.label_z = at<float>(c, p.label_z);
-    if ((rc = d.top ? launch_logits<false, true>(a, d.device, c.stream) : launch_logits<false, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
+    if ((rc = launch_logits<false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
     LossArgs l;
     std::memset(&l, 0, sizeof l);
     l.stats = a.stats;
@@ -1543,7 +1575,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         m.splits = (4 * m.tiles + p.dx.split_steps - 1) / p.dx.split_steps;
         m.add = i > 0;
         m.last = i + 1 == p.pieces && p.dx.splits == 1;
-        if ((rc = d.top ? launch_logits<true, true>(a, d.device, c.stream) : launch_logits<true, false>(a, d.device, c.stream)) != ALSGD_OK) return rc;
+        if ((rc = launch_logits<true>(a, d.device, c.stream)) != ALSGD_OK) return rc;
         m.dw_groups = (m.tiles + p.dw.subs - 1) / p.dw.subs;
         m.by_dw_groups = divide_by(m.dw_groups);
         const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.dx.splits + (int64_t)m.tiles * p.dim_tiles * p.dw.splits);
