@@ -57,7 +57,7 @@ __device__ __forceinline__ float teacher_at(const Labels& l, size_t i) {
     return l.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(l.teacher)[i] << 16) : static_cast<const float*>(l.teacher)[i];
 }
 
-constexpr int kCountRows = 256;        // rows of a counting block
+constexpr int kCountRows = 64;         // rows of a counting block
 
 // Which rows take part: their number in each block of rows, and each row's place among its block's (-1 - place among those
 // that do not).  A teacher's entries are read in a row by as many threads as a block may have.
@@ -115,96 +115,118 @@ struct GatherArgs {
     int* index;                        // [padded][top] ascending, then places that take no part; teacher only
     float* weight;                     // [padded][top]
     float* entropy;                    // [padded]: sum t log t
-    uint8_t* first;                    // [padded][4 * tiles + 1]: entries below the first word of each quarter of a tile
+    uint32_t* first;                   // [padded][tiles + 1]: four bytes, the entries below the first word of each quarter of a tile
     float *lse2, *coef;                // [padded]; backward only
 };
 
 constexpr int kGatherWarps = 4;
 
 // One row's list by one warp: the teacher's softmax over the entries that take part, then the entries in ascending order of
-// their words.
-__device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int slot, bool used, int* words, int* sorted, int lane) {
-    uint8_t* first = a.first + (size_t)slot * (4 * a.tiles + 1);
+// their words.  E: entries of a lane.
+template <int E>
+__device__ __forceinline__ void teacher_list(const GatherArgs& a, int r, int slot, bool used, int* keys, uint32_t* counts, int lane) {
+    uint32_t* first = a.first + (size_t)slot * (a.tiles + 1);
     if (!used) {
-        for (int t = lane; t <= 4 * a.tiles; t += 32) first[t] = 0;
+        for (int t = lane; t <= a.tiles; t += 32) first[t] = 0;
         if (a.plain && lane == 0) a.target[slot] = -1;
         return;
     }
-    constexpr int E = kMaxTop / 32;
+    constexpr int kNone = 1 << 30;                                 // behind every word's key
     const float c = a.scale * kLog2e;
-    int at[E];
+    int key[E];                                                    // word, then the entry's number: all different
     float v[E], top = -INFINITY, sum = 0.0f;
-    bool nan = false;
+    bool nan = false, any = false;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int k = lane + 32 * e;
-        at[e] = INT_MAX;
+        key[e] = kNone | k;
         v[e] = -INFINITY;
         if (k < a.l.top) {
             const size_t i = (size_t)r * a.l.top + k;
             const int word = label_at(a.l, i);
             const float t = teacher_at(a.l, i);
             if (word >= 0 && t != -INFINITY) {
-                at[e] = word;
+                key[e] = word * kMaxTop + k;
                 v[e] = t;
+                any = true;
             }
-            words[k] = at[e];
         }
+        keys[k] = key[e];                                          // those behind the list are behind every entry
         nan |= v[e] != v[e];
         top = fmaxf(top, v[e]);
     }
+    any = __any_sync(~0u, any);
     for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
     if (__any_sync(~0u, nan)) top = NAN;
-    if (a.plain) {
-        bool any = false;
+    if (!any) top = 0.0f;                                          // plain rows: the list is empty; so is everything below
+    if (a.plain && lane == 0) a.target[slot] = any ? 0 : -1;
 #pragma unroll
-        for (int e = 0; e < E; ++e) any |= at[e] != INT_MAX;
-        any = __any_sync(~0u, any);
-        if (lane == 0) a.target[slot] = any ? 0 : -1;
-        if (!any) top = 0.0f;                                      // the list is empty; so is everything below
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c);
+    for (int e = 0; e < E; ++e) sum += key[e] >= kNone ? 0.0f : exp2f((v[e] - top) * c);
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
     const float inv = 1.0f / sum, log_sum = logf(sum);
-    float entropy = 0.0f;
+    int rank[E] = {};
     __syncwarp();
+    for (int j = 0; j < a.l.top; j += 4) {
+        const int4 q = *reinterpret_cast<const int4*>(keys + j);
+#pragma unroll
+        for (int e = 0; e < E; ++e) rank[e] += (q.x < key[e]) + (q.y < key[e]) + (q.z < key[e]) + (q.w < key[e]);
+    }
+    float entropy = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int k = lane + 32 * e;
-        if (k >= a.l.top) continue;
-        const float t = at[e] == INT_MAX ? 0.0f : exp2f((v[e] - top) * c) * inv;
-        if (at[e] != INT_MAX) entropy += t * ((v[e] - top) * a.scale - log_sum);
-        int rank = 0;
-        for (int j = 0; j < a.l.top; ++j) rank += words[j] < at[e] || (words[j] == at[e] && j < k);
-        sorted[rank] = at[e];
-        a.index[(size_t)slot * a.l.top + rank] = at[e];
-        a.weight[(size_t)slot * a.l.top + rank] = t;
+        const bool is = key[e] < kNone;
+        const float t = is ? exp2f((v[e] - top) * c) * inv : 0.0f;
+        if (is) entropy += t * ((v[e] - top) * a.scale - log_sum);
+        if (lane + 32 * e >= a.l.top) continue;
+        const int word = is ? key[e] / kMaxTop : INT_MAX;
+        a.index[(size_t)slot * a.l.top + rank[e]] = word;
+        a.weight[(size_t)slot * a.l.top + rank[e]] = t;
     }
     for (int d = 16; d; d >>= 1) entropy += __shfl_xor_sync(~0u, entropy, d);
     if (lane == 0) a.entropy[slot] = entropy;
-    __syncwarp();
-#pragma unroll 4
-    for (int t = lane; t <= 4 * a.tiles; t += 32) {
-        const int word = min(t * (kTile / 4), a.l.vocab);          // places that take no part are behind every word
-        int low = 0;
+    // entries below each quarter of a tile: counted by quarters, 32 tiles at a time, then summed up: four quarters are the bytes
+    // of a word (there are at most 128 entries), and so many ones side by side multiply it into its own running sums.  (A binary
+    // search for every quarter took half of this kernel's instructions.)
+    int below = 0;
+    for (int t0 = 0; t0 <= a.tiles; t0 += 32) {
+        counts[lane] = 0;
+        __syncwarp();
 #pragma unroll
-        for (int step = kMaxTop / 2; step; step /= 2)
-            if (low + step <= a.l.top && sorted[low + step - 1] < word) low += step;
-        if (low < a.l.top && sorted[low] < word) ++low;            // the steps add up to one less than the longest list
-        first[t] = (uint8_t)low;
+        for (int e = 0; e < E; ++e) {
+            const int at = key[e] / kMaxTop / (kTile / 4) + 1 - 4 * t0;        // counts for the quarters behind its own
+            if (key[e] < kNone && at >= 0 && at < 128) atomicAdd(&counts[at / 4], 1u << (8 * (at & 3)));
+        }
+        __syncwarp();
+        const uint32_t sums = counts[lane] * 0x01010101u;
+        int before = sums >> 24;
+        for (int d = 1; d < 32; d *= 2) {
+            const int other = __shfl_up_sync(~0u, before, d);
+            if (lane >= d) before += other;
+        }
+        const uint32_t off = below + before - (sums >> 24);
+        if (t0 + lane <= a.tiles) first[t0 + lane] = sums + off * 0x01010101u;
+        below += __shfl_sync(~0u, before, 31);
+        __syncwarp();
     }
+}
+
+__device__ __forceinline__ void teacher_lists(const GatherArgs& a, int r, int slot, bool used, int* keys, uint32_t* counts, int lane) {
+    static_assert(kMaxTop == 128, "one more case");
+    if (a.l.top <= 32) teacher_list<1>(a, r, slot, used, keys, counts, lane);
+    else if (a.l.top <= 64) teacher_list<2>(a, r, slot, used, keys, counts, lane);
+    else teacher_list<4>(a, r, slot, used, keys, counts, lane);
 }
 
 // One warp per row: its place, its copy of x, its labels, what the gradient scales by.
 __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_constant__ GatherArgs a) {
-    __shared__ int s_index[kGatherWarps][kMaxTop], s_sorted[kGatherWarps][kMaxTop];
+    __shared__ __align__(16) int s_index[kGatherWarps][kMaxTop];
+    __shared__ uint32_t s_counts[kGatherWarps][32];
     __shared__ int s_sum[2];
     grid_dependency_sync();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int r0 = blockIdx.x * kGatherWarps, r = r0 + warp, block = r0 / kCountRows;     // a block's rows share a counting block
     if (a.plain) {
-        teacher_lists(a, r, r, r < a.l.rows, s_index[warp], s_sorted[warp], lane);
+        teacher_lists(a, r, r, r < a.l.rows, s_index[warp], s_counts[warp], lane);
         return;
     }
     int before = 0, total = 0;
@@ -251,7 +273,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
         }
         if (a.target) a.target[slot] = used ? label_at(a.l, r) : -1;
     }
-    if (a.l.teacher) teacher_lists(a, r, slot, used, s_index[warp], s_sorted[warp], lane);
+    if (a.l.teacher) teacher_lists(a, r, slot, used, s_index[warp], s_counts[warp], lane);
 }
 
 // ---------------------------------------------------------------------------------------------- the pair's machinery
@@ -619,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
             LabelQueue queue;
             const size_t list = (size_t)row * a.top;
             if (TOP) {
-                const uint8_t* f = a.first + (size_t)row * (4 * a.all_tiles + 1) + 4 * (a.tile0 + ct) + column0 / 64;
+                const uint8_t* f = a.first + 4 * ((size_t)row * (a.all_tiles + 1) + a.tile0 + ct) + column0 / 64;
                 const bool listed = row < count;                   // what fills the tile up has no list
                 queue.start(a.index + list, BACKWARD ? a.weight + list : nullptr, listed ? f[0] : 0, listed ? f[chunks / 2] : 0);
             }
@@ -739,7 +761,7 @@ constexpr int kLossRows = 32, kLossParts = 16;
 
 // 32 rows in gathered order, sixteen threads for each.  The rows that take no part get zeros.
 __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a, const int* row_of) {
-    __shared__ float s_top[kLossParts][kLossRows], s_sum[kLossParts][kLossRows], s_z[kLossParts][kLossRows], s_weight[kLossParts][kLossRows];
+    __shared__ float s_top[kLossParts][kLossRows], s_sum[kLossParts][kLossRows], s_z[kLossRows], s_weight[kLossRows];
     grid_dependency_sync();
     const int count = a.plain ? a.rows : *a.count, i = threadIdx.x % kLossRows, part = threadIdx.x / kLossRows, row = blockIdx.x * kLossRows + i;
     if (!a.plain && threadIdx.x < kLossRows && row < a.rows && a.slot[row] < 0) a.loss[row] = a.lse[row] = 0.0f;
@@ -760,27 +782,33 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
         for (int i = 0; i < N; ++i) sum += s[i].y * exp2f(fmaf(s[i].x, a.scale2, -ref));
         top = m;
     }
+    // a row's labels by sixteen threads next to one another
+    const int list_i = threadIdx.x / kLossParts, list_row = blockIdx.x * kLossRows + list_i;
     float z = 0.0f, weight = 0.0f;                             // sum t z, sum t
-    if (row < count && !(a.plain && a.top && a.target[row] < 0))
+    if (list_row < count && !(a.plain && a.top && a.target[list_row] < 0))
 #pragma unroll 4
-        for (int k = part; k < a.top; k += kLossParts) {
-            const size_t at = (size_t)row * a.top + k;
+        for (int k = threadIdx.x % kLossParts; k < a.top; k += kLossParts) {
+            const size_t at = (size_t)list_row * a.top + k;
             const float t = a.index[at] == INT_MAX ? 0.0f : a.weight[at], label = a.label_z[at];
             z += t == 0.0f ? 0.0f : t * label;                 // nothing was written for the entries that take no part
             weight += t;
         }
+    for (int d = kLossParts / 2; d; d >>= 1) {
+        z += __shfl_xor_sync(~0u, z, d);
+        weight += __shfl_xor_sync(~0u, weight, d);
+    }
+    if (threadIdx.x % kLossParts == 0) {
+        s_z[list_i] = z;
+        s_weight[list_i] = weight;
+    }
     s_top[part][i] = top;
     s_sum[part][i] = sum;
-    s_z[part][i] = z;
-    s_weight[part][i] = weight;
     __syncthreads();
     if (part || row >= count) return;
     for (int q = 1; q < kLossParts; ++q) {
         const float m = fmaxf(top, s_top[q][i]), ref = m == -INFINITY ? 0.0f : m * a.scale2;
         sum = sum * exp2f(fmaf(top, a.scale2, -ref)) + s_sum[q][i] * exp2f(fmaf(s_top[q][i], a.scale2, -ref));
         top = m;
-        z += s_z[q][i];
-        weight += s_weight[q][i];
     }
     const float lse = fmaf(top, a.scale, logf(sum));
     if (a.plain && (a.top ? a.target[row] : label_at(a.l, row)) < 0) {
@@ -788,7 +816,7 @@ __global__ void __launch_bounds__(kLossRows * kLossParts) loss_kernel(LossArgs a
         return;
     }
     const int r = a.plain ? row : row_of[row];
-    a.loss[r] = a.top ? a.entropy[row] - a.scale * z + lse * weight : lse - a.scale * a.label_z[row];
+    a.loss[r] = a.top ? a.entropy[row] - a.scale * s_z[i] + lse * s_weight[i] : lse - a.scale * a.label_z[row];
     a.lse[r] = lse;
 }
 
@@ -1237,7 +1265,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.index = take(4 * padded * d.top);
         p.weight = take(4 * padded * d.top);
         p.entropy = take(4 * padded);
-        p.first = take(padded * (4 * p.tiles + 1));
+        p.first = take(4 * padded * (p.tiles + 1));
     }
     p.target = take(4 * padded);
     if (backward) {
@@ -1378,7 +1406,7 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
         g.index = at<int>(c, p.index);
         g.weight = at<float>(c, p.weight);
         g.entropy = at<float>(c, p.entropy);
-        g.first = at<uint8_t>(c, p.first);
+        g.first = at<uint32_t>(c, p.first);
     }
     if (!d.top || g.plain) g.target = at<int>(c, p.target);
     if (lse) {
