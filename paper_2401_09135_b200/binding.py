@@ -655,7 +655,7 @@ class Rotary:
             d.base, d.factor, d.context, d.amplitude = float(base), float(factor), float(context), float(amplitude)
             d.turns_low, d.turns_high = float(turns[0]), float(turns[1])
             descs.append(d)
-        # a call's direction and the positions' type choose among descriptors, so that calls of several threads share nothing
+        # a call's direction and the positions' type choose among descriptors
         self._descs = {}
         for d in descs:
             for code in (I32, I64):
@@ -664,12 +664,15 @@ class Rotary:
                 self._descs[bool(d.flags & ROPE_INVERSE), code] = e
         self._q_shape, self._k_shape = (batch, length, heads_q, dim), (batch, length, heads_k, dim)
         self._index = int(device)
+        # filled at every call (making new ones costs as much again as all other checks), so calls go out one by one
+        self._slots, self._lock = [AttnTensor() for _ in range(4)], threading.Lock()
 
-    def _operand(self, t, shape):
+    def _operand(self, slot, t, shape):
         assert t.dtype is self.dtype and t.shape == shape and t.get_device() == self._index
-        b, s, h, d = t.stride()
+        slot.stride_batch, slot.stride_pos, slot.stride_head, d = t.stride()
         assert d == 1
-        return AttnTensor(t.data_ptr(), b, s, h)
+        slot.data = t.data_ptr()
+        return slot
 
     def alsgd_rope(self, q, k, q_out, k_out, positions=None, inverse=False, stream=None):
         """q_out and k_out are written and may be q and k; k and k_out are None without key heads.  positions: int32 or int64
@@ -680,10 +683,16 @@ class Rotary:
             code = _whole_code(self.torch, positions.dtype)
         keys = self._k_shape[2] > 0
         assert keys or (k is None and k_out is None)
-        _check(lib().alsgd_rope(self._descs[bool(inverse), code], self._operand(q, self._q_shape),
-                                self._operand(k, self._k_shape) if keys else None, positions.data_ptr() if positions is not None else None,
-                                self._operand(q_out, self._q_shape), self._operand(k_out, self._k_shape) if keys else None,
-                                _stream(self.torch, self._index, stream)), "alsgd_rope")
+        at = positions.data_ptr() if positions is not None else None
+        q_in, k_in, q_to, k_to = self._slots
+        with self._lock:
+            self._operand(q_in, q, self._q_shape)
+            self._operand(q_to, q_out, self._q_shape)
+            if keys:
+                self._operand(k_in, k, self._k_shape)
+                self._operand(k_to, k_out, self._k_shape)
+            _check(lib().alsgd_rope(self._descs[bool(inverse), code], q_in, k_in if keys else None, at, q_to, k_to if keys else None,
+                                    _stream(self.torch, self._index, stream)), "alsgd_rope")
 
     def alsgd_rope_frequencies(self):
         """Angle per position of every pair, scaled as the plan says."""
@@ -711,38 +720,48 @@ class VocabLoss:
         self._labels_shape = (rows, top) if top else (rows,)
         self._index = int(device)
         self._work = {}                    # of either pass, made at its first call
-        self._lock = threading.Lock()      # its calls go out one by one: they share the workspaces, in stream order
+        self._slots = [Matrix() for _ in range(4)]
+        # its calls go out one by one: they share the matrices' descriptors and, in stream order, the workspaces
+        self._lock = threading.Lock()
+        self._bf16, self._f32 = torch.bfloat16, torch.float32
 
-    def _matrix(self, t, shape):
-        assert t.dtype is self.torch.bfloat16 and t.shape == shape and t.get_device() == self._index
-        assert t.stride(1) == 1 or shape[1] == 1
-        return Matrix(t.data_ptr(), t.stride(0))
+    def _matrix(self, slot, t, shape):
+        assert t.dtype is self._bf16 and t.shape == shape and t.get_device() == self._index
+        slot.stride_row, d = t.stride()
+        assert d == 1 or shape[1] == 1
+        slot.data = t.data_ptr()
+        return slot
 
     def _plain(self, t, shape, dtype):
         assert t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous()
         return t.data_ptr()
 
-    def _call(self, name, backward, operands, stream):
-        raw = _stream(self.torch, self._index, stream)
-        with self._lock:
-            work = self._work.get(backward)
-            if work is None:
-                nbytes = C.c_uint64()
-                _check(lib().alsgd_vocab_bytes(self.desc, int(backward), C.byref(nbytes)), "alsgd_vocab_bytes")
-                work = self._work[backward] = _Workspace(self.torch, int(nbytes.value), self.device, raw)
-            work.used_on(raw)
-            _check(getattr(lib(), name)(self.desc, *operands, work.ptr, work.nbytes, raw), name)
+    def _workspace(self, backward, raw):
+        work = self._work.get(backward)
+        if work is None:
+            nbytes = C.c_uint64()
+            _check(lib().alsgd_vocab_bytes(self.desc, int(backward), C.byref(nbytes)), "alsgd_vocab_bytes")
+            work = self._work[backward] = _Workspace(self.torch, int(nbytes.value), self.device, raw)
+        work.used_on(raw)
+        return work
 
     def _forward(self, name, x, w, labels, loss, lse, stream):
-        f32 = self.torch.float32
-        self._call(name, False, (self._matrix(x, self._x_shape), self._matrix(w, self._w_shape), *labels, self._plain(loss, self._rows, f32),
-                                 self._plain(lse, self._rows, f32)), stream)
+        raw = _stream(self.torch, self._index, stream)
+        loss, lse = self._plain(loss, self._rows, self._f32), self._plain(lse, self._rows, self._f32)
+        with self._lock:
+            work, (sx, sw, _, _) = self._workspace(False, raw), self._slots
+            _check(getattr(lib(), name)(self.desc, self._matrix(sx, x, self._x_shape), self._matrix(sw, w, self._w_shape), *labels, loss, lse,
+                                        work.ptr, work.nbytes, raw), name)
 
     def _backward(self, name, x, w, labels, lse, dloss, dx, dw, stream):
-        f32 = self.torch.float32
-        assert dloss.dtype is f32 and dloss.shape == self._rows and dloss.get_device() == self._index
-        self._call(name, True, (self._matrix(x, self._x_shape), self._matrix(w, self._w_shape), *labels, self._plain(lse, self._rows, f32),
-                                dloss.data_ptr(), dloss.stride(0), self._matrix(dx, self._x_shape), self._matrix(dw, self._w_shape)), stream)
+        assert dloss.dtype is self._f32 and dloss.shape == self._rows and dloss.get_device() == self._index
+        raw = _stream(self.torch, self._index, stream)
+        lse = self._plain(lse, self._rows, self._f32)
+        with self._lock:
+            work, (sx, sw, sdx, sdw) = self._workspace(True, raw), self._slots
+            _check(getattr(lib(), name)(self.desc, self._matrix(sx, x, self._x_shape), self._matrix(sw, w, self._w_shape), *labels, lse,
+                                        dloss.data_ptr(), dloss.stride(0), self._matrix(sdx, dx, self._x_shape),
+                                        self._matrix(sdw, dw, self._w_shape), work.ptr, work.nbytes, raw), name)
 
     def _labels(self, index):
         return (self._plain(index, self._labels_shape, self.index_dtype),)

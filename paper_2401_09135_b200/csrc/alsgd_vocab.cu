@@ -1235,17 +1235,21 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     const uint64_t dx_bytes = 4ull * p.padded * d.dim, dw_bytes = 4ull * p.piece * kTile * d.dim;      // of a part's sums
     auto most = [](uint64_t bytes) { return (int)std::min<uint64_t>(kMaxSplits, std::max<uint64_t>(1, kPieceBytes / (bytes + 1))); };
     int64_t best = INT64_MAX;
-    for (int i = 0; i < 16 && p.padded; ++i) {
-        const Axis dx = split_axis(dx_steps, std::max<int64_t>(8, share / (1 + i % 4)), row_tiles > 1, most(dx_bytes));
-        const Axis dw = split_axis(dw_steps, std::max<int64_t>(8, share / (1 + i / 4)), p.piece > 1, most(dw_bytes));
-        const int64_t dx_n = (row_tiles + dx.subs - 1) / dx.subs * p.dim_tiles * dx.splits, dw_n = (p.piece + dw.subs - 1) / dw.subs * p.dim_tiles * dw.splits;
+    Axis dx[4], dw[4];
+    for (int i = 0; i < 4 && backward; ++i) {
+        dx[i] = split_axis(dx_steps, std::max<int64_t>(8, share / (1 + i)), row_tiles > 1, most(dx_bytes));
+        dw[i] = split_axis(dw_steps, std::max<int64_t>(8, share / (1 + i)), p.piece > 1, most(dw_bytes));
+    }
+    for (int i = 0; i < 16 && backward; ++i) {
+        const Axis &x = dx[i % 4], &w = dw[i / 4];
+        const int64_t dx_n = (row_tiles + x.subs - 1) / x.subs * p.dim_tiles * x.splits, dw_n = (p.piece + w.subs - 1) / w.subs * p.dim_tiles * w.splits;
         // parts are written and read again (a step's time moves about 1 MB) by one more launch (about 12 steps)
-        const int64_t sums = ((dx.splits > 1 ? dx.splits * dx_bytes : 0) + (dw.splits > 1 ? dw.splits * dw_bytes : 0)) >> 19;
-        const int64_t t = steps_until_done(dx_n, dx, dw_n, dw) + sums + (dx.splits > 1 || dw.splits > 1 ? 12 : 0);
+        const int64_t sums = ((x.splits > 1 ? x.splits * dx_bytes : 0) + (w.splits > 1 ? w.splits * dw_bytes : 0)) >> 19;
+        const int64_t t = steps_until_done(dx_n, x, dw_n, w) + sums + (x.splits > 1 || w.splits > 1 ? 12 : 0);
         if (t >= best) continue;
         best = t;
-        p.dx = dx;
-        p.dw = dw;
+        p.dx = x;
+        p.dw = w;
     }
 
     uint64_t at = 0;

@@ -45,8 +45,8 @@ def plan_with(monkeypatch, fake=None, **kw):
     monkeypatch.setattr(B, "lib", lambda: library)
     plan = B.VocabLoss(8, 100, 16, **kw)
     if fake is not None:
-        plan.torch = types.SimpleNamespace(**{n: getattr(fake, n) for n in ("uint8", "empty", "_C", "cuda")}, float32=None)
-    monkeypatch.setattr(plan, "_matrix", lambda t, shape: None)
+        plan.torch = types.SimpleNamespace(**{n: getattr(fake, n) for n in ("uint8", "empty", "_C", "cuda")})
+    monkeypatch.setattr(plan, "_matrix", lambda slot, t, shape: None)
     monkeypatch.setattr(plan, "_plain", lambda t, shape, dtype: None)
     return library, plan
 
@@ -77,7 +77,7 @@ def test_rotary_directions_and_types_have_descriptors_of_their_own(monkeypatch):
     monkeypatch.setattr(B, "lib", lambda: library)
     monkeypatch.setattr(B, "_stream", lambda *a: 0)
     plan = B.Rotary(2, 5, 2, 1, 16, interleaved=True)
-    monkeypatch.setattr(plan, "_operand", lambda t, shape: None)
+    monkeypatch.setattr(plan, "_operand", lambda slot, t, shape: slot)
     for inverse in (False, True):
         for dtype in (None, torch.int32, torch.int64):
             at = None if dtype is None else types.SimpleNamespace(shape=(2, 5), is_contiguous=lambda: True, get_device=lambda: 0, dtype=dtype, data_ptr=lambda: 0)
