@@ -548,9 +548,10 @@ int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out);
  *     dz[i][j] = dloss_i scale (exp(z[i][j] - lse_i) - sum_k t_ik [index_ik = j])    (labels: t = 1)
  *     dx_i = sum_j dz[i][j] w_j,   dw_j = sum_i dz[i][j] x_i
  * Logits, sums and statistics are binary32; dz is rounded to bf16 before the products with w and x.  Results are written, not
- * added to, and do not depend on the order in which blocks run.  The workspace holds a copy of the rows that take part and,
- * backward, dz of a piece of the vocabulary (256 MiB, or 8 KiB a row where that is more) and sums of dx and dw (256 MiB of
- * either, or one of dx where that is more).
+ * added to, and do not depend on the order in which blocks run; they must not overlap the operands.  The workspace holds a
+ * copy of the rows that take part and the teacher's entries; forward, 8 bytes for each row and 256 words; backward, dz of a piece
+ * of the vocabulary (256 MiB, or 8 KiB a row where that is more) and sums of dx and dw (256 MiB of either, or one of dx where that
+ * is more).
  * A NaN or infinity in w or in the x of a row that takes part reaches what is computed from it: the row's loss, all of dw. */
 typedef struct alsgd_vocab_desc {
     uint32_t rows;                     /* up to 2^22; may be 0 */
@@ -576,7 +577,8 @@ int alsgd_vocab_bytes(const alsgd_vocab_desc* desc, int backward_pass, uint64_t*
 /* target: device, [rows] of index_dtype.  index, teacher: device, [rows][top].  loss, lse: device, fp32 [rows].  dloss: device,
  * fp32, dloss_step (>= 0) elements apart: 0 gives every row the same.  dx: [rows][dim], dw: [vocab][dim].  work: device, 256-byte
  * aligned, alsgd_vocab_bytes bytes, any content; calls that share it must be ordered.
- * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step, labels with top > 0 or a teacher without.
+ * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step, labels with top > 0 or a teacher without, a
+ * gradient at its operand's address.
  * ALSGD_E_UNSUPPORTED: top > 128, dim > 16384.  ALSGD_E_RANGE: rows or vocab beyond 2^22, device ordinal outside 0..63.
  * ALSGD_E_NOMEM: work too small. */
 int alsgd_xent_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, float* loss, float* lse,

@@ -51,7 +51,7 @@ def check(p, dloss=None):
 
 @pytest.mark.parametrize("rows,vocab,dim", [
     (1, 1, 8), (1, 300, 64), (2, 7, 16), (5, 256, 64), (64, 255, 72), (77, 257, 136), (128, 1000, 64), (129, 513, 200), (255, 2000, 256),
-    (256, 640, 264), (257, 1024, 96), (300, 5003, 384), (513, 300, 520), (700, 1500, 896), (1000, 1280, 1032), (33, 32000, 384), (512, 700, 64), (5000, 300, 64), (2600, 64, 64), (3000, 1000, 520), (6000, 1, 8),
+    (256, 640, 264), (257, 1024, 96), (300, 5003, 384), (513, 300, 520), (700, 1500, 896), (1000, 1280, 1032), (33, 32000, 384), (512, 700, 64), (5000, 300, 64), (2600, 64, 64), (3000, 1000, 520), (6000, 1, 8), (130, 300, 2056),
 ])
 def test_labels(rows, vocab, dim):
     check(Problem(rows, vocab, dim, seed=rows))
@@ -149,6 +149,19 @@ def test_teacher_rows_of_one_kind():
     loss, lse = forward(plan_of(p), p)
     assert bool(torch.isnan(loss[4:]).all()) and float(loss[2]) == 0.0 and float(lse[2]) == 0.0
     p.teacher[4, 0] = p.teacher[5, 1] = 1.0
+    check(p)
+
+
+@pytest.mark.parametrize("teacher", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [0.25, 1.0, 4.0])
+def test_teacher_masked_by_the_lowest_value(teacher, scale):
+    """Entries at the type's lowest value beside ordinary ones, and beside its highest: no weight, and no NaN."""
+    p = Problem(8, 300, 64, top=5, left_out=0.0, teacher=teacher, scale=scale)
+    p.index[:] = torch.arange(5, device="cuda") * 50
+    p.teacher[:] = torch.randn(8, 5, device="cuda").to(teacher)
+    info = torch.finfo(teacher)
+    p.teacher[:4, 1:3] = info.min
+    p.teacher[4:6, 0], p.teacher[4:6, 1] = info.max, info.min
     check(p)
 
 

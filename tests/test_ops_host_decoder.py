@@ -93,9 +93,9 @@ def call(name, desc=None, x=None, w=None, index=PTR, teacher=PTR, loss=PTR, lse=
     desc = desc if desc is not None else vocab_desc()
     if top and desc.top == 0:
         desc.top = 5
-    m = matrix(step=max(64, desc.dim))
+    m, to = matrix(step=max(64, desc.dim)), matrix(2 * PTR, max(64, desc.dim))
     labels = (index, teacher) if top else (index,)
-    rest = (loss, lse) if name.endswith("fwd") else (lse, dloss, dloss_step, dx or m, dw or m)
+    rest = (loss, lse) if name.endswith("fwd") else (lse, dloss, dloss_step, dx or to, dw or to)
     return getattr(B.lib(), "alsgd_" + name)(desc, x or m, w or m, *labels, *rest, work, work_bytes, None)
 
 
@@ -125,7 +125,7 @@ def test_vocab_refuses_operands(name, kw):
 
 @pytest.mark.parametrize("name", ["xent_bwd", "distill_bwd"])
 @pytest.mark.parametrize("kw", [dict(dloss=None), dict(dloss=PTR + 2), dict(dloss_step=-1), dict(dx=matrix(step=0)), dict(dx=matrix(step=56)),
-                                dict(dw=matrix(step=56)), dict(dw=matrix(PTR + 8)), dict(dx=matrix(None))])
+                                dict(dw=matrix(step=56)), dict(dw=matrix(PTR + 8)), dict(dx=matrix(None)), dict(dx=matrix()), dict(dw=matrix())])
 def test_vocab_refuses_gradients(name, kw):
     assert call(name, **kw) == B.E_ARG
 
