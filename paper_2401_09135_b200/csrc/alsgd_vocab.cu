@@ -967,9 +967,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         tma_prefetch(&a.w);
     }
     const Pair<kProductStages, 2, true> p = pair_begin<kProductStages, 2, true>(sm.stages, &sm.bars);
+    // dealt before the kernel in front has ended, as if every row took part, and once more if not
+    Deal deal = deal_of(a, a.rows, blockIdx.x / 2);
+    asm volatile("" ::"r"(deal.longs), "r"(deal.over), "r"(deal.from));
     grid_dependency_sync();
     const int count = a.plain ? a.rows : *a.count;
-    const Deal deal = deal_of(a, count, blockIdx.x / 2);
+    if (count != a.rows) deal = deal_of(a, count, blockIdx.x / 2);
     const int boxes = (a.n / 2 + 63) / 64;                         // of B in either block
 
     if (count == 0) {
