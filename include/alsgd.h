@@ -526,7 +526,8 @@ typedef struct alsgd_rope_desc {
 /* Operands and results as attention's (steps of fp32 tensors: multiples of 4 elements).  positions: device, [batch][len] of
  * position_dtype, or NULL.  Results may be the operands themselves (same address and steps); any other overlap is undefined.
  * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step.  ALSGD_E_UNSUPPORTED: dim > 256.
- * ALSGD_E_RANGE: len beyond 2^22, more than 2^16 heads, 2^31 tokens, device ordinal outside 0..63. */
+ * ALSGD_E_RANGE: len beyond 2^22, more than 2^16 heads, 2^31 tokens, steps over positions or heads of 2^31 and more, device
+ * ordinal outside 0..63. */
 int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* q, const alsgd_attn_tensor* k, const void* positions,
                const alsgd_attn_tensor* q_out, const alsgd_attn_tensor* k_out, void* stream);
 

@@ -18,20 +18,33 @@ using namespace alsgd_ops;
 
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
-// Units of two groups that a thread has in flight, with five blocks per SM: 23.0 us at 64 x 256 tokens and 32 heads of 64, 33.3 at
-// 4 x 4099 tokens and 20 heads of 128 (5.8 and 5.0 TB/s).  Four units, four blocks: 24.2 and 35.0; two and six: 25.9 and 33.0 (spills).
+// Units of two groups that a thread has in flight, with five blocks per SM: 23.2 us at 64 x 256 tokens and 32 heads of 64, 29.8 at
+// 4 x 4099 tokens and 20 heads of 128 (5.8 and 5.6 TB/s; instructions, 70 % of the issue slots, as much as memory).  With four
+// blocks 24.3 and 31.8, with six (spills) 26.5 and 33.9; four units and four blocks lost as much before.
 constexpr int kUnits = 2;
 constexpr int kMaxTokens = 16;         // of a block
 
+// From one sequence, position, head to the next.
+struct Steps {
+    int64_t batch;
+    int pos, head;
+};
+
+// An operand and its result.
+struct Side {
+    const void* in;
+    void* out;
+    Steps from, to;
+};
+
 struct RopeArgs {
-    const void *q, *k;
-    void *q_out, *k_out;
-    int64_t q_step[3], k_step[3], q_out_step[3], k_out_step[3];    // batch, position, head
+    Side side[2];                      // q, k
     const void* positions;             // may be null
     int wide_positions;                // binary64 whole numbers
     int64_t pos0;
     int len, heads_q, heads, dim, rot, interleaved, tokens, per_block;
     int units, turned, angles;         // of a head; turned: units that begin the two halves
+    int angle_step;                    // angles, to a multiple of four
     Divide by_token, by_units, by_len, by_angles;                  // units of a token, of a head; tokens of a sequence; angles
     float amplitude, turn;             // turn: 1, or -1 for the inverse
     double turns[kMaxDim / 2];         // f_i / (2 pi)
@@ -86,14 +99,14 @@ struct Group {
     }
 };
 
-__device__ __forceinline__ void turn_pair(float2 cs, float& a, float& b) {
+__device__ __forceinline__ void turn_pair(float c, float s, float& a, float& b) {
     const float x = a, y = b;
-    a = fmaf(x, cs.x, -(y * cs.y));
-    b = fmaf(x, cs.y, y * cs.x);
+    a = fmaf(x, c, -(y * s));
+    b = fmaf(x, s, y * c);
 }
 
-// Cosine and sine (times the amplitude) of the block's tokens, [token][angle].
-__device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, int token0, int tokens) {
+// Cosines (times the amplitude) of the block's tokens, [token][angle], and behind them the sines.  A token's begin on 16 bytes.
+__device__ __forceinline__ void fill_angles(const RopeArgs& a, float* table, int token0, int tokens) {
     for (int i = threadIdx.x; i < tokens * a.angles; i += kThreads) {
         const int t = a.by_angles(i), n = i - t * a.angles, token = token0 + t;
         int64_t pos;
@@ -102,7 +115,8 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, in
         const double turns = (double)pos * a.turns[n];
         float s, c;
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        table[i] = make_float2(c * a.amplitude, s * (a.amplitude * a.turn));
+        table[t * a.angle_step + n] = c * a.amplitude;
+        table[(a.per_block + t) * a.angle_step + n] = s * (a.amplitude * a.turn);
     }
 }
 
@@ -111,11 +125,11 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, in
 //   head.  Neighbouring threads take neighbouring groups: 32 bytes a thread in a row took 39 us in place of 35.5 (4 x 4099
 //   tokens, 20 heads of 128, half of each turned).
 struct Unit {
-    int64_t batch, pos, head;          // to be multiplied by steps
+    int batch, pos, head;
     int at[2];
     int token, n;                      // token of the block, unit of the head
-    bool is_q;
-    __device__ __forceinline__ int64_t offset(const int64_t (&step)[3]) const { return batch * step[0] + pos * step[1] + head * step[2]; }
+    int side;
+    __device__ __forceinline__ int64_t offset(const Steps& s) const { return batch * s.batch + (int64_t)pos * s.pos + (int64_t)head * s.head; }
 };
 // (Plain divisions and remainders here bounded the kernel by its instructions: 33 us at 64 x 256 tokens against 26 with
 // reciprocals.)
@@ -128,8 +142,8 @@ __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
     const int token = token0 + u.token, b = a.by_len(token);
     u.batch = b;
     u.pos = token - b * a.len;
-    u.is_q = head < a.heads_q;
-    u.head = u.is_q ? head : head - a.heads_q;
+    u.side = head >= a.heads_q;
+    u.head = head - (u.side ? a.heads_q : 0);
     if (u.n < a.turned) {
         u.at[0] = N * u.n;
         u.at[1] = a.rot / 2 + u.at[0];
@@ -143,11 +157,11 @@ __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
 // N: 8, or what divides half of the turned part where the halves are apart (every group then lies where a load of its size may).
 template <typename T, int N>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
-    extern __shared__ float2 table[];
+    extern __shared__ __align__(16) float table[];
     grid_dependency_sync();
     const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
     const int units = tokens * a.heads * a.units;
-    const bool copies = a.q != a.q_out || a.k != a.k_out;              // in place, what is not turned stays
+    const bool copies = a.side[0].in != a.side[0].out || a.side[1].in != a.side[1].out;      // in place, what is not turned stays
     bool angles = false;
     for (int u0 = threadIdx.x; u0 < units || !angles; u0 += kThreads * kUnits) {
         Group<T, N> raw[kUnits][2];
@@ -156,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
             const Unit u = unit_of<N>(a, token0, i);
-            const T* p = u.is_q ? static_cast<const T*>(a.q) + u.offset(a.q_step) : static_cast<const T*>(a.k) + u.offset(a.k_step);
+            const T* p = static_cast<const T*>(a.side[u.side].in) + u.offset(a.side[u.side].from);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (u.at[h] < a.dim) raw[j][h].load(p + u.at[h]);
@@ -171,22 +185,32 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(
             const int i = u0 + j * kThreads;
             if (i >= units) continue;
             const Unit u = unit_of<N>(a, token0, i);
-            T* p = u.is_q ? static_cast<T*>(a.q_out) + u.offset(a.q_out_step) : static_cast<T*>(a.k_out) + u.offset(a.k_out_step);
-            const float2* cs = table + u.token * a.angles;
+            T* p = static_cast<T*>(a.side[u.side].out) + u.offset(a.side[u.side].to);
+            const float *cosine = table + u.token * a.angle_step, *sine = cosine + a.per_block * a.angle_step;
             float e[2][N];
             raw[j][0].widen(e[0]);
             raw[j][1].widen(e[1]);
             if (u.n < a.turned) {
+                constexpr int M = N < 4 ? N : 4;                   // angles at a time
 #pragma unroll
-                for (int x = 0; x < N; ++x) turn_pair(cs[N * u.n + x], e[0][x], e[1][x]);
+                for (int x0 = 0; x0 < N; x0 += M) {
+                    Group<float, M> c, s;
+                    c.load(cosine + N * u.n + x0);
+                    s.load(sine + N * u.n + x0);
+#pragma unroll
+                    for (int x = 0; x < M; ++x) turn_pair(__uint_as_float(c.w[x]), __uint_as_float(s.w[x]), e[0][x0 + x], e[1][x0 + x]);
+                }
             } else if (N == 8 && a.interleaved) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int x = 0; x < N / 2; ++x) {
-                        const int pair = u.at[h] / 2 + x;
-                        if (pair < a.angles) turn_pair(cs[pair], e[h][2 * x], e[h][2 * x + 1]);
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    const int pair = u.at[h] / 2;
+                    if (pair >= a.angles) continue;
+                    const float4 c = *reinterpret_cast<const float4*>(cosine + pair), s = *reinterpret_cast<const float4*>(sine + pair);
+                    turn_pair(c.x, s.x, e[h][0], e[h][1]);
+                    if (pair + 1 < a.angles) turn_pair(c.y, s.y, e[h][2 % N], e[h][3 % N]);
+                    if (pair + 2 < a.angles) turn_pair(c.z, s.z, e[h][4 % N], e[h][5 % N]);
+                    if (pair + 3 < a.angles) turn_pair(c.w, s.w, e[h][6 % N], e[h][7 % N]);
+                }
             } else if (!copies) {
                 continue;
             }
@@ -207,14 +231,13 @@ int check_rope_tensor(const alsgd_attn_tensor* t, const alsgd_rope_desc& d, uint
         if (extent[i] == 1) continue;
         if (step[i] < 0 || step[i] % unit || step[i] >= (1ll << 39)) return ALSGD_E_ARG;
         if (step[i] == 0 && output) return ALSGD_E_ARG;
+        if (i < 2 && step[i] > INT32_MAX) return ALSGD_E_RANGE;
     }
     return ALSGD_OK;
 }
 
-void steps_of(const alsgd_attn_tensor& t, int64_t (&step)[3]) {
-    step[0] = t.stride_batch;
-    step[1] = t.stride_pos;
-    step[2] = t.stride_head;
+Steps steps_of(const alsgd_attn_tensor& t, const alsgd_rope_desc& d, uint32_t heads) {
+    return {d.batch > 1 ? t.stride_batch : 0, d.len > 1 ? (int)t.stride_pos : 0, heads > 1 ? (int)t.stride_head : 0};
 }
 
 int check_rope(const alsgd_rope_desc* d) {
@@ -289,16 +312,8 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
 
     RopeArgs a;
     std::memset(&a, 0, sizeof a);
-    a.q = q->data;
-    a.q_out = q_out->data;
-    steps_of(*q, a.q_step);
-    steps_of(*q_out, a.q_out_step);
-    if (d.heads_k) {
-        a.k = k->data;
-        a.k_out = k_out->data;
-        steps_of(*k, a.k_step);
-        steps_of(*k_out, a.k_out_step);
-    }
+    a.side[0] = {q->data, q_out->data, steps_of(*q, d, d.heads_q), steps_of(*q_out, d, d.heads_q)};
+    if (d.heads_k) a.side[1] = {k->data, k_out->data, steps_of(*k, d, d.heads_k), steps_of(*k_out, d, d.heads_k)};
     a.positions = positions;
     a.wide_positions = d.position_dtype == ALSGD_I64;
     a.pos0 = d.pos0;
@@ -310,6 +325,7 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     a.interleaved = (d.flags & ALSGD_ROPE_INTERLEAVED) != 0;
     a.tokens = (int)(d.batch * d.len);
     a.angles = a.rot / 2;
+    a.angle_step = (a.angles + 3) / 4 * 4;
     a.amplitude = (float)d.amplitude;
     a.turn = d.flags & ALSGD_ROPE_INVERSE ? -1.0f : 1.0f;
     frequencies(d, a.turns);
@@ -330,7 +346,7 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     if (a.per_block > kMaxTokens) a.per_block = kMaxTokens;
     if (a.per_block < 1) a.per_block = 1;
     const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kThreads);
-    const size_t smem = (size_t)a.per_block * a.angles * sizeof(float2);       // at most 16 KB
+    const size_t smem = 2ull * a.per_block * a.angle_step * sizeof(float);     // at most 16 KB
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = d.dtype == ALSGD_F32 ? launch<float>(group, grid, block, smem, s, a) : launch<uint16_t>(group, grid, block, smem, s, a);
     return e == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;

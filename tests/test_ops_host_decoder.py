@@ -58,6 +58,7 @@ def test_rope_refuses_nothing_at_all():
     assert L.alsgd_rope(rope_desc(), t, None, None, t, t, None) == B.E_ARG and L.alsgd_rope_frequencies(rope_desc(), None) == B.E_ARG
     assert rope(desc=rope_desc(position_dtype=B.I64), positions=PTR + 4) == B.E_ARG
     assert rope(desc=rope_desc(dtype=B.F32), q=tensor(h=130)) == B.E_ARG
+    assert rope(q=tensor(s=1 << 31)) == B.E_RANGE and rope(k_out=tensor(h=1 << 31)) == B.E_RANGE
     assert L.alsgd_rope(rope_desc(len=0), None, None, None, None, None, None) == B.OK
 
 
