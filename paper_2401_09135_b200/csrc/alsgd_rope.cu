@@ -18,9 +18,9 @@ using namespace alsgd_ops;
 
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
-// Units of two groups that a thread has in flight, with five blocks per SM: 23.2 us at 64 x 256 tokens and 32 heads of 64, 29.8 at
-// 4 x 4099 tokens and 20 heads of 128 (5.8 and 5.6 TB/s; instructions, 70 % of the issue slots, as much as memory).  With four
-// blocks 24.3 and 31.8, with six (spills) 26.5 and 33.9; four units and four blocks lost as much before.
+// Units of two groups that a thread has in flight, with five blocks per SM: 21.6 us at 64 x 256 tokens and 32 heads of 64, 28.8 at
+// 4 x 4099 tokens and 20 heads of 128 (6.2 and 5.8 TB/s).  Instructions count here as much as memory (70 % of the issue slots): with
+// four blocks, or six and spilled registers, both were 5 to 15 % slower, and with four units.
 constexpr int kUnits = 2;
 constexpr int kMaxTokens = 16;         // of a block
 
@@ -40,11 +40,11 @@ struct Side {
 struct RopeArgs {
     Side side[2];                      // q, k
     const void* positions;             // may be null
-    int wide_positions;                // binary64 whole numbers
+    int wide_positions;                // of 64 bits
     int64_t pos0;
     int len, heads_q, heads, dim, rot, interleaved, tokens, per_block;
     int units, turned, angles;         // of a head; turned: units that begin the two halves
-    int angle_step;                    // angles, to a multiple of four
+    int angle_step;                    // angles, to an even number
     Divide by_token, by_units, by_len, by_angles;                  // units of a token, of a head; tokens of a sequence; angles
     float amplitude, turn;             // turn: 1, or -1 for the inverse
     double turns[kMaxDim / 2];         // f_i / (2 pi)
@@ -105,8 +105,8 @@ __device__ __forceinline__ void turn_pair(float c, float s, float& a, float& b) 
     b = fmaf(x, s, y * c);
 }
 
-// Cosines (times the amplitude) of the block's tokens, [token][angle], and behind them the sines.  A token's begin on 16 bytes.
-__device__ __forceinline__ void fill_angles(const RopeArgs& a, float* table, int token0, int tokens) {
+// Cosine and sine (times the amplitude) of the block's tokens, [token][angle].  A token's begin on 16 bytes.
+__device__ __forceinline__ void fill_angles(const RopeArgs& a, float2* table, int token0, int tokens) {
     for (int i = threadIdx.x; i < tokens * a.angles; i += kThreads) {
         const int t = a.by_angles(i), n = i - t * a.angles, token = token0 + t;
         int64_t pos;
@@ -115,8 +115,7 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& a, float* table, int
         const double turns = (double)pos * a.turns[n];
         float s, c;
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        table[t * a.angle_step + n] = c * a.amplitude;
-        table[(a.per_block + t) * a.angle_step + n] = s * (a.amplitude * a.turn);
+        table[t * a.angle_step + n] = make_float2(c * a.amplitude, s * (a.amplitude * a.turn));
     }
 }
 
@@ -157,7 +156,7 @@ __device__ __forceinline__ Unit unit_of(const RopeArgs& a, int token0, int i) {
 // N: 8, or what divides half of the turned part where the halves are apart (every group then lies where a load of its size may).
 template <typename T, int N>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
-    extern __shared__ __align__(16) float table[];
+    extern __shared__ __align__(16) float2 table[];
     grid_dependency_sync();
     const int token0 = blockIdx.x * a.per_block, tokens = min(a.per_block, a.tokens - token0);
     const int units = tokens * a.heads * a.units;
@@ -186,30 +185,32 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3) rope_kernel(
             if (i >= units) continue;
             const Unit u = unit_of<N>(a, token0, i);
             T* p = static_cast<T*>(a.side[u.side].out) + u.offset(a.side[u.side].to);
-            const float *cosine = table + u.token * a.angle_step, *sine = cosine + a.per_block * a.angle_step;
+            const float2* cs = table + u.token * a.angle_step;
             float e[2][N];
             raw[j][0].widen(e[0]);
             raw[j][1].widen(e[1]);
             if (u.n < a.turned) {
-                constexpr int M = N < 4 ? N : 4;                   // angles at a time
+                if constexpr (N == 1) {
+                    turn_pair(cs[u.n].x, cs[u.n].y, e[0][0], e[1][0]);
+                } else {
 #pragma unroll
-                for (int x0 = 0; x0 < N; x0 += M) {
-                    Group<float, M> c, s;
-                    c.load(cosine + N * u.n + x0);
-                    s.load(sine + N * u.n + x0);
-#pragma unroll
-                    for (int x = 0; x < M; ++x) turn_pair(__uint_as_float(c.w[x]), __uint_as_float(s.w[x]), e[0][x0 + x], e[1][x0 + x]);
+                    for (int x = 0; x < N; x += 2) {
+                        const float4 two = *reinterpret_cast<const float4*>(cs + N * u.n + x);
+                        turn_pair(two.x, two.y, e[0][x], e[1][x]);
+                        turn_pair(two.z, two.w, e[0][x + 1], e[1][x + 1]);
+                    }
                 }
             } else if (N == 8 && a.interleaved) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int pair = u.at[h] / 2;
-                    if (pair >= a.angles) continue;
-                    const float4 c = *reinterpret_cast<const float4*>(cosine + pair), s = *reinterpret_cast<const float4*>(sine + pair);
-                    turn_pair(c.x, s.x, e[h][0], e[h][1]);
-                    if (pair + 1 < a.angles) turn_pair(c.y, s.y, e[h][2 % N], e[h][3 % N]);
-                    if (pair + 2 < a.angles) turn_pair(c.z, s.z, e[h][4 % N], e[h][5 % N]);
-                    if (pair + 3 < a.angles) turn_pair(c.w, s.w, e[h][6 % N], e[h][7 % N]);
+#pragma unroll
+                    for (int x = 0; x < N / 2; x += 2) {
+                        if (pair + x >= a.angles) break;
+                        const float4 two = *reinterpret_cast<const float4*>(cs + pair + x);
+                        turn_pair(two.x, two.y, e[h][2 * x], e[h][2 * x + 1]);
+                        if (pair + x + 1 < a.angles) turn_pair(two.z, two.w, e[h][2 * x + 2], e[h][2 * x + 3]);
+                    }
                 }
             } else if (!copies) {
                 continue;
@@ -325,7 +326,7 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     a.interleaved = (d.flags & ALSGD_ROPE_INTERLEAVED) != 0;
     a.tokens = (int)(d.batch * d.len);
     a.angles = a.rot / 2;
-    a.angle_step = (a.angles + 3) / 4 * 4;
+    a.angle_step = (a.angles + 1) / 2 * 2;
     a.amplitude = (float)d.amplitude;
     a.turn = d.flags & ALSGD_ROPE_INVERSE ? -1.0f : 1.0f;
     frequencies(d, a.turns);
@@ -346,7 +347,7 @@ extern "C" int alsgd_rope(const alsgd_rope_desc* desc, const alsgd_attn_tensor* 
     if (a.per_block > kMaxTokens) a.per_block = kMaxTokens;
     if (a.per_block < 1) a.per_block = 1;
     const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kThreads);
-    const size_t smem = 2ull * a.per_block * a.angle_step * sizeof(float);     // at most 16 KB
+    const size_t smem = (size_t)a.per_block * a.angle_step * sizeof(float2);   // at most 16 KB
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = d.dtype == ALSGD_F32 ? launch<float>(group, grid, block, smem, s, a) : launch<uint16_t>(group, grid, block, smem, s, a);
     return e == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
