@@ -13,6 +13,11 @@
 // fewer stay where they are: there is nothing to save, and the two launches in front would cost more than the rest
 // (77 rows x 32000 words x 384: forward 18.4 -> 15.4 us, backward 43.9 -> 35.3 us when this was measured).
 //
+// dz becomes an operand of the tensor cores and is rounded to bf16 for it; sums over many rows or words average that out to about
+// what the results' own rounding costs.  Few rows need not average anything: dw of a word is often the gradient of one.  So up to 64
+// rows dz goes in two parts, the rounded value and what rounding left, as so many more rows, for which the tiles have room anyway.
+// (From 65 to 128 rows it would take a step more of every product: 28.5 -> 33.0 us at 77 rows.)
+//
 // The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
 // of either operand, so that a tile needs half of the shared memory traffic of two single ones.  (Up to 128 rows there is no
 // second half of the rows: every block then forms logits by itself, 128 x 256.)  One warp copies, one
@@ -39,6 +44,7 @@ constexpr int kMaxTop = 128;
 constexpr uint64_t kPieceBytes = 256ull << 20;
 constexpr int kLeastPiece = 16;        // tiles of a piece: below that, adding dx up would cost more than the memory is worth
 constexpr int kMaxSplits = 64;
+constexpr int kMostRest = 64;          // rows up to which dz is kept to two bf16 parts
 
 // ---------------------------------------------------------------------------------------------- rows that take part
 
@@ -426,6 +432,7 @@ struct LogitArgs {
     const int* count;
     int all_rows;                      // with as many rows that take part, x_all is read; -1: never
     int plain, rows;                   // rows stay in their places
+    int rest;                          // backward: where what rounding left of dz begins; 0: it is dropped
     Labels l;
     const float *lse, *dloss;          // backward, plain
     int64_t dloss_step;
@@ -625,11 +632,12 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
         if (BACKWARD && a.plain) {
             // for the products behind: zeros in the rows that take no part
 #pragma unroll 4
-            for (int r = (warp - 2) * gridDim.x + blockIdx.x; r < a.padded; r += kOutWarps * gridDim.x) {
+            for (int place = (warp - 2) * gridDim.x + blockIdx.x; place < a.padded; place += kOutWarps * gridDim.x) {
+                const int r = a.rest && place >= a.rest ? place - a.rest : place;      // the rows twice, for either part of dz
                 const bool used = r < a.rows && (TOP ? a.target[r] : label_at(a.l, r)) >= 0;
                 for (int c = 8 * lane; c < a.dim; c += 256)
-                    *reinterpret_cast<uint4*>(a.xc + (size_t)r * a.dim + c) = used ? *reinterpret_cast<const uint4*>(a.x_rows + r * a.x_step + c) : make_uint4(0, 0, 0, 0);
-                if (lane == 0) a.row[r] = used ? r : ~r;
+                    *reinterpret_cast<uint4*>(a.xc + (size_t)place * a.dim + c) = used ? *reinterpret_cast<const uint4*>(a.x_rows + r * a.x_step + c) : make_uint4(0, 0, 0, 0);
+                if (lane == 0 && place == r) a.row[r] = used ? r : ~r;
             }
         }
         for (int i = first + acc * pairs; i < tiles; i += every * pairs, acc += every) {
@@ -662,6 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
                 }
             }
             const bool all_used = __all_sync(~0u, used);
+            const bool is_rest = a.rest && row >= a.rest && row < a.rest + count;      // written with the row it is left of
             float top = -INFINITY, sum = 0.0f;
             wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
             tc_fence_after();
@@ -717,7 +726,13 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
                         uint32_t v[4];
 #pragma unroll
                         for (int h = 0; h < 4; ++h) v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]), __uint_as_float(z[8 * j + 2 * h + 1]));
-                        *reinterpret_cast<uint4*>(to + j * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
+                        if (TWO || !is_rest) *reinterpret_cast<uint4*>(to + j * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
+                        if (!TWO && a.rest && row < count) {       // what rounding left
+#pragma unroll
+                            for (int h = 0; h < 4; ++h)
+                                v[h] = pack_bf16(__uint_as_float(z[8 * j + 2 * h]) - bf16_lo(v[h]), __uint_as_float(z[8 * j + 2 * h + 1]) - bf16_hi(v[h]));
+                            *reinterpret_cast<uint4*>(to + a.rest * 16 + j * 2048) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
                     }
                 }
             }
@@ -829,6 +844,7 @@ struct ProductArgs {
     const int* count;
     int all_rows;
     int plain, rows;                   // rows stay in their places
+    int rest;                          // as for the logits
     int dim, vocab;
     int tile0, tiles;                  // of the vocabulary: the piece
     int dx_subs, splits, split_steps;  // dx: tiles of an item (where there are as many), parts of the inner axis
@@ -879,7 +895,7 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
     d.pair = pair;
     d.pairs = gridDim.x / 2;
     d.row_tiles = (count + kTile - 1) / kTile;
-    d.dw_steps = (count + kStep - 1) / kStep;
+    d.dw_steps = (a.rest + count + kStep - 1) / kStep;
     d.dx_subs = d.row_tiles > 1 ? a.dx_subs : 1;
     // parts of dw that have steps
     const int dw_parts = a.dw_splits == 1 ? 1 : (d.dw_steps + a.dw_split_steps - 1) / a.dw_split_steps;
@@ -954,6 +970,16 @@ __device__ __forceinline__ bool item_at(const ProductArgs& a, const Deal& d, int
     }
     t.subs = min(t.subs, end - t.rt);
     return true;
+}
+
+__device__ __forceinline__ void add_to(uint32_t (&v)[32], const float4 (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + x[j].x);
+        v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + x[j].y);
+        v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + x[j].z);
+        v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + x[j].w);
+    }
 }
 
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product_kernel(const __grid_constant__ ProductArgs a) {
@@ -1043,8 +1069,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             const int block = (t.rt + sub) * 2 + p.rank, word = (a.tile0 + t.rt + sub) * kTile + p.rank * 128 + 32 * quad;
             float4* const sums = (t.is_dw ? a.dw_sums + ((size_t)t.split * (2 * a.tiles) + block) * (a.dim / 4) * 128
                                           : a.sums + ((size_t)t.split * (a.padded / 128) + block) * (a.dim / 4) * 128) + 32 * quad + lane;
-            const bool out = t.is_dw ? a.dw_splits == 1 : a.last, adds = !t.is_dw && a.add && row < count;
-            const bool writes = t.is_dw ? word + lane < a.vocab : row < count;
+            const bool writes = t.is_dw ? word + lane < a.vocab : row < a.rest + count;
+            const bool out = t.is_dw ? a.dw_splits == 1 : a.last, adds = !t.is_dw && a.add && writes;
             // the rows that the lane writes in turn: 8 at a time, four lanes for 64 bytes of each
             int64_t to[4];
             bool zero[4] = {};
@@ -1071,24 +1097,24 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
                 }
-                if (adds) {
+                if (adds) add_to(v, before);
+                const bool joins = !t.is_dw && a.rest && out;      // what rounding left meets its row, by way of its place in the sums
+                if (joins ? row >= a.rest && writes : !out && writes)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + before[j].x);
-                        v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + before[j].y);
-                        v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + before[j].z);
-                        v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + before[j].w);
+                    for (int j = 0; j < 8; ++j)
+                        if (d0 + 4 * j < a.dim)
+                            sums[(size_t)(d0 / 4 + j) * 128] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
+                                                                           __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
+                __syncwarp();
+                if (!out) continue;
+                if (joins) {
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + part) : "memory");      // the four warps with these columns
+                    if (row < count) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) before[j] = d0 + 4 * j < a.dim ? sums[(size_t)(d0 / 4 + j) * 128 + a.rest] : make_float4(0, 0, 0, 0);
+                        add_to(v, before);
                     }
-                }
-                if (!out) {
-                    if (writes)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (d0 + 4 * j < a.dim)
-                                sums[(size_t)(d0 / 4 + j) * 128] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
-                                                                               __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
                     __syncwarp();
-                    continue;
                 }
                 // 32 rows of 64 bytes, in the 64-byte swizzle that the tensor map reads, when those before have left
                 if (lane == 0) tma_store_wait_read();
@@ -1134,19 +1160,24 @@ struct Parts {
     const int* row;                    // of a place; null: the place itself
     uint16_t* out;
     int64_t step;
-    int ways;                          // warps that share the parts: 1, 2, 4 or 8
+    int ways;                          // warps that share the parts: 1, 2, 4, 8 or 16
+    int rest;                          // so many places further on is what rounding left; 0: nowhere
 };
 
-// A block takes 32 rows x 64 / ways columns; the warps that share a column's parts add their sums in order.
-__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Parts dx, const __grid_constant__ Parts dw, const int* count, int rows, int dim) {
-    __shared__ float s[8][8][32];
+// A block takes 32 rows x 128 / ways columns; the warps that share a column's parts add their sums in order.  Many warps and little
+// code: a kernel this short waits for its instructions about as long as for its data (eight warps with loops unrolled eight
+// times: 9 us for 2 x 64 parts of 5 rows x 200, 6 us so).
+constexpr int kPartWarps = 16;
+__global__ void __launch_bounds__(32 * kPartWarps) parts_kernel(const __grid_constant__ Parts dx, const __grid_constant__ Parts dw, const int* count, int rows, int dim) {
+    __shared__ float s[kPartWarps][8][32];
     grid_dependency_sync();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n = count ? *count : rows;
     const bool is_dw = (int)blockIdx.x >= dx.blocks;
     const Parts& p = is_dw ? dw : dx;
     const int row0 = (blockIdx.x - (is_dw ? dx.blocks : 0)) * 32, row = row0 + lane, end = is_dw ? p.rows : n;
     const int parts = is_dw ? min(p.parts, ((n + kStep - 1) / kStep + p.part_steps - 1) / p.part_steps) : p.parts;
-    const int columns = 8 / p.ways, way = warp % p.ways, groups = dim / 8, group0 = blockIdx.y * columns;
+    const int all = p.rest ? 2 * parts : parts;                // what rounding left counts as parts of its own
+    const int columns = kPartWarps / p.ways, way = warp % p.ways, groups = dim / 8, group0 = blockIdx.y * columns;
     if (row0 >= end || group0 >= groups) return;
     const int group = group0 + warp / p.ways;
     const int64_t part = (int64_t)(p.padded / 128) * (dim / 4) * 128;
@@ -1155,9 +1186,10 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Part
     const bool mine = row < end && group < groups;
     float v[8] = {};
     if (mine)
-#pragma unroll 4
-        for (int k = way; k < parts; k += p.ways) {
-            const float4 lo = from[k * part], hi = from[k * part + 128];
+#pragma unroll 1
+        for (int k = way; k < all; k += p.ways) {
+            const float4* const at = from + (k < parts ? k * part : (k - parts) * part + p.rest);
+            const float4 lo = at[0], hi = at[128];
             const float add[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += add[j];
@@ -1166,9 +1198,10 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Part
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[warp][j][lane] = v[j];
         __syncthreads();
-        for (int w = 1; w < p.ways; ++w)
+#pragma unroll 1
+        for (int w = 1; way == 0 && w < p.ways; ++w)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += s[(warp + w) & 7][j][lane];
+            for (int j = 0; j < 8; ++j) v[j] += s[warp + w][j][lane];
     }
     if (!mine || way) return;
     const uint4 out = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
@@ -1279,7 +1312,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
         p.lse2 = take(4 * padded);
         p.coef = take(4 * padded);
         p.dz = take(tile_bytes * p.piece);
-        if (p.pieces > 1 || p.dx.splits > 1) p.sums = take(p.dx.splits * dx_bytes);
+        if (p.pieces > 1 || p.dx.splits > 1 || d.rows <= kMostRest) p.sums = take(p.dx.splits * dx_bytes);
         if (p.dw.splits > 1) p.dw_sums = take(p.dw.splits * dw_bytes);
     } else {
         p.stats = take(8 * padded * p.tiles);
@@ -1471,10 +1504,13 @@ int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
     return launch_dependent(logit_kernel<BACKWARD, TOP, TWO>, dim3(grid), dim3(kThreads), smem, s, a) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
-// Up to 128 rows every block forms logits by itself: 77 rows x 32000 words x 384 forward 12.3 -> 9.7 us, backward 31.0 -> 28.9 us.
+// Up to 128 rows that stay in their places.
+bool alone(const LogitArgs& a) { return a.plain && a.rows <= kTile / 2; }
+
+// There every block forms logits by itself: 77 rows x 32000 words x 384 forward 12.3 -> 9.7 us, backward 31.0 -> 28.9 us.
 template <bool BACKWARD>
 int launch_logits(const LogitArgs& a, int device, cudaStream_t s) {
-    if (a.plain && a.rows <= kTile / 2)
+    if (alone(a))
         return a.top ? launch_logits<BACKWARD, true, false>(a, device, s) : launch_logits<BACKWARD, false, false>(a, device, s);
     return a.top ? launch_logits<BACKWARD, true, true>(a, device, s) : launch_logits<BACKWARD, false, true>(a, device, s);
 }
@@ -1530,14 +1566,18 @@ int add_parts(const Plan& p, const ProductArgs& m, cudaStream_t stream) {
     Parts of_dx, of_dw;
     std::memset(&of_dx, 0, sizeof of_dx);
     std::memset(&of_dw, 0, sizeof of_dw);
-    auto ways = [](int parts) { return parts >= 8 ? 8 : parts >= 4 ? 4 : parts >= 2 ? 2 : 1; };
+    auto ways = [](int parts) {
+        int n = 1;
+        while (2 * n <= parts && n < kPartWarps) n *= 2;
+        return n;
+    };
     const int words = std::min(m.vocab - m.tile0 * kTile, m.tiles * kTile);
-    if (dx) of_dx = {m.sums, p.dx.splits, p.dx.split_steps, (m.rows + 31) / 32, m.rows, p.padded, m.row, m.dx, m.dx_step, ways(p.dx.splits)};
+    if (dx) of_dx = {m.sums, p.dx.splits, p.dx.split_steps, (m.rows + 31) / 32, m.rows, p.padded, m.row, m.dx, m.dx_step, ways(m.rest ? 2 * p.dx.splits : p.dx.splits), m.rest};
     if (dw)
         of_dw = {m.dw_sums, p.dw.splits, p.dw.split_steps, (words + 31) / 32, words, m.tiles * kTile, nullptr, m.dw + (int64_t)m.tile0 * kTile * m.dw_step, m.dw_step,
-                 ways(p.dw.splits)};
-    const int columns = 8 / std::max(of_dx.ways, of_dw.ways), groups = m.dim / 8;
-    return launch_dependent(parts_kernel, dim3(of_dx.blocks + of_dw.blocks, (groups + columns - 1) / columns), dim3(256), 0, stream, of_dx, of_dw,
+                 ways(p.dw.splits), 0};
+    const int columns = kPartWarps / std::max(of_dx.ways, of_dw.ways), groups = m.dim / 8;
+    return launch_dependent(parts_kernel, dim3(of_dx.blocks + of_dw.blocks, (groups + columns - 1) / columns), dim3(32 * kPartWarps), 0, stream, of_dx, of_dw,
                             m.plain ? (const int*)nullptr : m.count, m.rows, m.dim) == cudaSuccess
                ? ALSGD_OK
                : ALSGD_E_CUDA;
@@ -1579,6 +1619,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 64, &m.x_all)) != ALSGD_OK) return rc;
     m.plain = a.plain;
     m.rows = a.rows;
+    a.rest = m.rest = !alone(a) || a.rows > kMostRest ? 0 : a.rows > kMostRest / 2 ? kMostRest : kMostRest / 2;
     m.all_rows = a.plain ? -1 : a.all_rows;
     m.count = a.count;
     m.dim = (int)d.dim;

@@ -44,8 +44,9 @@ class Problem:
         t = torch.where(ok, (t - torch.where(top == -math.inf, 0.0, top)).exp(), 0.0)
         return at.clamp(0, self.vocab - 1), t / t.sum(1, keepdim=True).clamp(min=1e-300)
 
-    def solve(self, lse=None, dloss=None):
-        """loss, lse, dx, dw and a bound on the error of each.  lse, dloss: what the backward pass is given (else its own)."""
+    def solve(self, lse=None, dloss=None, gathered=False):
+        """loss, lse, dx, dw and a bound on the error of each.  lse, dloss: what the backward pass is given (else its own).
+        Up to 64 rows, unless they are gathered, dz goes in two bf16 parts: what is left is off by a rounding of a rounding."""
         at, t = self.weights()
         used = t.sum(1) > 0
         x, w = torch.where(used[:, None], self.x.double(), 0.0), self.w.double()
@@ -66,7 +67,7 @@ class Problem:
         both = p.scatter_add(1, at, t)
         dz = p.scatter_add(1, at, -t) * (self.scale * dloss)[:, None]
         p_off = z_off + (2 * top + 4 + lse.abs()) * EPS
-        dz_off = HALF_BF16 * dz.abs() + (self.scale * dloss.abs() * (p_off + (4 + self.top) * EPS))[:, None] * both
+        dz_off = (HALF_BF16 if gathered or self.rows > 64 else HALF_BF16 ** 2) * dz.abs() + (self.scale * dloss.abs() * (p_off + (4 + self.top) * EPS))[:, None] * both
         self.dx, self.dw = dz @ w, dz.T @ x
         self.dx_off = dz_off @ w.abs() + self.vocab * EPS * (dz.abs() @ w.abs()) + HALF_BF16 * self.dx.abs() + 1e-30
         self.dw_off = dz_off.T @ x.abs() + self.rows * EPS * (dz.abs().T @ x.abs()) + HALF_BF16 * self.dw.abs() + 1e-30
