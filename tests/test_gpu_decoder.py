@@ -129,3 +129,71 @@ def test_the_papers_vocabulary_with_a_clipped_step():
     ctx.alsgd_sync()
     assert bool(torch.isfinite(ctx.alsgd_worker_state_ptrs(0)["p"]).all())
     ctx.close()
+
+
+def test_calls_on_several_streams_at_once():
+    """Plans of their own, streams of their own: losses, attention and rotary positions side by side give the bits that they give
+    one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    jobs = []
+    for rows, vocab, dim in ((700, 3000, 264), (90, 5000, 128), (2000, 1000, 64)):
+        x, w, target = rnd(rows, dim), rnd(vocab, dim) * 0.1, torch.randint(-1, vocab, (rows,), generator=g, device="cuda")
+        plan, dloss = B.VocabLoss(rows, vocab, dim), torch.full((rows,), 1 / rows, device="cuda")
+
+        def loss(x=x, w=w, target=target, plan=plan, dloss=dloss, rows=rows):
+            out = [torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x), torch.empty_like(w)]
+            plan.alsgd_xent_fwd(x, w, target, *out[:2])
+            plan.alsgd_xent_bwd(x, w, target, out[1], dloss, *out[2:])
+            return out
+        jobs.append(loss)
+    q, k, v = (rnd(4, 500, 4, 64) for _ in range(3))
+    attention_plan, rotary = B.Attention(4, 500, 500, 4, 4, 64), B.Rotary(4, 500, 4, 4, 64)
+
+    def attends():
+        out = [torch.empty_like(q) for _ in range(3)] + [torch.empty(4, 4, 500, device="cuda")]
+        rotary.alsgd_rope(q, k, *out[:2])
+        attention_plan.alsgd_attn_fwd(out[0], out[1], v, out[2], out[3])
+        return out
+    jobs.append(attends)
+    want = [j() for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(10):
+        got = []
+        for s, j in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                got.append(j())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+    assert B.alsgd_vocab_status() == 0 and B.alsgd_attn_status() == 0
+
+
+@pytest.mark.parametrize("rows", [40, 300, 700])
+def test_two_graphs_that_share_a_plan(rows):
+    """Captured one after the other, replayed in any order on one stream."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    vocab, dim = 2000, 128
+    plan, dloss = B.VocabLoss(rows, vocab, dim), torch.full((), 1 / rows, device="cuda").expand(rows)
+    w = (0.1 * torch.randn(vocab, dim, generator=g, device="cuda")).bfloat16()
+    graphs, outs, want, steps = [], [], [], []     # steps: a graph reads its operands where they were
+    for i in range(2):
+        x, target = torch.randn(rows, dim, generator=g, device="cuda").bfloat16(), torch.randint(-1, vocab, (rows,), generator=g, device="cuda")
+        out = [torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.zeros_like(x), torch.zeros_like(w)]
+
+        def step(x=x, target=target, out=out):
+            plan.alsgd_xent_fwd(x, w, target, *out[:2])
+            plan.alsgd_xent_bwd(x, w, target, out[1], dloss, *out[2:])
+        step()
+        want.append([t.clone() for t in out])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        graphs.append(graph)
+        outs.append(out)
+        steps.append(step)
+    for i in (0, 1, 1, 0, 1):
+        for t in outs[i]:
+            t.fill_(3.0)
+        graphs[i].replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
