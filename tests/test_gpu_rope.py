@@ -168,3 +168,19 @@ def test_captured_and_replayed():
         plan.alsgd_rope(q, k, *out)
     graph.replay()
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_offsets_beyond_32_bits():
+    """Positions 2^20 + 8 elements apart."""
+    b, n, h, d = 1, 2200, 2, 64
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 10 GB")
+    q = torch.randn(b, n, h, d, device="cuda").bfloat16()
+    plan = B.Rotary(b, n, h, h, d)
+    want = torch.empty_like(q), torch.empty_like(q)
+    plan.alsgd_rope(q, q, *want)
+    far = torch.empty(n * ((1 << 20) + 8), dtype=torch.bfloat16, device="cuda").view(1, n, -1)[:, :, :h * d].view(b, n, h, d)
+    far.copy_(q)
+    out = torch.empty_like(q)
+    plan.alsgd_rope(q, far, out, far)
+    assert torch.equal(out, want[0]) and torch.equal(far, want[1])

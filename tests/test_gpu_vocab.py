@@ -283,3 +283,27 @@ def test_second_derivatives_are_refused():
     first = torch.autograd.grad(loss, (x, w), create_graph=True)
     with pytest.raises(RuntimeError):
         sum((g.float() ** 2).sum() for g in first).backward()
+
+
+@pytest.mark.parametrize("rows,vocab,dim,top", [(300000, 700, 64, 0), (200001, 300, 32, 2), (50, 600007, 64, 0), (50, 600007, 64, 3)])
+def test_many_rows_and_long_vocabularies(rows, vocab, dim, top):
+    check(Problem(rows, vocab, dim, top=top, seed=20, left_out=0.01))
+
+
+@pytest.mark.parametrize("top", [0, 3])
+def test_offsets_beyond_32_bits(top):
+    """Rows of every operand 2^20 + 8 elements apart: the last ones lie more than 2^31 elements behind the first."""
+    rows, vocab, dim = 2200, 2100, 64
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 20 GB")
+    p = Problem(rows, vocab, dim, top=top, seed=21)
+    want = check(p)
+    step = (1 << 20) + 8
+    apart = lambda n: torch.empty(n * step, dtype=torch.bfloat16, device="cuda").view(n, step)[:, 8:8 + dim]  # noqa: E731
+    x, w, dx, dw = apart(rows), apart(vocab), apart(rows), apart(vocab)
+    x.copy_(p.x)
+    w.copy_(p.w)
+    plan = plan_of(p)
+    loss, lse = forward(plan, p, x=x, w=w)
+    backward(plan, p, lse, x=x, w=w, dx=dx, dw=dw)
+    assert all(torch.equal(a, b) for a, b in zip((loss, lse, dx, dw), want))
