@@ -9,8 +9,8 @@
 // dw = dz^T x in one launch.
 //
 // The rows that take part are gathered first (a padded batch pays for its tokens, not for its padding; what the other rows
-// hold reaches nothing) and everything behind works on their number, which only the device knows.  Two tiles' worth of rows or
-// fewer stay where they are: there is nothing to save, and the two launches in front would cost more than the rest
+// hold reaches nothing) and everything behind works on their number, which only the device knows.  Few rows and short passes stay
+// where they are: there is little to save, and the two launches in front would cost more than the rest
 // (77 rows x 32000 words x 384: forward 18.4 -> 15.4 us, backward 43.9 -> 35.3 us when this was measured).
 //
 // dz becomes an operand of the tensor cores and is rounded to bf16 for it; sums over many rows or words average that out to about
@@ -44,6 +44,7 @@ constexpr int kMaxTop = 128;
 constexpr uint64_t kPieceBytes = 256ull << 20;
 constexpr int kLeastPiece = 16;        // tiles of a piece: below that, adding dx up would cost more than the memory is worth
 constexpr int kMaxSplits = 64;
+constexpr uint64_t kPlainProducts = 9000000000;                // 13 us of them
 constexpr int kMostRest = 64;          // rows up to which dz is kept to two bf16 parts
 
 // ---------------------------------------------------------------------------------------------- rows that take part
@@ -1379,8 +1380,12 @@ struct Call {
 // x as it is can be an operand of the products, unless its rows overlap.
 bool direct_x(const Call& c) { return c.d->rows == 1 || c.x->stride_row >= (int64_t)c.d->dim; }
 
-// Rows that fit two tiles stay in their places.
-bool plain_rows(const Call& c) { return c.d->rows <= 2 * kTile && direct_x(c); }
+// Rows that fit two tiles stay in their places, and those of passes so short that a third of their products, which is what padding
+// often is, takes no longer than the two launches in front would (about 4.5 us: 1464 rows x 4486 x 128 forward 16.2 -> 13.0 us,
+// 1856 x 5124 x 272 forward 20.4 -> 17.4, 10604 x 1240 x 104 backward 40.2 -> 35.8).
+bool plain_rows(const Call& c, bool backward) {
+    return direct_x(c) && (c.d->rows <= 2 * kTile || (uint64_t)c.d->rows * c.d->vocab * c.d->dim * (backward ? 3 : 1) <= kPlainProducts);
+}
 
 uint64_t step_of(const alsgd_matrix& m, uint32_t rows, uint32_t dim) {
     return rows == 1 || m.stride_row == 0 ? (uint64_t)dim : (uint64_t)m.stride_row;
@@ -1419,7 +1424,7 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
     GatherArgs g;
     std::memset(&g, 0, sizeof g);
     g.l = labels_of(c);
-    g.plain = plain_rows(c);
+    g.plain = plain_rows(c, lse != nullptr);
     if (g.plain && !d.top) return ALSGD_OK;                        // nothing to do
     g.x = static_cast<const uint16_t*>(c.x->data);
     g.x_step = d.rows == 1 ? 0 : c.x->stride_row;
@@ -1460,7 +1465,7 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
     return launch_dependent(gather_kernel, dim3(rows / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
 }
 
-int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
+int make_logits(const Call& c, const Plan& p, bool backward, LogitArgs* a) {
     const alsgd_vocab_desc& d = *c.d;
     std::memset(a, 0, sizeof *a);
     int rc;
@@ -1468,7 +1473,7 @@ int make_logits(const Call& c, const Plan& p, LogitArgs* a) {
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 128, &a->w)) != ALSGD_OK) return rc;
     a->all_rows = direct_x(c) ? (int)d.rows : -1;
     if (direct_x(c) && (rc = make_map(c.x->data, d.rows, d.dim, 2 * step_of(*c.x, d.rows, d.dim), 128, &a->x_all)) != ALSGD_OK) return rc;
-    a->plain = plain_rows(c);
+    a->plain = plain_rows(c, backward);
     a->rows = (int)d.rows;
     a->l = labels_of(c);
     a->scale = d.scale;
@@ -1526,7 +1531,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
     UseDevice use(d.device);
     if (!use.ok) return ALSGD_E_CUDA;
     LogitArgs a;
-    if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
+    if ((rc = make_logits(c, p, false, &a)) != ALSGD_OK) return rc;
     if ((rc = gather_rows(c, p, nullptr, nullptr, 0, nullptr)) != ALSGD_OK) return rc;
     a.tiles = p.tiles;
     a.by_group = divide_by(kGroup * a.tiles);
@@ -1600,7 +1605,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     LogitArgs a;
     ProductArgs m;
     std::memset(&m, 0, sizeof m);
-    if ((rc = make_logits(c, p, &a)) != ALSGD_OK) return rc;
+    if ((rc = make_logits(c, p, true, &a)) != ALSGD_OK) return rc;
     a.lse2 = at<float>(c, p.lse2);
     a.coef = at<float>(c, p.coef);
     a.dz = at<uint8_t>(c, p.dz);
