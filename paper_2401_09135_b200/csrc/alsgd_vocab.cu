@@ -477,7 +477,7 @@ struct LogitSmem {
     Bars<kStages> bars;
 };
 
-// Replaces / reads the value of one of 32 registers, chosen at run time.
+// One of 32 registers, chosen at run time.
 __device__ __forceinline__ float pick(const uint32_t (&z)[32], int at) {
     float v = 0.0f;
 #pragma unroll
@@ -538,7 +538,7 @@ __device__ __forceinline__ void take_off(uint32_t (&z)[32], int at, float t) {
 }
 
 // A row's labels within some words, in ascending order, four of them on the way: a list read one by one costs its warp the
-// memory's latency at every label (169 to 222 us against 155 for single labels, 5461 rows x 8192 words x 768).
+// memory's latency at every label (a piece of 5461 rows x 16384 words x 768 backward, 64 labels a row: 169 to 222 us, so 95 to 110).
 struct LabelQueue {
     static constexpr int kAhead = 4;
     const int* indices;
@@ -865,6 +865,8 @@ struct ProductArgs {
 // Two tiles, one above the other, share every copy of B where the inner axis is long: a step's copies are then 96 KB for
 // two tiles instead of 128, and what a pair can draw from the L2 (about 100 bytes a cycle) is what bounds the steps.  Both
 // halves of tensor memory belong to one item then, which its way out is not hidden behind: not worth it for short inner axes.
+// Backward passes with two tiles from 8, 16, 32 steps on, and never: 13622 rows x 10070 x 184 244, 244, 276, 250 us; 1686 x 3622 x 816
+// 55, 46, 49, 49; 1188 x 53029 x 888 304, 304, 329, 321; 10598 x 10748 x 360 256, 256, 257, 297.
 constexpr int kProductStages = 4;
 constexpr int kLongSteps = 16;          // fewer: one tile
 constexpr int kOutSteps = 4;            // what a tile's way out costs, in steps
