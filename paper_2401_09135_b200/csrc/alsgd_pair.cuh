@@ -21,6 +21,15 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// A wait of one of two blocks.  What it waits for in vain the other block works with too: the first issues the products over both
+// blocks' shared memory, and either copies half of an operand.  So the other block is marked as well, and first: whoever sees this
+// block's mark may go on to hand over a tile.
+__device__ __forceinline__ void wait_pair(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code, uint32_t tries = kWaitTries) {
+    wait(bar, parity, dead, code, tries, [dead] {
+        asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(at_rank(smem_u32(const_cast<const uint32_t*>(dead)), cluster_rank() ^ 1)), "r"(1) : "memory");
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    });
+}
 // `bar` as at_rank gives it.  What it announces is tensor memory that has been read (the reads have completed, a
 // tc_fence_before behind them): ordering wider than the block's own would wait for every store in flight, most of a microsecond.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar, uint32_t times) {

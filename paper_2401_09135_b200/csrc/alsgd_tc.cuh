@@ -44,17 +44,23 @@ static __device__ unsigned int g_wait_error;
 // through the loops costs more than the wait itself, which most often finds its phase complete.
 constexpr uint32_t kWaitTries = 1u << 22;
 
-__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
+// `also` is done before the block is marked.
+template <typename ALSO>
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code, uint32_t tries, ALSO also) {
     if (bar_test(bar, parity)) return;
     for (uint32_t i = 1; !bar_test(bar, parity); ++i) {
         if ((i & 63) != 0) continue;
         if (*dead) return;
-        if (i >= kWaitTries) {
+        if (i >= tries) {
+            also();
             *dead = 1;
             atomicOr(&g_wait_error, code);
             return;
         }
     }
+}
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t code) {
+    wait(bar, parity, dead, code, kWaitTries, [] {});
 }
 
 // The same for a warp that goes on with warp-wide instructions.

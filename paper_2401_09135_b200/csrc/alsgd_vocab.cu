@@ -306,6 +306,14 @@ struct Pair {
 
     __device__ __forceinline__ uint32_t a(int s) const { return stage0 + s * kStageBytes; }
     __device__ __forceinline__ uint32_t b(int s) const { return stage0 + s * kStageBytes + SUBS * kOperandBytes; }
+    __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, uint32_t code) const {
+        if (TWO) wait_pair(bar, parity, dead, code);
+        else alsgd_tc::wait(bar, parity, dead, code);
+    }
+    __device__ __forceinline__ void wait_warp(uint32_t bar, uint32_t parity, uint32_t code) const {
+        wait(bar, parity, code);
+        __syncwarp();
+    }
 };
 
 // Barriers and tensor memory of both blocks.  Full: one arrival (the first block's copying thread, for the bytes of
@@ -388,7 +396,7 @@ __device__ __forceinline__ void ring_drain(const Pair<STAGES, SUBS, TWO>& p, Rin
 template <int STAGES, int SUBS, bool TWO, typename DESC_A, typename DESC_B>
 __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS, TWO>& p, Ring& ring, uint32_t acc, int subs, int steps, uint32_t desc, DESC_A a, DESC_B b) {
     for (int k = 0; k < steps; ++k) {
-        wait(p.full + 8 * ring.stage, ring.phase, p.dead, kWaitFull);
+        p.wait(p.full + 8 * ring.stage, ring.phase, kWaitFull);
         tc_fence_after();
         const uint32_t sa = p.a(ring.stage), sb = p.b(ring.stage);
 #pragma unroll
@@ -396,7 +404,7 @@ __device__ __forceinline__ void tile_products(const Pair<STAGES, SUBS, TWO>& p, 
             if (s >= subs) break;
             const uint32_t buf = (acc + s) & 1;
             if (k == 0) {
-                wait(p.acc_empty + 8 * buf, (((acc + s) >> 1) & 1) ^ 1, p.dead, kWaitAccEmpty);
+                p.wait(p.acc_empty + 8 * buf, (((acc + s) >> 1) & 1) ^ 1, kWaitAccEmpty);
                 tc_fence_after();
             }
 #pragma unroll
@@ -595,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
                 tile_at(a, i, row_tiles, rt, ct);
                 const int row = rt * ROWS + p.rank * 128, word = (a.tile0 + ct) * kTile + p.rank * 128;
                 for (int k = 0; k < steps; ++k) {
-                    wait(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    p.wait(p.empty + 8 * ring.stage, ring.phase ^ 1, kWaitEmpty);
                     if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, BLOCKS * p.kStageBytes);
                     if (TWO) {
                         const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
@@ -673,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
             const bool all_used = __all_sync(~0u, used);
             const bool is_rest = a.rest && row >= a.rest && row < a.rest + count;      // written with the row it is left of
             float top = -INFINITY, sum = 0.0f;
-            wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
+            p.wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
 #pragma unroll 1
@@ -1019,7 +1027,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
             for (int i = 0; item_at(a, deal, i, t); ++i) {
                 const int d0 = t.dt * a.n + p.rank * (a.n / 2), row_blocks = a.tiles * 4;      // of one block's rows
                 for (int k = t.k0; k < t.k0 + t.steps; ++k) {
-                    wait(p.empty + 8 * ring.stage, ring.phase ^ 1, p.dead, kWaitEmpty);
+                    p.wait(p.empty + 8 * ring.stage, ring.phase ^ 1, kWaitEmpty);
                     if (p.rank == 0) bar_expect(p.full + 8 * ring.stage, 2 * (t.subs * kOperandBytes + boxes * 8192));
                     const uint32_t full = at_rank(p.full + 8 * ring.stage, 0);
                     for (int s = 0; s < t.subs; ++s) {
@@ -1066,7 +1074,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
         uint32_t acc = 0;
         for (int i = 0, sub = 0; item_at(a, deal, i, t); ++acc, sub = sub + 1 < t.subs ? sub + 1 : (++i, 0)) {
             const int row = (t.rt + sub) * kTile + p.rank * 128 + 32 * quad + lane;
-            wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, p.dead, kWaitAccFull);
+            p.wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;
             const int block = (t.rt + sub) * 2 + p.rank, word = (a.tile0 + t.rt + sub) * kTile + p.rank * 128 + 32 * quad;
