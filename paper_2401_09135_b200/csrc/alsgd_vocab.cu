@@ -545,6 +545,16 @@ __device__ __forceinline__ void take_off(uint32_t (&z)[32], int at, float t) {
     for (int i = 0; i < 32; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) - (i == at ? t : 0.0f));
 }
 
+// What a row's exponentials and labels are multiplied by.  lost: a wait has run out, and dz shows it in every word, since dw of a
+// word is made of its own entries only.
+__device__ __forceinline__ float factor_of(float coef, bool lost) { return lost ? NAN : coef; }
+// dz in rows that take no part (or fill the last tile) and behind the last word: zeros, whatever the operands hold.
+__device__ __forceinline__ void settle(uint32_t (&z)[32], bool used, bool all_used, int words) {
+    if (words >= 32 && all_used) return;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) z[j] = used && j < words ? z[j] : 0;
+}
+
 // A row's labels within some words, in ascending order, four of them on the way: a list read one by one costs its warp the
 // memory's latency at every label (a piece of 5461 rows x 16384 words x 768 backward, 64 labels a row: 169 to 222 us, so 95 to 110).
 struct LabelQueue {
@@ -684,6 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
             p.wait_warp(p.acc_full + 8 * (acc & 1), (acc >> 1) & 1, kWaitAccFull);
             tc_fence_after();
             const bool dead = *p.dead != 0;                        // a wait has run out: the results show it
+            if (BACKWARD) coef = factor_of(coef, dead);
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
                 uint32_t z[32];
@@ -723,12 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(TWO ? 2 : 1, 1, 
                         take_off(z, label - w0, coef);
                     }
                     __syncwarp();
-                    if (dead) z[0] = 0x7FC00000u;
-                    // rows that fill the last tile, words behind the last: zeros, whatever the operands hold
-                    if (w0 + 32 > a.vocab || !all_used) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = used && w0 + j < a.vocab ? z[j] : 0;
-                    }
+                    settle(z, used, all_used, a.vocab - w0);
                     uint8_t* const to = a.dz + ((size_t)(rt * BLOCKS + p.rank) * (a.tiles * 4) + ct * 4) * 16384 + (column0 / 8 + 4 * c) * 2048 + block_row * 16;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
