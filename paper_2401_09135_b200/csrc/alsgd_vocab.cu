@@ -1275,6 +1275,7 @@ Plan make_plan(const alsgd_vocab_desc& d, bool backward) {
     const uint64_t tile_bytes = (uint64_t)p.padded * kTile * 2;
     uint64_t piece = tile_bytes ? kPieceBytes / tile_bytes : p.tiles;
     if (piece < kLeastPiece) piece = kLeastPiece;
+    piece -= piece % 2;                                            // two tiles share an operand: rounded up, a piece stays within this
     if (piece > (uint64_t)p.tiles) piece = p.tiles;
     p.pieces = (int)((p.tiles + piece - 1) / piece);
     p.piece = (p.tiles + p.pieces - 1) / p.pieces;
