@@ -549,11 +549,12 @@ int alsgd_rope_frequencies(const alsgd_rope_desc* desc, double* out);
  *     dz[i][j] = dloss_i scale (exp(z[i][j] - lse_i) - sum_k t_ik [index_ik = j])    (labels: t = 1)
  *     dx_i = sum_j dz[i][j] w_j,   dw_j = sum_i dz[i][j] x_i
  * Logits, sums and statistics are binary32; dz is rounded to bf16 before the products with w and x (up to 64 rows that do not
- * overlap, to the sum of two bf16).  Results are written, not
- * added to, and do not depend on the order in which blocks run; they must not overlap the operands.  The workspace holds a
- * copy of the rows that take part and the teacher's entries; forward, 8 bytes for each row and 256 words; backward, dz of a piece
- * of the vocabulary (256 MiB, or 8 KiB a row where that is more) and sums of dx and dw (256 MiB of either, or one of dx where that
- * is more).
+ * overlap, to the sum of two bf16).  Results are written, not added to, and do not depend on the order in which blocks run; they must
+ * not overlap the operands.
+ * The workspace holds, for rows in whole tiles of 256: a place for a copy of each (2 dim bytes; how far apart x's rows are, and so
+ * whether they have to be copied, only the call says) and 32 bytes more; with a teacher 8 bytes for each entry and 4 for each 256
+ * words; forward 8 bytes for each 256 words and 4 for the label or each entry; backward dz of a piece of the vocabulary (256 MiB, or 8
+ * KiB a row where that is more) and sums of dx and dw (256 MiB of either, or one of dx where that is more).
  * A NaN or infinity in w or in the x of a row that takes part reaches what is computed from it: the row's loss, all of dw. */
 typedef struct alsgd_vocab_desc {
     uint32_t rows;                     /* up to 2^22; may be 0 */
