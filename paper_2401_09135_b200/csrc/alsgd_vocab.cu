@@ -101,6 +101,44 @@ __global__ void __launch_bounds__(1024) count_kernel(Labels l, int* block_count,
     if (threadIdx.x == 0) block_count[blockIdx.x] = total;
 }
 
+constexpr int kPrefixThreads = 1024;
+// Counting blocks up to which every block of the gathering kernel adds up all counts for itself: that saves a launch, and grows with
+// the square of the rows.  Forward of one word x 8, labels and two entries a row, each block by itself and with prefixes: 16384 rows
+// 16.6 and 17.6, 21.7 and 21.5 us; 32768 25.4 and 26.8, 35.1 and 32.7; 65536 38.8 and 39.6, 56.9 and 50.6; 131072 71 and 67,
+// 107 and 89; 2^22 14400 and 2010, 15500 and 2850.
+constexpr int kFewBlocks = 512;
+
+// Rows that take part before each counting block's, in place of their number in it, and all of them: by one block, a run of counts
+// a thread.
+__global__ void __launch_bounds__(kPrefixThreads) prefix_kernel(int* block_count, int blocks, int* count) {
+    __shared__ int warp_sum[kPrefixThreads / 32];
+    grid_dependency_sync();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, run = (blocks + kPrefixThreads - 1) / kPrefixThreads;
+    const int from = min(blocks, (int)threadIdx.x * run), to = min(blocks, from + run);
+    int sum = 0;
+#pragma unroll 8
+    for (int i = from; i < to; ++i) sum += block_count[i];
+    int before = sum;                                              // with the thread's own, at first
+    for (int d = 1; d < 32; d *= 2) {
+        const int other = __shfl_up_sync(~0u, before, d);
+        if (lane >= d) before += other;
+    }
+    if (lane == 31) warp_sum[warp] = before;
+    before -= sum;
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < kPrefixThreads / 32; ++w) {
+        if (w < warp) before += warp_sum[w];
+        total += warp_sum[w];
+    }
+    for (int i = from; i < to; ++i) {
+        const int n = block_count[i];
+        block_count[i] = before;
+        before += n;
+    }
+    if (threadIdx.x == 0) *count = total;
+}
+
 struct GatherArgs {
     Labels l;
     const uint16_t* x;
@@ -114,6 +152,7 @@ struct GatherArgs {
     uint16_t* dx;                      // backward only: zeros for the rows that take no part
     int64_t dx_step;
     const int *block_count, *place;
+    int summed;                        // block_count: rows that take part before the block's; count is there
     int* count;                        // one: rows that take part
     int* slot;                         // [rows]: place among them, or -1
     int* row;                          // [padded]: the row at a place
@@ -236,24 +275,30 @@ __global__ void __launch_bounds__(32 * kGatherWarps) gather_kernel(const __grid_
         teacher_lists(a, r, r, r < a.l.rows, s_index[warp], s_counts[warp], lane);
         return;
     }
-    int before = 0, total = 0;
-    for (int i = threadIdx.x; i < a.blocks; i += 32 * kGatherWarps) {
-        const int n = a.block_count[i];
-        total += n;
-        if (i < block) before += n;
+    int before, count;
+    if (a.summed) {
+        before = a.block_count[block];
+        count = *a.count;
+    } else {
+        int total = before = 0;
+        for (int i = threadIdx.x; i < a.blocks; i += 32 * kGatherWarps) {
+            const int n = a.block_count[i];
+            total += n;
+            if (i < block) before += n;
+        }
+        if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
+        __syncthreads();
+        before = __reduce_add_sync(~0u, before);
+        total = __reduce_add_sync(~0u, total);
+        if (lane == 0) {
+            atomicAdd(&s_sum[0], before);          // whole numbers: any order
+            atomicAdd(&s_sum[1], total);
+        }
+        __syncthreads();
+        before = s_sum[0];
+        count = s_sum[1];
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = count;
     }
-    if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
-    __syncthreads();
-    before = __reduce_add_sync(~0u, before);
-    total = __reduce_add_sync(~0u, total);
-    if (lane == 0) {
-        atomicAdd(&s_sum[0], before);          // whole numbers: any order
-        atomicAdd(&s_sum[1], total);
-    }
-    __syncthreads();
-    before = s_sum[0];
-    const int count = s_sum[1];
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = count;
     if (r >= a.padded) return;
     const int place = a.place[r];
     const bool used = place >= 0;
@@ -1475,8 +1520,12 @@ int gather_rows(const Call& c, const Plan& p, const float* lse, const float* dlo
         g.lse2 = at<float>(c, p.lse2);
         g.coef = at<float>(c, p.coef);
     }
+    g.summed = p.count_blocks > kFewBlocks;
     if (!g.plain && launch_dependent(count_kernel, dim3(p.count_blocks), dim3(d.top ? 1024 : kCountRows), 0, c.stream, g.l, at<int>(c, p.block_count),
                                      at<int>(c, p.place)) != cudaSuccess)
+        return ALSGD_E_CUDA;
+    if (!g.plain && g.summed && launch_dependent(prefix_kernel, dim3(1), dim3(kPrefixThreads), 0, c.stream, at<int>(c, p.block_count), p.count_blocks,
+                                                 at<int>(c, p.count)) != cudaSuccess)
         return ALSGD_E_CUDA;
     const int rows = g.plain ? ((int)d.rows + kGatherWarps - 1) / kGatherWarps * kGatherWarps : p.padded;
     return launch_dependent(gather_kernel, dim3(rows / kGatherWarps), dim3(32 * kGatherWarps), 0, c.stream, g) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
