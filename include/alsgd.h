@@ -520,7 +520,7 @@ typedef struct alsgd_rope_desc {
     int64_t pos0;                      /* without positions: token s of every sequence is at pos0 + s */
     double base;                       /* > 1 */
     double factor, context, turns_low, turns_high; /* factor >= 1; the others unused at 1.  turns_high above turns_low >= 0, or 0 */
-    double amplitude;                  /* finite, not 0; usually 1 */
+    double amplitude;                  /* finite and not 0 in binary32; usually 1 */
 } alsgd_rope_desc;
 
 /* Operands and results as attention's (steps of fp32 tensors: multiples of 4 elements).  positions: device, [batch][len] of

@@ -9,6 +9,7 @@
 #include "../../include/alsgd.h"
 #include "alsgd_ops.cuh"
 
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -248,7 +249,7 @@ int check_rope(const alsgd_rope_desc* d) {
     if (d->dtype != ALSGD_F32 && d->dtype != ALSGD_BF16) return ALSGD_E_ARG;
     if (d->position_dtype != ALSGD_I32 && d->position_dtype != ALSGD_I64) return ALSGD_E_ARG;
     if (!(d->base > 1.0) || !std::isfinite(d->base) || !(d->factor >= 1.0) || !std::isfinite(d->factor)) return ALSGD_E_ARG;
-    if (!std::isfinite(d->amplitude) || d->amplitude == 0.0) return ALSGD_E_ARG;
+    if (!(std::fabs(d->amplitude) <= FLT_MAX) || (float)d->amplitude == 0.0f) return ALSGD_E_ARG;      // the kernel has it in binary32
     if (!(d->context >= 0.0) || !std::isfinite(d->context) || !(d->turns_low >= 0.0) || !std::isfinite(d->turns_high)) return ALSGD_E_ARG;
     if (d->turns_high != 0.0 && !(d->turns_high > d->turns_low)) return ALSGD_E_ARG;
     if (d->dim > kMaxDim) return ALSGD_E_UNSUPPORTED;
