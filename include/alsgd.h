@@ -578,10 +578,11 @@ typedef struct alsgd_matrix {
 int alsgd_vocab_bytes(const alsgd_vocab_desc* desc, int backward_pass, uint64_t* bytes_out);
 
 /* target: device, [rows] of index_dtype.  index, teacher: device, [rows][top].  loss, lse: device, fp32 [rows].  dloss: device,
- * fp32, dloss_step (>= 0) elements apart: 0 gives every row the same.  dx: [rows][dim], dw: [vocab][dim].  work: device, 256-byte
- * aligned, alsgd_vocab_bytes bytes, any content; calls that share it must be ordered.
- * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step, labels with top > 0 or a teacher without, a
- * gradient at its operand's address.
+ * fp32, dloss_step (>= 0) elements apart: 0 gives every row the same.  dx: [rows][dim], dw: [vocab][dim]; one of them may be NULL and
+ * is then not formed (the other has the same bits).  work: device, 256-byte aligned, alsgd_vocab_bytes bytes, any content; calls that
+ * share it must be ordered.
+ * ALSGD_E_ARG: a value outside the domains above, null or misaligned pointer, step, labels with top > 0 or a teacher without,
+ * neither gradient, a gradient at its operand's address.
  * ALSGD_E_UNSUPPORTED: top > 128, dim > 16384.  ALSGD_E_RANGE: rows or vocab beyond 2^22, device ordinal outside 0..63.
  * ALSGD_E_NOMEM: work too small. */
 int alsgd_xent_fwd(const alsgd_vocab_desc* desc, const alsgd_matrix* x, const alsgd_matrix* w, const void* target, float* loss, float* lse,

@@ -760,8 +760,8 @@ class VocabLoss:
         with self._lock:
             work, (sx, sw, sdx, sdw) = self._workspace(True, raw), self._slots
             _check(getattr(lib(), name)(self.desc, self._matrix(sx, x, self._x_shape), self._matrix(sw, w, self._w_shape), *labels, lse,
-                                        dloss.data_ptr(), dloss.stride(0), self._matrix(sdx, dx, self._x_shape),
-                                        self._matrix(sdw, dw, self._w_shape), work.ptr, work.nbytes, raw), name)
+                                        dloss.data_ptr(), dloss.stride(0), self._matrix(sdx, dx, self._x_shape) if dx is not None else None,
+                                        self._matrix(sdw, dw, self._w_shape) if dw is not None else None, work.ptr, work.nbytes, raw), name)
 
     def _labels(self, index):
         return (self._plain(index, self._labels_shape, self.index_dtype),)
@@ -774,7 +774,7 @@ class VocabLoss:
         self._forward("alsgd_xent_fwd", x, w, self._labels(target), loss, lse, stream)
 
     def alsgd_xent_bwd(self, x, w, target, lse, dloss, dx, dw, stream=None):
-        """dx and dw are written.  dloss: fp32 [rows], which may be one number expanded."""
+        """dx and dw are written, or the one that is not None.  dloss: fp32 [rows], which may be one number expanded."""
         self._backward("alsgd_xent_bwd", x, w, self._labels(target), lse, dloss, dx, dw, stream)
 
     def alsgd_distill_fwd(self, x, w, index, teacher, loss, lse, stream=None):
@@ -782,5 +782,5 @@ class VocabLoss:
         self._forward("alsgd_distill_fwd", x, w, self._teacher(index, teacher), loss, lse, stream)
 
     def alsgd_distill_bwd(self, x, w, index, teacher, lse, dloss, dx, dw, stream=None):
-        """dx and dw are written.  dloss: fp32 [rows], which may be one number expanded."""
+        """dx and dw are written, or the one that is not None.  dloss: fp32 [rows], which may be one number expanded."""
         self._backward("alsgd_distill_bwd", x, w, self._teacher(index, teacher), lse, dloss, dx, dw, stream)

@@ -907,6 +907,7 @@ struct ProductArgs {
     int rest;                          // as for the logits
     int dim, vocab;
     int tile0, tiles;                  // of the vocabulary: the piece
+    int wants_dx, wants_dw;            // one of them at least
     int dx_subs, splits, split_steps;  // dx: tiles of an item (where there are as many), parts of the inner axis
     int dw_subs, dw_splits, dw_split_steps, dw_groups;             // dw: the same; items of one part and column
     int n, dim_tiles;                  // columns of a tile, tiles of dim
@@ -961,9 +962,10 @@ __device__ __forceinline__ Deal deal_of(const ProductArgs& a, int count, int pai
     d.dx_subs = d.row_tiles > 1 ? a.dx_subs : 1;
     // parts of dw that have steps
     const int dw_parts = a.dw_splits == 1 ? 1 : (d.dw_steps + a.dw_split_steps - 1) / a.dw_split_steps;
-    const int dx_n = (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits, dw_n = dw_parts * a.dw_groups * a.dim_tiles;
+    const int dx_n = a.wants_dx ? (d.row_tiles + d.dx_subs - 1) / d.dx_subs * a.dim_tiles * a.splits : 0;
+    const int dw_n = a.wants_dw ? dw_parts * a.dw_groups * a.dim_tiles : 0;
     const int dx_cost = (a.split_steps + kOutSteps) * d.dx_subs, dw_cost = (min(d.dw_steps, a.dw_split_steps) + kOutSteps) * a.dw_subs;
-    d.dw_long = dw_cost >= dx_cost;
+    d.dw_long = a.wants_dw && (dw_cost >= dx_cost || !a.wants_dx);
     const int long_n = d.dw_long ? dw_n : dx_n, more = d.dw_long ? dw_cost : dx_cost, less = d.dw_long ? dx_cost : dw_cost;
     d.short_n = d.dw_long ? dx_n : dw_n;
     d.longs = a.by_pairs(long_n);
@@ -1065,7 +1067,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1) product
 
     if (count == 0) {
         // nobody takes part: dw of the piece is zero, and nothing reads dx
-        const int per_row = a.dim / 8, words = min(a.vocab - a.tile0 * kTile, a.tiles * kTile);
+        const int per_row = a.dim / 8, words = a.wants_dw ? min(a.vocab - a.tile0 * kTile, a.tiles * kTile) : 0;
         for (int64_t i = blockIdx.x * kThreads + threadIdx.x; i < (int64_t)words * per_row; i += (int64_t)gridDim.x * kThreads) {
             const int64_t v = i / per_row;
             *reinterpret_cast<uint4*>(a.dw + (a.tile0 * (int64_t)kTile + v) * a.dw_step + 8 * (i - v * per_row)) = make_uint4(0, 0, 0, 0);
@@ -1632,7 +1634,7 @@ int forward(const Call& c, bool teacher, float* loss, float* lse) {
 
 // What a piece leaves in parts: dw of its words, with the last piece dx.
 int add_parts(const Plan& p, const ProductArgs& m, cudaStream_t stream) {
-    const bool dx = p.dx.splits > 1 && m.tile0 + m.tiles == p.tiles, dw = p.dw.splits > 1;
+    const bool dx = m.wants_dx && p.dx.splits > 1 && m.tile0 + m.tiles == p.tiles, dw = m.wants_dw && p.dw.splits > 1;
     if (!dx && !dw) return ALSGD_OK;
     Parts of_dx, of_dw;
     std::memset(&of_dx, 0, sizeof of_dx);
@@ -1658,16 +1660,18 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     int rc = check_call(c, teacher);
     if (rc != ALSGD_OK) return rc;
     const alsgd_vocab_desc& d = *c.d;
-    if ((rc = check_matrix(dx, d.rows, d.dim, true)) != ALSGD_OK || (rc = check_matrix(dw, d.vocab, d.dim, true)) != ALSGD_OK) return rc;
-    if ((d.rows && dx->data == c.x->data) || dw->data == c.w->data) return ALSGD_E_ARG;         // the operands are read until the end
+    if (!dx && !dw) return ALSGD_E_ARG;
+    if (dx && (rc = check_matrix(dx, d.rows, d.dim, true)) != ALSGD_OK) return rc;
+    if (dw && (rc = check_matrix(dw, d.vocab, d.dim, true)) != ALSGD_OK) return rc;
+    if ((dx && d.rows && dx->data == c.x->data) || (dw && dw->data == c.w->data)) return ALSGD_E_ARG;      // the operands are read until the end
     if (d.rows && (!lse || !dloss || reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(dloss) % 4 || dloss_step < 0)) return ALSGD_E_ARG;
     const Plan p = make_plan(d, true);
     if (d.rows && c.work_bytes < p.bytes) return ALSGD_E_NOMEM;
     UseDevice use(d.device);
     if (!use.ok) return ALSGD_E_CUDA;
-    const uint64_t dw_step = step_of(*dw, d.vocab, d.dim);
+    const uint64_t dw_step = dw ? step_of(*dw, d.vocab, d.dim) : 0;
     if (d.rows == 0)
-        return cudaMemset2DAsync(dw->data, 2 * dw_step, 0, 2ull * d.dim, d.vocab, c.stream) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
+        return !dw || cudaMemset2DAsync(dw->data, 2 * dw_step, 0, 2ull * d.dim, d.vocab, c.stream) == cudaSuccess ? ALSGD_OK : ALSGD_E_CUDA;
     LogitArgs a;
     ProductArgs m;
     std::memset(&m, 0, sizeof m);
@@ -1682,7 +1686,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     if ((rc = make_map(c.w->data, d.vocab, d.dim, 2 * step_of(*c.w, d.vocab, d.dim), 64, &m.w)) != ALSGD_OK) return rc;
     const uint64_t blocks = (uint64_t)(p.padded / 128) * p.piece * 4;
     if ((rc = make_dz_map(a.dz, blocks, 16, &m.dz_block)) != ALSGD_OK || (rc = make_dz_map(a.dz, blocks, 8, &m.dz_half)) != ALSGD_OK) return rc;
-    {
+    if (dw) {
         const cuuint64_t size[2] = {d.dim, d.vocab}, step_bytes = 2 * dw_step;
         const cuuint32_t box[2] = {32, 32};
         if ((rc = encode_map(2, dw->data, size, &step_bytes, box, CU_TENSOR_MAP_SWIZZLE_64B, &m.dw_map)) != ALSGD_OK) return rc;
@@ -1706,10 +1710,16 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
     m.sums = at<float4>(c, p.sums);
     m.dw_sums = at<float4>(c, p.dw_sums);
     m.row = at<int>(c, p.row);
-    m.dx = static_cast<uint16_t*>(dx->data);
-    m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
-    m.dw = static_cast<uint16_t*>(dw->data);
-    m.dw_step = (int64_t)dw_step;
+    m.wants_dx = dx != nullptr;
+    m.wants_dw = dw != nullptr;
+    if (dx) {
+        m.dx = static_cast<uint16_t*>(dx->data);
+        m.dx_step = (int64_t)step_of(*dx, d.rows, d.dim);
+    }
+    if (dw) {
+        m.dw = static_cast<uint16_t*>(dw->data);
+        m.dw_step = (int64_t)dw_step;
+    }
     if ((rc = gather_rows(c, p, lse, dloss, dloss_step, dx)) != ALSGD_OK) return rc;
     static SmemLimit limit;
     constexpr size_t smem = sizeof(ProductSmem) + 1024;
@@ -1726,7 +1736,7 @@ int backward(const Call& c, bool teacher, const float* lse, const float* dloss, 
         if ((rc = launch_logits<true>(a, d.device, c.stream)) != ALSGD_OK) return rc;
         m.dw_groups = (m.tiles + p.dw.subs - 1) / p.dw.subs;
         m.by_dw_groups = divide_by(m.dw_groups);
-        const int grid = grid_of((int64_t)(p.padded / kTile) * p.dim_tiles * p.dx.splits + (int64_t)m.tiles * p.dim_tiles * p.dw.splits);
+        const int grid = grid_of(p.dim_tiles * ((dx ? (int64_t)(p.padded / kTile) * p.dx.splits : 0) + (dw ? (int64_t)m.tiles * p.dw.splits : 0)));
         m.by_pairs = divide_by(grid / 2);
         m.by_splits = divide_by(m.splits);
         if (launch_dependent(product_kernel, dim3(grid), dim3(kThreads), smem, c.stream, m) != cudaSuccess) return ALSGD_E_CUDA;

@@ -28,7 +28,10 @@ class _Loss(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dloss):
         x, w, index, teacher, lse = ctx.saved_tensors
-        dx, dw = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (x, w))
+        # a frozen embedding, or rows that nothing is learnt through, has no gradient made for it
+        dx, dw = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if needed else None for t, needed in zip((x, w), ctx.needs_input_grad[1:3]))
+        if dx is None and dw is None:
+            return None, None, None, None, None
         if teacher is None:
             ctx.plan.alsgd_xent_bwd(x, w, index, lse, dloss, dx, dw)
         else:
