@@ -655,13 +655,14 @@ class Rotary:
             d.base, d.factor, d.context, d.amplitude = float(base), float(factor), float(context), float(amplitude)
             d.turns_low, d.turns_high = float(turns[0]), float(turns[1])
             descs.append(d)
-        # a call's direction and the positions' type choose among descriptors
+        # a call's direction, the positions' type and which operands there are choose among descriptors
         self._descs = {}
         for d in descs:
             for code in (I32, I64):
-                e = RopeDesc.from_buffer_copy(d)
-                e.position_dtype = code
-                self._descs[bool(d.flags & ROPE_INVERSE), code] = e
+                for which, heads in (("both", (d.heads_q, d.heads_k)), ("q", (d.heads_q, 0)), ("k", (d.heads_k, 0))):
+                    e = RopeDesc.from_buffer_copy(d)
+                    e.position_dtype, (e.heads_q, e.heads_k) = code, heads
+                    self._descs[bool(d.flags & ROPE_INVERSE), code, which] = e
         self._q_shape, self._k_shape = (batch, length, heads_q, dim), (batch, length, heads_k, dim)
         self._index = int(device)
         # filled at every call (making new ones costs as much again as all other checks), so calls go out one by one
@@ -675,28 +676,32 @@ class Rotary:
         return slot
 
     def alsgd_rope(self, q, k, q_out, k_out, positions=None, inverse=False, stream=None):
-        """q_out and k_out are written and may be q and k; k and k_out are None without key heads.  positions: int32 or int64
-        [batch, position]; inverse: the backward pass, on gradients."""
+        """q_out and k_out are written and may be q and k.  k and k_out are None without key heads or to turn q alone, q and q_out to
+        turn k alone.  positions: int32 or int64 [batch, position]; inverse: the backward pass, on gradients."""
         code = I32
         if positions is not None:
             assert positions.shape == self._q_shape[:2] and positions.is_contiguous() and positions.get_device() == self._index
             code = _whole_code(self.torch, positions.dtype)
-        keys = self._k_shape[2] > 0
-        assert keys or (k is None and k_out is None)
+        assert (q is None) == (q_out is None) and (k is None) == (k_out is None)
         at = positions.data_ptr() if positions is not None else None
         q_in, k_in, q_to, k_to = self._slots
+        shape, which = self._q_shape, "both"
+        if k is None:
+            which = "q"
+        elif q is None:
+            q, q_out, shape, which = k, k_out, self._k_shape, "k"
         with self._lock:
-            self._operand(q_in, q, self._q_shape)
-            self._operand(q_to, q_out, self._q_shape)
-            if keys:
+            self._operand(q_in, q, shape)
+            self._operand(q_to, q_out, shape)
+            if which == "both":
                 self._operand(k_in, k, self._k_shape)
                 self._operand(k_to, k_out, self._k_shape)
-            _check(lib().alsgd_rope(self._descs[bool(inverse), code], q_in, k_in if keys else None, at, q_to, k_to if keys else None,
-                                    _stream(self.torch, self._index, stream)), "alsgd_rope")
+            _check(lib().alsgd_rope(self._descs[bool(inverse), code, which], q_in, k_in if which == "both" else None, at, q_to,
+                                    k_to if which == "both" else None, _stream(self.torch, self._index, stream)), "alsgd_rope")
 
     def alsgd_rope_frequencies(self):
         """Angle per position of every pair, scaled as the plan says."""
-        d = self._descs[False, I32]
+        d = self._descs[False, I32, "both"]
         out = (C.c_double * (d.rot // 2))()
         _check(lib().alsgd_rope_frequencies(d, out), "alsgd_rope_frequencies")
         return [float(x) for x in out]

@@ -37,7 +37,8 @@ class _Rotate(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dq, dk):
         positions, = ctx.saved_tensors
-        dq, dk = _laid_out(dq), _laid_out(dk)
+        # what needs no gradient is not turned back
+        dq, dk = (_laid_out(t) if needed else None for t, needed in zip((dq, dk), ctx.needs_input_grad[1:3]))
         dq_in, dk_in = _like(dq), _like(dk)
         ctx.plan.alsgd_rope(dq, dk, dq_in, dk_in, positions=positions, inverse=True)
         return None, dq_in, dk_in, None
@@ -45,5 +46,5 @@ class _Rotate(torch.autograd.Function):
 
 def rotate(plan: B.Rotary, q, k, positions=None):
     """q and k [batch, position, head, dim] at their positions, with gradients; second derivatives raise.  k is None, and so is its
-    result, where the plan has no key heads."""
+    result, where the plan has no key heads or q is turned alone."""
     return _Rotate.apply(plan, q, k, positions)

@@ -25,3 +25,14 @@ def test_without_key_heads():
     up = torch.randn_like(got)
     assert torch.equal(torch.autograd.grad(got, q, up)[0], 2 * up)
     assert plan.calls == [(False, True, False), (True, True, False)]
+
+
+def test_only_what_needs_a_gradient_is_turned_back():
+    for needs in ((True, False), (False, True), (True, True)):
+        plan = Plan()
+        q, k = (torch.randn(1, 3, h, 8, requires_grad=n) for h, n in zip((2, 1), needs))
+        outs = [t for t, n in zip(rotate(plan, q, k), needs) if n]
+        ups = [torch.randn_like(t) for t in outs]
+        got = torch.autograd.grad(outs, [t for t, n in zip((q, k), needs) if n], ups)
+        assert all(torch.equal(a, 2 * b) for a, b in zip(got, ups))
+        assert plan.calls == [(False, True, True), (True,) + needs]
