@@ -644,25 +644,16 @@ class Rotary:
         import torch
         self.torch = torch
         self.dtype = dtype if dtype is not None else torch.bfloat16
-        descs = []
-        for flags in (0, ROPE_INVERSE):
-            d = RopeDesc()
-            d.batch, d.len, d.heads_q, d.heads_k, d.dim = [int(x) for x in (batch, length, heads_q, heads_k, dim)]
-            d.rot = int(dim if rot is None else rot)
-            d.flags = flags | (ROPE_INTERLEAVED if interleaved else 0)
-            d.dtype, d.position_dtype = _dtype_code(torch, self.dtype), I32
-            d.pos0, d.device = int(pos0), int(device)
-            d.base, d.factor, d.context, d.amplitude = float(base), float(factor), float(context), float(amplitude)
-            d.turns_low, d.turns_high = float(turns[0]), float(turns[1])
-            descs.append(d)
-        # a call's direction, the positions' type and which operands there are choose among descriptors
-        self._descs = {}
-        for d in descs:
-            for code in (I32, I64):
-                for which, heads in (("both", (d.heads_q, d.heads_k)), ("q", (d.heads_q, 0)), ("k", (d.heads_k, 0))):
-                    e = RopeDesc.from_buffer_copy(d)
-                    e.position_dtype, (e.heads_q, e.heads_k) = code, heads
-                    self._descs[bool(d.flags & ROPE_INVERSE), code, which] = e
+        d = RopeDesc()
+        d.batch, d.len, d.heads_q, d.heads_k, d.dim = [int(x) for x in (batch, length, heads_q, heads_k, dim)]
+        d.rot = int(dim if rot is None else rot)
+        d.flags = ROPE_INTERLEAVED if interleaved else 0
+        d.dtype, d.position_dtype = _dtype_code(torch, self.dtype), I32
+        d.pos0, d.device = int(pos0), int(device)
+        d.base, d.factor, d.context, d.amplitude = float(base), float(factor), float(context), float(amplitude)
+        d.turns_low, d.turns_high = float(turns[0]), float(turns[1])
+        # a call's direction, the positions' type and which operands there are choose among descriptors, each made at its first call
+        self._descs = {(False, I32, "both"): d}
         self._q_shape, self._k_shape = (batch, length, heads_q, dim), (batch, length, heads_k, dim)
         self._index = int(device)
         # filled at every call (making new ones costs as much again as all other checks), so calls go out one by one
@@ -674,6 +665,16 @@ class Rotary:
         assert d == 1
         slot.data = t.data_ptr()
         return slot
+
+    def _desc(self, inverse, code, which):
+        d = self._descs.get((inverse, code, which))
+        if d is None:
+            d = RopeDesc.from_buffer_copy(self._descs[False, I32, "both"])
+            d.flags |= ROPE_INVERSE if inverse else 0
+            d.position_dtype = code
+            d.heads_q, d.heads_k = {"both": (d.heads_q, d.heads_k), "q": (d.heads_q, 0), "k": (d.heads_k, 0)}[which]
+            self._descs[inverse, code, which] = d
+        return d
 
     def alsgd_rope(self, q, k, q_out, k_out, positions=None, inverse=False, stream=None):
         """q_out and k_out are written and may be q and k.  k and k_out are None without key heads or to turn q alone, q and q_out to
@@ -696,7 +697,7 @@ class Rotary:
             if which == "both":
                 self._operand(k_in, k, self._k_shape)
                 self._operand(k_to, k_out, self._k_shape)
-            _check(lib().alsgd_rope(self._descs[bool(inverse), code, which], q_in, k_in if which == "both" else None, at, q_to,
+            _check(lib().alsgd_rope(self._desc(bool(inverse), code, which), q_in, k_in if which == "both" else None, at, q_to,
                                     k_to if which == "both" else None, _stream(self.torch, self._index, stream)), "alsgd_rope")
 
     def alsgd_rope_frequencies(self):
