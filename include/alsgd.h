@@ -519,7 +519,8 @@ typedef struct alsgd_rope_desc {
     int32_t device;
     int64_t pos0;                      /* without positions: token s of every sequence is at pos0 + s */
     double base;                       /* > 1 */
-    double factor, context, turns_low, turns_high; /* factor >= 1; the others unused at 1.  turns_high above turns_low >= 0, or 0 */
+    double factor, context, turns_low, turns_high; /* factor >= 1, context >= 0, turns_high above turns_low >= 0 or 0.  The last
+                                                      three are checked, but not used, with factor 1 */
     double amplitude;                  /* finite and not 0 in binary32; usually 1 */
 } alsgd_rope_desc;
 

@@ -13,10 +13,14 @@
 // where they are: there is little to save, and the two launches in front would cost more than the rest
 // (77 rows x 32000 words x 384: forward 18.4 -> 15.4 us, backward 43.9 -> 35.3 us when this was measured).
 //
-// dz becomes an operand of the tensor cores and is rounded to bf16 for it; sums over many rows or words average that out to about
-// what the results' own rounding costs.  Few rows need not average anything: dw of a word is often the gradient of one.  So up to 64
-// rows dz goes in two parts, the rounded value and what rounding left, as so many more rows, for which the tiles have room anyway.
-// (From 65 to 128 rows it would take a step more of every product: 28.5 -> 33.0 us at 77 rows.)
+// dz becomes an operand of the tensor cores and is rounded to bf16 for it.  The roundings of a sum's terms are independent of one
+// another, as the terms are, so that a sum is off by about the same share as each of them, and that is about what rounding the
+// result costs once more: together 0.0018 to 0.0023 of it, against 0.0017 (the squares add up).  Up to 64 rows the tiles have room for
+// dz in two parts, the rounded value and what rounding left, as so many more rows, and only the result's rounding stays.  More rows
+// are off as above and would take longer for it: from 65 to 128 a step more of every product (28.5 -> 33.0 us at 77 rows), many
+// rows twice the products with dz, two thirds more in all.
+//
+// Times in this file are those of calls captured in a loop over one set of inputs: what fits the L2 is found there.
 //
 // The matrix products bound it.  Two blocks of a cluster form one 256 x 256 tile: each holds 128 of its rows and copies half
 // of either operand, so that a tile needs half of the shared memory traffic of two single ones.  (Up to 128 rows there is no
