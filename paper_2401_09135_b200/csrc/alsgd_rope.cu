@@ -20,7 +20,7 @@ using namespace alsgd_ops;
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
 // Units of two groups that a thread has in flight, with five blocks per SM: 21.6 us at 64 x 256 tokens and 32 heads of 64, 28.8 at
-// 4 x 4099 tokens and 20 heads of 128, of calls captured in a loop over one set of tensors, part of which stays in the L2; 24.1 to 24.6
+// 4 x 4099 tokens and 20 heads of 128, of calls captured in a loop over one set of tensors, part of which stays in the L2; 24.0 to 24.6
 // and 30.6 to 31.3 (5.5 and 5.4 TB/s) of calls on tensors that change.  Instructions count here as much as memory (70 % of the issue
 // slots): with four blocks, or six and spilled registers, both were 5 to 15 % slower, and with four units.
 constexpr int kUnits = 2;
