@@ -29,7 +29,7 @@ def counted(backward, rows, vocab, dim, top):
 @pytest.mark.parametrize("backward", [0, 1])
 @pytest.mark.parametrize("top", [0, 1, 128])
 def test_the_workspace_is_what_its_account_says(backward, top):
-    for rows, vocab, dim in itertools.product([1, 77, 300, 8144, 30720, 65536, 70001, 1 << 20], [1, 5000, 8704, 32000, 100003, 1 << 20], [8, 384, 1024]):
+    for rows, vocab, dim in itertools.product([1, 77, 300, 8144, 30208, 65536, 70001, 1 << 20], [1, 5000, 8704, 32000, 100003, 1 << 20], [8, 384, 1024]):
         kw = dict(rows=rows, vocab=vocab, dim=dim, top=top)
         assert taken(backward, **kw) <= counted(backward, **kw), kw
 
@@ -37,4 +37,4 @@ def test_the_workspace_is_what_its_account_says(backward, top):
 def test_a_piece_of_dz_is_no_larger_than_said():
     """Narrow rows and no teacher: dz is nearly all there is.  A piece of 17 tiles' worth, rounded up to pairs of tiles, took 18."""
     for tiles in range(16, 80):
-        assert taken(1, rows=30720, vocab=256 * tiles, dim=8) <= (256 + 8) * MIB, tiles
+        assert taken(1, rows=30208, vocab=256 * tiles, dim=8) <= (256 + 8) * MIB, tiles
